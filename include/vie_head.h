@@ -25,8 +25,8 @@
  *     time-out are unspecified (every write still stays inside them).
  *   - Logits are fp32.  Ranking is by logit descending; equal logits are
  *     ranked by ascending vocabulary index, and -0.0 ranks as +0.0 (and is
- *     returned as +0.0).  Inputs must be finite; results for NaN or infinite
- *     inputs are unspecified.
+ *     returned as +0.0).  Inputs must be finite, and results for NaN or
+ *     infinite inputs are unspecified, unless a call says otherwise.
  */
 #ifndef VIE_HEAD_H
 #define VIE_HEAD_H
@@ -49,7 +49,10 @@ typedef enum {
     VIE_ERR_DEVICE = 5       /* a kernel recorded a device-side problem       */
 } vie_status;
 
-typedef enum { VIE_DTYPE_BF16 = 0 } vie_dtype;
+typedef enum {
+    VIE_DTYPE_BF16 = 0,
+    VIE_DTYPE_F32 = 1 /* logits, tables and gradients below; heads hold bf16 or e4m3 rows */
+} vie_dtype;
 
 /* Limits of this library. */
 #define VIE_K_MAX 1024     /* largest k of vie_head_topk                    */
@@ -58,6 +61,7 @@ typedef enum { VIE_DTYPE_BF16 = 0 } vie_dtype;
 #define VIE_MANY_MAX (1 << 24)     /* largest n of vie_head_topk_many       */
 #define VIE_RECALL_N_MAX (1 << 28) /* largest n of vie_recall_hits          */
 #define VIE_RECALL_M_MAX (1 << 20) /* largest candidate count m             */
+#define VIE_SAMPLE_V_MAX (1 << 22) /* largest V of vie_sample_logits        */
 
 /* Read-only facts about a handle (for callers that size buffers or report). */
 typedef struct {
@@ -80,7 +84,7 @@ typedef struct {
  *          of 2 bytes.  Only read during the call; the caller may free it
  *          afterwards.
  *   V      1 <= V <= 2^31 - 2;   d   1 <= d <= VIE_D_MAX;
- *   dtype  VIE_DTYPE_BF16 (the only dtype of this library).
+ *   dtype  VIE_DTYPE_BF16 (the only dtype that a head takes).
  *   out    host; receives the new handle.
  *
  * The handle owns a padded copy [V, d_pad] (d_pad = d rounded up to a
@@ -408,6 +412,153 @@ vie_status vie_scatter_sparse_logits(const int32_t *idx, const float *logits, in
 vie_status vie_head_topk_noalloc(const void *W_out, int64_t V, int32_t d, const float *h,
                                  int32_t batch, int32_t k, int32_t *out_idx, float *out_logits,
                                  vie_stream stream);
+
+/*
+ * Training and sampling around the head.  A small model that is trained on
+ * what an exact head says (vie_head_topk_many: the teacher's top-k logits)
+ * looks its tokens up in an embedding table (vie_embed), takes the loss of its
+ * own full logits against the teacher's list and the gradient
+ * (vie_distill_topk*), sums the table's gradient (vie_embed_grad), and draws
+ * the tokens that it goes on with (vie_sample_logits).  These calls need no
+ * handle.  Matrices are row-major with a row pitch in values ("ld", at least
+ * the number of columns; rows need no alignment beyond a value's), bf16 or
+ * fp32.  All arithmetic is fp32, each result rounded once to its type.  n = 0
+ * is a valid call that does nothing (vie_embed_grad without accumulate still
+ * clears its output).  No allocation and no host synchronisation happen inside
+ * these calls, they may be captured in a graph, and calls on different streams
+ * do not disturb each other (vie_embed_grad: with workspaces of their own).
+ */
+
+/*
+ * vie_distill_topk - loss of a student's logits against a teacher's top-k
+ * logits.  The teacher is the softmax of the sparse logit tensor (Section 3:
+ * -inf except the k logits) over its k entries.  Per row, with z the
+ * student's V logits, (i_j, t_j) the teacher's entries and T the temperature:
+ *   p   = softmax(t / T) over the valid entries (i_j in [0, V), t_j > -inf);
+ *   q   = softmax(z / T) over the vocabulary;
+ *   loss = T^2 sum_j p_j (log p_j - log q[i_j])       (T^2 KL(p || q)).
+ * Entries with an index outside [0, V) are empty slots, whatever their logit;
+ * repeated indices add up.  A row without valid entries has loss 0 and stats
+ * (0, 0), and its logits are not read.  Student logits of -inf have q = 0: the
+ * loss is +inf where p > 0 there.  NaN or +inf logits give a NaN loss in
+ * their row only.
+ *
+ *   logits      device, dtype [n, V], row pitch ld.
+ *   n, V        0 <= n <= VIE_MANY_MAX;  1 <= V <= 2^31 - 2.
+ *   t_idx, t_logits  device, int32 / fp32 [n, k], in any order;
+ *               1 <= k <= VIE_K_MAX.
+ *   temperature > 0 and finite.
+ *   out_loss    device, fp32 [n].
+ *   out_stats   device, fp32 [n, 2]: max z and sum_v exp((z_v - max z) / T), what
+ *               vie_distill_topk_grad needs; may be NULL.
+ *
+ * Errors: VIE_ERR_INVALID_ARG, VIE_ERR_UNSUPPORTED (dtype), VIE_ERR_CUDA.
+ */
+vie_status vie_distill_topk(const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                            const int32_t *t_idx, const float *t_logits, int32_t k, float temperature,
+                            float *out_loss, float *out_stats, vie_stream stream);
+
+/*
+ * vie_distill_topk_grad - the gradient of sum_i grad_loss[i] loss[i] with
+ * respect to the student's logits:
+ *   out_grad[i, v] = grad_loss[i] T (q_v - sum over j with i_j = v of p_j),
+ * 0 in rows without valid entries.  Arguments as for vie_distill_topk, and
+ *   stats       device, fp32 [n, 2]: out_stats of vie_distill_topk on the same
+ *               logits and temperature.
+ *   grad_loss   device, fp32 [n].
+ *   out_grad    device, dtype [n, V], row pitch ld_grad; may be logits itself
+ *               (with ld_grad = ld), but not overlap it in any other way.
+ */
+vie_status vie_distill_topk_grad(const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                                 const int32_t *t_idx, const float *t_logits, int32_t k, float temperature,
+                                 const float *stats, const float *grad_loss, void *out_grad, int64_t ld_grad,
+                                 vie_stream stream);
+
+/*
+ * vie_distill_topk_step - vie_distill_topk and vie_distill_topk_grad in one
+ * call, for programs that know grad_loss beforehand.  Arguments as for those
+ * two; out_stats may be NULL.
+ */
+vie_status vie_distill_topk_step(const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                                 const int32_t *t_idx, const float *t_logits, int32_t k, float temperature,
+                                 const float *grad_loss, float *out_loss, float *out_stats, void *out_grad,
+                                 int64_t ld_grad, vie_stream stream);
+
+/*
+ * vie_embed - rows of an embedding table, scaled (models with tied embeddings
+ * look tokens up in the matrix that the head projects on):
+ *   out[i, :] = scale * table[tokens[i], :].
+ * Negative tokens are empty slots: a row of zeros.  A token of V or more gives
+ * a row of zeros as well and sets the device flag that vie_device_status
+ * reports.
+ *
+ *   table    device, dtype [V, d], row pitch ld;  1 <= V <= 2^31 - 2;
+ *            1 <= d <= VIE_D_MAX.
+ *   tokens   device, int32 [n];  0 <= n <= VIE_MANY_MAX.
+ *   out      device, out_dtype [n, d], row pitch ld_out (fp32 rows are what
+ *            vie_head_topk takes).
+ *
+ * Errors: VIE_ERR_INVALID_ARG, VIE_ERR_UNSUPPORTED (dtype), VIE_ERR_CUDA.
+ */
+vie_status vie_embed(const void *table, vie_dtype dtype, int64_t V, int32_t d, int64_t ld, const int32_t *tokens,
+                     int64_t n, float scale, void *out, vie_dtype out_dtype, int64_t ld_out, vie_stream stream);
+
+/* Bytes of workspace that vie_embed_grad needs for n tokens (into *bytes, host). */
+vie_status vie_embed_grad_workspace(int64_t n, int64_t V, int32_t d, int64_t *bytes);
+
+/*
+ * vie_embed_grad - the table's gradient:
+ *   accumulate 0:  out[v, :]  = scale * sum over i with tokens[i] = v of grad[i, :]
+ *                  (zeros for tokens that do not occur);
+ *   otherwise:     out[v, :] += the same, for tokens that occur; the other rows
+ *                  are not touched.
+ * The sum of a token's rows is fp32, in an order that depends on the tokens
+ * alone: the same call gives the same bits.  Tokens outside [0, V) are left
+ * out (V or more: the device flag, as in vie_embed).
+ *
+ *   tokens, n, V, d  as for vie_embed.
+ *   grad     device, dtype [n, d], row pitch ld_grad.
+ *   out      device, out_dtype [V, d], row pitch ld.
+ *   workspace  device, 16-byte aligned, workspace_bytes bytes, at least what
+ *            vie_embed_grad_workspace says; its contents need not be kept.
+ *
+ * Errors: VIE_ERR_INVALID_ARG, VIE_ERR_UNSUPPORTED (dtype), VIE_ERR_CUDA.
+ */
+vie_status vie_embed_grad(const int32_t *tokens, int64_t n, const void *grad, vie_dtype dtype, int64_t ld_grad,
+                          float scale, int64_t V, int32_t d, void *out, vie_dtype out_dtype, int64_t ld,
+                          int32_t accumulate, void *workspace, int64_t workspace_bytes, vie_stream stream);
+
+/*
+ * vie_sample_logits - tokens drawn from full logits (dense ones, or the sparse
+ * tensor of vie_head_topk_sparse after a program's own processors), each row
+ * with its own settings and a uniform number that the caller gives.  Tokens
+ * rank by (logit descending, index ascending).  Per row, with b = max z:
+ *   w_v = floor(2^40 exp((z_v - b) (1 / T))), the products and the exp in fp32;
+ *   top_k keeps the best top_k tokens (0 or less, or V and more: all), mass S;
+ *   top_p keeps the shortest prefix of mass >= top_p S (1 or more: all);
+ *   min_p keeps the tokens with w >= min_p 2^40 (0 or less: all);
+ *   the shortest of these prefixes is kept, the best token always; mass M;
+ *   the token is the first one whose running mass exceeds u M.
+ * Weights are whole numbers, so their sums are exact in any order: the same
+ * inputs give the same tokens on any device.  u and top_p count in steps of
+ * 2^-24 (u rounded down and held in [0, 1), top_p rounded up).  T of 0 (or
+ * anything not above 0) takes the best token.  Logits of -inf and NaN are
+ * never drawn; a row that has no others gives token -1 and probability 0.
+ * Logits of +inf share the whole mass.
+ *
+ *   logits   device, dtype [batch, V], row pitch ld;  0 <= batch <= VIE_MANY_MAX;
+ *            1 <= V <= VIE_SAMPLE_V_MAX.
+ *   u        device, fp32 [batch].
+ *   temperature, top_k, top_p, min_p  device, fp32 / int32 / fp32 / fp32
+ *            [batch]; each may be NULL (1, 0, 1, 0).
+ *   out_token  device, int32 [batch].
+ *   out_prob   device, fp32 [batch]: w / M of the token.
+ *
+ * Errors: VIE_ERR_INVALID_ARG, VIE_ERR_UNSUPPORTED (dtype), VIE_ERR_CUDA.
+ */
+vie_status vie_sample_logits(const void *logits, vie_dtype dtype, int64_t batch, int64_t V, int64_t ld, const float *u,
+                             const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                             int32_t *out_token, float *out_prob, vie_stream stream);
 
 /*
  * vie_device_status - synchronises `stream`, then reads and clears the

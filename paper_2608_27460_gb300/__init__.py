@@ -27,12 +27,14 @@ VIE_ERR_CUDA = 3
 VIE_ERR_OOM = 4
 VIE_ERR_DEVICE = 5
 VIE_DTYPE_BF16 = 0
+VIE_DTYPE_F32 = 1
 VIE_K_MAX = 1024
 VIE_BATCH_MAX = 1024
 VIE_D_MAX = 16384
 VIE_MANY_MAX = 1 << 24
 VIE_RECALL_N_MAX = 1 << 28
 VIE_RECALL_M_MAX = 1 << 20
+VIE_SAMPLE_V_MAX = 1 << 22
 
 # Launch options (vie_launch_option): tuning and test hooks, never results.
 VIE_OPT_STAGE_MIN_KB = 0
@@ -55,7 +57,9 @@ EXPORTS = ("vie_head_create", "vie_head_destroy", "vie_head_get_props", "vie_hea
            "vie_head_topk_sparse", "vie_head_topk_host", "vie_sample_topk", "vie_head_topk_sample",
            "vie_head_create_e4m3", "vie_head_export_e4m3", "vie_head_topk_many", "vie_recall_hits",
            "vie_head_topk_noalloc", "vie_scatter_sparse_logits", "vie_device_status",
-           "vie_head_device_status", "vie_last_error", "vie_set_launch_option", "vie_get_launch_option")
+           "vie_head_device_status", "vie_last_error", "vie_set_launch_option", "vie_get_launch_option",
+           "vie_distill_topk", "vie_distill_topk_grad", "vie_distill_topk_step", "vie_embed",
+           "vie_embed_grad_workspace", "vie_embed_grad", "vie_sample_logits")
 
 
 class VieError(RuntimeError):
@@ -121,6 +125,15 @@ def load(path: str | None = None, build_if_missing: bool = True):
             "vie_last_error": ([], ctypes.c_char_p),
             "vie_set_launch_option": ([ctypes.c_int, I32], ctypes.c_int),
             "vie_get_launch_option": ([ctypes.c_int, ctypes.POINTER(I32)], ctypes.c_int),
+            "vie_distill_topk": ([P, ctypes.c_int, I64, I64, I64, P, P, I32, F32, P, P, P], ctypes.c_int),
+            "vie_distill_topk_grad": ([P, ctypes.c_int, I64, I64, I64, P, P, I32, F32, P, P, P, I64, P], ctypes.c_int),
+            "vie_distill_topk_step": ([P, ctypes.c_int, I64, I64, I64, P, P, I32, F32, P, P, P, P, I64, P],
+                                      ctypes.c_int),
+            "vie_embed": ([P, ctypes.c_int, I64, I32, I64, P, I64, F32, P, ctypes.c_int, I64, P], ctypes.c_int),
+            "vie_embed_grad_workspace": ([I64, I64, I32, ctypes.POINTER(I64)], ctypes.c_int),
+            "vie_embed_grad": ([P, I64, P, ctypes.c_int, I64, F32, I64, I32, P, ctypes.c_int, I64, I32, P, I64, P],
+                               ctypes.c_int),
+            "vie_sample_logits": ([P, ctypes.c_int, I64, I64, I64, P, P, P, P, P, P, P, P], ctypes.c_int),
         }
         for name, (args, res) in sig.items():
             fn = getattr(lib, name)
@@ -254,6 +267,51 @@ def vie_head_topk_noalloc(W_out: int, V: int, d: int, h: int, batch: int, k: int
     return load().vie_head_topk_noalloc(W_out, V, d, h, batch, k, out_idx, out_logits, stream)
 
 
+def vie_distill_topk(logits: int, dtype: int, n: int, V: int, ld: int, t_idx: int, t_logits: int, k: int,
+                     temperature: float, out_loss: int, out_stats: int = 0, stream: int = 0) -> int:
+    return load().vie_distill_topk(logits, dtype, n, V, ld, t_idx, t_logits, k, temperature, out_loss, out_stats,
+                                   stream)
+
+
+def vie_distill_topk_grad(logits: int, dtype: int, n: int, V: int, ld: int, t_idx: int, t_logits: int, k: int,
+                          temperature: float, stats: int, grad_loss: int, out_grad: int, ld_grad: int,
+                          stream: int = 0) -> int:
+    return load().vie_distill_topk_grad(logits, dtype, n, V, ld, t_idx, t_logits, k, temperature, stats, grad_loss,
+                                        out_grad, ld_grad, stream)
+
+
+def vie_distill_topk_step(logits: int, dtype: int, n: int, V: int, ld: int, t_idx: int, t_logits: int, k: int,
+                          temperature: float, grad_loss: int, out_loss: int, out_stats: int, out_grad: int,
+                          ld_grad: int, stream: int = 0) -> int:
+    return load().vie_distill_topk_step(logits, dtype, n, V, ld, t_idx, t_logits, k, temperature, grad_loss, out_loss,
+                                        out_stats, out_grad, ld_grad, stream)
+
+
+def vie_embed(table: int, dtype: int, V: int, d: int, ld: int, tokens: int, n: int, scale: float, out: int,
+              out_dtype: int, ld_out: int, stream: int = 0) -> int:
+    return load().vie_embed(table, dtype, V, d, ld, tokens, n, scale, out, out_dtype, ld_out, stream)
+
+
+def vie_embed_grad_workspace(n: int, V: int, d: int):
+    """Returns (status, bytes)."""
+    v = ctypes.c_int64(0)
+    st = load().vie_embed_grad_workspace(n, V, d, ctypes.byref(v))
+    return st, v.value
+
+
+def vie_embed_grad(tokens: int, n: int, grad: int, dtype: int, ld_grad: int, scale: float, V: int, d: int, out: int,
+                   out_dtype: int, ld: int, accumulate: int, workspace: int, workspace_bytes: int,
+                   stream: int = 0) -> int:
+    return load().vie_embed_grad(tokens, n, grad, dtype, ld_grad, scale, V, d, out, out_dtype, ld, accumulate,
+                                 workspace, workspace_bytes, stream)
+
+
+def vie_sample_logits(logits: int, dtype: int, batch: int, V: int, ld: int, u: int, temperature: int, top_k: int,
+                      top_p: int, min_p: int, out_token: int, out_prob: int, stream: int = 0) -> int:
+    return load().vie_sample_logits(logits, dtype, batch, V, ld, u, temperature, top_k, top_p, min_p, out_token,
+                                    out_prob, stream)
+
+
 def vie_scatter_sparse_logits(idx: int, logits: int, batch: int, k: int, V: int, out: int,
                               stream: int = 0) -> int:
     return load().vie_scatter_sparse_logits(idx, logits, batch, k, V, out, stream)
@@ -328,6 +386,235 @@ def _stream_ptr(stream) -> int:
         else:
             _current_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
     return _current_stream()
+
+
+# ---- training and sampling around the head (torch tensors) ------------------
+
+def _dtype_code(x, name):
+    import torch
+    if x.dtype == torch.bfloat16:
+        return VIE_DTYPE_BF16
+    if x.dtype == torch.float32:
+        return VIE_DTYPE_F32
+    raise ValueError(f"{name} must be bfloat16 or float32, not {x.dtype}")
+
+
+def _pitch(x):
+    """Row pitch of a 2-D tensor whose rows are runs of values that do not
+    overlap, or 0 if it is laid out in another way."""
+    n, c = x.shape
+    if c > 1 and x.stride(1) != 1:
+        return 0
+    if n <= 1:
+        return max(c, 1)
+    return x.stride(0) if x.stride(0) >= c else 0
+
+
+def _matrix(x, name):
+    """(x, pitch) of a CUDA matrix argument; one laid out in another way than
+    by rows is copied."""
+    if x.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D CUDA tensor")
+    ld = _pitch(x)
+    if ld:
+        return x, ld
+    x = x.contiguous()
+    return x, max(x.shape[1], 1)
+
+
+def _vector(x, name, dtype, n, like):
+    """A contiguous CUDA vector argument of n values."""
+    if x.dtype != dtype or not x.is_cuda or x.dim() != 1 or x.shape[0] != n or x.device != like.device:
+        raise ValueError(f"{name} must be a {dtype} tensor [{n}] on {like.device}")
+    return x if x.is_contiguous() else x.contiguous()
+
+
+def _output(x, name, shape, dtype, like):
+    """An output tensor: `x` if it fits, a new one if it is None.  Vectors
+    must be contiguous, matrices laid out by rows."""
+    import torch
+    if x is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    if tuple(x.shape) != tuple(shape) or x.dtype != dtype or x.device != like.device:
+        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {like.device}")
+    return x
+
+
+def _contiguous_output(x, name, shape, dtype, like):
+    x = _output(x, name, shape, dtype, like)
+    if not x.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return x
+
+
+def _matrix_output(x, name, shape, dtype, like):
+    x = _output(x, name, shape, dtype, like)
+    ld = _pitch(x)
+    if not ld:
+        raise ValueError(f"{name} must be laid out by rows")
+    return x, ld
+
+
+class _on:
+    """Makes a call's own copies and new tensors belong to the stream it runs
+    on, and its device the current one."""
+
+    def __init__(self, like, name, stream):
+        import torch
+        if not like.is_cuda:
+            raise ValueError(f"{name} must be a CUDA tensor")
+        self.ctx = []
+        if like.device.index != torch.cuda.current_device():
+            self.ctx.append(torch.cuda.device(like.device))
+        if stream is not None:
+            self.ctx.append(torch.cuda.stream(stream))
+
+    def __enter__(self):
+        for c in self.ctx:
+            c.__enter__()
+        return _stream_ptr(None)
+
+    def __exit__(self, *exc):
+        for c in reversed(self.ctx):
+            c.__exit__(*exc)
+
+
+def _teacher(logits, t_idx, t_logits):
+    """The checked arguments that the distillation calls share."""
+    import torch
+    n = logits.shape[0] if logits.dim() else 0
+    for x, name, dt in ((t_idx, "t_idx", torch.int32), (t_logits, "t_logits", torch.float32)):
+        if x.dtype != dt or x.dim() != 2 or x.device != logits.device or x.shape[0] != n or x.shape != t_idx.shape:
+            raise ValueError(f"{name} must be a {dt} tensor [{n}, k] on {logits.device}")
+    return t_idx.contiguous(), t_logits.contiguous()
+
+
+def distill_topk(logits, t_idx, t_logits, temperature: float = 1.0, out_loss=None, out_stats=None, stream=None):
+    """Loss of a student's logits [n, V] (bf16 or fp32) against a teacher's
+    top-k logits (int32 / float32 [n, k], as :meth:`Head.topk_many` returns
+    them; negative indices are empty slots): T^2 KL(teacher || student) per
+    row.  Returns (loss [n], stats [n, 2]); stats go to distill_topk_grad."""
+    import torch
+    with _on(logits, "logits", stream) as s:
+        t_idx, t_logits = _teacher(logits, t_idx, t_logits)
+        logits, ld = _matrix(logits, "logits")
+        n, V = logits.shape
+        out_loss = _contiguous_output(out_loss, "out_loss", (n,), torch.float32, logits)
+        out_stats = _contiguous_output(out_stats, "out_stats", (n, 2), torch.float32, logits)
+        check(vie_distill_topk(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
+                               t_logits.data_ptr(), t_idx.shape[1], temperature, out_loss.data_ptr(),
+                               out_stats.data_ptr(), s))
+    return out_loss, out_stats
+
+
+def distill_topk_grad(logits, t_idx, t_logits, stats, grad_loss, temperature: float = 1.0, out_grad=None,
+                      stream=None):
+    """Gradient of sum(grad_loss * loss) with respect to the student's logits,
+    in their type; `stats` come from distill_topk.  out_grad may be logits."""
+    import torch
+    with _on(logits, "logits", stream) as s:
+        t_idx, t_logits = _teacher(logits, t_idx, t_logits)
+        logits, ld = _matrix(logits, "logits")
+        n, V = logits.shape
+        if stats.dtype != torch.float32 or tuple(stats.shape) != (n, 2) or stats.device != logits.device:
+            raise ValueError(f"stats must be a float32 tensor [{n}, 2] on {logits.device}")
+        stats = stats.contiguous()
+        grad_loss = _vector(grad_loss, "grad_loss", torch.float32, n, logits)
+        out_grad, ld_grad = _matrix_output(out_grad, "out_grad", (n, V), logits.dtype, logits)
+        check(vie_distill_topk_grad(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
+                                    t_logits.data_ptr(), t_idx.shape[1], temperature, stats.data_ptr(),
+                                    grad_loss.data_ptr(), out_grad.data_ptr(), ld_grad, s))
+    return out_grad
+
+
+def distill_topk_step(logits, t_idx, t_logits, grad_loss, temperature: float = 1.0, out_loss=None, out_grad=None,
+                      stream=None):
+    """distill_topk and distill_topk_grad in one call: (loss [n], gradient
+    [n, V]).  grad_loss [n] is the weight of each row's loss; out_grad may be
+    logits."""
+    import torch
+    with _on(logits, "logits", stream) as s:
+        t_idx, t_logits = _teacher(logits, t_idx, t_logits)
+        logits, ld = _matrix(logits, "logits")
+        n, V = logits.shape
+        grad_loss = _vector(grad_loss, "grad_loss", torch.float32, n, logits)
+        out_loss = _contiguous_output(out_loss, "out_loss", (n,), torch.float32, logits)
+        out_grad, ld_grad = _matrix_output(out_grad, "out_grad", (n, V), logits.dtype, logits)
+        check(vie_distill_topk_step(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
+                                    t_logits.data_ptr(), t_idx.shape[1], temperature, grad_loss.data_ptr(),
+                                    out_loss.data_ptr(), 0, out_grad.data_ptr(), ld_grad, s))
+    return out_loss, out_grad
+
+
+def embed(table, tokens, scale: float = 1.0, out=None, out_dtype=None, stream=None):
+    """scale * table[tokens] (table [V, d] and out [n, d] bf16 or fp32, tokens
+    int32 [n]); negative tokens give zeros.  out_dtype (of a new `out`)
+    defaults to the table's type; float32 rows are what a Head takes."""
+    import torch
+    with _on(table, "table", stream) as s:
+        table, ld = _matrix(table, "table")
+        n, (V, d) = tokens.numel(), table.shape
+        tokens = _vector(tokens, "tokens", torch.int32, n, table)
+        if out is not None and out_dtype is None:
+            out_dtype = out.dtype
+        out, ld_out = _matrix_output(out, "out", (n, d), out_dtype or table.dtype, table)
+        check(vie_embed(table.data_ptr(), _dtype_code(table, "table"), V, d, ld, tokens.data_ptr(), n, scale,
+                        out.data_ptr(), _dtype_code(out, "out"), ld_out, s))
+    return out
+
+
+def embed_grad(tokens, grad, V: int, scale: float = 1.0, out=None, accumulate: bool = False, out_dtype=None,
+               workspace=None, stream=None):
+    """Gradient of embed with respect to its table: out[v] = scale * sum of the
+    rows grad[i] with tokens[i] = v ([V, d], bf16 or fp32), or with
+    accumulate out[v] += that.  out_dtype (of a new `out`) defaults to
+    float32.  workspace: a uint8 CUDA tensor that is used if it is large
+    enough (vie_embed_grad_workspace), else the call allocates one."""
+    import torch
+    with _on(grad, "grad", stream) as s:
+        grad, ld_grad = _matrix(grad, "grad")
+        n, d = grad.shape
+        tokens = _vector(tokens, "tokens", torch.int32, n, grad)
+        if out is None and accumulate:
+            raise ValueError("accumulate needs the gradient to add to (out)")
+        if out is not None and out_dtype is None:
+            out_dtype = out.dtype
+        out, ld = _matrix_output(out, "out", (V, d), out_dtype or torch.float32, grad)
+        st, need = vie_embed_grad_workspace(n, V, d)
+        check(st)
+        if workspace is None or workspace.numel() < need:
+            workspace = torch.empty((need,), dtype=torch.uint8, device=grad.device)
+        elif workspace.dtype != torch.uint8 or workspace.device != grad.device or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous uint8 tensor on {grad.device}")
+        check(vie_embed_grad(tokens.data_ptr(), n, grad.data_ptr(), _dtype_code(grad, "grad"), ld_grad, scale, V, d,
+                             out.data_ptr(), _dtype_code(out, "out"), ld, 1 if accumulate else 0,
+                             workspace.data_ptr(), workspace.numel(), s))
+    return out
+
+
+def sample_logits(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, out_token=None, out_prob=None,
+                  stream=None):
+    """Tokens drawn from full logits [batch, V] (bf16 or fp32): one uniform
+    number u in [0, 1) and one setting of each kind per row (float32 [batch];
+    top_k int32; None: 1, off, off, off).  Returns (token int32 [batch],
+    probability float32 [batch])."""
+    import torch
+    with _on(logits, "logits", stream) as s:
+        logits, ld = _matrix(logits, "logits")
+        b, V = logits.shape
+        u = _vector(u, "u", torch.float32, b, logits)
+        kept, ptr = [], []
+        for x, name, dt in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
+                            (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
+            if x is not None:
+                x = _vector(x, name, dt, b, logits)
+            kept.append(x)
+            ptr.append(0 if x is None else x.data_ptr())
+        out_token = _contiguous_output(out_token, "out_token", (b,), torch.int32, logits)
+        out_prob = _contiguous_output(out_prob, "out_prob", (b,), torch.float32, logits)
+        check(vie_sample_logits(logits.data_ptr(), _dtype_code(logits, "logits"), b, V, ld, u.data_ptr(), *ptr,
+                                out_token.data_ptr(), out_prob.data_ptr(), s))
+    return out_token, out_prob
 
 
 class Head:

@@ -12,6 +12,7 @@ namespace vie {
 enum : uint32_t {
     kErrWaitTimeout = 1u << 0,   // a pipeline wait ran past its time limit
     kErrScatterIndex = 1u << 1,  // a scatter index fell outside [0, V)
+    kErrTokenIndex = 1u << 2,    // a token was V or more
 };
 
 // A pipeline wait gives up after this many nanoseconds of %globaltimer.

@@ -15,6 +15,7 @@
 #include <mutex>
 #include <new>
 
+#include "vie_api.h"
 #include "vie_head.h"
 #include "vie_launch.h"
 #include "vie_plan.h"
@@ -24,6 +25,10 @@
 namespace {
 
 thread_local char g_err[512] = "";
+
+}  // namespace
+
+namespace vie {
 
 vie_status fail(vie_status st, const char *fmt, ...) {
     va_list ap;
@@ -38,8 +43,36 @@ vie_status fail_cuda(cudaError_t e, const char *what) {
                 cudaGetErrorString(e), cudaGetErrorName(e));
 }
 
+vie_status check_matrix(const char *fn, const char *name, const void *p, vie_dtype t, int64_t rows, int64_t cols,
+                        int64_t ld) {
+    if (!dtype_known(t)) return fail(VIE_ERR_UNSUPPORTED, "%s: dtype %d of %s is not supported", fn, int(t), name);
+    if (ld < cols)
+        return fail(VIE_ERR_INVALID_ARG, "%s: row pitch %lld of %s is below its %lld columns", fn,
+                    static_cast<long long>(ld), name, static_cast<long long>(cols));
+    if (rows > 0 && ld > (INT64_MAX / 16) / rows) return fail(VIE_ERR_INVALID_ARG, "%s: size of %s overflows", fn, name);
+    if (p == nullptr && rows > 0) return fail(VIE_ERR_INVALID_ARG, "%s: %s is NULL", fn, name);
+    if (!aligned_to(p, static_cast<uintptr_t>(dtype_size(t))))
+        return fail(VIE_ERR_INVALID_ARG, "%s: %s is not aligned to its values", fn, name);
+    return VIE_OK;
+}
+
+}  // namespace vie
+
+namespace {
+
+using vie::fail;
+using vie::fail_cuda;
+
 // Library-wide device flag word (used by kernels that have no handle).
 __device__ uint32_t g_dev_err = 0;
+
+}  // namespace
+
+cudaError_t vie::device_flag_word(uint32_t **word) {
+    return cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_dev_err);
+}
+
+namespace {
 
 constexpr int kMaxSmem = 232448;  // 227 KB opt-in dynamic shared memory per CTA
 constexpr int kMaxNB = 8;
@@ -1094,8 +1127,9 @@ vie_status vie_device_status(vie_stream stream) {
     const uint32_t zero = 0;
     e = cudaMemcpyToSymbol(g_dev_err, &zero, sizeof zero);
     if (e != cudaSuccess) return fail_cuda(e, "vie_device_status: clear flag");
-    return fail(VIE_ERR_DEVICE, "device flag 0x%x:%s%s", w,
+    return fail(VIE_ERR_DEVICE, "device flag 0x%x:%s%s%s", w,
                 (w & vie::kErrScatterIndex) ? " scatter index outside [0, V)" : "",
+                (w & vie::kErrTokenIndex) ? " token at or above V" : "",
                 (w & vie::kErrWaitTimeout) ? " pipeline wait timed out" : "");
 }
 
