@@ -61,6 +61,7 @@ typedef enum {
 #define VIE_MANY_MAX (1 << 24)     /* largest n of vie_head_topk_many       */
 #define VIE_RECALL_N_MAX (1 << 28) /* largest n of vie_recall_hits          */
 #define VIE_RECALL_M_MAX (1 << 20) /* largest candidate count m             */
+#define VIE_DISTILL_V_MAX (1 << 30) /* largest V of vie_distill_topk*       */
 #define VIE_SAMPLE_V_MAX (1 << 22) /* largest V of vie_sample_logits        */
 
 /* Read-only facts about a handle (for callers that size buffers or report). */
@@ -444,7 +445,7 @@ vie_status vie_head_topk_noalloc(const void *W_out, int64_t V, int32_t d, const 
  * their row only.
  *
  *   logits      device, dtype [n, V], row pitch ld.
- *   n, V        0 <= n <= VIE_MANY_MAX;  1 <= V <= 2^31 - 2.
+ *   n, V        0 <= n <= VIE_MANY_MAX;  1 <= V <= VIE_DISTILL_V_MAX.
  *   t_idx, t_logits  device, int32 / fp32 [n, k], in any order;
  *               1 <= k <= VIE_K_MAX.
  *   temperature > 0 and finite.

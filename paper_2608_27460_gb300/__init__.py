@@ -34,6 +34,7 @@ VIE_D_MAX = 16384
 VIE_MANY_MAX = 1 << 24
 VIE_RECALL_N_MAX = 1 << 28
 VIE_RECALL_M_MAX = 1 << 20
+VIE_DISTILL_V_MAX = 1 << 30
 VIE_SAMPLE_V_MAX = 1 << 22
 
 # Launch options (vie_launch_option): tuning and test hooks, never results.

@@ -1,5 +1,6 @@
-// vie_block.cuh - sums and maxima over the threads of a CTA, and one value
-// of a matrix in either of the library's storage types.
+// vie_block.cuh - building blocks of the kernels on matrices of either storage
+// type: values and 16-byte vectors of them, sums and maxima over a CTA, the
+// exponential, and cluster primitives in inline PTX.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -45,6 +46,73 @@ __device__ __forceinline__ float block_max(float v, float *scratch) {
     if (lane == 0) scratch[warp] = v;
     __syncthreads();
     return warp_max(lane < NT / 32 ? scratch[lane] : -INFINITY);
+}
+
+// 16 bytes of a matrix row: kVec values.
+template <typename T>
+struct Vec16;
+template <>
+struct Vec16<float> {
+    static constexpr int kVec = 4;
+    static __device__ __forceinline__ void unpack(const uint4 &r, float *v) {
+        v[0] = __uint_as_float(r.x), v[1] = __uint_as_float(r.y);
+        v[2] = __uint_as_float(r.z), v[3] = __uint_as_float(r.w);
+    }
+    static __device__ __forceinline__ uint4 pack(const float *v) {
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    }
+};
+template <>
+struct Vec16<__nv_bfloat16> {
+    static constexpr int kVec = 8;
+    static __device__ __forceinline__ void unpack(const uint4 &r, float *v) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+    }
+    static __device__ __forceinline__ uint4 pack(const float *v) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+
+// 2^x of the special function unit (2 ulp), denormal results flushed to 0.
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Thread-block clusters: this CTA's rank, the barrier in its two halves, and a
+// store into another CTA's shared memory.
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive_relaxed() {
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_addr(const void *p, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                 : "=r"(a)
+                 : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void cluster_store(uint32_t addr, float4 v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
+                 : "memory");
 }
 
 }  // namespace vie
