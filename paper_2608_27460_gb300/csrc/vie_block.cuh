@@ -26,34 +26,61 @@ __device__ __forceinline__ float warp_max(float v) {
     return v;
 }
 
-// The sum / maximum of v over the NT threads of the CTA, in all of them, in
-// an order that depends on NT alone.  `scratch`: 32 floats of shared memory;
-// every thread of the CTA calls, and may call again at once.
+// The maximum / sum of v over the NT threads of the CTA, in all of them, in an
+// order that depends on NT alone.  `scratch`: shared memory of this call
+// alone; every thread of the CTA calls.
 template <int NT>
-__device__ __forceinline__ float block_sum(float v, float *scratch) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    v = warp_sum(v);
-    __syncthreads();  // the last call's reads
-    if (lane == 0) scratch[warp] = v;
+__device__ __forceinline__ float block_max(float v, float (&scratch)[NT / 32]) {
+    const int lane = threadIdx.x & 31;
+    v = warp_max(v);
+    if (lane == 0) scratch[threadIdx.x >> 5] = v;
     __syncthreads();
-    return warp_sum(lane < NT / 32 ? scratch[lane] : 0.0f);
+    v = scratch[lane & (NT / 32 - 1)];
+#pragma unroll
+    for (int o = NT / 64; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    return v;
 }
 template <int NT>
-__device__ __forceinline__ float block_max(float v, float *scratch) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    v = warp_max(v);
-    __syncthreads();  // the last call's reads
-    if (lane == 0) scratch[warp] = v;
+__device__ __forceinline__ float block_sum(float v, float (&scratch)[NT / 32]) {
+    const int lane = threadIdx.x & 31;
+    v = warp_sum(v);
+    if (lane == 0) scratch[threadIdx.x >> 5] = v;
     __syncthreads();
-    return warp_max(lane < NT / 32 ? scratch[lane] : -INFINITY);
+    v = scratch[lane & (NT / 32 - 1)];
+#pragma unroll
+    for (int o = NT / 64; o >= 1; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+__device__ __forceinline__ float4 shfl_xor_add(float4 v, int o) {
+    v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
+    v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
+    v.z += __shfl_xor_sync(0xFFFFFFFFu, v.z, o);
+    v.w += __shfl_xor_sync(0xFFFFFFFFu, v.w, o);
+    return v;
+}
+template <int NT>
+__device__ __forceinline__ float4 block_sum(float4 v, float4 (&scratch)[NT / 32]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) v = shfl_xor_add(v, o);
+    if (lane == 0) scratch[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = scratch[lane & (NT / 32 - 1)];
+#pragma unroll
+    for (int o = NT / 64; o >= 1; o >>= 1) v = shfl_xor_add(v, o);
+    return v;
 }
 
 // 16 bytes of a matrix row: kVec values.
+// max_of: the largest of them, NaN aside.
 template <typename T>
 struct Vec16;
 template <>
 struct Vec16<float> {
     static constexpr int kVec = 4;
+    static __device__ __forceinline__ float max_of(const uint4 &r) {
+        return fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
+    }
     static __device__ __forceinline__ void unpack(const uint4 &r, float *v) {
         v[0] = __uint_as_float(r.x), v[1] = __uint_as_float(r.y);
         v[2] = __uint_as_float(r.z), v[3] = __uint_as_float(r.w);
@@ -65,6 +92,14 @@ struct Vec16<float> {
 template <>
 struct Vec16<__nv_bfloat16> {
     static constexpr int kVec = 8;
+    static __device__ __forceinline__ float max_of(const uint4 &r) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+        __nv_bfloat162 h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = *reinterpret_cast<const __nv_bfloat162 *>(&w[i]);
+        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
     static __device__ __forceinline__ void unpack(const uint4 &r, float *v) {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll

@@ -58,7 +58,7 @@ struct Weigh {
 };
 
 struct SampleSmem {
-    float scratch[32];
+    float scratch[kSampleThreads / 32];
     uint64_t mass[256];
     uint32_t count[256];
     uint64_t sum;
