@@ -72,15 +72,19 @@ __device__ __forceinline__ float4 block_sum(float4 v, float4 (&scratch)[NT / 32]
 }
 
 // 16 bytes of a matrix row: kVec values.
-// max_of: the largest of them, NaN aside.
 template <typename T>
 struct Vec16;
 template <>
 struct Vec16<float> {
     static constexpr int kVec = 4;
-    static __device__ __forceinline__ float max_of(const uint4 &r) {
-        return fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
-    }
+    struct Max {  // running maxima, one per position, of vectors; NaN aside
+        float v[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        __device__ __forceinline__ void add(const uint4 &r) {
+            v[0] = fmaxf(v[0], __uint_as_float(r.x)), v[1] = fmaxf(v[1], __uint_as_float(r.y));
+            v[2] = fmaxf(v[2], __uint_as_float(r.z)), v[3] = fmaxf(v[3], __uint_as_float(r.w));
+        }
+        __device__ __forceinline__ float top() const { return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])); }
+    };
     static __device__ __forceinline__ void unpack(const uint4 &r, float *v) {
         v[0] = __uint_as_float(r.x), v[1] = __uint_as_float(r.y);
         v[2] = __uint_as_float(r.z), v[3] = __uint_as_float(r.w);
@@ -92,14 +96,22 @@ struct Vec16<float> {
 template <>
 struct Vec16<__nv_bfloat16> {
     static constexpr int kVec = 8;
-    static __device__ __forceinline__ float max_of(const uint4 &r) {
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-        __nv_bfloat162 h[4];
+    struct Max {  // running maxima, one per position, of vectors; NaN aside
+        __nv_bfloat162 v[4];
+        __device__ __forceinline__ Max() {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = *reinterpret_cast<const __nv_bfloat162 *>(&w[i]);
-        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-        return fmaxf(__low2float(m), __high2float(m));
-    }
+            for (int i = 0; i < 4; ++i) v[i] = __float2bfloat162_rn(-INFINITY);
+        }
+        __device__ __forceinline__ void add(const uint4 &r) {
+            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __hmax2(v[i], *reinterpret_cast<const __nv_bfloat162 *>(&w[i]));
+        }
+        __device__ __forceinline__ float top() const {
+            const __nv_bfloat162 m = __hmax2(__hmax2(v[0], v[1]), __hmax2(v[2], v[3]));
+            return fmaxf(__low2float(m), __high2float(m));
+        }
+    };
     static __device__ __forceinline__ void unpack(const uint4 &r, float *v) {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
@@ -126,17 +138,11 @@ __device__ __forceinline__ float exp2_approx(float x) {
     return y;
 }
 
-// Thread-block clusters: this CTA's rank, the barrier in its two halves, and a
-// store into another CTA's shared memory.
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
+// Thread-block clusters: the barrier in its two halves (no ordering of its own
+// in the first), and addresses in the other CTAs' shared memory.
 __device__ __forceinline__ void cluster_arrive_relaxed() {
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t cluster_addr(const void *p, uint32_t rank) {
     uint32_t a;
@@ -145,8 +151,11 @@ __device__ __forceinline__ uint32_t cluster_addr(const void *p, uint32_t rank) {
                  : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(rank));
     return a;
 }
-__device__ __forceinline__ void cluster_store(uint32_t addr, float4 v) {
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
+// Two values into another CTA's shared memory, which count 8 bytes on that CTA's
+// mbarrier when they are there: no fence, no barrier of all threads.
+__device__ __forceinline__ void cluster_send(uint32_t addr, float2 v, uint32_t bar) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(addr),
+                 "f"(v.x), "f"(v.y), "r"(bar)
                  : "memory");
 }
 

@@ -41,10 +41,11 @@ struct DistillParams {
 // A row is cut into 16-byte vectors at 16-byte addresses; its first and last
 // one may reach over its ends.  The `slices` CTAs of a row take consecutive
 // runs of vectors.
-constexpr int kMaxSlices = 16;
+constexpr int kSlices = 8, kMaxSlices = 16;  // per row: as many as clusters may have everywhere, and for a few rows alone
+constexpr int kFewRows = 8;
 
-// exp2((z - m) c) = exp((z - m) / T).  The difference comes first: the type's
-// lowest value is a usual mask, and z c - m c overflows there.
+// exp2((z - m) c) = exp((z - m) / T), with c = log2(e) / T.  The difference comes
+// first: the type's lowest value is a usual mask, and z c - m c overflows there.
 struct Exponent {
     float m, c;
     __device__ __forceinline__ float operator()(float z) const { return exp2_approx((z - m) * c); }
@@ -54,15 +55,15 @@ __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0
 
 constexpr int kDistillThreads = 256;
 constexpr int kDistillWarps = kDistillThreads / 32;
-constexpr int kEntries = VIE_K_MAX / kDistillThreads;  // teacher entries per thread of a teacher warp, at most
+constexpr int kUnroll = 8;  // vectors in flight per thread
+static_assert(VIE_K_MAX <= 128 * kDistillWarps, "a warp for every 128 entries of a teacher");
 
 struct DistillSmem {
-    float4 gathered[kMaxSlices];      // per slice: max z and the sums of exp((z - m) / T), p (z - m) / T and p
-    float4 teacher[kDistillWarps];    // per teacher warp: the sums of p (z - m) / T, p and p log p
-    float2 t_part[kDistillWarps];     // per teacher warp: max t and the sum of exp((t - max t) / T)
-    float row_max[kDistillWarps], row_sum[kDistillWarps];
-    uint64_t bar;
-    int abort;
+    float2 gathered[kMaxSlices];    // per slice of the row: max z and the sum of exp((z - max z) / T)
+    uint64_t gather_bar;
+    float2 part[kDistillWarps];     // the same per warp of a slice
+    float3 teacher[kDistillWarps];  // per teacher warp: max t, the sum of exp((t - max t) / T), part of the loss
+    int repeats, abort;
 };
 
 // Slots of the hash table of a slice's entries: a power of two, at least
@@ -73,403 +74,445 @@ __host__ __device__ inline int seen_slots(int k) {
     return slots;
 }
 
-// FWD: loss and statistics; BWD: the gradient.  RESIDENT: the CTA's slice stays
-// in shared memory between the two, so the logits are read once; otherwise
-// each of them reads the slice again.
-// The first warps (one per 128 entries) deal with the teacher while the others
-// wait for the slice: a thread's share of the row is small, and what every
-// thread does besides counts (27 instructions per logit when all warps took
-// part in the teacher's sums, 14 are the row's own).
-// Dynamic shared memory: the slice (RESIDENT); from entries_at on (BWD) p and
-// the indices of the teacher's entries and the hash table.
-template <typename T, bool FWD, bool BWD, bool RESIDENT>
-__global__ void __launch_bounds__(kDistillThreads, RESIDENT ? 5 : 4)
-    distill_kernel(const DistillParams a, int log2_slices, uint32_t entries_at) {
-    constexpr int NT = kDistillThreads, U = RESIDENT ? 2 : 8;  // U: vectors in flight per thread
-    constexpr int kVec = Vec16<T>::kVec;
-    extern __shared__ __align__(16) unsigned char distill_slice[];
+// The part of a row that a CTA deals with.  Vector i of the slice holds values
+// e0 + i kVec .. + kVec - 1 of the row; vectors lo .. hi - 1 of nv lie inside
+// it.  At most two do not: `edge` is one of them in thread 0 or 1.
+template <typename T>
+struct Slice {
+    static constexpr int kVec = Vec16<T>::kVec;
+    const T *z;
+    int e0, e1, nv, lo, hi, V;
+
+    __device__ __forceinline__ Slice(const DistillParams &a, int64_t row, int log2_slices, int rank)
+        : z(static_cast<const T *>(a.logits) + row * a.ld), V(a.V) {
+        const int first = -static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15u) / sizeof(T));
+        const int vectors = (V - first + kVec - 1) / kVec;
+        const int per = (vectors + (1 << log2_slices) - 1) >> log2_slices;
+        const int v0 = min(rank * per, vectors);
+        nv = min(per, vectors - v0);
+        e0 = first + v0 * kVec;
+        e1 = e0 + nv * kVec;
+        lo = e0 < 0 ? 1 : 0;
+        hi = e1 > V ? nv - 1 : nv;
+    }
+    __device__ __forceinline__ const uint4 *vectors() const { return reinterpret_cast<const uint4 *>(z + e0); }
+    __device__ __forceinline__ int edge() const { return threadIdx.x == 0 ? 0 : nv - 1; }
+    __device__ __forceinline__ bool has_edge() const {
+        return threadIdx.x < min(nv, 2) && (edge() < lo || edge() >= hi);
+    }
+    __device__ __forceinline__ uint4 load_edge() const {  // values outside the row: -inf
+        const int e = e0 + edge() * kVec;
+        float v[kVec];
+#pragma unroll
+        for (int x = 0; x < kVec; ++x) v[x] = e + x >= 0 && e + x < V ? load_value(z + e + x) : -INFINITY;
+        return Vec16<T>::pack(v);
+    }
+};
+
+// Where a slice's gradient goes: by vectors if its rows lie to 16-byte
+// addresses as the logits' do, else value by value.
+template <typename T>
+struct GradSlice {
+    static constexpr int kVec = Vec16<T>::kVec;
+    T *g;
+    int e0, V;
+    bool by_vector;
+
+    __device__ __forceinline__ GradSlice(const DistillParams &a, int64_t row, const Slice<T> &sl)
+        : g(static_cast<T *>(a.grad) + row * a.ld_grad), e0(sl.e0), V(sl.V),
+          by_vector(((reinterpret_cast<uintptr_t>(sl.z) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0) {}
+    __device__ __forceinline__ void store_values(int i, const float *v) const {  // those inside the row
+        const int e = e0 + i * kVec;
+#pragma unroll
+        for (int x = 0; x < kVec; ++x)
+            if (e + x >= 0 && e + x < V) store_value(g + e + x, v[x]);
+    }
+    __device__ __forceinline__ void store(int i, const float *v) const {
+        if (by_vector) reinterpret_cast<uint4 *>(g + e0)[i] = Vec16<T>::pack(v);
+        else store_values(i, v);
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ void clear_gradient(const Slice<T> &sl, const GradSlice<T> &out, int threads) {
+    const float zero[Slice<T>::kVec] = {};
+    for (int i = sl.lo + threadIdx.x; i < sl.hi; i += threads) out.store(i, zero);
+    if (sl.has_edge()) out.store_values(sl.edge(), zero);
+}
+
+template <typename T>
+__device__ __forceinline__ void gradient_of(const Exponent &e, float coef, const uint4 &raw, float *v) {
+    Vec16<T>::unpack(raw, v);
+#pragma unroll
+    for (int x = 0; x < Slice<T>::kVec; ++x) v[x] = coef * e(v[x]);
+}
+// Running sums of exponentials, one per position of a vector: chains that do
+// not wait for one another.
+template <typename T>
+struct Sums {
+    float v[Slice<T>::kVec] = {};
+    __device__ __forceinline__ void add(const Exponent &e, const uint4 &raw) {
+        float x[Slice<T>::kVec];
+        Vec16<T>::unpack(raw, x);
+#pragma unroll
+        for (int i = 0; i < Slice<T>::kVec; ++i) v[i] += e(x[i]);
+    }
+    __device__ __forceinline__ float total() const {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < Slice<T>::kVec; i += 2) s += v[i] + v[i + 1];
+        return s;
+    }
+};
+
+// The teacher's entries of a row in shared memory, and the warps of the CTA that
+// deal with them: `me` is a thread's number among theirs, below 0 in the
+// others, which call nothing but mine().
+struct Teacher {
+    int32_t *idx;   // -1 where the entry does not count
+    float *p;       // its logit, then the softmax
+    float *z;       // the student's logit there
+    int32_t *seen;  // hash table of the slice's entries
+    int k, warps, me;
+    bool repeats;
+
+    __device__ __forceinline__ Teacher(int k_, int warps_, int me_, int32_t *list, float *z_, int32_t *seen_)
+        : z(z_), seen(seen_), k(k_), warps(warps_), me(me_), repeats(false) {
+        point_at(list);
+    }
+    __device__ __forceinline__ void point_at(int32_t *list) {
+        idx = list;
+        p = reinterpret_cast<float *>(list + k);
+    }
+    __device__ __forceinline__ bool mine() const { return me >= 0; }
+    __device__ __forceinline__ int step() const { return 32 * warps; }
+    __device__ __forceinline__ void barrier() const {
+        if (warps > 1) named_barrier_sync(1, 32 * warps);
+        else __syncwarp();
+    }
+    // Entry j as it was read: whether it counts.
+    __device__ __forceinline__ bool validate(const DistillParams &a, int j) const {
+        if (idx[j] >= 0 && idx[j] < a.V && p[j] != -INFINITY) return true;
+        idx[j] = -1;
+        return false;
+    }
+    // The student's logits at the entries from value e0 to e1 of the row; slice[0] is value e0.
+    template <typename T>
+    __device__ __forceinline__ void read_logits(const T *slice, int e0, int e1) const {
+#pragma unroll 4
+        for (int j = me; j < k; j += step())
+            if (idx[j] >= e0 && idx[j] < e1) z[j] = load_value(slice + (idx[j] - e0));
+    }
+    // p: from logits to the softmax.
+    __device__ __forceinline__ void softmax(DistillSmem &sm, float inv_T) const {
+        const int warp = me >> 5, lane = me & 31;
+        float tm = -INFINITY, ts = 0.0f;
+#pragma unroll 4
+        for (int j = me; j < k; j += step())
+            if (idx[j] >= 0) tm = fmaxf(tm, p[j]);
+        tm = warp_max(tm);
+        if (warps > 1) {
+            if (lane == 0) sm.teacher[warp].x = tm;
+            barrier();
+            for (int w = 0; w < warps; ++w) tm = fmaxf(tm, sm.teacher[w].x);
+        }
+#pragma unroll 4
+        for (int j = me; j < k; j += step()) {
+            const float e = idx[j] >= 0 ? expf((p[j] - tm) * inv_T) : 0.0f;
+            p[j] = e;
+            ts += e;
+        }
+        ts = warp_sum(ts);
+        if (warps > 1) {
+            if (lane == 0) sm.teacher[warp].y = ts;
+            barrier();
+            ts = 0.0f;
+            for (int w = 0; w < warps; ++w) ts += sm.teacher[w].y;
+        }
+        const float inv = 1.0f / ts;
+#pragma unroll 4
+        for (int j = me; j < k; j += step()) p[j] *= inv;
+        barrier();
+    }
+    // Indices seldom repeat: a hash table finds out whether those of this slice do.
+    __device__ __forceinline__ void find_repeats(DistillSmem &sm, int e0, int e1) {
+        const int slots = seen_slots(k);
+        for (int i = me; i < slots; i += step()) seen[i] = -1;
+        if (me == 0) sm.repeats = 0;
+        barrier();
+        for (int j = me; j < k; j += step()) {
+            const int32_t i = idx[j];
+            if (i < e0 || i >= e1 || i < 0) continue;
+            uint32_t h = (static_cast<uint32_t>(i) * 0x9E3779B1u) >> 16 & (slots - 1);
+            while (true) {  // ends: at most half the slots are taken
+                const int32_t old = atomicCAS(&seen[h], -1, i);
+                if (old == i) sm.repeats = 1;
+                if (old == -1 || old == i) break;
+                h = (h + 1) & (slots - 1);
+            }
+        }
+        barrier();
+        repeats = sm.repeats != 0;
+    }
+    // T^2 sum p (log p - log q) over all entries, in all of the warps; m, s: the student's statistics.
+    __device__ __forceinline__ float loss(DistillSmem &sm, float T, float inv_T, float m, float s) const {
+        float kl = 0.0f;
+        const float log_s = logf(s), m0 = finite_max(m);
+#pragma unroll 4
+        for (int j = me; j < k; j += step())
+            if (p[j] != 0.0f) kl += p[j] * (logf(p[j]) - (z[j] - m0) * inv_T + log_s);
+        kl = warp_sum(kl);
+        if (warps > 1) {
+            if ((me & 31) == 0) sm.teacher[me >> 5].z = kl;
+            barrier();
+            kl = 0.0f;
+            for (int w = 0; w < warps; ++w) kl += sm.teacher[w].z;
+        }
+        return s == 0.0f ? INFINITY : T * T * kl;  // (no softmax: no logit above -inf)
+    }
+    // q - p over what the slice's loop has written at its entries; the first
+    // entry of an index takes off the sum of all.
+    template <typename T>
+    __device__ __forceinline__ void store_gradient(T *g, int e0, int e1, const Exponent &e, float cg, float inv) const {
+        for (int j = me; j < k; j += step()) {
+            const int32_t i = idx[j];
+            if (i < e0 || i >= e1 || i < 0) continue;
+            float take = p[j];
+            bool leads = true;
+            if (repeats) {
+                take = 0.0f;
+                for (int x = 0; x < k; ++x)
+                    if (idx[x] == i) {
+                        leads &= x >= j;
+                        take += p[x];
+                    }
+            }
+            if (leads) store_value(g + i, cg * (e(z[j]) * inv - take));
+        }
+    }
+};
+
+// One warp: the maximum and sum of this CTA's slice, joined from its warps'
+// (sm.part, written before the last barrier), to all CTAs of the row.
+__device__ __forceinline__ void send_partial(DistillSmem &sm, int slices, int rank, float c) {
+    const int lane = threadIdx.x & 31;
+    const float2 part = lane < kDistillWarps ? sm.part[lane] : make_float2(-INFINITY, 0.0f);
+    const float m = warp_max(part.x);
+    const float s = warp_sum(part.y != 0.0f ? part.y * Exponent{finite_max(m), c}(finite_max(part.x)) : 0.0f);
+    if (lane == 0) mbar_arrive_expect_tx(&sm.gather_bar, 8u * slices);
+    if (lane < slices)
+        cluster_send(cluster_addr(&sm.gathered[rank], lane), make_float2(m, s),
+                     cluster_addr(&sm.gather_bar, lane));
+    __syncwarp();
+}
+// The row's, from those of all its slices, in the same order in every warp.
+__device__ __forceinline__ void join_partials(const DistillParams &a, DistillSmem &sm, int slices, float c, float *m,
+                                              float *s) {
+    if (!mbar_wait(&sm.gather_bar, 0, &sm.abort) && threadIdx.x == 0) atomicOr(a.flag, kErrWaitTimeout);
+    const int lane = threadIdx.x & 31;
+    const float2 part = lane < slices ? sm.gathered[lane] : make_float2(-INFINITY, 0.0f);
+    *m = warp_max(part.x);
+    *s = warp_sum(part.y != 0.0f ? part.y * Exponent{finite_max(*m), c}(finite_max(part.x)) : 0.0f);
+}
+
+__device__ __forceinline__ void init_smem(DistillSmem &sm) {
+    sm.abort = 0;
+    mbar_init(&sm.gather_bar, 1);
+    fence_mbar_init();
+}
+
+__device__ __forceinline__ void write_row(const DistillParams &a, int64_t row, float loss, float m, float s) {
+    a.loss[row] = loss;
+    if (a.stats_out != nullptr) {
+        a.stats_out[2 * row] = m;
+        a.stats_out[2 * row + 1] = s;
+    }
+}
+
+// Loss and statistics (FWD) or the gradient (BWD) or both, one row per cluster,
+// its slices read from global memory, twice for both.
+// Dynamic shared memory: the teacher's entries (indices, logits, the student's
+// logits there), the hash table (BWD).
+template <typename T, bool FWD, bool BWD>
+__global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const DistillParams a, int log2_slices) {
+    constexpr int NT = kDistillThreads, U = kUnroll;
+    extern __shared__ __align__(16) unsigned char distill_smem[];
     __shared__ DistillSmem sm;
-    float *const sp = reinterpret_cast<float *>(distill_slice + entries_at);
-    int32_t *const sidx = reinterpret_cast<int32_t *>(sp + a.k), *const seen = sidx + a.k;
+    int32_t *const list = reinterpret_cast<int32_t *>(distill_smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int t_warps = (a.k + 127) / 128;  // the first ones, besides their part of the row
+    Teacher tea(a.k, t_warps, tid < 32 * t_warps ? tid : -1, list, reinterpret_cast<float *>(list + 2 * a.k),
+                list + 3 * a.k);
     const int slices = 1 << log2_slices, rank = blockIdx.x & (slices - 1);
     const int64_t row = blockIdx.x >> log2_slices;
-    const int t_warps = (a.k + 32 * kEntries - 1) / (32 * kEntries);
-    const bool teaches = warp < t_warps;
-    if (FWD && slices > 1) cluster_arrive_relaxed();  // all CTAs of the cluster run, before their memory is written
-    if (RESIDENT && tid == 0) {
-        sm.abort = 0;
-        mbar_init(&sm.bar, 1);
-        fence_mbar_init();
+    if (FWD) {
+        if (tid == 0) init_smem(sm);
+        __syncwarp();
+        cluster_arrive_relaxed();  // all CTAs of the cluster run and wait, before their memory is written
     }
     griddep_launch_dependents();
     griddep_wait();  // the inputs may come from the kernel before this one
 
-    // a teacher warp's entries: idx -1 where there is none
-    int32_t idx[kEntries];
-    float t[kEntries];
     bool any = false;
-    if (teaches) {
-#pragma unroll
-        for (int u = 0; u < kEntries; ++u) {
-            const int j = tid + u * 32 * t_warps;
-            idx[u] = -1, t[u] = -INFINITY;
-            if (j < a.k) {
-                idx[u] = a.t_idx[row * a.k + j];
-                t[u] = a.t[row * a.k + j];
-                if (idx[u] < 0 || idx[u] >= a.V || t[u] == -INFINITY) idx[u] = -1, t[u] = -INFINITY;
-            }
-            any |= idx[u] >= 0;
-        }
+    for (int j = tid; j < a.k; j += NT) {
+        tea.idx[j] = a.t_idx[row * a.k + j], tea.p[j] = a.t[row * a.k + j];
+        any |= tea.validate(a, j);
     }
     const bool has = __syncthreads_or(any);
-
-    const T *z = static_cast<const T *>(a.logits) + row * a.ld;
-    T *g = static_cast<T *>(a.grad) + row * a.ld_grad;
-    // vector i holds the values first + i kVec .. + kVec - 1 of the row; this
-    // slice has nv of them, from value e0 (may be below 0) to e1; those
-    // from lo to hi lie inside the row
-    const int first = -static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15u) / sizeof(T));
-    const int vectors = (a.V - first + kVec - 1) / kVec;
-    const int per = (vectors + slices - 1) >> log2_slices;
-    const int v0 = min(rank * per, vectors), nv = min(per, vectors - v0);
-    const int e0 = first + v0 * kVec, e1 = e0 + nv * kVec;
-    const int lo = e0 < 0 ? 1 : 0, hi = e1 > a.V ? nv - 1 : nv;
-    const int edge = tid == 0 ? 0 : nv - 1;  // threads 0 and 1: the vector that is not, if there is one
-    const bool has_edge = tid < min(nv, 2) && (edge < lo || edge >= hi);
-    auto load_edge = [&]() {  // values outside the row: -inf
-        const int e = e0 + edge * kVec;
-        float v[kVec];
-#pragma unroll
-        for (int x = 0; x < kVec; ++x) v[x] = e + x >= 0 && e + x < a.V ? load_value(z + e + x) : -INFINITY;
-        return Vec16<T>::pack(v);
-    };
-    auto store_some = [&](int i, const float *v) {  // of the gradient: value by value, those inside the row
-        const int e = e0 + i * kVec;
-#pragma unroll
-        for (int x = 0; x < kVec; ++x)
-            if (e + x >= 0 && e + x < a.V) store_value(g + e + x, v[x]);
-    };
-    const bool same_phase = BWD && ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
-    const uint4 *const zv = reinterpret_cast<const uint4 *>(z + e0);  // (only lo .. hi are read)
-    uint4 *const gv = reinterpret_cast<uint4 *>(g + e0);
+    const Slice<T> sl(a, row, log2_slices, rank);
+    const GradSlice<T> out(a, row, sl);
+    if (FWD) cluster_wait();
     if (!has) {
-        if (BWD) {
-            const float zero[kVec] = {};
-            if (same_phase)
-                for (int i = lo + tid; i < hi; i += NT) gv[i] = make_uint4(0, 0, 0, 0);
-            else
-                for (int i = lo + tid; i < hi; i += NT) store_some(i, zero);
-            if (has_edge) store_some(edge, zero);
-        }
-        if (FWD && rank == 0 && tid == 0) {
-            a.loss[row] = 0.0f;
-            if (a.stats_out != nullptr) a.stats_out[2 * row] = a.stats_out[2 * row + 1] = 0.0f;
-        }
-        __syncwarp();
-        if (FWD && slices > 1) cluster_wait();
+        if (BWD) clear_gradient(sl, out, NT);
+        if (FWD && rank == 0 && tid == 0) write_row(a, row, 0.0f, 0.0f, 0.0f);
         return;
     }
-    uint4 *const slice = reinterpret_cast<uint4 *>(distill_slice);
-    if (RESIDENT) {  // one bulk copy of the vectors inside the row; the others by hand
-        if (tid == 0) {
-            const uint32_t bytes = hi > lo ? static_cast<uint32_t>(hi - lo) * 16u : 0u;
-            mbar_arrive_expect_tx(&sm.bar, bytes);
-            if (bytes > 0) bulk_g2s(slice + lo, zv + lo, bytes, &sm.bar, l2_evict_first_policy());
-        }
-        if (has_edge) slice[edge] = load_edge();
-    }
-
     const float inv_T = fminf(1.0f / a.T, 3.4e38f);
     const float c = fminf(1.44269504f / a.T, 3.4e38f);  // log2 e / T
-    float p[kEntries];   // the teacher's softmax, of the entries before the sums over repeats
-    float take[kEntries];  // what the gradient takes off at the entry's index
-    bool repeats = false;
-    if (teaches) {
-        float tm = -INFINITY, ts = 0.0f;
-#pragma unroll
-        for (int u = 0; u < kEntries; ++u) tm = fmaxf(tm, t[u]);
-        tm = warp_max(tm);
-#pragma unroll
-        for (int u = 0; u < kEntries; ++u) {
-            p[u] = idx[u] >= 0 ? expf((t[u] - tm) * inv_T) : 0.0f;
-            ts += p[u];
-        }
-        ts = warp_sum(ts);
-        if (t_warps > 1) {
-            if (lane == 0) sm.t_part[warp] = make_float2(tm, ts);
-            named_barrier_sync(1, 32 * t_warps);
-            const float own = tm;
-            for (int w = 0; w < t_warps; ++w) tm = fmaxf(tm, sm.t_part[w].x);
-            ts = 0.0f;
-            for (int w = 0; w < t_warps; ++w)
-                if (sm.t_part[w].y != 0.0f) ts += sm.t_part[w].y * expf((sm.t_part[w].x - tm) * inv_T);
-            const float scale = own == -INFINITY ? 0.0f : expf((own - tm) * inv_T);
-#pragma unroll
-            for (int u = 0; u < kEntries; ++u) p[u] = idx[u] >= 0 ? p[u] * scale : 0.0f;
-        }
-        const float log_ts = logf(ts);
-        float plogp = 0.0f;
-#pragma unroll
-        for (int u = 0; u < kEntries; ++u) {
-            const int j = tid + u * 32 * t_warps;
-            if (u > 0 && u * 32 * t_warps >= a.k) continue;
-            p[u] /= ts;
-            if (FWD && rank == 0 && p[u] != 0.0f) plogp += p[u] * ((t[u] - tm) * inv_T - log_ts);
-            if (BWD && j < a.k) sp[j] = p[u], sidx[j] = idx[u];
-            if (idx[u] < e0 || idx[u] >= e1) idx[u] = -1;  // from here on: the slice's entries
-        }
-        if (FWD && rank == 0) {
-            plogp = warp_sum(plogp);
-            if (lane == 0) sm.teacher[warp].z = plogp;
-        }
-        if (BWD) {
-            // Indices seldom repeat; where the table finds one that does, the
-            // first entry of an index takes the sum of all.
-            const int slots = seen_slots(a.k);
-            for (int i = tid; i < slots; i += 32 * t_warps) seen[i] = -1;
-            named_barrier_sync(1, 32 * t_warps);
-#pragma unroll
-            for (int u = 0; u < kEntries; ++u) {
-                take[u] = p[u];
-                if (idx[u] < 0) continue;
-                uint32_t h = (static_cast<uint32_t>(idx[u]) * 0x9E3779B1u) >> 16 & (slots - 1);
-                while (true) {  // ends: at most half the slots are taken
-                    const int32_t old = atomicCAS(&seen[h], -1, idx[u]);
-                    repeats |= old == idx[u];
-                    if (old == -1 || old == idx[u]) break;
-                    h = (h + 1) & (slots - 1);
-                }
-            }
-            // (of a repeated index, some thread has found the slot taken: all of them look)
-            if (t_warps > 1) {
-                if (lane == 0) sm.t_part[warp].x = 0.0f;
-                named_barrier_sync(1, 32 * t_warps);
-            }
-            repeats = __any_sync(0xFFFFFFFFu, repeats);
-            if (t_warps > 1) {
-                if (lane == 0 && repeats) sm.t_part[0].x = 1.0f;
-                named_barrier_sync(1, 32 * t_warps);
-                repeats = sm.t_part[0].x != 0.0f;
-            }
-        }
-    }
-    if (RESIDENT) {
-        __syncthreads();  // the vectors that were copied by hand
-        if (!mbar_wait(&sm.bar, 0, &sm.abort) && tid == 0) atomicOr(a.flag, kErrWaitTimeout);
-    }
-    float zt[kEntries];  // the entries' logits, before a gradient may overwrite them
-    if (teaches) {
-#pragma unroll
-        for (int u = 0; u < kEntries; ++u) {
-            zt[u] = 0.0f;
-            if (idx[u] >= 0) zt[u] = load_value(RESIDENT ? reinterpret_cast<const T *>(slice) + (idx[u] - e0) : z + idx[u]);
-        }
-        if (BWD && repeats) {
-#pragma unroll
-            for (int u = 0; u < kEntries; ++u) {
-                if (idx[u] < 0) continue;
-                const int j = tid + u * 32 * t_warps;
-                bool leads = true;
-                take[u] = 0.0f;
-                for (int i = 0; i < a.k; ++i)
-                    if (sidx[i] == idx[u]) {
-                        leads &= i >= j;
-                        take[u] += sp[i];
-                    }
-                if (!leads) take[u] = -1.0f;  // (no sum of probabilities: nothing to store)
-            }
-        }
-    }
-
+    const uint4 *const zv = sl.vectors();
+    // The entries' logits, before a gradient may overwrite them; the loss (rank
+    // 0) needs those of the whole row.
+    const bool whole = FWD && rank == 0;
+    if (tea.mine()) tea.read_logits(whole ? sl.z : sl.z + sl.e0, whole ? 0 : sl.e0, whole ? a.V : sl.e1);
     float m, s;
     if (FWD) {
         m = -INFINITY, s = 0.0f;  // of this thread, then of the CTA, then of the row
-        auto add = [&](const Exponent &e, const uint4 &raw) {
-            float v[kVec], part = 0.0f;
-            Vec16<T>::unpack(raw, v);
-#pragma unroll
-            for (int x = 0; x < kVec; ++x) part += e(v[x]);
-            s += part;
+        auto raise = [&](float mx) {  // the thread's maximum, and its sum with it
+            if (s != 0.0f) s *= Exponent{finite_max(mx), c}(finite_max(m));
+            m = mx;
         };
-        if (RESIDENT) {
-            for (int i = tid; i < nv; i += NT) m = fmaxf(m, Vec16<T>::max_of(slice[i]));
-            m = block_max<NT>(m, sm.row_max);
+        for (int i = sl.lo + tid; i < sl.hi; i += U * NT) {
+            uint4 raw[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u * NT < sl.hi) raw[u] = BWD ? __ldcg(zv + i + u * NT) : __ldcs(zv + i + u * NT);
+            typename Vec16<T>::Max top;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u * NT < sl.hi) top.add(raw[u]);
+            raise(fmaxf(m, top.top()));
+            Sums<T> part;
             const Exponent e{finite_max(m), c};
-#pragma unroll 2
-            for (int i = tid; i < nv; i += NT) add(e, slice[i]);
-        } else {
-            auto raise = [&](float mx) {  // the thread's maximum, and its sum with it
-                if (s != 0.0f) s *= Exponent{finite_max(mx), c}(finite_max(m));
-                m = mx;
-            };
-            for (int i = lo + tid; i < hi; i += U * NT) {
-                uint4 raw[U];
-                float mx = m;
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (i + u * NT < hi) raw[u] = __ldcs(zv + i + u * NT);
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (i + u * NT < hi) mx = fmaxf(mx, Vec16<T>::max_of(raw[u]));
-                raise(mx);
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (i + u * NT < hi) add(Exponent{finite_max(m), c}, raw[u]);
-            }
-            if (has_edge) {
-                const uint4 raw = load_edge();
-                raise(fmaxf(m, Vec16<T>::max_of(raw)));
-                add(Exponent{finite_max(m), c}, raw);
-            }
-            const float top = block_max<NT>(m, sm.row_max);
-            raise(top);
+            for (int u = 0; u < U; ++u)
+                if (i + u * NT < sl.hi) part.add(e, raw[u]);
+            s += part.total();
         }
+        if (sl.has_edge()) {
+            const uint4 raw = sl.load_edge();
+            typename Vec16<T>::Max top;
+            top.add(raw);
+            raise(fmaxf(m, top.top()));
+            Sums<T> part;
+            part.add(Exponent{finite_max(m), c}, raw);
+            s += part.total();
+        }
+        raise(warp_max(m));
         s = warp_sum(s);
-        if (lane == 0) sm.row_sum[warp] = s;
-        if (teaches) {
-            float cross = 0.0f, mass = 0.0f;
-#pragma unroll
-            for (int u = 0; u < kEntries; ++u)
-                if (idx[u] >= 0 && p[u] != 0.0f) {
-                    cross += p[u] * ((zt[u] - finite_max(m)) * inv_T);
-                    mass += p[u];
-                }
-            cross = warp_sum(cross), mass = warp_sum(mass);
-            if (lane == 0) sm.teacher[warp].x = cross, sm.teacher[warp].y = mass;
-        }
+        if (lane == 0) sm.part[warp] = make_float2(m, s);
         __syncthreads();
-        s = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kDistillWarps; ++w) s += sm.row_sum[w];
-        float4 mine = make_float4(m, s, 0.0f, 0.0f);
-        if (warp == 0)
-            for (int w = 0; w < t_warps; ++w) mine.z += sm.teacher[w].x, mine.w += sm.teacher[w].y;
-        if (slices > 1) {
-            cluster_wait();
-            if (tid < slices) cluster_store(cluster_addr(&sm.gathered[rank], tid), mine);
-            __syncwarp();
-            cluster_arrive();
-            cluster_wait();
-            // lane r: slice r; every warp joins them all, in the same order
-            mine = lane < slices ? sm.gathered[lane] : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
-            m = warp_max(mine.x);
-            const float m0 = finite_max(m), mr = finite_max(mine.x);
-            s = warp_sum(mine.y != 0.0f ? mine.y * Exponent{m0, c}(mr) : 0.0f);
-            if (rank == 0 && warp == 0) {
-                mine.z = warp_sum(mine.w != 0.0f ? mine.z + mine.w * ((mr - m0) * inv_T) : 0.0f);
-                mine.w = warp_sum(mine.w);
-            }
-        }
-        if (rank == 0 && tid == 0) {
-            float plogp = 0.0f;
-            for (int w = 0; w < t_warps; ++w) plogp += sm.teacher[w].z;
-            const float kl = s == 0.0f ? INFINITY : plogp - mine.z + mine.w * logf(s);
-            a.loss[row] = a.T * a.T * kl;
-            if (a.stats_out != nullptr) {
-                a.stats_out[2 * row] = m;
-                a.stats_out[2 * row + 1] = s;
-            }
+        if (warp == 0) send_partial(sm, slices, rank, c);
+        if (tea.mine()) tea.softmax(sm, inv_T);
+        join_partials(a, sm, slices, c, &m, &s);
+        if (rank == 0 && tea.mine()) {
+            const float loss = tea.loss(sm, a.T, inv_T, m, s);
+            if (tid == 0) write_row(a, row, loss, m, s);
         }
     } else {
         m = a.stats_in[2 * row];
         s = a.stats_in[2 * row + 1];
+        __syncthreads();  // (grad may be logits: the entries' logits are read before it is written)
     }
-
     if (BWD) {
         const Exponent e{finite_max(m), c};
         const float cg = a.T * a.grad_loss[row], inv = s == 0.0f ? 0.0f : 1.0f / s, coef = cg * inv;
-        if (!FWD) __syncthreads();  // (grad may be logits: the entries' logits are read before it is written)
-        auto grad_of = [&](const uint4 &raw, float *v) {
-            Vec16<T>::unpack(raw, v);
+        for (int i = sl.lo + tid; i < sl.hi; i += U * NT) {
+            uint4 raw[U];
 #pragma unroll
-            for (int x = 0; x < kVec; ++x) v[x] = coef * e(v[x]);
-        };
-        auto store = [&](int i, const uint4 &raw) {
-            float v[kVec];
-            grad_of(raw, v);
-            if (same_phase) gv[i] = Vec16<T>::pack(v);
-            else store_some(i, v);
-        };
-        if (RESIDENT) {
-#pragma unroll 2
-            for (int i = lo + tid; i < hi; i += NT) store(i, slice[i]);
-        } else {
-            for (int i = lo + tid; i < hi; i += U * NT) {
-                uint4 raw[U];
+            for (int u = 0; u < U; ++u)
+                if (i + u * NT < sl.hi) raw[u] = __ldcs(zv + i + u * NT);
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (i + u * NT < hi) raw[u] = __ldcs(zv + i + u * NT);
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (i + u * NT < hi) store(i + u * NT, raw[u]);
-            }
+            for (int u = 0; u < U; ++u)
+                if (i + u * NT < sl.hi) {
+                    float v[Slice<T>::kVec];
+                    gradient_of<T>(e, coef, raw[u], v);
+                    out.store(i + u * NT, v);
+                }
         }
-        if (has_edge) {
-            float v[kVec];
-            grad_of(RESIDENT ? slice[edge] : load_edge(), v);
-            store_some(edge, v);
+        if (sl.has_edge()) {
+            float v[Slice<T>::kVec];
+            gradient_of<T>(e, coef, sl.load_edge(), v);
+            out.store_values(sl.edge(), v);
+        }
+        if (tea.mine()) {
+            if (!FWD) tea.softmax(sm, inv_T);
+            tea.find_repeats(sm, sl.e0, sl.e1);
         }
         __syncthreads();
-        if (teaches) {  // q - p over what the loop above has written at the entries
-#pragma unroll
-            for (int u = 0; u < kEntries; ++u)
-                if (idx[u] >= 0 && !(take[u] < 0.0f)) store_value(g + idx[u], cg * (e(zt[u]) * inv - take[u]));
-        }
+        if (tea.mine()) tea.store_gradient(out.g, sl.e0, sl.e1, e, cg, inv);
     }
 }
 
-template <typename T, bool FWD, bool BWD, bool RESIDENT>
-static cudaError_t start_distill(const DistillParams &p, int64_t n, int slices, int64_t slice, cudaStream_t s) {
-    auto kernel = distill_kernel<T, FWD, BWD, RESIDENT>;
-    int log2_slices = 0;
-    while ((1 << log2_slices) < slices) ++log2_slices;
-    const size_t smem = static_cast<size_t>(slice) + (BWD ? 8 * static_cast<size_t>(p.k) + 4 * seen_slots(p.k) : 0);
-    cudaError_t e = cudaSuccess;
-    if (smem > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-    if (e == cudaSuccess && slices > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(n * slices));
-    cfg.blockDim = dim3(kDistillThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = static_cast<unsigned>(slices);
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = FWD && slices > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, p, log2_slices, static_cast<uint32_t>(slice));
+static int log2_of(int slices) {
+    int l = 0;
+    while ((1 << l) < slices) ++l;
+    return l;
 }
 
-// Bytes of a slice that leave room for four CTAs per SM beside it, and the
-// most that one CTA holds.
-constexpr int64_t kSliceGood = 48 * 1024, kSliceMost = 200 * 1024;
-constexpr int64_t kSliceStream = 128 * 1024;
+struct DistillLaunch {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    DistillLaunch(int threads, int slices, bool cluster, size_t smem, cudaStream_t s) {
+        cfg.blockDim = dim3(static_cast<unsigned>(threads));
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = s;
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = static_cast<unsigned>(slices);
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = cluster ? 2 : 1;
+    }
+};
+
+template <typename F>
+static cudaError_t allow(F kernel, size_t smem, int slices) {
+    cudaError_t e = cudaSuccess;
+    if (smem > 40 * 1024)
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e == cudaSuccess && slices > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return e;
+}
+
+template <typename T, bool FWD, bool BWD>
+static cudaError_t start_distill(const DistillParams &p, int64_t n, int slices, cudaStream_t s) {
+    auto kernel = distill_kernel<T, FWD, BWD>;
+    const size_t smem = 12 * static_cast<size_t>(p.k) + (BWD ? 4 * seen_slots(p.k) : 0);
+    const cudaError_t e = allow(kernel, smem, FWD ? slices : 1);
+    if (e != cudaSuccess) return e;
+    DistillLaunch l(kDistillThreads, slices, FWD, smem, s);
+    l.cfg.gridDim = dim3(static_cast<unsigned>(n * slices));
+    return cudaLaunchKernelEx(&l.cfg, kernel, p, log2_of(slices));
+}
+
+// Bytes of a slice that one CTA takes, at most, while a cluster can have more CTAs.
+constexpr int64_t kSliceBytes = 128 * 1024;
 
 template <bool FWD, bool BWD>
 static cudaError_t launch_distill(const DistillParams &p, vie_dtype dtype, int64_t n, cudaStream_t s) {
-    const int64_t bytes = static_cast<int64_t>(p.V) * dtype_size(dtype) + 32;  // with both ends' overhang
+    const int64_t bytes = static_cast<int64_t>(p.V) * dtype_size(dtype);
     int slices = 1;
-    if constexpr (FWD && BWD) {
-        const auto slice_of = [&](int c) { return (bytes / 16 + c - 1) / c * 16; };
-        while (slices < kMaxSlices && slice_of(slices) > kSliceGood) slices *= 2;
-        if (slice_of(slices) <= kSliceMost)
-            return dtype == VIE_DTYPE_BF16
-                       ? start_distill<__nv_bfloat16, FWD, BWD, true>(p, n, slices, slice_of(slices), s)
-                       : start_distill<float, FWD, BWD, true>(p, n, slices, slice_of(slices), s);
-    } else if constexpr (FWD) {
-        // enough CTAs for the chip, of 32 KB of the row or more
-        while (slices < kMaxSlices && n * slices < 1024 && bytes / slices > 32768) slices *= 2;
+    if (!FWD) {  // no partials to join
+        while (bytes / slices > kSliceBytes && n * slices < (1 << 30)) slices *= 2;
     } else {
-        // no partials to join: all of a thread's vectors in flight at once
-        while (bytes / slices > kSliceStream && n * slices < (1 << 30)) slices *= 2;
+        if (BWD)
+            while (slices < kSlices && bytes / slices > kSliceBytes) slices *= 2;
+        // enough CTAs for the chip, of 32 KB of the row or more
+        while (slices < (n <= kFewRows ? kMaxSlices : kSlices) && n * slices < 1024 && bytes / slices > 32768) slices *= 2;
     }
-    return dtype == VIE_DTYPE_BF16 ? start_distill<__nv_bfloat16, FWD, BWD, false>(p, n, slices, 0, s)
-                                   : start_distill<float, FWD, BWD, false>(p, n, slices, 0, s);
+    return dtype == VIE_DTYPE_BF16 ? start_distill<__nv_bfloat16, FWD, BWD>(p, n, slices, s)
+                                   : start_distill<float, FWD, BWD>(p, n, slices, s);
 }
 
 static vie_status check_distill(const char *fn, const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
