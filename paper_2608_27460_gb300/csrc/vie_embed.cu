@@ -12,6 +12,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <type_traits>
 
@@ -21,63 +22,365 @@
 
 namespace vie {
 
-// ---- lookup -----------------------------------------------------------------
-
 constexpr int kEmbedThreads = 256;
+constexpr int kEmbedWarps = kEmbedThreads / 32;
+
+// kW values of a row per lane.  kVector: a run of kW at 16-byte (or 8-byte)
+// addresses; otherwise 32 apart, value by value: rows of any width, pitch
+// and alignment.
+template <typename T, int kW, bool kVector>
+struct LaneRow {
+    static constexpr int kBlock = 32 * kW;  // columns per warp
+    float v[kW];
+
+    __device__ __forceinline__ static int column(int lane) { return kVector ? lane * kW : lane; }
+    __device__ __forceinline__ void load(const T *row, int c, int d) {  // c: this lane's first column
+        if constexpr (kVector) {
+            if (c < d) load_run(row + c);
+        } else {
+#pragma unroll
+            for (int w = 0; w < kW; ++w)
+                if (c + 32 * w < d) v[w] = load_value(row + c + 32 * w);
+        }
+    }
+    __device__ __forceinline__ void store(T *row, int c, int d) const {
+        if constexpr (kVector) {
+            if (c < d) store_run(row + c);
+        } else {
+#pragma unroll
+            for (int w = 0; w < kW; ++w)
+                if (c + 32 * w < d) store_value(row + c + 32 * w, v[w]);
+        }
+    }
+
+  private:
+    __device__ __forceinline__ void load_run(const float *p) {
+#pragma unroll
+        for (int w = 0; w < kW; w += 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(p + w);
+            v[w] = x.x, v[w + 1] = x.y, v[w + 2] = x.z, v[w + 3] = x.w;
+        }
+    }
+    __device__ __forceinline__ void load_run(const __nv_bfloat16 *p) {
+        if constexpr (kW == 8) {
+            Vec16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4 *>(p), v);
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2 *>(p);
+            v[0] = bf16_lo(x.x), v[1] = bf16_hi(x.x), v[2] = bf16_lo(x.y), v[3] = bf16_hi(x.y);
+        }
+    }
+    __device__ __forceinline__ void store_run(float *p) const {
+#pragma unroll
+        for (int w = 0; w < kW; w += 4) *reinterpret_cast<float4 *>(p + w) = make_float4(v[w], v[w + 1], v[w + 2], v[w + 3]);
+    }
+    __device__ __forceinline__ void store_run(__nv_bfloat16 *p) const {
+        if constexpr (kW == 8) {
+            *reinterpret_cast<uint4 *>(p) = Vec16<__nv_bfloat16>::pack(v);
+        } else {
+            const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+            *reinterpret_cast<uint2 *>(p) =
+                make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+        }
+    }
+};
+
+// ---- lookup -----------------------------------------------------------------
+// A warp per row and block of columns; bound by the bytes of the rows.
 
 struct EmbedParams {
     const void *table;
     const int32_t *tokens;
     void *out;
-    int64_t ld, ld_out, n;
-    int64_t V;
+    int64_t ld, ld_out, n, V;
     int d;
     float scale;
     uint32_t *flag;
 };
 
-template <typename TI, typename TO>
+template <typename TI, typename TO, int kW, bool kVector>
 __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedParams a) {
-    for (int64_t i = blockIdx.x; i < a.n; i += gridDim.x) {
-        const int32_t tok = a.tokens[i];
-        TO *out = static_cast<TO *>(a.out) + i * a.ld_out;
-        const bool in = tok >= 0 && tok < a.V;
-        if (tok >= a.V && threadIdx.x == 0) atomicOr(a.flag, kErrTokenIndex);
-        const TI *row = static_cast<const TI *>(a.table) + (in ? tok : 0) * a.ld;
-        if constexpr (std::is_same<TI, TO>::value) {
-            if (a.scale == 1.0f && in) {  // a copy: every bit is kept
-                for (int c = threadIdx.x; c < a.d; c += kEmbedThreads) out[c] = row[c];
-                continue;
-            }
+    constexpr int kBlock = 32 * kW, kBlocks = 4;  // a warp's columns at a time, and how many it has in flight
+    griddep_launch_dependents();
+    griddep_wait();  // the inputs may come from the kernel before this one
+    const int lane = threadIdx.x & 31;
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kEmbedWarps + (threadIdx.x >> 5);
+    if (i >= a.n) return;
+    const int32_t tok = a.tokens[i];
+    const bool in = tok >= 0 && tok < a.V;
+    if (tok >= a.V && lane == 0 && blockIdx.y == 0) atomicOr(a.flag, kErrTokenIndex);
+    const TI *row = static_cast<const TI *>(a.table) + (in ? tok : 0) * a.ld;
+    TO *out = static_cast<TO *>(a.out) + i * a.ld_out;
+    const int c0 = blockIdx.y * kBlocks * kBlock + LaneRow<TI, kW, kVector>::column(lane);
+    if constexpr (std::is_same<TI, TO>::value) {
+        if (a.scale == 1.0f) {  // a copy: every bit is kept
+            // a lane's values of a block, as kPer words
+            using Word = typename std::conditional<!kVector, TI,
+                                                   typename std::conditional<sizeof(TI) * kW == 8, uint2, uint4>::type>::type;
+            constexpr int kPer = sizeof(TI) * kW / sizeof(Word), kApart = kVector ? sizeof(Word) / sizeof(TI) : 32;
+            Word r[kBlocks][kPer];
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int x = 0; x < kPer; ++x) {
+                    r[b][x] = Word{};
+                    const int c = c0 + b * kBlock + x * kApart;
+                    if (in && c < a.d) r[b][x] = *reinterpret_cast<const Word *>(row + c);
+                }
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int x = 0; x < kPer; ++x) {
+                    const int c = c0 + b * kBlock + x * kApart;
+                    if (c < a.d) *reinterpret_cast<Word *>(out + c) = r[b][x];
+                }
+            return;
         }
-        for (int c = threadIdx.x; c < a.d; c += kEmbedThreads)
-            store_value(out + c, in ? a.scale * load_value(row + c) : 0.0f);
+    }
+    LaneRow<TI, kW, kVector> r[kBlocks];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+        if (in) r[b].load(row, c0 + b * kBlock, a.d);
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+        LaneRow<TO, kW, kVector> o;
+#pragma unroll
+        for (int w = 0; w < kW; ++w) o.v[w] = !in ? 0.0f : (a.scale == 1.0f ? r[b].v[w] : a.scale * r[b].v[w]);
+        o.store(out, c0 + b * kBlock, a.d);
     }
 }
 
-// ---- stable sort of the tokens ----------------------------------------------
-// Least significant digit first, 8 bits at a time.  A block takes kSortTile
-// consecutive pairs, its warps consecutive runs of it; a pair's place among
-// its block's pairs of the same digit follows from the warps' digit counts
-// and, inside a run, from the lanes before it with the same digit.
+// ---- tokens in order: entries (token, position) sorted by a key of the token,
+// then by position.  Entries of tokens outside [0, V) come last, as token V.
 
+using Entry = uint64_t;
+__device__ __forceinline__ Entry make_entry(uint32_t tok, uint32_t pos) { return static_cast<uint64_t>(tok) << 32 | pos; }
+__device__ __forceinline__ uint32_t entry_token(Entry e) { return static_cast<uint32_t>(e >> 32); }
+__device__ __forceinline__ uint32_t entry_pos(Entry e) { return static_cast<uint32_t>(e); }
+
+// The places of a warp's 32 entries, by digit: *at is where the warp's next
+// entry of a lane's digit goes.  Lanes without an entry: NULL, and a digit that
+// no other has.
+__device__ __forceinline__ uint32_t claim_place(uint32_t *at, uint32_t digit) {
+    const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
+    const uint32_t before = __popc(same & ((1u << (threadIdx.x & 31)) - 1u));
+    uint32_t place = 0;
+    if (at != nullptr) place = *at + before;
+    __syncwarp();
+    if (at != nullptr && before == 0) *at += __popc(same);
+    __syncwarp();
+    return place;
+}
+
+// Up to kGroupMax tokens: one kernel whose CTAs share nothing.  CTA b takes the
+// tokens with tok % 128 = b: it reads all tokens (they come from L2), keeps its
+// own in order, counts those of the CTAs before it, which gives the place of
+// its output, and sorts its own by tok / 128, 6 bits at a time.  Frequent
+// tokens often have neighbouring numbers, so this spreads them; a CTA with
+// more entries than fit its shared memory sorts in the output arrays.
+// More CTAs, if asked for, clear the gradient table meanwhile.
+constexpr int kBuckets = 128, kBucketBits = 7, kDigitBits = 6, kDigits = 1 << kDigitBits;
+constexpr int kGroupThreads = 1024, kGroupWarps = kGroupThreads / 32;  // (a lane per warp's count)
+static_assert(kGroupWarps == 32, "a warp's lanes hold the warps' counts");
+constexpr int kGroupCap = 2048;  // entries per list in shared memory
+constexpr int64_t kGroupMax = 131072;
+
+// Counter of a digit in a warp; a warp's counters lie in different banks.
+__device__ __forceinline__ int counter(int digit, int warp) { return digit * kGroupWarps + ((warp + digit) & (kGroupWarps - 1)); }
+
+// The counters as exclusive prefix sums, by digit, then by warp.  part: a word per warp.
+__device__ __forceinline__ void scan_counters(uint32_t *at, uint32_t *part) {
+    constexpr int kPer = kGroupWarps * kDigits / kGroupThreads;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t c[kPer], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int l = threadIdx.x * kPer + i;
+        c[i] = at[counter(l / kGroupWarps, l % kGroupWarps)];
+        sum += c[i];
+    }
+    uint32_t incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += x;
+    }
+    if (lane == 31) part[warp] = incl;
+    __syncthreads();
+    const uint32_t p = part[lane];
+    uint32_t run = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? p : 0) + incl - sum;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int l = threadIdx.x * kPer + i;
+        at[counter(l / kGroupWarps, l % kGroupWarps)] = run;
+        run += c[i];
+    }
+    __syncthreads();
+}
+
+struct GroupParams {
+    const int32_t *tokens;
+    Entry *sorted, *other;
+    uint32_t *flag;
+    uint32_t n, V;
+    int passes;
+    void *fill;          // rows to clear, or NULL
+    int64_t fill_pitch;  // bytes
+    int64_t fill_row;    // bytes per row, a multiple of 2
+};
+
+__device__ __forceinline__ void clear_bytes(unsigned char *p, int64_t bytes, int64_t at, int64_t step) {
+    // p and bytes are multiples of 2; the 16-byte middle by vectors
+    const int64_t head = min(static_cast<int64_t>(-reinterpret_cast<uintptr_t>(p) & 15u), bytes);
+    const int64_t vectors = (bytes - head) / 16;
+    for (int64_t i = at; i < vectors; i += step) reinterpret_cast<uint4 *>(p + head)[i] = make_uint4(0, 0, 0, 0);
+    const int64_t rest = (bytes - vectors * 16) / 2;  // 2-byte values outside it
+    for (int64_t i = at; i < rest; i += step) {
+        const int64_t o = 2 * i < head ? 2 * i : 2 * i + vectors * 16;
+        *reinterpret_cast<uint16_t *>(p + o) = 0;
+    }
+}
+
+// Rows of a table, cut into pieces that CTA `part` of `parts` clears.
+__device__ __forceinline__ void clear_rows(const GroupParams &a, int64_t part, int64_t parts) {
+    unsigned char *p = static_cast<unsigned char *>(a.fill);
+    if (a.fill_pitch == a.fill_row) {
+        const int64_t bytes = a.fill_row * a.V, per = ((bytes + parts - 1) / parts + 15) / 16 * 16;
+        const int64_t lo = min(part * per, bytes), hi = min(lo + per, bytes);
+        clear_bytes(p + lo, hi - lo, threadIdx.x, blockDim.x);
+    } else {
+        const int64_t per = (a.V + parts - 1) / parts, hi = min((part + 1) * per, static_cast<int64_t>(a.V));
+        for (int64_t r = part * per + (threadIdx.x >> 5); r < hi; r += blockDim.x >> 5)
+            clear_bytes(p + r * a.fill_pitch, a.fill_row, threadIdx.x & 31, 32);
+    }
+}
+
+__global__ void __launch_bounds__(kGroupThreads, 2) group_tokens_kernel(const GroupParams a) {
+    __shared__ Entry list[2][kGroupCap];
+    __shared__ uint32_t at[kGroupWarps * kDigits];  // [digit][warp], then where each warp's next entry goes
+    __shared__ uint32_t part[kGroupWarps], below;
+    griddep_launch_dependents();
+    griddep_wait();  // the inputs may come from the kernel before this one
+    if (blockIdx.x >= kBuckets) {
+        clear_rows(a, blockIdx.x - kBuckets, gridDim.x - kBuckets);
+        return;
+    }
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t bucket = blockIdx.x;
+    // each warp: a run of tokens, 128 (4 per lane) at a time
+    const uint32_t run = ((a.n + kGroupWarps - 1) / kGroupWarps + 127) / 128 * 128;
+    const uint32_t lo = warp * run, hi = min(lo + run, a.n);
+    const bool aligned = (reinterpret_cast<uintptr_t>(a.tokens) & 15u) == 0;
+    auto load4 = [&](uint32_t i, uint32_t *t) {  // tokens i .. i + 3; those outside [0, V): none
+        int4 x = make_int4(-1, -1, -1, -1);
+        if (aligned && i + 4 <= hi) {
+            x = *reinterpret_cast<const int4 *>(a.tokens + i);
+        } else {
+            if (i < hi) x.x = a.tokens[i];
+            if (i + 1 < hi) x.y = a.tokens[i + 1];
+            if (i + 2 < hi) x.z = a.tokens[i + 2];
+            if (i + 3 < hi) x.w = a.tokens[i + 3];
+        }
+        t[0] = static_cast<uint32_t>(x.x), t[1] = static_cast<uint32_t>(x.y);
+        t[2] = static_cast<uint32_t>(x.z), t[3] = static_cast<uint32_t>(x.w);
+    };
+    uint32_t mine = 0, before = 0;
+    bool beyond = false;
+#pragma unroll 4
+    for (uint32_t i = lo + 4 * lane; i < hi; i += 128) {
+        uint32_t t[4];
+        load4(i, t);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const bool in = t[x] < a.V;
+            beyond |= !in && t[x] < 0x80000000u;
+            mine += in && (t[x] & (kBuckets - 1)) == bucket;
+            before += in && (t[x] & (kBuckets - 1)) < bucket;
+        }
+    }
+    if (beyond && bucket == 0) atomicOr(a.flag, kErrTokenIndex);
+    mine = __reduce_add_sync(0xFFFFFFFFu, mine);
+    before = __reduce_add_sync(0xFFFFFFFFu, before);
+    if (tid == 0) below = 0;
+    __syncthreads();
+    if (lane == 0) {
+        part[warp] = mine;
+        atomicAdd(&below, before);
+    }
+    __syncthreads();
+    const uint32_t in_warp = part[lane];
+    const uint32_t count = __reduce_add_sync(0xFFFFFFFFu, in_warp);
+    uint32_t next = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? in_warp : 0);
+    Entry *const out = a.sorted + below;
+    if (bucket == kBuckets - 1)
+        for (uint32_t i = below + count + tid; i < a.n; i += kGroupThreads) a.sorted[i] = make_entry(a.V, 0);
+    // the lists that the passes go between; the last one to write is `out`, or is copied there
+    const bool small = count <= kGroupCap;
+    Entry *from = small ? list[0] : ((a.passes & 1) ? a.other + below : out);
+    Entry *to = small ? list[1] : ((a.passes & 1) ? out : a.other + below);
+    for (uint32_t i0 = lo; i0 < hi; i0 += 128) {  // the same for all lanes
+        const uint32_t i = i0 + 4 * lane;
+        uint32_t t[4], m[4], mask[4];
+        load4(i, t);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            m[x] = t[x] < a.V && (t[x] & (kBuckets - 1)) == bucket;
+            mask[x] = __ballot_sync(0xFFFFFFFFu, m[x]);
+        }
+        uint32_t o = next;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            o += __popc(mask[x] & ((1u << lane) - 1u));
+            next += __popc(mask[x]);
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            if (m[x]) from[o++] = make_entry(t[x], i + x);
+    }
+    __syncthreads();
+    const uint32_t chunk = ((count + kGroupWarps - 1) / kGroupWarps + 31) / 32 * 32;  // per warp
+    const uint32_t c0 = min(warp * chunk, count), c1 = min(c0 + chunk, count);
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const int shift = kBucketBits + pass * kDigitBits;
+        auto digit_of = [&](Entry e) { return (entry_token(e) >> shift) & (kDigits - 1); };
+        for (int i = tid; i < kGroupWarps * kDigits; i += kGroupThreads) at[i] = 0;
+        __syncthreads();
+        for (uint32_t i = c0 + lane; i < c1; i += 32) atomicAdd(&at[counter(digit_of(from[i]), warp)], 1u);
+        __syncthreads();
+        scan_counters(at, part);
+        for (uint32_t i0 = c0; i0 < c1; i0 += 32) {
+            const uint32_t i = i0 + lane;
+            const bool in = i < c1;
+            const Entry e = in ? from[i] : 0;
+            const uint32_t place = claim_place(in ? &at[counter(digit_of(e), warp)] : nullptr, in ? digit_of(e) : kDigits);
+            if (in) to[place] = e;
+        }
+        __syncthreads();
+        Entry *const swap = from;
+        from = to;
+        to = swap;
+    }
+    if (small)
+        for (uint32_t i = tid; i < count; i += kGroupThreads) out[i] = from[i];
+}
+
+// More tokens: a sort over the whole array, least significant digit first, 8
+// bits at a time, in three launches per pass.
 constexpr int kSortThreads = 256, kSortWarps = kSortThreads / 32, kSortRounds = 8;
 constexpr int kSortTile = kSortThreads * kSortRounds;
 
 struct SortPass {
     const int32_t *tokens;  // first pass: the caller's tokens, else NULL
-    const uint32_t *key_in, *pos_in;
-    uint32_t *key_out, *pos_out;
+    const Entry *from;
+    Entry *to;
     uint32_t *counts;  // [256][blocks]
     uint32_t n, blocks, V, shift;
     uint32_t *flag;
 };
 
-// Tokens outside [0, V) sort behind all others, as V.
-__device__ __forceinline__ uint32_t sort_key(const SortPass &a, uint32_t i) {
-    if (a.tokens == nullptr) return a.key_in[i];
-    const int32_t tok = a.tokens[i];
-    return tok >= 0 && static_cast<uint32_t>(tok) < a.V ? static_cast<uint32_t>(tok) : a.V;
+__device__ __forceinline__ Entry sort_entry(const SortPass &a, uint32_t i) {
+    if (a.tokens == nullptr) return a.from[i];
+    const uint32_t tok = static_cast<uint32_t>(a.tokens[i]);
+    return make_entry(tok < a.V ? tok : a.V, i);
 }
 
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortPass a) {
@@ -89,7 +392,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortPass
         if (i >= a.n) continue;
         if (a.tokens != nullptr && a.tokens[i] >= 0 && static_cast<uint32_t>(a.tokens[i]) >= a.V)
             atomicOr(a.flag, kErrTokenIndex);
-        atomicAdd(&count[(sort_key(a, i) >> a.shift) & 255u], 1u);
+        atomicAdd(&count[(entry_token(sort_entry(a, i)) >> a.shift) & 255u], 1u);
     }
     __syncthreads();
     a.counts[static_cast<size_t>(threadIdx.x) * a.blocks + blockIdx.x] = count[threadIdx.x];
@@ -129,7 +432,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortPa
     const uint32_t run = blockIdx.x * kSortTile + warp * (kSortTile / kSortWarps);
     for (int r = 0; r < kSortRounds; ++r) {
         const uint32_t i = run + r * 32 + lane;
-        if (i < a.n) atomicAdd(&at[warp][(sort_key(a, i) >> a.shift) & 255u], 1u);
+        if (i < a.n) atomicAdd(&at[warp][(entry_token(sort_entry(a, i)) >> a.shift) & 255u], 1u);
     }
     __syncthreads();
     {
@@ -144,88 +447,215 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortPa
     for (int r = 0; r < kSortRounds; ++r) {
         const uint32_t i = run + r * 32 + lane;
         const bool in = i < a.n;
-        const uint32_t key = in ? sort_key(a, i) : 0;
-        const uint32_t digit = in ? (key >> a.shift) & 255u : 256u;
-        const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
-        const uint32_t before = __popc(same & ((1u << lane) - 1u));
-        uint32_t to = 0;
-        if (in) to = at[warp][digit] + before;
-        __syncwarp();
-        if (in && before == 0) at[warp][digit] += __popc(same);
-        __syncwarp();
-        if (in) {
-            a.key_out[to] = key;
-            a.pos_out[to] = a.tokens != nullptr ? i : a.pos_in[i];
-        }
+        const Entry e = in ? sort_entry(a, i) : 0;
+        const uint32_t digit = (entry_token(e) >> a.shift) & 255u;
+        const uint32_t to = claim_place(in ? &at[warp][digit] : nullptr, in ? digit : 256u);
+        if (in) a.to[to] = e;
     }
 }
 
 // ---- sums over the runs of equal tokens -------------------------------------
+// A warp takes `chunk` sorted entries and a block of columns and adds the rows
+// up in order, eight of them in flight.  A token whose run lies within the
+// chunk is done; a run that goes on beyond either end leaves the chunk's
+// part of its sum in the workspace (0: of a run that began before the chunk, 1:
+// of one that begins in it), and join_runs_kernel adds the parts up in order.
 
 struct GradParams {
-    const uint32_t *key, *pos;  // sorted
+    const Entry *sorted;
     const void *grad;
     void *out;
+    float *parts;  // [chunks][2][d]
     int64_t ld_grad, ld;
-    uint32_t n, V;
+    uint32_t n, V, chunk;
     int d, accumulate;
     float scale;
 };
 
-// One CTA per sorted position; the first of a run sums it.
-template <typename TI, typename TO>
-__global__ void __launch_bounds__(kEmbedThreads) embed_grad_kernel(const GradParams a) {
-    const uint32_t i = blockIdx.x, key = a.key[i];
-    if (key >= a.V || (i > 0 && a.key[i - 1] == key)) return;
-    TO *out = static_cast<TO *>(a.out) + static_cast<int64_t>(key) * a.ld;
-    for (int c = threadIdx.x; c < a.d; c += kEmbedThreads) {
-        float sum = 0.0f;
-        for (uint32_t j = i; j < a.n && a.key[j] == key; ++j)
-            sum += load_value(static_cast<const TI *>(a.grad) + a.pos[j] * a.ld_grad + c);
-        sum *= a.scale;
-        if (a.accumulate) sum += load_value(out + c);
-        store_value(out + c, sum);
-    }
+template <typename T, int kW, bool kVector>
+__device__ __forceinline__ void put_row(const GradParams &a, uint32_t tok, int c, const float *sum) {
+    T *row = static_cast<T *>(a.out) + static_cast<int64_t>(tok) * a.ld;
+    LaneRow<T, kW, kVector> o;
+    if (a.accumulate) o.load(row, c, a.d);
+#pragma unroll
+    for (int w = 0; w < kW; ++w) o.v[w] = a.accumulate ? a.scale * sum[w] + o.v[w] : a.scale * sum[w];
+    o.store(row, c, a.d);
 }
 
+template <typename TI, typename TO, int kW, bool kVector>
+__global__ void __launch_bounds__(kEmbedThreads) sum_runs_kernel(const GradParams a) {
+    constexpr int kRows = 8;
+    griddep_launch_dependents();
+    griddep_wait();
+    const int lane = threadIdx.x & 31;
+    const uint32_t chunk = blockIdx.x * kEmbedWarps + (threadIdx.x >> 5);
+    const uint32_t lo = chunk * a.chunk;
+    if (lo >= a.n) return;
+    const uint32_t hi = min(lo + a.chunk, a.n);
+    const int c = blockIdx.y * 32 * kW + LaneRow<TI, kW, kVector>::column(lane);
+    const uint32_t before = lo > 0 ? entry_token(a.sorted[lo - 1]) : 0xFFFFFFFFu;
+    const uint32_t after = hi < a.n ? entry_token(a.sorted[hi]) : 0xFFFFFFFFu;
+    uint32_t cur = 0xFFFFFFFFu;  // the run's token
+    bool from_before = false;
+    float acc[kW];
+    auto close = [&](bool goes_on) {
+        if (cur >= a.V) return;  // none
+        if (from_before || goes_on) {
+            float *part = a.parts + (static_cast<int64_t>(chunk) * 2 + (from_before ? 0 : 1)) * a.d;
+#pragma unroll
+            for (int w = 0; w < kW; ++w) {
+                const int col = kVector ? c + w : c + 32 * w;
+                if (col < a.d) part[col] = acc[w];
+            }
+        } else {
+            put_row<TO, kW, kVector>(a, cur, c, acc);
+        }
+    };
+    for (uint32_t i0 = lo; i0 < hi; i0 += 32) {
+        const Entry e = i0 + lane < hi ? a.sorted[i0 + lane] : make_entry(a.V, 0);
+        const uint32_t count = min(hi - i0, 32u);
+        if (__shfl_sync(0xFFFFFFFFu, entry_token(e), 0) >= a.V) break;  // only empty slots from here on
+        for (uint32_t r0 = 0; r0 < count; r0 += kRows) {
+            uint32_t tok[kRows];
+            LaneRow<TI, kW, kVector> row[kRows];
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) {
+                tok[u] = __shfl_sync(0xFFFFFFFFu, entry_token(e), r0 + u);
+                const uint32_t pos = __shfl_sync(0xFFFFFFFFu, entry_pos(e), r0 + u);
+                if (tok[u] < a.V) row[u].load(static_cast<const TI *>(a.grad) + pos * a.ld_grad, c, a.d);
+            }
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) {
+                if (tok[u] != cur) {
+                    close(false);
+                    cur = tok[u];
+                    from_before = cur == before && i0 + r0 + u == lo;
+#pragma unroll
+                    for (int w = 0; w < kW; ++w) acc[w] = 0.0f;
+                }
+                if (tok[u] < a.V) {
+#pragma unroll
+                    for (int w = 0; w < kW; ++w) acc[w] += row[u].v[w];
+                }
+            }
+        }
+    }
+    close(cur == after);
+}
+
+// One warp per chunk and block of columns: if a run begins in the chunk and goes
+// on beyond it, its parts' sum.
+template <typename TO, int kW, bool kVector>
+__global__ void __launch_bounds__(kEmbedThreads) join_runs_kernel(const GradParams a) {
+    griddep_launch_dependents();
+    griddep_wait();
+    const int lane = threadIdx.x & 31;
+    const uint32_t chunk = blockIdx.x * kEmbedWarps + (threadIdx.x >> 5);
+    const uint64_t lo = static_cast<uint64_t>(chunk) * a.chunk, hi = lo + a.chunk;
+    if (hi >= a.n) return;
+    const uint32_t tok = entry_token(a.sorted[hi - 1]);
+    if (tok >= a.V || entry_token(a.sorted[hi]) != tok) return;
+    if (entry_token(a.sorted[lo]) == tok && lo > 0 && entry_token(a.sorted[lo - 1]) == tok) return;  // began before
+    const int c = blockIdx.y * 32 * kW + LaneRow<TO, kW, kVector>::column(lane);
+    float acc[kW];
+    auto add = [&](int64_t part, bool first) {
+        const float *p = a.parts + part * a.d;
+#pragma unroll
+        for (int w = 0; w < kW; ++w) {
+            const int col = kVector ? c + w : c + 32 * w;
+            const float v = col < a.d ? p[col] : 0.0f;
+            acc[w] = first ? v : acc[w] + v;
+        }
+    };
+    add(2 * static_cast<int64_t>(chunk) + 1, true);
+    for (uint32_t j0 = chunk + 1;; j0 += 32) {  // chunks that begin with the run
+        const uint64_t at = (static_cast<uint64_t>(j0) + lane) * a.chunk;
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, at < a.n && entry_token(a.sorted[at < a.n ? at : 0]) == tok);
+        const int m = mask == 0xFFFFFFFFu ? 32 : __ffs(~mask) - 1;
+#pragma unroll 8
+        for (int j = 0; j < m; ++j) add(2 * (static_cast<int64_t>(j0) + j), false);
+        if (m < 32) break;
+    }
+    put_row<TO, kW, kVector>(a, tok, c, acc);
+}
+
+// Workspace: the entries twice, the counts of the large sort, the parts of runs.
 struct GradWorkspace {
-    uint32_t blocks;
-    int64_t key, pos, counts, bytes;  // offsets: two arrays of n each for keys and positions
+    uint32_t blocks, chunk, chunks;
+    int64_t entries, counts, parts, bytes;  // offsets (entries: of the second array)
 };
 
-static GradWorkspace grad_workspace(int64_t n) {
+static GradWorkspace grad_workspace(int64_t n, int32_t d) {
+    auto round_up = [](int64_t v) { return (v + 255) / 256 * 256; };
     GradWorkspace w;
-    const int64_t arr = (4 * n + 255) / 256 * 256;
-    w.blocks = static_cast<uint32_t>((n + kSortTile - 1) / kSortTile);
-    w.key = 0;
-    w.pos = 2 * arr;
-    w.counts = 4 * arr;
-    w.bytes = w.counts + int64_t(w.blocks) * 1024;
+    w.blocks = n > kGroupMax ? static_cast<uint32_t>((n + kSortTile - 1) / kSortTile) : 0;
+    // 32 rows per warp fill the chip from a few thousand tokens on; longer
+    // chunks keep the parts of one very frequent token few
+    w.chunk = 32;
+    while (n / w.chunk > 16384) w.chunk *= 2;
+    w.chunks = static_cast<uint32_t>((n + w.chunk - 1) / w.chunk);
+    w.entries = round_up(8 * n);
+    w.counts = 2 * w.entries;
+    w.parts = w.counts + round_up(int64_t(w.blocks) * 1024);
+    // never more for fewer tokens: a program keeps one for its longest batch
+    w.bytes = w.parts + std::min<int64_t>((n + 31) / 32, 16385) * 8 * d;
     return w;
 }
 
-template <typename TI, typename TO>
-static void start_grad(const GradParams &p, cudaStream_t s) {
-    embed_grad_kernel<TI, TO><<<p.n, kEmbedThreads, 0, s>>>(p);
-}
-template <typename TI, typename TO>
-static void start_embed(const EmbedParams &p, cudaStream_t s) {
-    const unsigned grid = static_cast<unsigned>(p.n < 65536 ? p.n : 65536);
-    embed_kernel<TI, TO><<<grid, kEmbedThreads, 0, s>>>(p);
+// Launches a kernel that may start while the one before it ends.
+template <typename F, typename... A>
+static cudaError_t chain(F kernel, dim3 grid, int threads, cudaStream_t s, const A &...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// f<TI, TO>(p, s) for the two storage types.
-#define VIE_BY_TYPES(f, in, out, p, s)                                      \
-    do {                                                                    \
-        if ((in) == VIE_DTYPE_BF16 && (out) == VIE_DTYPE_BF16)              \
-            f<__nv_bfloat16, __nv_bfloat16>(p, s);                          \
-        else if ((in) == VIE_DTYPE_BF16)                                    \
-            f<__nv_bfloat16, float>(p, s);                                  \
-        else if ((out) == VIE_DTYPE_BF16)                                   \
-            f<float, __nv_bfloat16>(p, s);                                  \
-        else                                                                \
-            f<float, float>(p, s);                                          \
-    } while (0)
+template <typename TI, typename TO, int kW, bool kVector>
+static cudaError_t start_sums(const GradParams &p, uint32_t chunks, cudaStream_t s) {
+    const dim3 grid((chunks + kEmbedWarps - 1) / kEmbedWarps, static_cast<unsigned>((p.d + 32 * kW - 1) / (32 * kW)));
+    cudaError_t e = chain(sum_runs_kernel<TI, TO, kW, kVector>, grid, kEmbedThreads, s, p);
+    if (e == cudaSuccess && chunks > 1) e = chain(join_runs_kernel<TO, kW, kVector>, grid, kEmbedThreads, s, p);
+    return e;
+}
+template <typename TI, typename TO, int kW, bool kVector>
+static cudaError_t start_embed(const EmbedParams &p, cudaStream_t s) {
+    const dim3 grid(static_cast<unsigned>((p.n + kEmbedWarps - 1) / kEmbedWarps),
+                    static_cast<unsigned>((p.d + 128 * kW - 1) / (128 * kW)));
+    return chain(embed_kernel<TI, TO, kW, kVector>, grid, kEmbedThreads, s, p);
+}
+
+// How rows of two matrices are read and written: 8 values per lane where both
+// allow 16-byte vectors of bf16 (or two of fp32) and rows are wide, 4 where
+// they are narrow or all fp32, value by value otherwise.
+enum class Access { kWide, kNarrow, kValues };
+static Access access_of(const void *a, vie_dtype ta, int64_t lda, const void *b, vie_dtype tb, int64_t ldb, int d) {
+    auto fits = [&](const void *p, vie_dtype t, int64_t ld, int w) {
+        const int bytes = w * dtype_size(t) < 16 ? w * dtype_size(t) : 16;
+        return aligned_to(p, static_cast<uintptr_t>(bytes)) && ld * dtype_size(t) % bytes == 0 && d % w == 0;
+    };
+    if ((ta == VIE_DTYPE_BF16 || tb == VIE_DTYPE_BF16) && d > 128 && fits(a, ta, lda, 8) && fits(b, tb, ldb, 8))
+        return Access::kWide;
+    return fits(a, ta, lda, 4) && fits(b, tb, ldb, 4) ? Access::kNarrow : Access::kValues;
+}
+
+#define VIE_BY_ACCESS(f, TI, TO, access, ...)                                \
+    ((access) == Access::kWide     ? f<TI, TO, 8, true>(__VA_ARGS__)         \
+     : (access) == Access::kNarrow ? f<TI, TO, 4, true>(__VA_ARGS__)         \
+                                   : f<TI, TO, 8, false>(__VA_ARGS__))
+// f<TI, TO, kW, kVector>(...) for two storage types and how rows are accessed.
+#define VIE_BY_TYPES(f, in, out, access, ...)                                                          \
+    ((in) == VIE_DTYPE_BF16                                                                            \
+         ? ((out) == VIE_DTYPE_BF16 ? VIE_BY_ACCESS(f, __nv_bfloat16, __nv_bfloat16, access, __VA_ARGS__) \
+                                    : VIE_BY_ACCESS(f, __nv_bfloat16, float, access, __VA_ARGS__))     \
+         : ((out) == VIE_DTYPE_BF16 ? VIE_BY_ACCESS(f, float, __nv_bfloat16, access, __VA_ARGS__)      \
+                                    : VIE_BY_ACCESS(f, float, float, access, __VA_ARGS__)))
 
 static vie_status check_embed(const char *fn, const int32_t *tokens, int64_t n, int64_t V, int32_t d) {
     if (n < 0 || n > VIE_MANY_MAX)
@@ -256,8 +686,8 @@ vie_status vie_embed(const void *table, vie_dtype dtype, int64_t V, int32_t d, i
     p.scale = scale;
     cudaError_t e = device_flag_word(&p.flag);
     if (e != cudaSuccess) return fail_cuda(e, fn);
-    VIE_BY_TYPES(start_embed, dtype, out_dtype, p, static_cast<cudaStream_t>(stream));
-    e = cudaGetLastError();
+    e = VIE_BY_TYPES(start_embed, dtype, out_dtype, access_of(table, dtype, ld, out, out_dtype, ld_out, d), p,
+                     static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
 
@@ -267,7 +697,7 @@ vie_status vie_embed_grad_workspace(int64_t n, int64_t V, int32_t d, int64_t *by
     const vie_status st = check_embed(fn, &some, n, V, d);
     if (st != VIE_OK) return st;
     if (bytes == nullptr) return fail(VIE_ERR_INVALID_ARG, "%s: bytes is NULL", fn);
-    *bytes = grad_workspace(n).bytes;
+    *bytes = grad_workspace(n, d).bytes;
     return VIE_OK;
 }
 
@@ -279,43 +709,58 @@ vie_status vie_embed_grad(const int32_t *tokens, int64_t n, const void *grad, vi
     if (st == VIE_OK) st = check_matrix(fn, "grad", grad, dtype, n, d, ld_grad);
     if (st == VIE_OK) st = check_matrix(fn, "out", out, out_dtype, V, d, ld);
     if (st != VIE_OK) return st;
-    const GradWorkspace w = grad_workspace(n);
+    const GradWorkspace w = grad_workspace(n, d);
     if (n > 0 && (workspace == nullptr || workspace_bytes < w.bytes || !aligned_to(workspace, 16)))
         return fail(VIE_ERR_INVALID_ARG, "%s: workspace must be %lld bytes, 16-byte aligned (it has %lld)", fn,
                     static_cast<long long>(w.bytes), static_cast<long long>(workspace == nullptr ? 0 : workspace_bytes));
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int64_t row = int64_t(d) * dtype_size(out_dtype), pitch = ld * dtype_size(out_dtype);
+    const bool grouped = n <= kGroupMax;
     cudaError_t e = cudaSuccess;
-    if (!accumulate) {
-        const size_t row = static_cast<size_t>(d) * dtype_size(out_dtype);
-        const size_t pitch = static_cast<size_t>(ld) * dtype_size(out_dtype);
-        e = pitch == row ? cudaMemsetAsync(out, 0, row * V, s) : cudaMemset2DAsync(out, pitch, 0, row, V, s);
+    if (!accumulate && (n == 0 || !grouped)) {
+        e = pitch == row ? cudaMemsetAsync(out, 0, static_cast<size_t>(row * V), s)
+                         : cudaMemset2DAsync(out, static_cast<size_t>(pitch), 0, static_cast<size_t>(row),
+                                             static_cast<size_t>(V), s);
         if (e != cudaSuccess) return fail_cuda(e, fn);
     }
     if (n == 0) return VIE_OK;
     unsigned char *ws = static_cast<unsigned char *>(workspace);
-    uint32_t *key[2], *pos[2];
-    for (int i = 0; i < 2; ++i) {
-        key[i] = reinterpret_cast<uint32_t *>(ws + w.key) + i * (w.pos / 8);
-        pos[i] = reinterpret_cast<uint32_t *>(ws + w.pos) + i * (w.pos / 8);
-    }
-    SortPass a = {};
-    a.counts = reinterpret_cast<uint32_t *>(ws + w.counts);
-    a.n = static_cast<uint32_t>(n), a.blocks = w.blocks, a.V = static_cast<uint32_t>(V);
-    e = device_flag_word(&a.flag);
+    Entry *entries[2] = {reinterpret_cast<Entry *>(ws), reinterpret_cast<Entry *>(ws + w.entries)};
+    uint32_t *flag = nullptr;
+    e = device_flag_word(&flag);
     if (e != cudaSuccess) return fail_cuda(e, fn);
-    int to = 0;
-    for (a.shift = 0; a.shift < 32 && (V >> a.shift) != 0; a.shift += 8, to ^= 1) {
-        a.tokens = a.shift == 0 ? tokens : nullptr;
-        a.key_in = key[to ^ 1], a.pos_in = pos[to ^ 1], a.key_out = key[to], a.pos_out = pos[to];
-        sort_count_kernel<<<w.blocks, kSortThreads, 0, s>>>(a);
-        sort_scan_kernel<<<1, 1024, 0, s>>>(a.counts, 256 * w.blocks);
-        sort_scatter_kernel<<<w.blocks, kSortThreads, 0, s>>>(a);
+    int sorted = 0;
+    if (grouped) {
+        GroupParams g = {};
+        g.tokens = tokens, g.sorted = entries[0], g.other = entries[1], g.flag = flag;
+        g.n = static_cast<uint32_t>(n), g.V = static_cast<uint32_t>(V);
+        while (((V - 1) >> kBucketBits) >> (g.passes * kDigitBits)) ++g.passes;
+        unsigned clearing = 0;
+        if (!accumulate) {
+            g.fill = out, g.fill_pitch = pitch, g.fill_row = row;
+            clearing = static_cast<unsigned>(std::min<int64_t>(4096, (row * V + (1 << 17) - 1) >> 17));  // 128 KB each
+        }
+        e = chain(group_tokens_kernel, dim3(kBuckets + clearing), kGroupThreads, s, g);
+    } else {
+        SortPass a = {};
+        a.counts = reinterpret_cast<uint32_t *>(ws + w.counts);
+        a.n = static_cast<uint32_t>(n), a.blocks = w.blocks, a.V = static_cast<uint32_t>(V), a.flag = flag;
+        for (a.shift = 0; a.shift < 32 && (V >> a.shift) != 0; a.shift += 8) {
+            a.tokens = a.shift == 0 ? tokens : nullptr;
+            a.from = entries[sorted], a.to = entries[sorted ^ 1];
+            sorted ^= 1;
+            sort_count_kernel<<<w.blocks, kSortThreads, 0, s>>>(a);
+            sort_scan_kernel<<<1, 1024, 0, s>>>(a.counts, 256 * w.blocks);
+            sort_scatter_kernel<<<w.blocks, kSortThreads, 0, s>>>(a);
+        }
+        e = cudaGetLastError();
     }
+    if (e != cudaSuccess) return fail_cuda(e, fn);
     GradParams p = {};
-    p.key = key[to ^ 1], p.pos = pos[to ^ 1], p.grad = grad, p.out = out, p.ld_grad = ld_grad, p.ld = ld;
-    p.n = a.n, p.V = a.V, p.d = d, p.accumulate = accumulate != 0, p.scale = scale;
-    VIE_BY_TYPES(start_grad, dtype, out_dtype, p, s);
-    e = cudaGetLastError();
+    p.sorted = entries[sorted], p.grad = grad, p.out = out, p.parts = reinterpret_cast<float *>(ws + w.parts);
+    p.ld_grad = ld_grad, p.ld = ld, p.n = static_cast<uint32_t>(n), p.V = static_cast<uint32_t>(V), p.chunk = w.chunk;
+    p.d = d, p.accumulate = accumulate != 0, p.scale = scale;
+    e = VIE_BY_TYPES(start_sums, dtype, out_dtype, access_of(grad, dtype, ld_grad, out, out_dtype, ld, d), p, w.chunks, s);
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
 
