@@ -24,64 +24,62 @@ namespace vie {
 
 constexpr int kEmbedThreads = 256;
 constexpr int kEmbedWarps = kEmbedThreads / 32;
+constexpr int kEmbedBlocks = 4;  // blocks of columns that a lookup's warp has in flight
 
-// kW values of a row per lane.  kVector: a run of kW at 16-byte (or 8-byte)
-// addresses; otherwise 32 apart, value by value: rows of any width, pitch
-// and alignment.
+// kW values of a row per lane, as loaded.  kVector: a run of kW at 16-byte (or
+// 8-byte) addresses; otherwise 32 apart, value by value: rows of any width,
+// pitch and alignment.  Loads do not branch: a lane beyond the row reads the
+// row's first values.
 template <typename T, int kW, bool kVector>
 struct LaneRow {
-    static constexpr int kBlock = 32 * kW;  // columns per warp
-    float v[kW];
+    using Word = typename std::conditional<!kVector, T, typename std::conditional<sizeof(T) * kW == 8, uint2, uint4>::type>::type;
+    static constexpr int kWords = sizeof(T) * kW / sizeof(Word);
+    static constexpr int kApart = kVector ? sizeof(Word) / sizeof(T) : 32;  // columns from word to word
+    static constexpr int kBlock = 32 * kW;                                  // columns per warp
+    Word r[kWords];
 
     __device__ __forceinline__ static int column(int lane) { return kVector ? lane * kW : lane; }
-    __device__ __forceinline__ void load(const T *row, int c, int d) {  // c: this lane's first column
-        if constexpr (kVector) {
-            if (c < d) load_run(row + c);
-        } else {
+    // row: the row's start; c: this lane's first column
+    __device__ __forceinline__ void load(const T *row, int c, int d) {
 #pragma unroll
-            for (int w = 0; w < kW; ++w)
-                if (c + 32 * w < d) v[w] = load_value(row + c + 32 * w);
+        for (int x = 0; x < kWords; ++x) {
+            const int at = c + x * kApart;
+            r[x] = *reinterpret_cast<const Word *>(row + (at < d ? at : 0));
         }
     }
     __device__ __forceinline__ void store(T *row, int c, int d) const {
-        if constexpr (kVector) {
-            if (c < d) store_run(row + c);
-        } else {
 #pragma unroll
-            for (int w = 0; w < kW; ++w)
-                if (c + 32 * w < d) store_value(row + c + 32 * w, v[w]);
-        }
+        for (int x = 0; x < kWords; ++x)
+            if (c + x * kApart < d) *reinterpret_cast<Word *>(row + c + x * kApart) = r[x];
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int x = 0; x < kWords; ++x) r[x] = Word{};
+    }
+    __device__ __forceinline__ void values(float *v) const {
+#pragma unroll
+        for (int x = 0; x < kWords; ++x) split(r[x], v + x * (kW / kWords));
+    }
+    __device__ __forceinline__ void set(const float *v) {
+#pragma unroll
+        for (int x = 0; x < kWords; ++x) join(v + x * (kW / kWords), r[x]);
     }
 
   private:
-    __device__ __forceinline__ void load_run(const float *p) {
-#pragma unroll
-        for (int w = 0; w < kW; w += 4) {
-            const float4 x = *reinterpret_cast<const float4 *>(p + w);
-            v[w] = x.x, v[w + 1] = x.y, v[w + 2] = x.z, v[w + 3] = x.w;
-        }
+    static __device__ __forceinline__ uint32_t pack2(float a, float b) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t *>(&h);
     }
-    __device__ __forceinline__ void load_run(const __nv_bfloat16 *p) {
-        if constexpr (kW == 8) {
-            Vec16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4 *>(p), v);
-        } else {
-            const uint2 x = *reinterpret_cast<const uint2 *>(p);
-            v[0] = bf16_lo(x.x), v[1] = bf16_hi(x.x), v[2] = bf16_lo(x.y), v[3] = bf16_hi(x.y);
-        }
+    static __device__ __forceinline__ void split(float x, float *v) { *v = x; }
+    static __device__ __forceinline__ void split(__nv_bfloat16 x, float *v) { *v = __bfloat162float(x); }
+    static __device__ __forceinline__ void split(const uint2 &x, float *v) {  // four bf16
+        v[0] = bf16_lo(x.x), v[1] = bf16_hi(x.x), v[2] = bf16_lo(x.y), v[3] = bf16_hi(x.y);
     }
-    __device__ __forceinline__ void store_run(float *p) const {
-#pragma unroll
-        for (int w = 0; w < kW; w += 4) *reinterpret_cast<float4 *>(p + w) = make_float4(v[w], v[w + 1], v[w + 2], v[w + 3]);
-    }
-    __device__ __forceinline__ void store_run(__nv_bfloat16 *p) const {
-        if constexpr (kW == 8) {
-            *reinterpret_cast<uint4 *>(p) = Vec16<__nv_bfloat16>::pack(v);
-        } else {
-            const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
-            *reinterpret_cast<uint2 *>(p) =
-                make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
-        }
-    }
+    static __device__ __forceinline__ void split(const uint4 &x, float *v) { Vec16<T>::unpack(x, v); }
+    static __device__ __forceinline__ void join(const float *v, float &x) { x = *v; }
+    static __device__ __forceinline__ void join(const float *v, __nv_bfloat16 &x) { x = __float2bfloat16_rn(*v); }
+    static __device__ __forceinline__ void join(const float *v, uint2 &x) { x = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3])); }
+    static __device__ __forceinline__ void join(const float *v, uint4 &x) { x = Vec16<T>::pack(v); }
 };
 
 // ---- lookup -----------------------------------------------------------------
@@ -99,7 +97,7 @@ struct EmbedParams {
 
 template <typename TI, typename TO, int kW, bool kVector>
 __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedParams a) {
-    constexpr int kBlock = 32 * kW, kBlocks = 4;  // a warp's columns at a time, and how many it has in flight
+    constexpr int kBlock = 32 * kW, kBlocks = kEmbedBlocks;  // a warp's columns at a time, and how many it has in flight
     griddep_launch_dependents();
     griddep_wait();  // the inputs may come from the kernel before this one
     const int lane = threadIdx.x & 31;
@@ -111,40 +109,27 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const EmbedParams 
     const TI *row = static_cast<const TI *>(a.table) + (in ? tok : 0) * a.ld;
     TO *out = static_cast<TO *>(a.out) + i * a.ld_out;
     const int c0 = blockIdx.y * kBlocks * kBlock + LaneRow<TI, kW, kVector>::column(lane);
+    LaneRow<TI, kW, kVector> r[kBlocks];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) r[b].load(row, c0 + b * kBlock, a.d);
     if constexpr (std::is_same<TI, TO>::value) {
         if (a.scale == 1.0f) {  // a copy: every bit is kept
-            // a lane's values of a block, as kPer words
-            using Word = typename std::conditional<!kVector, TI,
-                                                   typename std::conditional<sizeof(TI) * kW == 8, uint2, uint4>::type>::type;
-            constexpr int kPer = sizeof(TI) * kW / sizeof(Word), kApart = kVector ? sizeof(Word) / sizeof(TI) : 32;
-            Word r[kBlocks][kPer];
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                for (int x = 0; x < kPer; ++x) {
-                    r[b][x] = Word{};
-                    const int c = c0 + b * kBlock + x * kApart;
-                    if (in && c < a.d) r[b][x] = *reinterpret_cast<const Word *>(row + c);
-                }
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                for (int x = 0; x < kPer; ++x) {
-                    const int c = c0 + b * kBlock + x * kApart;
-                    if (c < a.d) *reinterpret_cast<Word *>(out + c) = r[b][x];
-                }
+            for (int b = 0; b < kBlocks; ++b) {
+                if (!in) r[b].clear();
+                r[b].store(out, c0 + b * kBlock, a.d);
+            }
             return;
         }
     }
-    LaneRow<TI, kW, kVector> r[kBlocks];
-#pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
-        if (in) r[b].load(row, c0 + b * kBlock, a.d);
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
-        LaneRow<TO, kW, kVector> o;
+        float v[kW];
+        r[b].values(v);
 #pragma unroll
-        for (int w = 0; w < kW; ++w) o.v[w] = !in ? 0.0f : (a.scale == 1.0f ? r[b].v[w] : a.scale * r[b].v[w]);
+        for (int w = 0; w < kW; ++w) v[w] = in ? a.scale * v[w] : 0.0f;
+        LaneRow<TO, kW, kVector> o;
+        o.set(v);
         o.store(out, c0 + b * kBlock, a.d);
     }
 }
@@ -456,10 +441,11 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortPa
 
 // ---- sums over the runs of equal tokens -------------------------------------
 // A warp takes `chunk` sorted entries and a block of columns and adds the rows
-// up in order, eight of them in flight.  A token whose run lies within the
-// chunk is done; a run that goes on beyond either end leaves the chunk's
-// part of its sum in the workspace (0: of a run that began before the chunk, 1:
-// of one that begins in it), and join_runs_kernel adds the parts up in order.
+// up in order, eight of them in flight, and with them the rows of the table
+// that they are added to.  A run of a token that goes on beyond the chunk at
+// either end leaves the chunk's part of its sum in the workspace (0: of a run
+// that began before the chunk, 1: of one that begins in it), and
+// join_runs_kernel adds the parts up in order.
 
 struct GradParams {
     const Entry *sorted;
@@ -472,18 +458,27 @@ struct GradParams {
     float scale;
 };
 
+// scale * sum (+ what was there) into a row of the table.
 template <typename T, int kW, bool kVector>
-__device__ __forceinline__ void put_row(const GradParams &a, uint32_t tok, int c, const float *sum) {
-    T *row = static_cast<T *>(a.out) + static_cast<int64_t>(tok) * a.ld;
-    LaneRow<T, kW, kVector> o;
-    if (a.accumulate) o.load(row, c, a.d);
+__device__ __forceinline__ void put_row(const GradParams &a, T *row, int c, const float *sum,
+                                        const LaneRow<T, kW, kVector> &there) {
+    float v[kW];
+    if (a.accumulate) there.values(v);
 #pragma unroll
-    for (int w = 0; w < kW; ++w) o.v[w] = a.accumulate ? a.scale * sum[w] + o.v[w] : a.scale * sum[w];
+    for (int w = 0; w < kW; ++w) v[w] = a.accumulate ? fmaf(a.scale, sum[w], v[w]) : a.scale * sum[w];
+    LaneRow<T, kW, kVector> o;
+    o.set(v);
     o.store(row, c, a.d);
 }
 
+// A lane's columns of a row of fp32 parts.
+template <int kW, bool kVector>
+struct PartRow {
+    __device__ __forceinline__ static int column(int c, int w) { return kVector ? c + w : c + 32 * w; }
+};
+
 template <typename TI, typename TO, int kW, bool kVector>
-__global__ void __launch_bounds__(kEmbedThreads) sum_runs_kernel(const GradParams a) {
+__global__ void __launch_bounds__(kEmbedThreads, 2) sum_runs_kernel(const GradParams a) {
     constexpr int kRows = 8;
     griddep_launch_dependents();
     griddep_wait();
@@ -493,91 +488,162 @@ __global__ void __launch_bounds__(kEmbedThreads) sum_runs_kernel(const GradParam
     if (lo >= a.n) return;
     const uint32_t hi = min(lo + a.chunk, a.n);
     const int c = blockIdx.y * 32 * kW + LaneRow<TI, kW, kVector>::column(lane);
-    const uint32_t before = lo > 0 ? entry_token(a.sorted[lo - 1]) : 0xFFFFFFFFu;
-    const uint32_t after = hi < a.n ? entry_token(a.sorted[hi]) : 0xFFFFFFFFu;
-    uint32_t cur = 0xFFFFFFFFu;  // the run's token
-    bool from_before = false;
     float acc[kW];
-    auto close = [&](bool goes_on) {
-        if (cur >= a.V) return;  // none
-        if (from_before || goes_on) {
-            float *part = a.parts + (static_cast<int64_t>(chunk) * 2 + (from_before ? 0 : 1)) * a.d;
+    auto restart = [&] {
 #pragma unroll
-            for (int w = 0; w < kW; ++w) {
-                const int col = kVector ? c + w : c + 32 * w;
-                if (col < a.d) part[col] = acc[w];
-            }
-        } else {
-            put_row<TO, kW, kVector>(a, cur, c, acc);
-        }
+        for (int w = 0; w < kW; ++w) acc[w] = 0.0f;
     };
-    for (uint32_t i0 = lo; i0 < hi; i0 += 32) {
-        const Entry e = i0 + lane < hi ? a.sorted[i0 + lane] : make_entry(a.V, 0);
-        const uint32_t count = min(hi - i0, 32u);
-        if (__shfl_sync(0xFFFFFFFFu, entry_token(e), 0) >= a.V) break;  // only empty slots from here on
-        for (uint32_t r0 = 0; r0 < count; r0 += kRows) {
-            uint32_t tok[kRows];
-            LaneRow<TI, kW, kVector> row[kRows];
+    auto leave_part = [&](int which) {
+        float *part = a.parts + (static_cast<int64_t>(chunk) * 2 + which) * a.d;
 #pragma unroll
-            for (int u = 0; u < kRows; ++u) {
-                tok[u] = __shfl_sync(0xFFFFFFFFu, entry_token(e), r0 + u);
+        for (int w = 0; w < kW; ++w)
+            if (PartRow<kW, kVector>::column(c, w) < a.d) part[PartRow<kW, kVector>::column(c, w)] = acc[w];
+    };
+    restart();
+    bool from_before = lo > 0 && entry_token(a.sorted[lo - 1]) == entry_token(a.sorted[lo]);
+    bool open = false;
+    for (uint32_t i0 = lo; i0 < hi; i0 += 32) {
+        const uint32_t i = i0 + lane;
+        const Entry e = i < hi ? a.sorted[i] : make_entry(a.V, 0);
+        const bool valid = entry_token(e) < a.V;  // the empty slots come last
+        const uint32_t next = i + 1 < a.n ? entry_token(a.sorted[i + 1]) : a.V;
+        const uint32_t ends = __ballot_sync(0xFFFFFFFFu, valid && entry_token(e) != next);
+        const int count = __popc(__ballot_sync(0xFFFFFFFFu, valid));
+        for (int r0 = 0; r0 < count; r0 += kRows) {
+            LaneRow<TI, kW, kVector> row[kRows];
+            LaneRow<TO, kW, kVector> there[kRows];
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) {  // (beyond `count`: row 0, not used)
                 const uint32_t pos = __shfl_sync(0xFFFFFFFFu, entry_pos(e), r0 + u);
-                if (tok[u] < a.V) row[u].load(static_cast<const TI *>(a.grad) + pos * a.ld_grad, c, a.d);
+                row[u].load(static_cast<const TI *>(a.grad) + pos * a.ld_grad, c, a.d);
+            }
+            if (a.accumulate) {
+#pragma unroll
+                for (int u = 0; u < kRows; ++u) {
+                    const int64_t tok = __shfl_sync(0xFFFFFFFFu, entry_token(e), r0 + u);
+                    if (ends >> (r0 + u) & 1u) there[u].load(static_cast<const TO *>(a.out) + tok * a.ld, c, a.d);
+                }
             }
 #pragma unroll
             for (int u = 0; u < kRows; ++u) {
-                if (tok[u] != cur) {
-                    close(false);
-                    cur = tok[u];
-                    from_before = cur == before && i0 + r0 + u == lo;
+                if (r0 + u >= count) break;
+                float v[kW];
+                row[u].values(v);
 #pragma unroll
-                    for (int w = 0; w < kW; ++w) acc[w] = 0.0f;
-                }
-                if (tok[u] < a.V) {
-#pragma unroll
-                    for (int w = 0; w < kW; ++w) acc[w] += row[u].v[w];
+                for (int w = 0; w < kW; ++w) acc[w] += v[w];
+                open = true;
+                if (ends >> (r0 + u) & 1u) {
+                    const int64_t tok = __shfl_sync(0xFFFFFFFFu, entry_token(e), r0 + u);
+                    if (from_before) leave_part(0);
+                    else put_row<TO, kW, kVector>(a, static_cast<TO *>(a.out) + tok * a.ld, c, acc, there[u]);
+                    from_before = open = false;
+                    restart();
                 }
             }
         }
+        if (count < 32) break;
     }
-    close(cur == after);
+    if (open) leave_part(from_before ? 0 : 1);
 }
 
-// One warp per chunk and block of columns: if a run begins in the chunk and goes
-// on beyond it, its parts' sum.
+// A warp per chunk and block of columns: if a run begins in the chunk and goes on
+// beyond it, the sum of its parts.  Runs of many parts (a very frequent token)
+// are shared by the warps of the CTA, each of which adds up consecutive parts.
 template <typename TO, int kW, bool kVector>
 __global__ void __launch_bounds__(kEmbedThreads) join_runs_kernel(const GradParams a) {
+    constexpr int kParts = 8;  // in flight
+    constexpr uint32_t kOwn = 16;  // parts that a warp adds up alone
+    __shared__ uint32_t run_token[kEmbedWarps], run_parts[kEmbedWarps];
+    __shared__ float share[kEmbedWarps][32 * kW];
     griddep_launch_dependents();
     griddep_wait();
-    const int lane = threadIdx.x & 31;
-    const uint32_t chunk = blockIdx.x * kEmbedWarps + (threadIdx.x >> 5);
-    const uint64_t lo = static_cast<uint64_t>(chunk) * a.chunk, hi = lo + a.chunk;
-    if (hi >= a.n) return;
-    const uint32_t tok = entry_token(a.sorted[hi - 1]);
-    if (tok >= a.V || entry_token(a.sorted[hi]) != tok) return;
-    if (entry_token(a.sorted[lo]) == tok && lo > 0 && entry_token(a.sorted[lo - 1]) == tok) return;  // began before
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.y * 32 * kW + LaneRow<TO, kW, kVector>::column(lane);
-    float acc[kW];
-    auto add = [&](int64_t part, bool first) {
-        const float *p = a.parts + part * a.d;
+    const uint32_t chunk0 = blockIdx.x * kEmbedWarps, chunk = chunk0 + warp;
+    // parts lo .. hi - 1 of the run that begins in chunk `begin` (part 0 in slot 1, the others in slots 0)
+    auto add_parts = [&](uint32_t begin, uint32_t lo, uint32_t hi, float *acc) {
 #pragma unroll
-        for (int w = 0; w < kW; ++w) {
-            const int col = kVector ? c + w : c + 32 * w;
-            const float v = col < a.d ? p[col] : 0.0f;
-            acc[w] = first ? v : acc[w] + v;
+        for (int w = 0; w < kW; ++w) acc[w] = 0.0f;
+        for (uint32_t j = lo; j < hi; j += kParts) {
+            float v[kParts][kW];
+#pragma unroll
+            for (int u = 0; u < kParts; ++u) {
+                const uint32_t x = min(j + u, hi - 1);
+                const float *part = a.parts + (2 * (static_cast<int64_t>(begin) + x) + (x == 0)) * a.d;
+#pragma unroll
+                for (int w = 0; w < kW; ++w) {
+                    const int col = PartRow<kW, kVector>::column(c, w);
+                    v[u][w] = part[col < a.d ? col : 0];
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kParts; ++u)
+                if (j + u < hi) {
+#pragma unroll
+                    for (int w = 0; w < kW; ++w) acc[w] += v[u][w];
+                }
         }
     };
-    add(2 * static_cast<int64_t>(chunk) + 1, true);
-    for (uint32_t j0 = chunk + 1;; j0 += 32) {  // chunks that begin with the run
-        const uint64_t at = (static_cast<uint64_t>(j0) + lane) * a.chunk;
-        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, at < a.n && entry_token(a.sorted[at < a.n ? at : 0]) == tok);
-        const int m = mask == 0xFFFFFFFFu ? 32 : __ffs(~mask) - 1;
-#pragma unroll 8
-        for (int j = 0; j < m; ++j) add(2 * (static_cast<int64_t>(j0) + j), false);
-        if (m < 32) break;
+    auto put = [&](uint32_t tok, const float *acc) {
+        TO *const row = static_cast<TO *>(a.out) + static_cast<int64_t>(tok) * a.ld;
+        LaneRow<TO, kW, kVector> there;
+        if (a.accumulate) there.load(row, c, a.d);
+        put_row<TO, kW, kVector>(a, row, c, acc, there);
+    };
+    // the run that begins in this warp's chunk and goes on, and its parts
+    const uint64_t lo = static_cast<uint64_t>(chunk) * a.chunk, hi = lo + a.chunk;
+    uint32_t tok = a.V, parts = 0;
+    if (hi < a.n) {
+        const uint32_t last = entry_token(a.sorted[hi - 1]), after = entry_token(a.sorted[hi]);
+        const uint32_t first = entry_token(a.sorted[lo]), before = lo > 0 ? entry_token(a.sorted[lo - 1]) : a.V;
+        if (last < a.V && after == last && !(first == last && before == last)) tok = last;
     }
-    put_row<TO, kW, kVector>(a, tok, c, acc);
+    if (tok < a.V) {
+        parts = 1;
+        auto begins = [&](uint64_t ch) {  // whether chunk ch begins with the run's token
+            const uint64_t at = ch * a.chunk;
+            return at < a.n && entry_token(a.sorted[at < a.n ? at : 0]) == tok;
+        };
+        while (true) {  // 32 chunks at a time, 1024 where all of those belong to it
+            const uint64_t next = static_cast<uint64_t>(chunk) + parts;
+            const uint32_t near = __ballot_sync(0xFFFFFFFFu, begins(next + lane));
+            if (near != 0xFFFFFFFFu) {
+                parts += __ffs(~near) - 1;
+                break;
+            }
+            const uint32_t far = __ballot_sync(0xFFFFFFFFu, begins(next + 32 * lane + 31));
+            parts += far == 0xFFFFFFFFu ? 1024 : 32 * (__ffs(~far) - 1);
+        }
+        if (parts <= kOwn) {
+            float acc[kW];
+            add_parts(chunk, 0, parts, acc);
+            put(tok, acc);
+        }
+    }
+    if (lane == 0) run_token[warp] = tok, run_parts[warp] = parts;
+    if (!__syncthreads_or(parts > kOwn)) return;
+    for (int r = 0; r < kEmbedWarps; ++r) {
+        const uint32_t m = run_parts[r];
+        if (m <= kOwn) continue;
+        const uint32_t per = (m + kEmbedWarps - 1) / kEmbedWarps;
+        float acc[kW];
+        add_parts(chunk0 + r, min(warp * per, m), min((warp + 1) * per, m), acc);
+#pragma unroll
+        for (int w = 0; w < kW; ++w) share[warp][w * 32 + lane] = acc[w];
+        __syncthreads();
+        if (warp == r) {
+#pragma unroll
+            for (int w = 0; w < kW; ++w) {
+                acc[w] = 0.0f;
+                for (int x = 0; x < kEmbedWarps; ++x) acc[w] += share[x][w * 32 + lane];
+            }
+            put(run_token[r], acc);
+        }
+        __syncthreads();
+    }
 }
+
+constexpr int64_t kChunkMin = 8, kChunksMost = 4096;
 
 // Workspace: the entries twice, the counts of the large sort, the parts of runs.
 struct GradWorkspace {
@@ -589,16 +655,16 @@ static GradWorkspace grad_workspace(int64_t n, int32_t d) {
     auto round_up = [](int64_t v) { return (v + 255) / 256 * 256; };
     GradWorkspace w;
     w.blocks = n > kGroupMax ? static_cast<uint32_t>((n + kSortTile - 1) / kSortTile) : 0;
-    // 32 rows per warp fill the chip from a few thousand tokens on; longer
-    // chunks keep the parts of one very frequent token few
-    w.chunk = 32;
-    while (n / w.chunk > 16384) w.chunk *= 2;
+    // short chunks: many rows in flight from few tokens; longer ones keep the
+    // parts of one very frequent token few
+    w.chunk = kChunkMin;
+    while (n / w.chunk > kChunksMost) w.chunk *= 2;
     w.chunks = static_cast<uint32_t>((n + w.chunk - 1) / w.chunk);
     w.entries = round_up(8 * n);
     w.counts = 2 * w.entries;
     w.parts = w.counts + round_up(int64_t(w.blocks) * 1024);
     // never more for fewer tokens: a program keeps one for its longest batch
-    w.bytes = w.parts + std::min<int64_t>((n + 31) / 32, 16385) * 8 * d;
+    w.bytes = w.parts + std::min<int64_t>((n + kChunkMin - 1) / kChunkMin, kChunksMost + 1) * 8 * d;
     return w;
 }
 
@@ -627,20 +693,21 @@ static cudaError_t start_sums(const GradParams &p, uint32_t chunks, cudaStream_t
 template <typename TI, typename TO, int kW, bool kVector>
 static cudaError_t start_embed(const EmbedParams &p, cudaStream_t s) {
     const dim3 grid(static_cast<unsigned>((p.n + kEmbedWarps - 1) / kEmbedWarps),
-                    static_cast<unsigned>((p.d + 128 * kW - 1) / (128 * kW)));
+                    static_cast<unsigned>((p.d + kEmbedBlocks * 32 * kW - 1) / (kEmbedBlocks * 32 * kW)));
     return chain(embed_kernel<TI, TO, kW, kVector>, grid, kEmbedThreads, s, p);
 }
 
-// How rows of two matrices are read and written: 8 values per lane where both
-// allow 16-byte vectors of bf16 (or two of fp32) and rows are wide, 4 where
-// they are narrow or all fp32, value by value otherwise.
+// How rows of two matrices are read and written: 8 values per lane (one 16-byte
+// vector of bf16, two of fp32) if asked for and rows are wide enough for a warp, 4 otherwise; value by
+// value where addresses do not allow either.
 enum class Access { kWide, kNarrow, kValues };
-static Access access_of(const void *a, vie_dtype ta, int64_t lda, const void *b, vie_dtype tb, int64_t ldb, int d) {
+static Access access_of(const void *a, vie_dtype ta, int64_t lda, const void *b, vie_dtype tb, int64_t ldb, int d,
+                        bool wide) {
     auto fits = [&](const void *p, vie_dtype t, int64_t ld, int w) {
         const int bytes = w * dtype_size(t) < 16 ? w * dtype_size(t) : 16;
         return aligned_to(p, static_cast<uintptr_t>(bytes)) && ld * dtype_size(t) % bytes == 0 && d % w == 0;
     };
-    if ((ta == VIE_DTYPE_BF16 || tb == VIE_DTYPE_BF16) && d > 128 && fits(a, ta, lda, 8) && fits(b, tb, ldb, 8))
+    if (wide && d > 128 && fits(a, ta, lda, 8) && fits(b, tb, ldb, 8))
         return Access::kWide;
     return fits(a, ta, lda, 4) && fits(b, tb, ldb, 4) ? Access::kNarrow : Access::kValues;
 }
@@ -648,7 +715,7 @@ static Access access_of(const void *a, vie_dtype ta, int64_t lda, const void *b,
 #define VIE_BY_ACCESS(f, TI, TO, access, ...)                                \
     ((access) == Access::kWide     ? f<TI, TO, 8, true>(__VA_ARGS__)         \
      : (access) == Access::kNarrow ? f<TI, TO, 4, true>(__VA_ARGS__)         \
-                                   : f<TI, TO, 8, false>(__VA_ARGS__))
+                                   : f<TI, TO, 4, false>(__VA_ARGS__))
 // f<TI, TO, kW, kVector>(...) for two storage types and how rows are accessed.
 #define VIE_BY_TYPES(f, in, out, access, ...)                                                          \
     ((in) == VIE_DTYPE_BF16                                                                            \
@@ -686,7 +753,7 @@ vie_status vie_embed(const void *table, vie_dtype dtype, int64_t V, int32_t d, i
     p.scale = scale;
     cudaError_t e = device_flag_word(&p.flag);
     if (e != cudaSuccess) return fail_cuda(e, fn);
-    e = VIE_BY_TYPES(start_embed, dtype, out_dtype, access_of(table, dtype, ld, out, out_dtype, ld_out, d), p,
+    e = VIE_BY_TYPES(start_embed, dtype, out_dtype, access_of(table, dtype, ld, out, out_dtype, ld_out, d, dtype == VIE_DTYPE_BF16 || out_dtype == VIE_DTYPE_BF16), p,
                      static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
@@ -760,7 +827,7 @@ vie_status vie_embed_grad(const int32_t *tokens, int64_t n, const void *grad, vi
     p.sorted = entries[sorted], p.grad = grad, p.out = out, p.parts = reinterpret_cast<float *>(ws + w.parts);
     p.ld_grad = ld_grad, p.ld = ld, p.n = static_cast<uint32_t>(n), p.V = static_cast<uint32_t>(V), p.chunk = w.chunk;
     p.d = d, p.accumulate = accumulate != 0, p.scale = scale;
-    e = VIE_BY_TYPES(start_sums, dtype, out_dtype, access_of(grad, dtype, ld_grad, out, out_dtype, ld, d), p, w.chunks, s);
+    e = VIE_BY_TYPES(start_sums, dtype, out_dtype, access_of(grad, dtype, ld_grad, out, out_dtype, ld, d, dtype == VIE_DTYPE_BF16 && out_dtype == VIE_DTYPE_BF16), p, w.chunks, s);
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
 
