@@ -131,6 +131,42 @@ struct Vec16<__nv_bfloat16> {
     }
 };
 
+// The part of a row that a CTA deals with: a row is cut into 16-byte vectors at
+// 16-byte addresses, and its 2^log2_slices CTAs take consecutive runs of them.
+// Vector i of the slice holds values
+// e0 + i kVec .. + kVec - 1 of the row; vectors lo .. hi - 1 of nv lie inside
+// it.  At most two do not: `edge` is one of them in thread 0 or 1.
+template <typename T>
+struct Slice {
+    static constexpr int kVec = Vec16<T>::kVec;
+    const T *z;
+    int e0, e1, nv, lo, hi, V;
+
+    __device__ __forceinline__ Slice(const T *row, int V_, int log2_slices, int rank) : z(row), V(V_) {
+        const int first = -static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15u) / sizeof(T));
+        const int vectors = (V - first + kVec - 1) / kVec;
+        const int per = (vectors + (1 << log2_slices) - 1) >> log2_slices;
+        const int v0 = min(rank * per, vectors);
+        nv = min(per, vectors - v0);
+        e0 = first + v0 * kVec;
+        e1 = e0 + nv * kVec;
+        lo = e0 < 0 ? 1 : 0;
+        hi = e1 > V ? nv - 1 : nv;
+    }
+    __device__ __forceinline__ const uint4 *vectors() const { return reinterpret_cast<const uint4 *>(z + e0); }
+    __device__ __forceinline__ int edge() const { return threadIdx.x == 0 ? 0 : nv - 1; }
+    __device__ __forceinline__ bool has_edge() const {
+        return threadIdx.x < min(nv, 2) && (edge() < lo || edge() >= hi);
+    }
+    __device__ __forceinline__ uint4 load_edge() const {  // values outside the row: -inf
+        const int e = e0 + edge() * kVec;
+        float v[kVec];
+#pragma unroll
+        for (int x = 0; x < kVec; ++x) v[x] = e + x >= 0 && e + x < V ? load_value(z + e + x) : -INFINITY;
+        return Vec16<T>::pack(v);
+    }
+};
+
 // 2^x of the special function unit (2 ulp), denormal results flushed to 0.
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
@@ -141,15 +177,23 @@ __device__ __forceinline__ float exp2_approx(float x) {
 // Thread-block clusters: the barrier in its two halves (no ordering of its own
 // in the first), and addresses in the other CTAs' shared memory.
 __device__ __forceinline__ void cluster_arrive_relaxed() {
-    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
 }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ uint32_t cluster_addr(const void *p, uint32_t rank) {
     uint32_t a;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
                  : "=r"(a)
                  : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(rank));
     return a;
+}
+// The same variable of another CTA of the cluster, as a generic pointer.
+template <typename T>
+__device__ __forceinline__ T *cluster_peer(T *p, uint32_t rank) {
+    uint64_t a;
+    asm volatile("mapa.u64 %0, %1, %2;" : "=l"(a) : "l"(reinterpret_cast<uint64_t>(p)), "r"(rank));
+    return reinterpret_cast<T *>(a);
 }
 // Two values into another CTA's shared memory, which count 8 bytes on that CTA's
 // mbarrier when they are there: no fence, no barrier of all threads.

@@ -38,9 +38,6 @@ struct DistillParams {
     uint32_t *flag;
 };
 
-// A row is cut into 16-byte vectors at 16-byte addresses; its first and last
-// one may reach over its ends.  The `slices` CTAs of a row take consecutive
-// runs of vectors.
 constexpr int kSlices = 8, kMaxSlices = 16;  // per row: as many as clusters may have everywhere, and for a few rows alone
 constexpr int kFewRows = 8;
 
@@ -73,41 +70,6 @@ __host__ __device__ inline int seen_slots(int k) {
     while (slots < 2 * k) slots <<= 1;
     return slots;
 }
-
-// The part of a row that a CTA deals with.  Vector i of the slice holds values
-// e0 + i kVec .. + kVec - 1 of the row; vectors lo .. hi - 1 of nv lie inside
-// it.  At most two do not: `edge` is one of them in thread 0 or 1.
-template <typename T>
-struct Slice {
-    static constexpr int kVec = Vec16<T>::kVec;
-    const T *z;
-    int e0, e1, nv, lo, hi, V;
-
-    __device__ __forceinline__ Slice(const DistillParams &a, int64_t row, int log2_slices, int rank)
-        : z(static_cast<const T *>(a.logits) + row * a.ld), V(a.V) {
-        const int first = -static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15u) / sizeof(T));
-        const int vectors = (V - first + kVec - 1) / kVec;
-        const int per = (vectors + (1 << log2_slices) - 1) >> log2_slices;
-        const int v0 = min(rank * per, vectors);
-        nv = min(per, vectors - v0);
-        e0 = first + v0 * kVec;
-        e1 = e0 + nv * kVec;
-        lo = e0 < 0 ? 1 : 0;
-        hi = e1 > V ? nv - 1 : nv;
-    }
-    __device__ __forceinline__ const uint4 *vectors() const { return reinterpret_cast<const uint4 *>(z + e0); }
-    __device__ __forceinline__ int edge() const { return threadIdx.x == 0 ? 0 : nv - 1; }
-    __device__ __forceinline__ bool has_edge() const {
-        return threadIdx.x < min(nv, 2) && (edge() < lo || edge() >= hi);
-    }
-    __device__ __forceinline__ uint4 load_edge() const {  // values outside the row: -inf
-        const int e = e0 + edge() * kVec;
-        float v[kVec];
-#pragma unroll
-        for (int x = 0; x < kVec; ++x) v[x] = e + x >= 0 && e + x < V ? load_value(z + e + x) : -INFINITY;
-        return Vec16<T>::pack(v);
-    }
-};
 
 // Where a slice's gradient goes: by vectors if its rows lie to 16-byte
 // addresses as the logits' do, else value by value.
@@ -359,7 +321,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         any |= tea.validate(a, j);
     }
     const bool has = __syncthreads_or(any);
-    const Slice<T> sl(a, row, log2_slices, rank);
+    const Slice<T> sl(static_cast<const T *>(a.logits) + row * a.ld, a.V, log2_slices, rank);
     const GradSlice<T> out(a, row, sl);
     if (FWD) cluster_wait();
     if (!has) {

@@ -12,9 +12,18 @@
 //   P  = C_i for the first i with C_i >= top_p S   (C: running mass)
 //   Q  = mass of the tokens with w >= min_p 2^40
 //   M  = max(2^40, min(S, P, Q))        (the best token alone weighs 2^40)
-// and the draw is the first token with C_i > floor(u M): the shortest prefix
-// of a given mass, found by narrowing the logits' ranking key digit by digit.
+// and the draw is the first token with C_i > floor(u M): twice the shortest
+// prefix of a given mass, nothing is ranked as a whole.
 // top_p and u count in steps of 2^-24 (top_p rounded up, u down).
+//
+// A cluster of CTAs takes a row; each reads its slice once from memory and a few
+// times more from L2:
+//   1. the maximum;
+//   2. a histogram over 1024 steps of (max z - z) / T, of counts if the row has
+//      a top_k, else of masses; the bin in which a prefix ends follows;
+//   3. the tokens of that bin (with a top_k: of it and the bins before it) go to
+//      the first CTA, which ranks them and finds the prefix exactly.
+// A bin of more tokens than fit is cut further by the logits' ranking keys.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -36,8 +45,13 @@ struct SampleLogitsParams {
     int V;
 };
 
-constexpr int kSampleThreads = 512;
+constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
+constexpr int kBins = 1024;       // two per thread
+constexpr int kBinsPerUnit = 36;  // bins per unit of (max z - z) / T: weights are 0 from 27.8 units on
+constexpr int kCap = 4096;        // tokens that the first CTA ranks
+constexpr int kMaxSplit = 16;     // CTAs per row, at most
 constexpr uint64_t kOne = 1ull << 40;  // the best token's weight
+static_assert(kBins == 2 * kSampleThreads, "two bins per thread");
 
 // floor(mass * count / 2^24), and whether that left a rest; mass < 2^62.
 __device__ __forceinline__ uint64_t share_of(uint64_t mass, uint32_t count, bool *rest) {
@@ -49,154 +63,553 @@ __device__ __forceinline__ uint64_t share_of(uint64_t mass, uint32_t count, bool
 struct Weigh {
     float best, inv;
     bool warm;
-    __device__ __forceinline__ uint64_t operator()(float z) const {
-        if (!(z > -INFINITY)) return 0;  // masked out, or NaN
-        if (z == best) return kOne;
-        if (!warm) return 0;
-        return static_cast<uint64_t>(expf((z - best) * inv) * 1099511627776.0f);
+    // -(z - max z) / T >= 0: nothing to draw from (-inf, NaN) is +inf
+    __device__ __forceinline__ float depth(float z) const {
+        if (!(z > -INFINITY)) return INFINITY;
+        if (z == best) return 0.0f;
+        const float d = -((z - best) * inv);
+        return warm && d >= 0.0f ? d : INFINITY;
+    }
+    // floor(2^40 exp(-depth)), from the bits of the fp32 exponential
+    static __device__ __forceinline__ uint64_t of_depth(float depth) {
+        const uint32_t e = __float_as_uint(expf(-depth));
+        const int shift = static_cast<int>(e >> 23) - (127 + 23 - 40);
+        const uint64_t mantissa = (e & 0x7FFFFFu) | 0x800000u;
+        return shift >= 0 ? mantissa << shift : (shift > -24 ? mantissa >> -shift : 0);
+    }
+    __device__ __forceinline__ uint64_t operator()(float z) const { return of_depth(depth(z)); }
+    // Larger logits never have larger bins; kBins and more: weight 0.
+    static __device__ __forceinline__ int bin_of(float depth) {
+        return static_cast<int>(fminf(depth * kBinsPerUnit, static_cast<float>(kBins)));
     }
 };
 
 struct SampleSmem {
-    float scratch[kSampleThreads / 32];
-    uint64_t mass[256];
-    uint32_t count[256];
-    uint64_t sum;
-    uint64_t above;  // of the ranks before the chosen bin
-    uint32_t bin, found;
-    int32_t token;
+    uint64_t cand[kCap];         // of the first CTA: tokens to rank, as ranking keys
+    uint64_t before[kBins];      // of the first CTA: what the bins before this one amount to
+    uint32_t hist[3][kBins];     // counts in [0], or masses in parts: their low 14 bits, the next 14, the rest
+    uint64_t slots[2][kMaxSplit][2];
+    uint64_t warp_sums[kSampleWarps];
+    float scratch[kSampleWarps];
+    uint64_t told[2][3];         // of the first CTA: what it has found, for all
+    uint64_t found[2], total;    // of the first CTA: what its threads have found, and all bins' amount
+    uint32_t cand_count;
 };
 
-__device__ __forceinline__ uint64_t block_sum_u64(SampleSmem &sm, uint64_t v) {
-    __syncthreads();
-    if (threadIdx.x == 0) sm.sum = 0;
-    __syncthreads();
-    atomicAdd(reinterpret_cast<unsigned long long *>(&sm.sum), static_cast<unsigned long long>(v));
-    __syncthreads();
-    return sm.sum;
-}
+// What all CTAs of a row know and do together.
+template <typename T>
+struct SampleRow {
+    SampleSmem &sm;
+    const Slice<T> sl;
+    Weigh weigh;
+    int slices, rank;
+    int turn, tale;  // of the exchanges, and of what the first CTA tells
+    bool crowded;    // the last prefix has taken the histograms
 
-// The shortest prefix of the ranked tokens with mass (BY_COUNT: with a number
-// of tokens) >= target, of which the row has that much: the last token's key,
-// how many of the tokens with this key it takes, and the mass before them.
-template <typename T, bool BY_COUNT>
-__device__ void shortest_prefix(SampleSmem &sm, const T *z, int V, const Weigh &weigh, uint64_t target, uint32_t *key,
-                                uint64_t *ties, uint64_t *mass_before) {
-    uint32_t prefix = 0;
-    uint64_t before = 0, mass = 0;  // what the ranks before `prefix` amount to
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        __syncthreads();
-        for (int b = threadIdx.x; b < 256; b += kSampleThreads) sm.mass[b] = 0, sm.count[b] = 0;
-        __syncthreads();
-        for (int v = threadIdx.x; v < V; v += kSampleThreads) {
-            const float x = load_value(z + v);
-            const uint64_t w = weigh(x);
-            if (w == 0) continue;
-            const uint32_t o = order_f32(x);
-            if (shift < 24 && (o >> (shift + 8)) != prefix) continue;
-            const uint32_t b = (o >> shift) & 255u;
-            atomicAdd(&sm.count[b], 1u);
-            atomicAdd(reinterpret_cast<unsigned long long *>(&sm.mass[b]), static_cast<unsigned long long>(w));
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            uint64_t c = before;
-            int b = 255;
-            for (; b > 0; --b) {
-                const uint64_t add = BY_COUNT ? sm.count[b] : sm.mass[b];
-                if (c + add >= target) break;
-                c += add;
-                mass += sm.mass[b];
-            }
-            sm.bin = static_cast<uint32_t>(b);
-            sm.above = c;
-            sm.sum = mass;
-        }
-        __syncthreads();
-        prefix = (prefix << 8) | sm.bin;
-        before = sm.above;
-        mass = sm.sum;
+    __device__ __forceinline__ SampleRow(SampleSmem &sm_, const T *row, int V, int log2_slices, int rank_)
+        : sm(sm_), sl(row, V, log2_slices, rank_), weigh{0.0f, 0.0f, false}, slices(1 << log2_slices), rank(rank_), turn(0), tale(0), crowded(false) {}
+
+    __device__ __forceinline__ void sync() const {
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
     }
-    *key = prefix;
-    *mass_before = mass;
-    const uint64_t w = weigh(unorder_f32(prefix));
-    *ties = BY_COUNT ? target - before : (target - before + w - 1) / w;
-    __syncthreads();
+    // f(z, index) for the slice's values, in no order.
+    template <typename F>
+    __device__ __forceinline__ void each(const F &f) const {
+        constexpr int kVec = Slice<T>::kVec, U = 4;
+        const uint4 *const zv = sl.vectors();
+        auto of_vector = [&](const uint4 &raw, int i) {
+            float v[kVec];
+            Vec16<T>::unpack(raw, v);
+#pragma unroll
+            for (int x = 0; x < kVec; ++x) f(v[x], sl.e0 + i * kVec + x);
+        };
+        for (int i = sl.lo + threadIdx.x; i < sl.hi; i += U * kSampleThreads) {
+            uint4 raw[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u * kSampleThreads < sl.hi) raw[u] = zv[i + u * kSampleThreads];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u * kSampleThreads < sl.hi) of_vector(raw[u], i + u * kSampleThreads);
+        }
+        if (sl.has_edge()) of_vector(sl.load_edge(), sl.edge());  // (values outside the row: -inf)
+    }
+    // Two numbers of each CTA (any thread's: all have them) to all CTAs.
+    __device__ __forceinline__ void exchange(uint64_t a, uint64_t b) {
+        turn ^= 1;
+        if (threadIdx.x < slices) {
+            uint64_t *const to = cluster_peer(&sm.slots[turn][rank][0], threadIdx.x);
+            to[0] = a;
+            to[1] = b;
+        }
+        sync();
+    }
+    __device__ __forceinline__ uint64_t sum_all(int which) const {
+        uint64_t s = 0;
+        for (int r = 0; r < slices; ++r) s += sm.slots[turn][r][which];
+        return s;
+    }
+    __device__ __forceinline__ uint64_t max_all(int which) const {
+        uint64_t s = 0;
+        for (int r = 0; r < slices; ++r) s = max(s, sm.slots[turn][r][which]);
+        return s;
+    }
+    __device__ __forceinline__ uint64_t block_sum(uint64_t v) const {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) v += shfl_xor_u64(v, o);
+        __syncthreads();
+        if (lane == 0) sm.warp_sums[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = lane < kSampleWarps ? sm.warp_sums[lane] : 0;
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) v += shfl_xor_u64(v, o);
+        return v;
+    }
+    // Sum of the threads before this one; *total: of all.
+    __device__ __forceinline__ uint64_t block_before(uint64_t v, uint64_t *total) const {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        uint64_t incl = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint64_t x = shfl_up_u64(incl, o);
+            if (lane >= o) incl += x;
+        }
+        __syncthreads();
+        if (lane == 31) sm.warp_sums[warp] = incl;
+        __syncthreads();
+        uint64_t run = incl - v, all = 0;
+#pragma unroll
+        for (int w = 0; w < kSampleWarps; ++w) {
+            run += w < warp ? sm.warp_sums[w] : 0;
+            all += sm.warp_sums[w];
+        }
+        *total = all;
+        return run;
+    }
+
+    // ---- histograms
+    __device__ __forceinline__ void clear_hist() const {
+        for (int b = threadIdx.x; b < kBins; b += kSampleThreads) sm.hist[0][b] = sm.hist[1][b] = sm.hist[2][b] = 0;
+        __syncthreads();
+    }
+    // A slice has at most 2^18 values, and w is at most 2^40: the sums of the
+    // parts stay below 2^32 (2^18 (2^14 - 1), and 2^18 2^12).
+    __device__ __forceinline__ void count_mass(int bin, uint64_t w) const {
+        const uint32_t a = static_cast<uint32_t>(w) & 0x3FFFu, b = static_cast<uint32_t>(w >> 14) & 0x3FFFu;
+        const uint32_t c = static_cast<uint32_t>(w >> 28);
+        if (a) atomicAdd(&sm.hist[0][bin], a);
+        if (b) atomicAdd(&sm.hist[1][bin], b);
+        if (c) atomicAdd(&sm.hist[2][bin], c);
+    }
+    // First CTA: sm.before from the histograms of all CTAs (complete, after a sync).
+    __device__ __forceinline__ void join_hists(bool by_count) const {
+        const int b = 2 * threadIdx.x;
+        uint64_t v0 = 0, v1 = 0;
+        for (int r = 0; r < slices; ++r)
+#pragma unroll
+            for (int part = 0; part < 3; ++part) {
+                if (by_count && part > 0) continue;
+                const uint2 x = *reinterpret_cast<const uint2 *>(cluster_peer(&sm.hist[part][b], r));
+                v0 += static_cast<uint64_t>(x.x) << (14 * part);
+                v1 += static_cast<uint64_t>(x.y) << (14 * part);
+            }
+        uint64_t total;
+        const uint64_t run = block_before(v0 + v1, &total);
+        sm.before[b] = run;
+        sm.before[b + 1] = run + v0;
+        if (threadIdx.x == 0) sm.total = total;
+        __syncthreads();
+    }
+    // First CTA: the bin in which the prefix of `target` ends, and what is
+    // before it, in sm.found; no candidates yet.  The bins have that much.
+    __device__ __forceinline__ void find_bin(uint64_t target) const {
+        forget();
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int b = 2 * threadIdx.x + x;
+            const uint64_t end = b + 1 < kBins ? sm.before[b + 1] : sm.total;
+            if (sm.before[b] < target && target <= end) sm.found[0] = b, sm.found[1] = sm.before[b];
+        }
+        if (threadIdx.x == 0) sm.cand_count = 0;
+        __syncthreads();
+    }
+    __device__ __forceinline__ void forget() const {  // what is looked for is always there; never an index of chance
+        __syncthreads();
+        if (threadIdx.x == 0) sm.found[0] = sm.found[1] = 0;
+        __syncthreads();
+    }
+    // What the first CTA's threads have (a, b, c there), in all CTAs: two
+    // buffers, so that a CTA may still read the last while the next is written.
+    __device__ __forceinline__ void tell(uint64_t *a, uint64_t *b, uint64_t *c) {
+        tale ^= 1;
+        if (rank == 0 && threadIdx.x == 0) sm.told[tale][0] = *a, sm.told[tale][1] = *b, sm.told[tale][2] = *c;
+        sync();
+        const uint64_t *const told = cluster_peer(&sm.told[tale][0], 0);
+        *a = told[0];
+        *b = told[1];
+        *c = told[2];
+    }
+    __device__ __forceinline__ void find_bin_for_all(uint64_t target, uint64_t *bin, uint64_t *before) {
+        uint64_t none = 0;
+        if (rank == 0) {
+            find_bin(target);
+            *bin = sm.found[0], *before = sm.found[1];
+        }
+        tell(bin, before, &none);
+    }
+
+    // ---- tokens to rank
+    // The slice's values for which in(z) holds go to the first CTA, unless they are too many.
+    template <typename F>
+    __device__ __forceinline__ void gather(const F &in) const {
+        uint32_t *const count = cluster_peer(&sm.cand_count, 0);
+        uint64_t *const cand = cluster_peer(&sm.cand[0], 0);
+        each([&](float z, int index) {
+            if (!in(z)) return;
+            const uint32_t at = atomicAdd(count, 1u);
+            if (at < kCap) cand[at] = make_key(z, static_cast<uint32_t>(index));
+        });
+    }
+    // First CTA: the candidates, best first.
+    __device__ __forceinline__ void rank_candidates(int n) const {
+        int size = 32;
+        while (size < n) size <<= 1;
+        for (int i = n + threadIdx.x; i < size; i += kSampleThreads) sm.cand[i] = 0;
+        __syncthreads();
+        for (int k = 2; k <= size; k <<= 1)
+            for (int j = k >> 1; j > 0; j >>= 1) {
+                for (int i = threadIdx.x; i < size / 2; i += kSampleThreads) {
+                    const int a = 2 * i - (i & (j - 1)), b = a + j;  // a: bit j clear
+                    const uint64_t x = sm.cand[a], y = sm.cand[b];
+                    if ((x < y) == ((a & k) == 0)) sm.cand[a] = y, sm.cand[b] = x;
+                }
+                __syncthreads();
+            }
+    }
+    __device__ __forceinline__ uint64_t weight_of(uint64_t key) const { return key == 0 ? 0 : weigh(key_value(key)); }
+    // First CTA: position of the first ranked candidate whose running mass (from
+    // `before` on) reaches target, and that mass, in all threads; they have that much.
+    __device__ __forceinline__ int end_of_prefix(int n, uint64_t before, uint64_t target, uint64_t *mass) const {
+        const int per = (n + kSampleThreads - 1) / kSampleThreads, lo = threadIdx.x * per, hi = min(lo + per, n);
+        forget();
+        uint64_t own = 0, total;
+        for (int i = lo; i < hi; ++i) own += weight_of(sm.cand[i]);
+        uint64_t run = before + block_before(own, &total);
+        for (int i = lo; i < hi; ++i) {
+            const uint64_t after = run + weight_of(sm.cand[i]);
+            if (run < target && target <= after) sm.found[0] = i, sm.found[1] = after;
+            run = after;
+        }
+        __syncthreads();
+        const int at = static_cast<int>(sm.found[0]);
+        *mass = sm.found[1];
+        __syncthreads();
+        return at;
+    }
+
+    // ---- a prefix in all of the row
+    struct Prefix {
+        uint32_t key;   // of its last token (the upper half of a ranking key)
+        uint64_t ties;  // how many of the tokens with this key it takes (by count, or where `index` is below 0)
+        uint64_t mass;  // its mass (not by count)
+        int index;      // the last token's, if it is known, else -1
+    };
+    // The tokens among which the shortest prefix with `target` tokens or mass
+    // ends go to the first CTA, which has joined the histograms of it: how many
+    // they are, what is before them (and, if they are one key too many to rank, that key).
+    __device__ __forceinline__ uint32_t collect(bool by_count, uint64_t target, uint64_t *before, uint32_t *only_key) {
+        uint64_t bin = 0;
+        crowded = false;
+        find_bin_for_all(target, &bin, before);
+        gather([&](float z) { return Weigh::bin_of(weigh.depth(z)) == static_cast<int>(bin); });
+        sync();
+        uint32_t n = *cluster_peer(&sm.cand_count, 0);
+        if (n <= kCap) return n;
+        // a crowded bin: cut by keys, low .. high are left
+        crowded = true;
+        uint64_t most = 0, least = 0;
+        each([&](float z, int) {
+            if (Weigh::bin_of(weigh.depth(z)) != static_cast<int>(bin)) return;
+            const uint32_t key = order_f32(z);
+            most = max(most, static_cast<uint64_t>(key));
+            least = max(least, static_cast<uint64_t>(~key));
+        });
+        most = block_max_u64(most), least = block_max_u64(least);
+        exchange(most, least);
+        uint32_t high = static_cast<uint32_t>(max_all(0)), low = ~static_cast<uint32_t>(max_all(1));
+        while (n > kCap && low != high) {  // ends: every turn takes 10 bits off high - low
+            const int bits = 32 - __clz(high - low), shift = bits > 10 ? bits - 10 : 0;
+            clear_hist();
+            each([&](float z, int) {
+                const uint32_t key = order_f32(z);
+                if (!(z > -INFINITY) || key < low || key > high) return;
+                const int b = (high - key) >> shift;
+                if (by_count) atomicAdd(&sm.hist[0][b], 1u);
+                else count_mass(b, weigh(z));
+            });
+            sync();
+            if (rank == 0) join_hists(by_count);
+            uint64_t b = 0, more = 0;
+            find_bin_for_all(target - *before, &b, &more);
+            *before += more;
+            high -= static_cast<uint32_t>(b) << shift;
+            const uint32_t width = (1u << shift) - 1u;
+            if (high - low > width) low = high - width;
+            gather([&](float z) { return z > -INFINITY && order_f32(z) >= low && order_f32(z) <= high; });
+            sync();
+            n = *cluster_peer(&sm.cand_count, 0);
+        }
+        *only_key = high;
+        return n;
+    }
+    // Of a key too many to rank: how many of its tokens the prefix takes.
+    __device__ __forceinline__ Prefix of_ties(bool by_count, uint64_t target, uint64_t before, uint32_t key) const {
+        const uint64_t w = weigh(unorder_f32(key));
+        const uint64_t ties = by_count ? target - before : (target - before + w - 1) / w;
+        return Prefix{key, ties, before + ties * w, -1};
+    }
+    // The shortest prefix with `target` tokens or mass, in all CTAs.
+    __device__ __forceinline__ Prefix shortest_prefix(bool by_count, uint64_t target) {
+        uint64_t before = 0, last = 0, mass = 0, ties = 0;
+        uint32_t only_key = 0;
+        const uint32_t n = collect(by_count, target, &before, &only_key);
+        if (n > kCap) return of_ties(by_count, target, before, only_key);
+        if (rank == 0) {
+            rank_candidates(static_cast<int>(n));
+            const int at = by_count ? static_cast<int>(min(max(target - before, static_cast<uint64_t>(1)), static_cast<uint64_t>(kCap))) - 1
+                                    : end_of_prefix(static_cast<int>(n), before, target, &mass);
+            last = sm.cand[at];
+            int lo = 0, hi = at;  // the first candidate with this key
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                if ((sm.cand[mid] >> 32) == (last >> 32)) hi = mid;
+                else lo = mid + 1;
+            }
+            ties = static_cast<uint64_t>(at - lo + 1);
+        }
+        tell(&last, &mass, &ties);
+        return Prefix{static_cast<uint32_t>(last >> 32), ties, mass, key_index(last)};
+    }
+    __device__ __forceinline__ uint64_t block_max_u64(uint64_t v) const {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) v = max(v, shfl_xor_u64(v, o));
+        __syncthreads();
+        if (lane == 0) sm.warp_sums[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = lane < kSampleWarps ? sm.warp_sums[lane] : 0;
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) v = max(v, shfl_xor_u64(v, o));
+        return v;
+    }
+    // The index of the ties-th token (from 1) with this key, written by the CTA that has it.
+    __device__ __forceinline__ void write_tie(uint32_t key, uint64_t ties, int32_t *token) {
+        uint64_t own = 0;
+        each([&](float z, int) { own += z > -INFINITY && order_f32(z) == key; });
+        own = block_sum(own);
+        exchange(own, 0);
+        uint64_t earlier = 0;
+        for (int r = 0; r < rank; ++r) earlier += sm.slots[turn][r][0];
+        if (ties <= earlier || ties > earlier + own) return;
+        // runs of kSampleThreads values in order
+        uint64_t found = earlier;
+        const int lo = max(sl.e0, 0), hi = min(sl.e1, sl.V);
+        for (int v0 = lo; v0 < hi; v0 += kSampleThreads) {
+            const int v = v0 + threadIdx.x;
+            const float z = v < hi ? load_value(sl.z + v) : -INFINITY;
+            const bool hit = z > -INFINITY && order_f32(z) == key;
+            uint64_t total;
+            const uint64_t at = found + block_before(hit, &total);
+            if (hit && at + 1 == ties) *token = v;
+            found += total;
+        }
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const SampleLogitsParams a, int log2_slices) {
+    extern __shared__ __align__(16) unsigned char sample_smem[];
+    SampleSmem &sm = *reinterpret_cast<SampleSmem *>(sample_smem);
+    const int rank = blockIdx.x & ((1 << log2_slices) - 1), tid = threadIdx.x;
+    const int64_t row = blockIdx.x >> log2_slices;
+    cluster_arrive_relaxed();  // all CTAs of the cluster run, before their memory is written
+    griddep_launch_dependents();
+    griddep_wait();  // the inputs may come from the kernel before this one
+    SampleRow<T> r(sm, static_cast<const T *>(a.logits) + row * a.ld, a.V, log2_slices, rank);
+    const float temp = a.temperature != nullptr ? a.temperature[row] : 1.0f;
+    const float top_p = a.top_p != nullptr ? a.top_p[row] : 1.0f, min_p = a.min_p != nullptr ? a.min_p[row] : 0.0f;
+    const float u = a.u[row];
+    const bool warm = temp > 0.0f;
+    const int top_k = !warm ? 1 : (a.top_k != nullptr ? a.top_k[row] : 0);
+    r.clear_hist();
+
+    float best = -INFINITY;
+    r.each([&](float z, int) { best = fmaxf(best, z); });
+    best = block_max<kSampleThreads>(best, sm.scratch);
+    cluster_wait();
+    r.exchange(order_f32(best), 0);
+    best = unorder_f32(static_cast<uint32_t>(r.max_all(0)));
+    if (best == -INFINITY) {  // nothing to draw from
+        if (rank == 0 && tid == 0) a.token[row] = -1, a.prob[row] = 0.0f;
+        return;
+    }
+    r.weigh = Weigh{best, 1.0f / temp, warm};
+    const Weigh weigh = r.weigh;
+
+    const uint64_t least_w = min_p > 0.0f ? static_cast<uint64_t>(ceilf(fminf(min_p, 2.0f) * 1099511627776.0f)) : 0;
+    const uint32_t p24 = top_p > 0.0f ? static_cast<uint32_t>(ceilf(fminf(top_p, 1.0f) * 16777216.0f)) : 0;
+    const bool cuts_p = top_p < 1.0f;
+    const uint32_t u24 = u > 0.0f ? static_cast<uint32_t>(fminf(u * 16777216.0f, 16777215.0f)) : 0;
+    bool rest;
+    auto least_of = [&](uint64_t S) {  // ceil(top_p S), at least 1
+        const uint64_t least = share_of(S, p24, &rest);
+        return max(least + rest, static_cast<uint64_t>(1));
+    };
+
+    uint64_t S = 0, Q = 0;
+    bool whole = true;  // all tokens of a weight are in
+    if (top_k > 0 && top_k < a.V) {
+        uint64_t positive = 0;
+        r.each([&](float z, int) {
+            const int bin = Weigh::bin_of(weigh.depth(z));
+            if (bin < kBins) {
+                atomicAdd(&sm.hist[0][bin], 1u);
+                ++positive;
+            }
+        });
+        positive = r.block_sum(positive);
+        r.exchange(positive, 0);
+        positive = r.sum_all(0);
+        if (rank == 0) r.join_hists(true);
+        if (static_cast<uint64_t>(top_k) < positive) {
+            whole = false;
+            uint64_t bin = 0, before = 0;
+            r.find_bin_for_all(static_cast<uint64_t>(top_k), &bin, &before);
+            const uint64_t *const firsts = cluster_peer(&sm.before[0], 0);
+            const uint64_t end = bin + 1 < kBins ? firsts[bin + 1] : positive;
+            if (end <= kCap) {
+                // all tokens down to that bin: the first CTA does the rest
+                r.gather([&](float z) { return Weigh::bin_of(weigh.depth(z)) <= static_cast<int>(bin); });
+                r.sync();
+                if (rank != 0) return;
+                r.rank_candidates(static_cast<int>(end));
+                uint64_t s = 0, q = 0;
+                for (int i = tid; i < top_k; i += kSampleThreads) {
+                    const uint64_t w = r.weight_of(sm.cand[i]);
+                    s += w;
+                    q += w >= least_w ? w : 0;
+                }
+                S = r.block_sum(s);
+                Q = r.block_sum(q);
+                uint64_t M = min(S, Q);
+                if (cuts_p && least_of(S) < M) {
+                    uint64_t P;
+                    r.end_of_prefix(top_k, 0, least_of(S), &P);
+                    M = min(M, P);
+                }
+                M = max(M, kOne);
+                uint64_t mass;
+                const int at = r.end_of_prefix(top_k, 0, share_of(M, u24, &rest) + 1, &mass);
+                if (tid == 0) {
+                    a.token[row] = key_index(sm.cand[at]);
+                    a.prob[row] = static_cast<float>(r.weight_of(sm.cand[at])) / static_cast<float>(M);
+                }
+                return;
+            }
+            // too many to rank: their last one's key, and the mass down to it
+            r.sync();  // (the bins before it are read)
+            const auto cut = r.shortest_prefix(true, static_cast<uint64_t>(top_k));
+            uint64_t s = 0;
+            r.each([&](float z, int) {
+                if (z > -INFINITY && order_f32(z) > cut.key) s += weigh(z);
+            });
+            s = r.block_sum(s);
+            r.exchange(s, 0);
+            S = r.sum_all(0) + cut.ties * weigh(unorder_f32(cut.key));
+        }
+        r.sync();  // (the histograms are read)
+        r.clear_hist();
+    }
+
+    // masses of all tokens
+    auto join_masses = [&] {
+        uint64_t s = 0, q = 0;
+        r.each([&](float z, int) {
+            const float depth = weigh.depth(z);
+            const int bin = Weigh::bin_of(depth);
+            if (bin >= kBins) return;
+            const uint64_t w = Weigh::of_depth(depth);
+            r.count_mass(bin, w);
+            s += w;
+            q += w >= least_w ? w : 0;
+        });
+        s = r.block_sum(s);
+        q = r.block_sum(q);
+        r.exchange(s, q);
+        if (rank == 0) r.join_hists(false);
+    };
+    join_masses();
+    if (whole) S = r.sum_all(0);
+    Q = r.sum_all(1);
+    uint64_t M = min(S, Q);
+    if (cuts_p && least_of(S) < M) {
+        M = min(M, r.shortest_prefix(false, least_of(S)).mass);
+        if (r.crowded) {
+            r.sync();  // (the histograms are read)
+            r.clear_hist();
+            join_masses();
+        }
+    }
+    M = max(M, kOne);
+    const uint64_t target = share_of(M, u24, &rest) + 1;
+    uint64_t before = 0, mass;
+    uint32_t key = 0;
+    const uint32_t n = r.collect(false, target, &before, &key);
+    cluster_arrive_relaxed();  // the first CTA stays until all have read how many there are
+    if (n > kCap) {
+        cluster_wait();
+        r.write_tie(key, r.of_ties(false, target, before, key).ties, a.token + row);
+    } else {
+        if (rank != 0) {  // the first CTA has all that it needs
+            cluster_wait();
+            return;
+        }
+        r.rank_candidates(static_cast<int>(n));
+        const uint64_t last = sm.cand[r.end_of_prefix(static_cast<int>(n), before, target, &mass)];
+        key = static_cast<uint32_t>(last >> 32);
+        if (tid == 0) a.token[row] = key_index(last);
+        cluster_wait();
+    }
+    if (rank == 0 && tid == 0) a.prob[row] = static_cast<float>(weigh(unorder_f32(key))) / static_cast<float>(M);
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kSampleThreads) sample_logits_kernel(const SampleLogitsParams a) {
-    __shared__ SampleSmem sm;
-    const int64_t row = blockIdx.x;
-    const T *z = static_cast<const T *>(a.logits) + row * a.ld;
-    const int V = a.V;
-    float best = -INFINITY;
-    for (int v = threadIdx.x; v < V; v += kSampleThreads) best = fmaxf(best, load_value(z + v));
-    best = block_max<kSampleThreads>(best, sm.scratch);
-    if (best == -INFINITY) {  // nothing to draw from
-        if (threadIdx.x == 0) a.token[row] = -1, a.prob[row] = 0.0f;
-        return;
-    }
-    const float temp = a.temperature != nullptr ? a.temperature[row] : 1.0f;
-    Weigh weigh{best, 1.0f / temp, temp > 0.0f};
-    const float top_p = a.top_p != nullptr ? a.top_p[row] : 1.0f, min_p = a.min_p != nullptr ? a.min_p[row] : 0.0f;
-    const int top_k = !weigh.warm ? 1 : (a.top_k != nullptr ? a.top_k[row] : 0);
-
-    uint64_t S = 0, Q = 0, positive = 0;
-    const uint64_t least_w = min_p > 0.0f ? static_cast<uint64_t>(ceilf(fminf(min_p, 2.0f) * 1099511627776.0f)) : 0;
-    for (int v = threadIdx.x; v < V; v += kSampleThreads) {
-        const uint64_t w = weigh(load_value(z + v));
-        S += w;
-        positive += w != 0;
-        Q += w >= least_w ? w : 0;
-    }
-    S = block_sum_u64(sm, S);
-    Q = block_sum_u64(sm, Q);
-    positive = block_sum_u64(sm, positive);
-    uint32_t key;
-    uint64_t ties, before;
-    if (top_k > 0 && static_cast<uint64_t>(top_k) < positive) {
-        shortest_prefix<T, true>(sm, z, V, weigh, static_cast<uint64_t>(top_k), &key, &ties, &before);
-        S = before + ties * weigh(unorder_f32(key));
-    }
-    uint64_t M = S < Q ? S : Q;
-    if (top_p < 1.0f) {
-        bool rest;
-        const uint32_t p24 = top_p > 0.0f ? static_cast<uint32_t>(ceilf(top_p * 16777216.0f)) : 0;
-        uint64_t least = share_of(S, p24, &rest);
-        least += rest;
-        if (least == 0) least = 1;
-        shortest_prefix<T, false>(sm, z, V, weigh, least, &key, &ties, &before);
-        const uint64_t P = before + ties * weigh(unorder_f32(key));
-        if (P < M) M = P;
-    }
-    if (M < kOne) M = kOne;
-    const float u = a.u[row];
-    const uint32_t u24 = u > 0.0f ? static_cast<uint32_t>(fminf(u * 16777216.0f, 16777215.0f)) : 0;
-    bool rest;
-    const uint64_t target = share_of(M, u24, &rest) + 1;
-    shortest_prefix<T, false>(sm, z, V, weigh, target, &key, &ties, &before);
-    // the ties-th token with this key, by index: runs of tokens in order
-    if (threadIdx.x == 0) sm.found = 0;
-    __syncthreads();
-    for (int v0 = 0; v0 < V; v0 += kSampleThreads) {
-        const int v = v0 + threadIdx.x;
-        const bool hit = v < V && order_f32(load_value(z + v)) == key;
-        const uint32_t in_warp = __ballot_sync(0xFFFFFFFFu, hit);
-        __syncthreads();
-        if ((threadIdx.x & 31) == 0) sm.count[threadIdx.x >> 5] = __popc(in_warp);
-        __syncthreads();
-        uint64_t at = sm.found;
-        for (unsigned w = 0; w < threadIdx.x >> 5; ++w) at += sm.count[w];
-        at += __popc(in_warp & ((1u << (threadIdx.x & 31)) - 1u));
-        if (hit && at + 1 == ties) {
-            a.token[row] = v;
-            a.prob[row] = static_cast<float>(weigh(unorder_f32(key))) / static_cast<float>(M);
-        }
-        __syncthreads();
-        if (threadIdx.x == 0)
-            for (int w = 0; w < kSampleThreads / 32; ++w) sm.found += sm.count[w];
-    }
+static cudaError_t start_sample(const SampleLogitsParams &p, int64_t batch, cudaStream_t s) {
+    // CTAs per row: enough for the chip, of 8192 values or more; 2^18 values at most
+    int log2_slices = 0;
+    while (((p.V - 1) >> log2_slices) >= (1 << 18)) ++log2_slices;
+    while (log2_slices < (batch <= 8 ? 4 : 3) && (batch << log2_slices) < 304 && (p.V >> log2_slices) >= 16384) ++log2_slices;
+    auto kernel = sample_logits_kernel<T>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SampleSmem));
+    if (e == cudaSuccess && log2_slices > 3) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(batch << log2_slices));
+    cfg.blockDim = dim3(kSampleThreads);
+    cfg.dynamicSmemBytes = sizeof(SampleSmem);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 1u << log2_slices;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, p, log2_slices);
 }
 
 }  // namespace vie
@@ -225,10 +638,6 @@ extern "C" vie_status vie_sample_logits(const void *logits, vie_dtype dtype, int
     p.logits = logits, p.u = u, p.temperature = temperature, p.top_p = top_p, p.min_p = min_p, p.top_k = top_k;
     p.token = out_token, p.prob = out_prob, p.ld = ld, p.V = static_cast<int>(V);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (dtype == VIE_DTYPE_BF16)
-        sample_logits_kernel<__nv_bfloat16><<<static_cast<unsigned>(batch), kSampleThreads, 0, s>>>(p);
-    else
-        sample_logits_kernel<float><<<static_cast<unsigned>(batch), kSampleThreads, 0, s>>>(p);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = dtype == VIE_DTYPE_BF16 ? start_sample<__nv_bfloat16>(p, batch, s) : start_sample<float>(p, batch, s);
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
