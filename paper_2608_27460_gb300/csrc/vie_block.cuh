@@ -192,7 +192,7 @@ __device__ __forceinline__ uint32_t cluster_addr(const void *p, uint32_t rank) {
 template <typename T>
 __device__ __forceinline__ T *cluster_peer(T *p, uint32_t rank) {
     uint64_t a;
-    asm volatile("mapa.u64 %0, %1, %2;" : "=l"(a) : "l"(reinterpret_cast<uint64_t>(p)), "r"(rank));
+    asm("mapa.u64 %0, %1, %2;" : "=l"(a) : "l"(reinterpret_cast<uint64_t>(p)), "r"(rank));
     return reinterpret_cast<T *>(a);
 }
 // Two values into another CTA's shared memory, which count 8 bytes on that CTA's

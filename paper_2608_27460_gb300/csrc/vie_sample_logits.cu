@@ -18,11 +18,15 @@
 //
 // A cluster of CTAs takes a row; each reads its slice once from memory and a few
 // times more from L2:
-//   1. the maximum;
-//   2. a histogram over 1024 steps of (max z - z) / T, of counts if the row has
-//      a top_k, else of masses; the bin in which a prefix ends follows;
-//   3. the tokens of that bin (with a top_k: of it and the bins before it) go to
-//      the first CTA, which ranks them and finds the prefix exactly.
+//   1. the maximum.  With a top_k, the threads' own maxima give a logit that at
+//      least top_k tokens reach: those that do go to the first CTA, which
+//      ranks them and does the rest.
+//   2. the masses S and Q, and those of the tokens less than 6 and 12 units of
+//      (max z - z) / T deep;
+//   3. a histogram of masses over 1024 steps of depth, of the tokens in the least of
+//      these ranges that holds the prefix; the bin in which it ends follows;
+//   4. the tokens of that bin go to the first CTA, which ranks them and finds
+//      the prefix exactly.
 // A bin of more tokens than fit is cut further by the logits' ranking keys.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -88,9 +92,10 @@ struct SampleSmem {
     uint64_t cand[kCap];         // of the first CTA: tokens to rank, as ranking keys
     uint64_t before[kBins];      // of the first CTA: what the bins before this one amount to
     uint32_t hist[3][kBins];     // counts in [0], or masses in parts: their low 14 bits, the next 14, the rest
-    uint64_t slots[2][kMaxSplit][2];
+    uint64_t slots[2][kMaxSplit][4];
     uint64_t warp_sums[kSampleWarps];
     float scratch[kSampleWarps];
+    float edge[2];               // least logits of the two depths
     uint64_t told[2][3];         // of the first CTA: what it has found, for all
     uint64_t found[2], total;    // of the first CTA: what its threads have found, and all bins' amount
     uint32_t cand_count;
@@ -136,13 +141,54 @@ struct SampleRow {
         }
         if (sl.has_edge()) of_vector(sl.load_edge(), sl.edge());  // (values outside the row: -inf)
     }
-    // Two numbers of each CTA (any thread's: all have them) to all CTAs.
-    __device__ __forceinline__ void exchange(uint64_t a, uint64_t b) {
+    // The same for the values of `least` and more, if any: a vector without one is passed over at once.
+    template <typename F>
+    __device__ __forceinline__ void each_above(float least, const F &f) const {
+        constexpr int kVec = Slice<T>::kVec, U = 4;
+        const uint4 *const zv = sl.vectors();
+        auto of_vector = [&](const uint4 &raw, int i) {
+            typename Vec16<T>::Max top;
+            top.add(raw);
+            if (!(top.top() >= least)) return;
+            float v[kVec];
+            Vec16<T>::unpack(raw, v);
+#pragma unroll
+            for (int x = 0; x < kVec; ++x)
+                if (v[x] >= least) f(v[x], sl.e0 + i * kVec + x);
+        };
+        for (int i = sl.lo + threadIdx.x; i < sl.hi; i += U * kSampleThreads) {
+            uint4 raw[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u * kSampleThreads < sl.hi) raw[u] = zv[i + u * kSampleThreads];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u * kSampleThreads < sl.hi) of_vector(raw[u], i + u * kSampleThreads);
+        }
+        if (sl.has_edge()) of_vector(sl.load_edge(), sl.edge());
+    }
+    // The least logit in bins 0 .. bin; a whole warp calls.
+    __device__ __forceinline__ float least_of_bins(int bin) const {
+        uint32_t lo = order_f32(-INFINITY) + 1, hi = order_f32(weigh.best);  // (the best is in bin 0)
+        while (lo < hi) {  // ends: hi - lo falls to a 32nd at each turn
+            const uint32_t step = (hi - lo) / 32 + 1, key = lo + min((threadIdx.x & 31u) * step, hi - lo);
+            const uint32_t in = __ballot_sync(0xFFFFFFFFu, Weigh::bin_of(weigh.depth(unorder_f32(key))) <= bin);
+            if (in == 0) {  // (the lanes end before hi)
+                lo += 31 * step + 1;
+                continue;
+            }
+            const uint32_t at = __ffs(in) - 1;
+            hi = min(hi, lo + at * step);
+            if (at > 0) lo += (at - 1) * step + 1;
+        }
+        return unorder_f32(hi);
+    }
+    // Up to four numbers of each CTA (any thread's: all have them) to all CTAs.
+    __device__ __forceinline__ void exchange(uint64_t a, uint64_t b = 0, uint64_t c = 0, uint64_t d = 0) {
         turn ^= 1;
         if (threadIdx.x < slices) {
             uint64_t *const to = cluster_peer(&sm.slots[turn][rank][0], threadIdx.x);
-            to[0] = a;
-            to[1] = b;
+            to[0] = a, to[1] = b, to[2] = c, to[3] = d;
         }
         sync();
     }
@@ -208,14 +254,24 @@ struct SampleRow {
     __device__ __forceinline__ void join_hists(bool by_count) const {
         const int b = 2 * threadIdx.x;
         uint64_t v0 = 0, v1 = 0;
-        for (int r = 0; r < slices; ++r)
+        for (int r0 = 0; r0 < slices; r0 += 4) {
+            uint2 x[4][3];
 #pragma unroll
-            for (int part = 0; part < 3; ++part) {
-                if (by_count && part > 0) continue;
-                const uint2 x = *reinterpret_cast<const uint2 *>(cluster_peer(&sm.hist[part][b], r));
-                v0 += static_cast<uint64_t>(x.x) << (14 * part);
-                v1 += static_cast<uint64_t>(x.y) << (14 * part);
-            }
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int part = 0; part < 3; ++part) {
+                    x[r][part] = make_uint2(0, 0);
+                    if (r0 + r < slices && !(by_count && part > 0))
+                        x[r][part] = *reinterpret_cast<const uint2 *>(cluster_peer(&sm.hist[part][b], r0 + r));
+                }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int part = 0; part < 3; ++part) {
+                    v0 += static_cast<uint64_t>(x[r][part].x) << (14 * part);
+                    v1 += static_cast<uint64_t>(x[r][part].y) << (14 * part);
+                }
+        }
         uint64_t total;
         const uint64_t run = block_before(v0 + v1, &total);
         sm.before[b] = run;
@@ -262,12 +318,12 @@ struct SampleRow {
     }
 
     // ---- tokens to rank
-    // The slice's values for which in(z) holds go to the first CTA, unless they are too many.
+    // The slice's values of `least` and more for which in(z) holds go to the first CTA, unless they are too many.
     template <typename F>
-    __device__ __forceinline__ void gather(const F &in) const {
+    __device__ __forceinline__ void gather(float least, const F &in) const {
         uint32_t *const count = cluster_peer(&sm.cand_count, 0);
         uint64_t *const cand = cluster_peer(&sm.cand[0], 0);
-        each([&](float z, int index) {
+        each_above(least, [&](float z, int index) {
             if (!in(z)) return;
             const uint32_t at = atomicAdd(count, 1u);
             if (at < kCap) cand[at] = make_key(z, static_cast<uint32_t>(index));
@@ -275,6 +331,21 @@ struct SampleRow {
     }
     // First CTA: the candidates, best first.
     __device__ __forceinline__ void rank_candidates(int n) const {
+        if (n <= 2 * kSampleThreads) {  // a token's rank is the number of better ones
+            uint64_t *const ranked = reinterpret_cast<uint64_t *>(&sm.hist[0][0]);
+            __syncthreads();
+            for (int i = threadIdx.x; i < n; i += kSampleThreads) {
+                const uint64_t own = sm.cand[i];
+                int rank_of = 0;
+#pragma unroll 8
+                for (int x = 0; x < n; ++x) rank_of += sm.cand[x] > own;
+                ranked[rank_of] = own;
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < n; i += kSampleThreads) sm.cand[i] = ranked[i];
+            __syncthreads();
+            return;
+        }
         int size = 32;
         while (size < n) size <<= 1;
         for (int i = n + threadIdx.x; i < size; i += kSampleThreads) sm.cand[i] = 0;
@@ -324,7 +395,8 @@ struct SampleRow {
         uint64_t bin = 0;
         crowded = false;
         find_bin_for_all(target, &bin, before);
-        gather([&](float z) { return Weigh::bin_of(weigh.depth(z)) == static_cast<int>(bin); });
+        gather(least_of_bins(static_cast<int>(bin)),
+               [&](float z) { return Weigh::bin_of(weigh.depth(z)) == static_cast<int>(bin); });
         sync();
         uint32_t n = *cluster_peer(&sm.cand_count, 0);
         if (n <= kCap) return n;
@@ -358,7 +430,7 @@ struct SampleRow {
             high -= static_cast<uint32_t>(b) << shift;
             const uint32_t width = (1u << shift) - 1u;
             if (high - low > width) low = high - width;
-            gather([&](float z) { return z > -INFINITY && order_f32(z) >= low && order_f32(z) <= high; });
+            gather(unorder_f32(low), [&](float z) { return order_f32(z) >= low && order_f32(z) <= high; });
             sync();
             n = *cluster_peer(&sm.cand_count, 0);
         }
@@ -410,7 +482,7 @@ struct SampleRow {
         uint64_t own = 0;
         each([&](float z, int) { own += z > -INFINITY && order_f32(z) == key; });
         own = block_sum(own);
-        exchange(own, 0);
+        exchange(own);
         uint64_t earlier = 0;
         for (int r = 0; r < rank; ++r) earlier += sm.slots[turn][r][0];
         if (ties <= earlier || ties > earlier + own) return;
@@ -446,11 +518,11 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
     const int top_k = !warm ? 1 : (a.top_k != nullptr ? a.top_k[row] : 0);
     r.clear_hist();
 
-    float best = -INFINITY;
-    r.each([&](float z, int) { best = fmaxf(best, z); });
-    best = block_max<kSampleThreads>(best, sm.scratch);
+    float own = -INFINITY;
+    r.each([&](float z, int) { own = fmaxf(own, z); });
+    float best = block_max<kSampleThreads>(own, sm.scratch);
     cluster_wait();
-    r.exchange(order_f32(best), 0);
+    r.exchange(order_f32(best));
     best = unorder_f32(static_cast<uint32_t>(r.max_all(0)));
     if (best == -INFINITY) {  // nothing to draw from
         if (rank == 0 && tid == 0) a.token[row] = -1, a.prob[row] = 0.0f;
@@ -469,9 +541,61 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
         return max(least + rest, static_cast<uint64_t>(1));
     };
 
+    // The first CTA has all tokens from some depth up, n of them and top_k at
+    // least: the row's token.
+    auto finish_top_k = [&](int n) {
+        r.rank_candidates(n);
+        uint64_t s = 0, q = 0;
+        for (int i = tid; i < top_k; i += kSampleThreads) {
+            const uint64_t w = r.weight_of(sm.cand[i]);
+            s += w;
+            q += w >= least_w ? w : 0;
+        }
+        const uint64_t S = r.block_sum(s), Q = r.block_sum(q);
+        uint64_t M = min(S, Q), mass;
+        if (cuts_p && least_of(S) < M) {
+            r.end_of_prefix(top_k, 0, least_of(S), &mass);
+            M = min(M, mass);
+        }
+        M = max(M, kOne);
+        const int at = r.end_of_prefix(top_k, 0, share_of(M, u24, &rest) + 1, &mass);
+        if (tid == 0) {
+            a.token[row] = key_index(sm.cand[at]);
+            a.prob[row] = static_cast<float>(r.weight_of(sm.cand[at])) / static_cast<float>(M);
+        }
+    };
     uint64_t S = 0, Q = 0;
     bool whole = true;  // all tokens of a weight are in
     if (top_k > 0 && top_k < a.V) {
+        // bins of the threads' maxima: where top_k of them are reached, at least top_k tokens are
+        if (top_k <= kSampleThreads << log2_slices) {
+            const int bin = Weigh::bin_of(weigh.depth(own));
+            if (bin < kBins) atomicAdd(&sm.hist[0][bin], 1u);
+            r.sync();
+            uint64_t last = kBins, none = 0, enough = 0;
+            if (rank == 0) {
+                r.join_hists(true);
+                if (sm.total >= static_cast<uint64_t>(top_k)) {
+                    r.find_bin(static_cast<uint64_t>(top_k));
+                    last = sm.found[0];
+                }
+            }
+            r.tell(&last, &none, &enough);
+            if (last < kBins) {
+                const float least = r.least_of_bins(static_cast<int>(last));
+                r.gather(least, [](float) { return true; });
+                r.sync();
+                const uint32_t n = *cluster_peer(&sm.cand_count, 0);
+                cluster_arrive_relaxed();  // the first CTA stays until all have read how many there are
+                if (n <= kCap) {
+                    if (rank == 0) finish_top_k(static_cast<int>(n));
+                    cluster_wait();
+                    return;
+                }
+                cluster_wait();
+            }
+            r.clear_hist();  // (after a sync that follows its reading)
+        }
         uint64_t positive = 0;
         r.each([&](float z, int) {
             const int bin = Weigh::bin_of(weigh.depth(z));
@@ -481,7 +605,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
             }
         });
         positive = r.block_sum(positive);
-        r.exchange(positive, 0);
+        r.exchange(positive);
         positive = r.sum_all(0);
         if (rank == 0) r.join_hists(true);
         if (static_cast<uint64_t>(top_k) < positive) {
@@ -492,31 +616,9 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
             const uint64_t end = bin + 1 < kBins ? firsts[bin + 1] : positive;
             if (end <= kCap) {
                 // all tokens down to that bin: the first CTA does the rest
-                r.gather([&](float z) { return Weigh::bin_of(weigh.depth(z)) <= static_cast<int>(bin); });
+                r.gather(r.least_of_bins(static_cast<int>(bin)), [](float) { return true; });
                 r.sync();
-                if (rank != 0) return;
-                r.rank_candidates(static_cast<int>(end));
-                uint64_t s = 0, q = 0;
-                for (int i = tid; i < top_k; i += kSampleThreads) {
-                    const uint64_t w = r.weight_of(sm.cand[i]);
-                    s += w;
-                    q += w >= least_w ? w : 0;
-                }
-                S = r.block_sum(s);
-                Q = r.block_sum(q);
-                uint64_t M = min(S, Q);
-                if (cuts_p && least_of(S) < M) {
-                    uint64_t P;
-                    r.end_of_prefix(top_k, 0, least_of(S), &P);
-                    M = min(M, P);
-                }
-                M = max(M, kOne);
-                uint64_t mass;
-                const int at = r.end_of_prefix(top_k, 0, share_of(M, u24, &rest) + 1, &mass);
-                if (tid == 0) {
-                    a.token[row] = key_index(sm.cand[at]);
-                    a.prob[row] = static_cast<float>(r.weight_of(sm.cand[at])) / static_cast<float>(M);
-                }
+                if (rank == 0) finish_top_k(static_cast<int>(end));
                 return;
             }
             // too many to rank: their last one's key, and the mass down to it
@@ -527,41 +629,78 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
                 if (z > -INFINITY && order_f32(z) > cut.key) s += weigh(z);
             });
             s = r.block_sum(s);
-            r.exchange(s, 0);
+            r.exchange(s);
             S = r.sum_all(0) + cut.ties * weigh(unorder_f32(cut.key));
         }
         r.sync();  // (the histograms are read)
         r.clear_hist();
     }
 
-    // masses of all tokens
-    auto join_masses = [&] {
-        uint64_t s = 0, q = 0;
-        r.each([&](float z, int) {
-            const float depth = weigh.depth(z);
-            const int bin = Weigh::bin_of(depth);
-            if (bin >= kBins) return;
-            const uint64_t w = Weigh::of_depth(depth);
-            r.count_mass(bin, w);
-            s += w;
-            q += w >= least_w ? w : 0;
+    // masses: of all tokens, of those that min_p keeps, and down to two depths
+    constexpr int kDepth1 = 6 * kBinsPerUnit, kDepth2 = 12 * kBinsPerUnit;  // bins
+    const bool usual = warm && best < INFINITY && weigh.inv < INFINITY;
+    uint64_t to_depth[2] = {0, 0};
+    {
+        if (tid < 64) {
+            const float least = r.least_of_bins(tid < 32 ? kDepth1 - 1 : kDepth2 - 1);
+            if ((tid & 31) == 0) sm.edge[tid >> 5] = least;
+        }
+        __syncthreads();
+        const float edge1 = sm.edge[0], edge2 = sm.edge[1];
+        uint64_t s = 0, q = 0, d1 = 0, d2 = 0;
+        if (usual) {
+            // w in two halves of 20 bits, each an addition that cuts off what is
+            // below 2^-20 (2^-40); a thread's at most 520 values leave their sums below 2^32
+            const float least_e = static_cast<float>(least_w) * 9.094947017729282e-13f;  // 2^-40
+            uint32_t hi[4] = {}, lo[4] = {};
+            r.each([&](float z, int) {
+                const float e = fmaxf(expf((z - best) * weigh.inv), 0.0f);  // (NaN: 0)
+                const float t = __fadd_rz(e, 8.0f), t2 = __fadd_rz(e - (t - 8.0f), 7.62939453125e-06f);  // 2^-17
+                const uint32_t h = __float_as_uint(t) - 0x41000000u, l = __float_as_uint(t2) - 0x37000000u;
+                hi[0] += h, lo[0] += l;
+                if (e >= least_e) hi[1] += h, lo[1] += l;
+                if (z >= edge1) hi[2] += h, lo[2] += l;
+                if (z >= edge2) hi[3] += h, lo[3] += l;
+            });
+            auto whole_of = [&](int i) { return (static_cast<uint64_t>(hi[i]) << 20) + lo[i]; };
+            s = whole_of(0), q = whole_of(1), d1 = whole_of(2), d2 = whole_of(3);
+        } else {
+            r.each([&](float z, int) {
+                const uint64_t w = weigh(z);
+                s += w;
+                q += w >= least_w ? w : 0;
+                d1 += z >= edge1 ? w : 0;
+                d2 += z >= edge2 ? w : 0;
+            });
+        }
+        s = r.block_sum(s), q = r.block_sum(q), d1 = r.block_sum(d1), d2 = r.block_sum(d2);
+        r.exchange(s, q, d1, d2);
+        if (whole) S = r.sum_all(0);
+        Q = r.sum_all(1);
+        to_depth[0] = r.sum_all(2), to_depth[1] = r.sum_all(3);
+    }
+    // the histogram down to a depth that holds `most`
+    auto join_masses = [&](uint64_t most) {
+        const int depth = most <= to_depth[0] ? kDepth1 : (most <= to_depth[1] ? kDepth2 : kBins);
+        const float least = depth == kBins ? r.least_of_bins(kBins - 1) : sm.edge[depth == kDepth2];
+        r.each_above(least, [&](float z, int) {
+            const float d = weigh.depth(z);
+            r.count_mass(Weigh::bin_of(d), Weigh::of_depth(d));
         });
-        s = r.block_sum(s);
-        q = r.block_sum(q);
-        r.exchange(s, q);
+        r.sync();
         if (rank == 0) r.join_hists(false);
     };
-    join_masses();
-    if (whole) S = r.sum_all(0);
-    Q = r.sum_all(1);
     uint64_t M = min(S, Q);
     if (cuts_p && least_of(S) < M) {
+        join_masses(least_of(S));
         M = min(M, r.shortest_prefix(false, least_of(S)).mass);
         if (r.crowded) {
             r.sync();  // (the histograms are read)
             r.clear_hist();
-            join_masses();
+            join_masses(max(M, kOne));
         }
+    } else {
+        join_masses(max(M, kOne));
     }
     M = max(M, kOne);
     const uint64_t target = share_of(M, u24, &rest) + 1;
