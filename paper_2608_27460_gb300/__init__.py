@@ -390,12 +390,45 @@ def _stream_ptr(stream) -> int:
 
 
 # ---- training and sampling around the head (torch tensors) ------------------
+# Small calls are bound by the host, so their checks are cheap ones: device
+# numbers instead of device objects, no context managers unless one is needed.
+
+_torch = None
+
+
+def _here(x, name):
+    """Whether x's device is the current one; refuses CPU tensors."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    return x.get_device() == _torch.cuda.current_device()
+
+
+class _on:
+    """Makes x's device the current one and, if a stream is given, the call's
+    own copies and new tensors belong to it."""
+
+    def __init__(self, x, stream):
+        self.ctx = [_torch.cuda.device(x.get_device())]
+        if stream is not None:
+            self.ctx.append(_torch.cuda.stream(stream))
+
+    def __enter__(self):
+        for c in self.ctx:
+            c.__enter__()
+
+    def __exit__(self, *exc):
+        for c in reversed(self.ctx):
+            c.__exit__(*exc)
+
 
 def _dtype_code(x, name):
-    import torch
-    if x.dtype == torch.bfloat16:
+    if x.dtype is _torch.bfloat16:
         return VIE_DTYPE_BF16
-    if x.dtype == torch.float32:
+    if x.dtype is _torch.float32:
         return VIE_DTYPE_F32
     raise ValueError(f"{name} must be bfloat16 or float32, not {x.dtype}")
 
@@ -404,16 +437,17 @@ def _pitch(x):
     """Row pitch of a 2-D tensor whose rows are runs of values that do not
     overlap, or 0 if it is laid out in another way."""
     n, c = x.shape
-    if c > 1 and x.stride(1) != 1:
+    ld, step = x.stride()
+    if c > 1 and step != 1:
         return 0
     if n <= 1:
         return max(c, 1)
-    return x.stride(0) if x.stride(0) >= c else 0
+    return ld if ld >= c else 0
 
 
 def _matrix(x, name):
-    """(x, pitch) of a CUDA matrix argument; one laid out in another way than
-    by rows is copied."""
+    """(x, pitch) of a matrix argument; one laid out in another way than by
+    rows is copied."""
     if x.dim() != 2:
         raise ValueError(f"{name} must be a 2-D CUDA tensor")
     ld = _pitch(x)
@@ -423,20 +457,18 @@ def _matrix(x, name):
     return x, max(x.shape[1], 1)
 
 
-def _vector(x, name, dtype, n, like):
-    """A contiguous CUDA vector argument of n values."""
-    if x.dtype != dtype or not x.is_cuda or x.dim() != 1 or x.shape[0] != n or x.device != like.device:
-        raise ValueError(f"{name} must be a {dtype} tensor [{n}] on {like.device}")
+def _given(x, name, shape, dtype, like):
+    """A contiguous argument of this shape and type on like's device."""
+    if x.dtype is not dtype or x.shape != shape or not x.is_cuda or x.get_device() != like.get_device():
+        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {like.device}")
     return x if x.is_contiguous() else x.contiguous()
 
 
 def _output(x, name, shape, dtype, like):
-    """An output tensor: `x` if it fits, a new one if it is None.  Vectors
-    must be contiguous, matrices laid out by rows."""
-    import torch
+    """An output tensor: `x` if it fits, a new one if it is None."""
     if x is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
-    if tuple(x.shape) != tuple(shape) or x.dtype != dtype or x.device != like.device:
+        return _torch.empty(shape, dtype=dtype, device=like.device)
+    if x.dtype is not dtype or x.shape != shape or not x.is_cuda or x.get_device() != like.get_device():
         raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {like.device}")
     return x
 
@@ -456,38 +488,15 @@ def _matrix_output(x, name, shape, dtype, like):
     return x, ld
 
 
-class _on:
-    """Makes a call's own copies and new tensors belong to the stream it runs
-    on, and its device the current one."""
-
-    def __init__(self, like, name, stream):
-        import torch
-        if not like.is_cuda:
-            raise ValueError(f"{name} must be a CUDA tensor")
-        self.ctx = []
-        if like.device.index != torch.cuda.current_device():
-            self.ctx.append(torch.cuda.device(like.device))
-        if stream is not None:
-            self.ctx.append(torch.cuda.stream(stream))
-
-    def __enter__(self):
-        for c in self.ctx:
-            c.__enter__()
-        return _stream_ptr(None)
-
-    def __exit__(self, *exc):
-        for c in reversed(self.ctx):
-            c.__exit__(*exc)
-
-
 def _teacher(logits, t_idx, t_logits):
-    """The checked arguments that the distillation calls share."""
-    import torch
-    n = logits.shape[0] if logits.dim() else 0
-    for x, name, dt in ((t_idx, "t_idx", torch.int32), (t_logits, "t_logits", torch.float32)):
-        if x.dtype != dt or x.dim() != 2 or x.device != logits.device or x.shape[0] != n or x.shape != t_idx.shape:
-            raise ValueError(f"{name} must be a {dt} tensor [{n}, k] on {logits.device}")
-    return t_idx.contiguous(), t_logits.contiguous()
+    """The checked arguments that the distillation calls share: logits and
+    their pitch, the teacher's lists and their width."""
+    logits, ld = _matrix(logits, "logits")
+    if t_idx.dim() != 2:
+        raise ValueError("t_idx must be a 2-D tensor")
+    shape = (logits.shape[0], t_idx.shape[1])
+    return (logits, ld, _given(t_idx, "t_idx", shape, _torch.int32, logits),
+            _given(t_logits, "t_logits", shape, _torch.float32, logits), shape[1])
 
 
 def distill_topk(logits, t_idx, t_logits, temperature: float = 1.0, out_loss=None, out_stats=None, stream=None):
@@ -495,16 +504,16 @@ def distill_topk(logits, t_idx, t_logits, temperature: float = 1.0, out_loss=Non
     top-k logits (int32 / float32 [n, k], as :meth:`Head.topk_many` returns
     them; negative indices are empty slots): T^2 KL(teacher || student) per
     row.  Returns (loss [n], stats [n, 2]); stats go to distill_topk_grad."""
-    import torch
-    with _on(logits, "logits", stream) as s:
-        t_idx, t_logits = _teacher(logits, t_idx, t_logits)
-        logits, ld = _matrix(logits, "logits")
-        n, V = logits.shape
-        out_loss = _contiguous_output(out_loss, "out_loss", (n,), torch.float32, logits)
-        out_stats = _contiguous_output(out_stats, "out_stats", (n, 2), torch.float32, logits)
-        check(vie_distill_topk(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
-                               t_logits.data_ptr(), t_idx.shape[1], temperature, out_loss.data_ptr(),
-                               out_stats.data_ptr(), s))
+    if not _here(logits, "logits") or stream is not None:
+        with _on(logits, stream):
+            return distill_topk(logits, t_idx, t_logits, temperature, out_loss, out_stats)
+    logits, ld, t_idx, t_logits, k = _teacher(logits, t_idx, t_logits)
+    n, V = logits.shape
+    out_loss = _contiguous_output(out_loss, "out_loss", (n,), _torch.float32, logits)
+    out_stats = _contiguous_output(out_stats, "out_stats", (n, 2), _torch.float32, logits)
+    check(vie_distill_topk(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
+                           t_logits.data_ptr(), k, temperature, out_loss.data_ptr(), out_stats.data_ptr(),
+                           _stream_ptr(None)))
     return out_loss, out_stats
 
 
@@ -512,19 +521,17 @@ def distill_topk_grad(logits, t_idx, t_logits, stats, grad_loss, temperature: fl
                       stream=None):
     """Gradient of sum(grad_loss * loss) with respect to the student's logits,
     in their type; `stats` come from distill_topk.  out_grad may be logits."""
-    import torch
-    with _on(logits, "logits", stream) as s:
-        t_idx, t_logits = _teacher(logits, t_idx, t_logits)
-        logits, ld = _matrix(logits, "logits")
-        n, V = logits.shape
-        if stats.dtype != torch.float32 or tuple(stats.shape) != (n, 2) or stats.device != logits.device:
-            raise ValueError(f"stats must be a float32 tensor [{n}, 2] on {logits.device}")
-        stats = stats.contiguous()
-        grad_loss = _vector(grad_loss, "grad_loss", torch.float32, n, logits)
-        out_grad, ld_grad = _matrix_output(out_grad, "out_grad", (n, V), logits.dtype, logits)
-        check(vie_distill_topk_grad(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
-                                    t_logits.data_ptr(), t_idx.shape[1], temperature, stats.data_ptr(),
-                                    grad_loss.data_ptr(), out_grad.data_ptr(), ld_grad, s))
+    if not _here(logits, "logits") or stream is not None:
+        with _on(logits, stream):
+            return distill_topk_grad(logits, t_idx, t_logits, stats, grad_loss, temperature, out_grad)
+    logits, ld, t_idx, t_logits, k = _teacher(logits, t_idx, t_logits)
+    n, V = logits.shape
+    stats = _given(stats, "stats", (n, 2), _torch.float32, logits)
+    grad_loss = _given(grad_loss, "grad_loss", (n,), _torch.float32, logits)
+    out_grad, ld_grad = _matrix_output(out_grad, "out_grad", (n, V), logits.dtype, logits)
+    check(vie_distill_topk_grad(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
+                                t_logits.data_ptr(), k, temperature, stats.data_ptr(), grad_loss.data_ptr(),
+                                out_grad.data_ptr(), ld_grad, _stream_ptr(None)))
     return out_grad
 
 
@@ -533,17 +540,17 @@ def distill_topk_step(logits, t_idx, t_logits, grad_loss, temperature: float = 1
     """distill_topk and distill_topk_grad in one call: (loss [n], gradient
     [n, V]).  grad_loss [n] is the weight of each row's loss; out_grad may be
     logits."""
-    import torch
-    with _on(logits, "logits", stream) as s:
-        t_idx, t_logits = _teacher(logits, t_idx, t_logits)
-        logits, ld = _matrix(logits, "logits")
-        n, V = logits.shape
-        grad_loss = _vector(grad_loss, "grad_loss", torch.float32, n, logits)
-        out_loss = _contiguous_output(out_loss, "out_loss", (n,), torch.float32, logits)
-        out_grad, ld_grad = _matrix_output(out_grad, "out_grad", (n, V), logits.dtype, logits)
-        check(vie_distill_topk_step(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
-                                    t_logits.data_ptr(), t_idx.shape[1], temperature, grad_loss.data_ptr(),
-                                    out_loss.data_ptr(), 0, out_grad.data_ptr(), ld_grad, s))
+    if not _here(logits, "logits") or stream is not None:
+        with _on(logits, stream):
+            return distill_topk_step(logits, t_idx, t_logits, grad_loss, temperature, out_loss, out_grad)
+    logits, ld, t_idx, t_logits, k = _teacher(logits, t_idx, t_logits)
+    n, V = logits.shape
+    grad_loss = _given(grad_loss, "grad_loss", (n,), _torch.float32, logits)
+    out_loss = _contiguous_output(out_loss, "out_loss", (n,), _torch.float32, logits)
+    out_grad, ld_grad = _matrix_output(out_grad, "out_grad", (n, V), logits.dtype, logits)
+    check(vie_distill_topk_step(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
+                                t_logits.data_ptr(), k, temperature, grad_loss.data_ptr(), out_loss.data_ptr(), 0,
+                                out_grad.data_ptr(), ld_grad, _stream_ptr(None)))
     return out_loss, out_grad
 
 
@@ -551,16 +558,17 @@ def embed(table, tokens, scale: float = 1.0, out=None, out_dtype=None, stream=No
     """scale * table[tokens] (table [V, d] and out [n, d] bf16 or fp32, tokens
     int32 [n]); negative tokens give zeros.  out_dtype (of a new `out`)
     defaults to the table's type; float32 rows are what a Head takes."""
-    import torch
-    with _on(table, "table", stream) as s:
-        table, ld = _matrix(table, "table")
-        n, (V, d) = tokens.numel(), table.shape
-        tokens = _vector(tokens, "tokens", torch.int32, n, table)
-        if out is not None and out_dtype is None:
-            out_dtype = out.dtype
-        out, ld_out = _matrix_output(out, "out", (n, d), out_dtype or table.dtype, table)
-        check(vie_embed(table.data_ptr(), _dtype_code(table, "table"), V, d, ld, tokens.data_ptr(), n, scale,
-                        out.data_ptr(), _dtype_code(out, "out"), ld_out, s))
+    if not _here(table, "table") or stream is not None:
+        with _on(table, stream):
+            return embed(table, tokens, scale, out, out_dtype)
+    table, ld = _matrix(table, "table")
+    n, (V, d) = tokens.numel(), table.shape
+    tokens = _given(tokens, "tokens", (n,), _torch.int32, table)
+    if out_dtype is None:
+        out_dtype = table.dtype if out is None else out.dtype
+    out, ld_out = _matrix_output(out, "out", (n, d), out_dtype, table)
+    check(vie_embed(table.data_ptr(), _dtype_code(table, "table"), V, d, ld, tokens.data_ptr(), n, scale,
+                    out.data_ptr(), _dtype_code(out, "out"), ld_out, _stream_ptr(None)))
     return out
 
 
@@ -571,25 +579,27 @@ def embed_grad(tokens, grad, V: int, scale: float = 1.0, out=None, accumulate: b
     accumulate out[v] += that.  out_dtype (of a new `out`) defaults to
     float32.  workspace: a uint8 CUDA tensor that is used if it is large
     enough (vie_embed_grad_workspace), else the call allocates one."""
-    import torch
-    with _on(grad, "grad", stream) as s:
-        grad, ld_grad = _matrix(grad, "grad")
-        n, d = grad.shape
-        tokens = _vector(tokens, "tokens", torch.int32, n, grad)
-        if out is None and accumulate:
-            raise ValueError("accumulate needs the gradient to add to (out)")
-        if out is not None and out_dtype is None:
-            out_dtype = out.dtype
-        out, ld = _matrix_output(out, "out", (V, d), out_dtype or torch.float32, grad)
-        st, need = vie_embed_grad_workspace(n, V, d)
-        check(st)
-        if workspace is None or workspace.numel() < need:
-            workspace = torch.empty((need,), dtype=torch.uint8, device=grad.device)
-        elif workspace.dtype != torch.uint8 or workspace.device != grad.device or not workspace.is_contiguous():
-            raise ValueError(f"workspace must be a contiguous uint8 tensor on {grad.device}")
-        check(vie_embed_grad(tokens.data_ptr(), n, grad.data_ptr(), _dtype_code(grad, "grad"), ld_grad, scale, V, d,
-                             out.data_ptr(), _dtype_code(out, "out"), ld, 1 if accumulate else 0,
-                             workspace.data_ptr(), workspace.numel(), s))
+    if not _here(grad, "grad") or stream is not None:
+        with _on(grad, stream):
+            return embed_grad(tokens, grad, V, scale, out, accumulate, out_dtype, workspace)
+    grad, ld_grad = _matrix(grad, "grad")
+    n, d = grad.shape
+    tokens = _given(tokens, "tokens", (n,), _torch.int32, grad)
+    if out is None and accumulate:
+        raise ValueError("accumulate needs the gradient to add to (out)")
+    if out_dtype is None:
+        out_dtype = _torch.float32 if out is None else out.dtype
+    st, need = vie_embed_grad_workspace(n, V, d)
+    check(st)
+    out, ld = _matrix_output(out, "out", (V, d), out_dtype, grad)
+    if workspace is None or workspace.numel() < need:
+        workspace = _torch.empty((need,), dtype=_torch.uint8, device=grad.device)
+    elif workspace.dtype is not _torch.uint8 or not workspace.is_contiguous() or not workspace.is_cuda or \
+            workspace.get_device() != grad.get_device():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {grad.device}")
+    check(vie_embed_grad(tokens.data_ptr(), n, grad.data_ptr(), _dtype_code(grad, "grad"), ld_grad, scale, V, d,
+                         out.data_ptr(), _dtype_code(out, "out"), ld, 1 if accumulate else 0, workspace.data_ptr(),
+                         workspace.numel(), _stream_ptr(None)))
     return out
 
 
@@ -599,22 +609,28 @@ def sample_logits(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
     number u in [0, 1) and one setting of each kind per row (float32 [batch];
     top_k int32; None: 1, off, off, off).  Returns (token int32 [batch],
     probability float32 [batch])."""
-    import torch
-    with _on(logits, "logits", stream) as s:
-        logits, ld = _matrix(logits, "logits")
-        b, V = logits.shape
-        u = _vector(u, "u", torch.float32, b, logits)
-        kept, ptr = [], []
-        for x, name, dt in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
-                            (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
-            if x is not None:
-                x = _vector(x, name, dt, b, logits)
-            kept.append(x)
-            ptr.append(0 if x is None else x.data_ptr())
-        out_token = _contiguous_output(out_token, "out_token", (b,), torch.int32, logits)
-        out_prob = _contiguous_output(out_prob, "out_prob", (b,), torch.float32, logits)
-        check(vie_sample_logits(logits.data_ptr(), _dtype_code(logits, "logits"), b, V, ld, u.data_ptr(), *ptr,
-                                out_token.data_ptr(), out_prob.data_ptr(), s))
+    if not _here(logits, "logits") or stream is not None:
+        with _on(logits, stream):
+            return sample_logits(logits, u, temperature, top_k, top_p, min_p, out_token, out_prob)
+    logits, ld = _matrix(logits, "logits")
+    b, V = logits.shape
+    f32, i32 = _torch.float32, _torch.int32
+    u = _given(u, "u", (b,), f32, logits)
+    if temperature is not None:
+        temperature = _given(temperature, "temperature", (b,), f32, logits)
+    if top_k is not None:
+        top_k = _given(top_k, "top_k", (b,), i32, logits)
+    if top_p is not None:
+        top_p = _given(top_p, "top_p", (b,), f32, logits)
+    if min_p is not None:
+        min_p = _given(min_p, "min_p", (b,), f32, logits)
+    out_token = _contiguous_output(out_token, "out_token", (b,), i32, logits)
+    out_prob = _contiguous_output(out_prob, "out_prob", (b,), f32, logits)
+    check(vie_sample_logits(logits.data_ptr(), _dtype_code(logits, "logits"), b, V, ld, u.data_ptr(),
+                            0 if temperature is None else temperature.data_ptr(),
+                            0 if top_k is None else top_k.data_ptr(), 0 if top_p is None else top_p.data_ptr(),
+                            0 if min_p is None else min_p.data_ptr(), out_token.data_ptr(), out_prob.data_ptr(),
+                            _stream_ptr(None)))
     return out_token, out_prob
 
 

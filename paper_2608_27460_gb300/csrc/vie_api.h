@@ -4,6 +4,7 @@
 
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 #include "vie_head.h"
@@ -18,6 +19,26 @@ vie_status fail_cuda(cudaError_t e, const char *what);
 // Device address of the flag word that vie_device_status reads, on the
 // current device.
 cudaError_t device_flag_word(uint32_t **word);
+
+// Runs set(), which prepares a kernel for the current device, on the first call
+// for that device (again after a failure).
+class PerDevice {
+  public:
+    template <typename F>
+    cudaError_t once(const F &set) {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+        if (done_.load(std::memory_order_acquire) & bit) return cudaSuccess;
+        e = set();
+        if (e == cudaSuccess) done_.fetch_or(bit, std::memory_order_release);
+        return e;
+    }
+
+  private:
+    std::atomic<uint64_t> done_{0};
+};
 
 inline bool aligned_to(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 

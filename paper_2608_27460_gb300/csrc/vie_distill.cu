@@ -438,21 +438,16 @@ struct DistillLaunch {
     }
 };
 
-template <typename F>
-static cudaError_t allow(F kernel, size_t smem, int slices) {
-    cudaError_t e = cudaSuccess;
-    if (smem > 40 * 1024)
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-    if (e == cudaSuccess && slices > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    return e;
-}
-
 template <typename T, bool FWD, bool BWD>
 static cudaError_t start_distill(const DistillParams &p, int64_t n, int slices, cudaStream_t s) {
     auto kernel = distill_kernel<T, FWD, BWD>;
-    const size_t smem = 12 * static_cast<size_t>(p.k) + (BWD ? 4 * seen_slots(p.k) : 0);
-    const cudaError_t e = allow(kernel, smem, FWD ? slices : 1);
-    if (e != cudaSuccess) return e;
+    const size_t smem = 12 * static_cast<size_t>(p.k) + (BWD ? 4 * seen_slots(p.k) : 0);  // 20 KB at most
+    if (FWD && slices > kSlices) {
+        static PerDevice prepared;
+        const cudaError_t e =
+            prepared.once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); });
+        if (e != cudaSuccess) return e;
+    }
     DistillLaunch l(kDistillThreads, slices, FWD, smem, s);
     l.cfg.gridDim = dim3(static_cast<unsigned>(n * slices));
     return cudaLaunchKernelEx(&l.cfg, kernel, p, log2_of(slices));

@@ -68,8 +68,18 @@ __device__ uint32_t g_dev_err = 0;
 
 }  // namespace
 
+// Looked up once per device.
 cudaError_t vie::device_flag_word(uint32_t **word) {
-    return cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_dev_err);
+    static std::atomic<uint32_t *> known[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const bool keeps = dev >= 0 && dev < 64;
+    *word = keeps ? known[dev].load(std::memory_order_acquire) : nullptr;
+    if (*word != nullptr) return cudaSuccess;
+    e = cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_dev_err);
+    if (e == cudaSuccess && keeps) known[dev].store(*word, std::memory_order_release);
+    return e;
 }
 
 namespace {

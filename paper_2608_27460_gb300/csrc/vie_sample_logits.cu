@@ -95,7 +95,7 @@ struct SampleSmem {
     uint64_t slots[2][kMaxSplit][4];
     uint64_t warp_sums[kSampleWarps];
     float scratch[kSampleWarps];
-    float edge[2];               // least logits of the two depths
+    float edge[2], bin_edge[2];  // least logits of the two depths; of a bin and those before it
     uint64_t told[2][3];         // of the first CTA: what it has found, for all
     uint64_t found[2], total;    // of the first CTA: what its threads have found, and all bins' amount
     uint32_t cand_count;
@@ -141,9 +141,10 @@ struct SampleRow {
         }
         if (sl.has_edge()) of_vector(sl.load_edge(), sl.edge());  // (values outside the row: -inf)
     }
-    // The same for the values of `least` and more, if any: a vector without one is passed over at once.
+    // The same for the values of `least` and more, and below `limit` (NaN: no
+    // limit), if any: a vector without one of `least` is passed over at once.
     template <typename F>
-    __device__ __forceinline__ void each_above(float least, const F &f) const {
+    __device__ __forceinline__ void each_above(float least, float limit, const F &f) const {
         constexpr int kVec = Slice<T>::kVec, U = 4;
         const uint4 *const zv = sl.vectors();
         auto of_vector = [&](const uint4 &raw, int i) {
@@ -154,7 +155,7 @@ struct SampleRow {
             Vec16<T>::unpack(raw, v);
 #pragma unroll
             for (int x = 0; x < kVec; ++x)
-                if (v[x] >= least) f(v[x], sl.e0 + i * kVec + x);
+                if (v[x] >= least && !(v[x] >= limit)) f(v[x], sl.e0 + i * kVec + x);
         };
         for (int i = sl.lo + threadIdx.x; i < sl.hi; i += U * kSampleThreads) {
             uint4 raw[U];
@@ -167,12 +168,63 @@ struct SampleRow {
         }
         if (sl.has_edge()) of_vector(sl.load_edge(), sl.edge());
     }
+    // f(z) for the values of `least` and more, 32 at a time: those that a warp
+    // finds wait in a queue until they fill it.  The candidates' memory is used.
+    template <typename F>
+    __device__ __forceinline__ void each_above_in_turn(float least, const F &f) const {
+        constexpr int kVec = Slice<T>::kVec, U = 4;
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        float *const queue = reinterpret_cast<float *>(sm.cand) + warp * (2 * kCap / kSampleWarps);  // 512 values
+        static_assert(2 * kCap / kSampleWarps >= 32 * 8 + 32, "a vector of every lane, and what waits");
+        int waiting = 0;  // the same in all lanes
+        auto work = [&] {
+            __syncwarp();
+            while (waiting >= 32) {
+                waiting -= 32;
+                f(queue[waiting + lane]);
+            }
+            __syncwarp();
+        };
+        auto of_vector = [&](const uint4 &raw) {
+            float v[kVec];
+            Vec16<T>::unpack(raw, v);
+#pragma unroll
+            for (int x = 0; x < kVec; ++x) {
+                const uint32_t in = __ballot_sync(0xFFFFFFFFu, v[x] >= least);
+                if (v[x] >= least) queue[waiting + __popc(in & ((1u << lane) - 1u))] = v[x];
+                waiting += __popc(in);
+            }
+            work();
+        };
+        constexpr uint32_t kNone = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;  // -inf
+        const uint4 none = make_uint4(kNone, kNone, kNone, kNone);
+        const uint4 *const zv = sl.vectors();
+        for (int i0 = sl.lo + 32 * warp; i0 < sl.hi; i0 += U * kSampleThreads) {  // the same in all lanes
+            const int i = i0 + lane;
+            uint4 raw[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u] = i + u * kSampleThreads < sl.hi ? zv[i + u * kSampleThreads] : none;
+#pragma unroll
+            for (int u = 0; u < U; ++u) of_vector(raw[u]);
+        }
+        if (warp == 0) of_vector(sl.has_edge() ? sl.load_edge() : none);
+        __syncwarp();
+        if (lane < waiting) f(queue[lane]);
+    }
     // The least logit in bins 0 .. bin; a whole warp calls.
     __device__ __forceinline__ float least_of_bins(int bin) const {
+        const uint32_t lane = threadIdx.x & 31;
+        auto within = [&](uint32_t key) { return Weigh::bin_of(weigh.depth(unorder_f32(key))) <= bin; };
         uint32_t lo = order_f32(-INFINITY) + 1, hi = order_f32(weigh.best);  // (the best is in bin 0)
+        {  // it is near where the real numbers have it
+            const float guess = weigh.best - static_cast<float>(bin + 1) / (kBinsPerUnit * weigh.inv);
+            const uint32_t key = order_f32(guess);
+            if (key > lo + 512 && key + 511 < hi && __ballot_sync(0xFFFFFFFFu, within(lane & 1 ? key + 511 : key - 512)) == 0xAAAAAAAAu)
+                lo = key - 511, hi = key + 511;
+        }
         while (lo < hi) {  // ends: hi - lo falls to a 32nd at each turn
-            const uint32_t step = (hi - lo) / 32 + 1, key = lo + min((threadIdx.x & 31u) * step, hi - lo);
-            const uint32_t in = __ballot_sync(0xFFFFFFFFu, Weigh::bin_of(weigh.depth(unorder_f32(key))) <= bin);
+            const uint32_t step = (hi - lo) / 32 + 1, key = lo + min(lane * step, hi - lo);
+            const uint32_t in = __ballot_sync(0xFFFFFFFFu, within(key));
             if (in == 0) {  // (the lanes end before hi)
                 lo += 31 * step + 1;
                 continue;
@@ -250,28 +302,35 @@ struct SampleRow {
         if (b) atomicAdd(&sm.hist[1][bin], b);
         if (c) atomicAdd(&sm.hist[2][bin], c);
     }
-    // First CTA: sm.before from the histograms of all CTAs (complete, after a sync).
+    // sm.before of the first CTA, from the histograms of all CTAs (complete, after
+    // a sync): each CTA adds up its share of the bins, the first one the
+    // running values.  All CTAs call; the candidates' memory is used.
     __device__ __forceinline__ void join_hists(bool by_count) const {
-        const int b = 2 * threadIdx.x;
-        uint64_t v0 = 0, v1 = 0;
-        for (int r0 = 0; r0 < slices; r0 += 4) {
-            uint2 x[4][3];
+        const int share = kBins / slices, groups = max(1, kSampleThreads / share);  // groups of threads share the CTAs
+        uint64_t *const stage = sm.cand;
+        for (int t = threadIdx.x; t < share * groups; t += kSampleThreads) {
+            const int b = rank * share + t % share;
+            uint64_t v = 0;
+            for (int r = t / share; r < slices; r += groups) {
+                uint32_t x[3] = {};
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+                for (int part = 0; part < 3; ++part)
+                    if (!(by_count && part > 0)) x[part] = *cluster_peer(&sm.hist[part][b], r);
 #pragma unroll
-                for (int part = 0; part < 3; ++part) {
-                    x[r][part] = make_uint2(0, 0);
-                    if (r0 + r < slices && !(by_count && part > 0))
-                        x[r][part] = *reinterpret_cast<const uint2 *>(cluster_peer(&sm.hist[part][b], r0 + r));
-                }
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int part = 0; part < 3; ++part) {
-                    v0 += static_cast<uint64_t>(x[r][part].x) << (14 * part);
-                    v1 += static_cast<uint64_t>(x[r][part].y) << (14 * part);
-                }
+                for (int part = 0; part < 3; ++part) v += static_cast<uint64_t>(x[part]) << (14 * part);
+            }
+            stage[t] = v;
         }
+        __syncthreads();
+        for (int t = threadIdx.x; t < share; t += kSampleThreads) {
+            uint64_t v = 0;
+            for (int g = 0; g < groups; ++g) v += stage[g * share + t];
+            *cluster_peer(&sm.before[rank * share + t], 0) = v;
+        }
+        sync();
+        if (rank != 0) return;
+        const int b = 2 * threadIdx.x;
+        const uint64_t v0 = sm.before[b], v1 = sm.before[b + 1];
         uint64_t total;
         const uint64_t run = block_before(v0 + v1, &total);
         sm.before[b] = run;
@@ -318,16 +377,26 @@ struct SampleRow {
     }
 
     // ---- tokens to rank
-    // The slice's values of `least` and more for which in(z) holds go to the first CTA, unless they are too many.
-    template <typename F>
-    __device__ __forceinline__ void gather(float least, const F &in) const {
+    // The slice's values of `least` and more, and below `limit` (NaN: no limit), go
+    // to the first CTA, unless they are too many.
+    __device__ __forceinline__ void gather(float least, float limit) const {
         uint32_t *const count = cluster_peer(&sm.cand_count, 0);
         uint64_t *const cand = cluster_peer(&sm.cand[0], 0);
-        each_above(least, [&](float z, int index) {
-            if (!in(z)) return;
+        each_above(least, limit, [&](float z, int index) {
             const uint32_t at = atomicAdd(count, 1u);
             if (at < kCap) cand[at] = make_key(z, static_cast<uint32_t>(index));
         });
+    }
+    // The least logit of bins 0 .. bin, and that of the bins before (NaN: none), in all threads of the CTA.
+    __device__ __forceinline__ void edges_of_bin(int bin, float *least, float *limit) const {
+        __syncthreads();
+        if (threadIdx.x < 64) {
+            const int b = bin - static_cast<int>(threadIdx.x >> 5);
+            const float edge = b >= 0 ? least_of_bins(b) : __int_as_float(0x7FC00000);
+            if ((threadIdx.x & 31) == 0) sm.bin_edge[threadIdx.x >> 5] = edge;
+        }
+        __syncthreads();
+        *least = sm.bin_edge[0], *limit = sm.bin_edge[1];
     }
     // First CTA: the candidates, best first.
     __device__ __forceinline__ void rank_candidates(int n) const {
@@ -395,16 +464,16 @@ struct SampleRow {
         uint64_t bin = 0;
         crowded = false;
         find_bin_for_all(target, &bin, before);
-        gather(least_of_bins(static_cast<int>(bin)),
-               [&](float z) { return Weigh::bin_of(weigh.depth(z)) == static_cast<int>(bin); });
+        float least_z, limit_z;
+        edges_of_bin(static_cast<int>(bin), &least_z, &limit_z);
+        gather(least_z, limit_z);
         sync();
         uint32_t n = *cluster_peer(&sm.cand_count, 0);
         if (n <= kCap) return n;
         // a crowded bin: cut by keys, low .. high are left
         crowded = true;
         uint64_t most = 0, least = 0;
-        each([&](float z, int) {
-            if (Weigh::bin_of(weigh.depth(z)) != static_cast<int>(bin)) return;
+        each_above(least_z, limit_z, [&](float z, int) {
             const uint32_t key = order_f32(z);
             most = max(most, static_cast<uint64_t>(key));
             least = max(least, static_cast<uint64_t>(~key));
@@ -423,14 +492,14 @@ struct SampleRow {
                 else count_mass(b, weigh(z));
             });
             sync();
-            if (rank == 0) join_hists(by_count);
+            join_hists(by_count);
             uint64_t b = 0, more = 0;
             find_bin_for_all(target - *before, &b, &more);
             *before += more;
             high -= static_cast<uint32_t>(b) << shift;
             const uint32_t width = (1u << shift) - 1u;
             if (high - low > width) low = high - width;
-            gather(unorder_f32(low), [&](float z) { return order_f32(z) >= low && order_f32(z) <= high; });
+            gather(unorder_f32(low), unorder_f32(high + 1));  // (above +inf: NaN)
             sync();
             n = *cluster_peer(&sm.cand_count, 0);
         }
@@ -564,6 +633,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
             a.prob[row] = static_cast<float>(r.weight_of(sm.cand[at])) / static_cast<float>(M);
         }
     };
+    const float kNoLimit = __int_as_float(0x7FC00000);
     uint64_t S = 0, Q = 0;
     bool whole = true;  // all tokens of a weight are in
     if (top_k > 0 && top_k < a.V) {
@@ -573,8 +643,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
             if (bin < kBins) atomicAdd(&sm.hist[0][bin], 1u);
             r.sync();
             uint64_t last = kBins, none = 0, enough = 0;
+            r.join_hists(true);
             if (rank == 0) {
-                r.join_hists(true);
                 if (sm.total >= static_cast<uint64_t>(top_k)) {
                     r.find_bin(static_cast<uint64_t>(top_k));
                     last = sm.found[0];
@@ -583,7 +653,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
             r.tell(&last, &none, &enough);
             if (last < kBins) {
                 const float least = r.least_of_bins(static_cast<int>(last));
-                r.gather(least, [](float) { return true; });
+                r.gather(least, kNoLimit);
                 r.sync();
                 const uint32_t n = *cluster_peer(&sm.cand_count, 0);
                 cluster_arrive_relaxed();  // the first CTA stays until all have read how many there are
@@ -607,7 +677,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
         positive = r.block_sum(positive);
         r.exchange(positive);
         positive = r.sum_all(0);
-        if (rank == 0) r.join_hists(true);
+        r.join_hists(true);
         if (static_cast<uint64_t>(top_k) < positive) {
             whole = false;
             uint64_t bin = 0, before = 0;
@@ -616,7 +686,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
             const uint64_t end = bin + 1 < kBins ? firsts[bin + 1] : positive;
             if (end <= kCap) {
                 // all tokens down to that bin: the first CTA does the rest
-                r.gather(r.least_of_bins(static_cast<int>(bin)), [](float) { return true; });
+                r.gather(r.least_of_bins(static_cast<int>(bin)), kNoLimit);
                 r.sync();
                 if (rank == 0) finish_top_k(static_cast<int>(end));
                 return;
@@ -683,27 +753,27 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
     auto join_masses = [&](uint64_t most) {
         const int depth = most <= to_depth[0] ? kDepth1 : (most <= to_depth[1] ? kDepth2 : kBins);
         const float least = depth == kBins ? r.least_of_bins(kBins - 1) : sm.edge[depth == kDepth2];
-        r.each_above(least, [&](float z, int) {
+        r.each_above_in_turn(least, [&](float z) {
             const float d = weigh.depth(z);
             r.count_mass(Weigh::bin_of(d), Weigh::of_depth(d));
         });
         r.sync();
-        if (rank == 0) r.join_hists(false);
+        r.join_hists(false);
     };
     uint64_t M = min(S, Q);
+    bool joined = false;
     if (cuts_p && least_of(S) < M) {
         join_masses(least_of(S));
         M = min(M, r.shortest_prefix(false, least_of(S)).mass);
         if (r.crowded) {
             r.sync();  // (the histograms are read)
             r.clear_hist();
-            join_masses(max(M, kOne));
         }
-    } else {
-        join_masses(max(M, kOne));
+        joined = !r.crowded;
     }
     M = max(M, kOne);
     const uint64_t target = share_of(M, u24, &rest) + 1;
+    if (!joined) join_masses(target);
     uint64_t before = 0, mass;
     uint32_t key = 0;
     const uint32_t n = r.collect(false, target, &before, &key);
@@ -725,15 +795,22 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
     if (rank == 0 && tid == 0) a.prob[row] = static_cast<float>(weigh(unorder_f32(key))) / static_cast<float>(M);
 }
 
+// CTAs of a launch, about: twice what runs at once (two per SM), since rows differ in their work (64 rows of
+// 262144: 106 us; 304 CTAs: 121).
+constexpr int64_t kCtas = 608;
+
 template <typename T>
 static cudaError_t start_sample(const SampleLogitsParams &p, int64_t batch, cudaStream_t s) {
     // CTAs per row: enough for the chip, of 8192 values or more; 2^18 values at most
     int log2_slices = 0;
     while (((p.V - 1) >> log2_slices) >= (1 << 18)) ++log2_slices;
-    while (log2_slices < (batch <= 8 ? 4 : 3) && (batch << log2_slices) < 304 && (p.V >> log2_slices) >= 16384) ++log2_slices;
+    while (log2_slices < (batch <= 8 ? 4 : 3) && (batch << (log2_slices + 1)) <= kCtas && (p.V >> log2_slices) >= 16384) ++log2_slices;
     auto kernel = sample_logits_kernel<T>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SampleSmem));
-    if (e == cudaSuccess && log2_slices > 3) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    static PerDevice prepared;
+    const cudaError_t e = prepared.once([&] {
+        const cudaError_t x = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SampleSmem));
+        return x != cudaSuccess ? x : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    });
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(batch << log2_slices));
