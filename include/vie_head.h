@@ -512,7 +512,8 @@ vie_status vie_embed_grad_workspace(int64_t n, int64_t V, int32_t d, int64_t *by
  *   accumulate 0:  out[v, :]  = scale * sum over i with tokens[i] = v of grad[i, :]
  *                  (zeros for tokens that do not occur);
  *   otherwise:     out[v, :] += the same, for tokens that occur; the other rows
- *                  are not touched.
+ *                  are not touched.  (In an fp32 table, results of magnitude
+ *                  below 2^-126 become 0.)
  * The sum of a token's rows is fp32, in an order that depends on the tokens
  * alone: the same call gives the same bits.  Tokens outside [0, V) are left
  * out (V or more: the device flag, as in vie_embed).
