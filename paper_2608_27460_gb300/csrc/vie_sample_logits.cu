@@ -21,8 +21,8 @@
 //   1. the maximum.  With a top_k, the threads' own maxima give a logit that at
 //      least top_k tokens reach: those that do go to the first CTA, which
 //      ranks them and does the rest.
-//   2. the masses S and Q, and those of the tokens less than 6 and 12 units of
-//      (max z - z) / T deep;
+//   2. the masses S and Q, and about those of the tokens down to four depths
+//      (max z - z) / T;
 //   3. a histogram of masses over 1024 steps of depth, of the tokens in the least of
 //      these ranges that holds the prefix; the bin in which it ends follows;
 //   4. the tokens of that bin go to the first CTA, which ranks them and finds
@@ -95,7 +95,8 @@ struct SampleSmem {
     uint64_t slots[2][kMaxSplit][4];
     uint64_t warp_sums[kSampleWarps];
     float scratch[kSampleWarps];
-    float edge[2], bin_edge[2];  // least logits of the two depths; of a bin and those before it
+    float edge[4], bin_edge[4];  // least logits of the depths; of two bins, and of those before each
+    float4 depth_sums[kSampleWarps];
     uint64_t told[2][3];         // of the first CTA: what it has found, for all
     uint64_t found[2], total;    // of the first CTA: what its threads have found, and all bins' amount
     uint32_t cand_count;
@@ -387,16 +388,34 @@ struct SampleRow {
             if (at < kCap) cand[at] = make_key(z, static_cast<uint32_t>(index));
         });
     }
-    // The least logit of bins 0 .. bin, and that of the bins before (NaN: none), in all threads of the CTA.
-    __device__ __forceinline__ void edges_of_bin(int bin, float *least, float *limit) const {
+    // The same for the values of two ranges.
+    template <typename R>
+    __device__ __forceinline__ void gather_two(const R &r0, const R &r1) const {
+        uint32_t *const count = cluster_peer(&sm.cand_count, 0);
+        uint64_t *const cand = cluster_peer(&sm.cand[0], 0);
+        each_above(fminf(r0.least, r1.least), __int_as_float(0x7FC00000), [&](float z, int index) {
+            if (!r0.has(z) && !r1.has(z)) return;
+            const uint32_t at = atomicAdd(count, 1u);
+            if (at < kCap) cand[at] = make_key(z, static_cast<uint32_t>(index));
+        });
+    }
+    // The logits of a bin: `least` and more, and below `limit` (NaN: no limit).
+    struct Range {
+        float least, limit;
+        __device__ __forceinline__ bool has(float z) const { return z >= least && !(z >= limit); }
+    };
+    // Those of two bins, in all threads of the CTA.
+    __device__ __forceinline__ void ranges_of(int bin0, int bin1, Range *r0, Range *r1) const {
         __syncthreads();
-        if (threadIdx.x < 64) {
-            const int b = bin - static_cast<int>(threadIdx.x >> 5);
+        const int warp = threadIdx.x >> 5;
+        if (warp < 4) {
+            const int b = (warp < 2 ? bin0 : bin1) - (warp & 1);
             const float edge = b >= 0 ? least_of_bins(b) : __int_as_float(0x7FC00000);
-            if ((threadIdx.x & 31) == 0) sm.bin_edge[threadIdx.x >> 5] = edge;
+            if ((threadIdx.x & 31) == 0) sm.bin_edge[warp] = edge;
         }
         __syncthreads();
-        *least = sm.bin_edge[0], *limit = sm.bin_edge[1];
+        *r0 = Range{sm.bin_edge[0], sm.bin_edge[1]};
+        *r1 = Range{sm.bin_edge[2], sm.bin_edge[3]};
     }
     // First CTA: the candidates, best first.
     __device__ __forceinline__ void rank_candidates(int n) const {
@@ -430,10 +449,12 @@ struct SampleRow {
             }
     }
     __device__ __forceinline__ uint64_t weight_of(uint64_t key) const { return key == 0 ? 0 : weigh(key_value(key)); }
-    // First CTA: position of the first ranked candidate whose running mass (from
-    // `before` on) reaches target, and that mass, in all threads; they have that much.
-    __device__ __forceinline__ int end_of_prefix(int n, uint64_t before, uint64_t target, uint64_t *mass) const {
-        const int per = (n + kSampleThreads - 1) / kSampleThreads, lo = threadIdx.x * per, hi = min(lo + per, n);
+    // First CTA: position of the first of the ranked candidates first .. n - 1
+    // whose running mass (from `before` on) reaches target, and that mass, in
+    // all threads; they have that much.
+    __device__ __forceinline__ int end_of_prefix(int first, int n, uint64_t before, uint64_t target, uint64_t *mass) const {
+        const int per = (n - first + kSampleThreads - 1) / kSampleThreads;
+        const int lo = min(first + static_cast<int>(threadIdx.x) * per, n), hi = min(lo + per, n);
         forget();
         uint64_t own = 0, total;
         for (int i = lo; i < hi; ++i) own += weight_of(sm.cand[i]);
@@ -464,16 +485,16 @@ struct SampleRow {
         uint64_t bin = 0;
         crowded = false;
         find_bin_for_all(target, &bin, before);
-        float least_z, limit_z;
-        edges_of_bin(static_cast<int>(bin), &least_z, &limit_z);
-        gather(least_z, limit_z);
+        Range range, same;
+        ranges_of(static_cast<int>(bin), static_cast<int>(bin), &range, &same);
+        gather(range.least, range.limit);
         sync();
         uint32_t n = *cluster_peer(&sm.cand_count, 0);
         if (n <= kCap) return n;
         // a crowded bin: cut by keys, low .. high are left
         crowded = true;
         uint64_t most = 0, least = 0;
-        each_above(least_z, limit_z, [&](float z, int) {
+        each_above(range.least, range.limit, [&](float z, int) {
             const uint32_t key = order_f32(z);
             most = max(most, static_cast<uint64_t>(key));
             least = max(least, static_cast<uint64_t>(~key));
@@ -521,7 +542,7 @@ struct SampleRow {
         if (rank == 0) {
             rank_candidates(static_cast<int>(n));
             const int at = by_count ? static_cast<int>(min(max(target - before, static_cast<uint64_t>(1)), static_cast<uint64_t>(kCap))) - 1
-                                    : end_of_prefix(static_cast<int>(n), before, target, &mass);
+                                    : end_of_prefix(0, static_cast<int>(n), before, target, &mass);
             last = sm.cand[at];
             int lo = 0, hi = at;  // the first candidate with this key
             while (lo < hi) {
@@ -623,11 +644,11 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
         const uint64_t S = r.block_sum(s), Q = r.block_sum(q);
         uint64_t M = min(S, Q), mass;
         if (cuts_p && least_of(S) < M) {
-            r.end_of_prefix(top_k, 0, least_of(S), &mass);
+            r.end_of_prefix(0, top_k, 0, least_of(S), &mass);
             M = min(M, mass);
         }
         M = max(M, kOne);
-        const int at = r.end_of_prefix(top_k, 0, share_of(M, u24, &rest) + 1, &mass);
+        const int at = r.end_of_prefix(0, top_k, 0, share_of(M, u24, &rest) + 1, &mass);
         if (tid == 0) {
             a.token[row] = key_index(sm.cand[at]);
             a.prob[row] = static_cast<float>(r.weight_of(sm.cand[at])) / static_cast<float>(M);
@@ -706,53 +727,72 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
         r.clear_hist();
     }
 
-    // masses: of all tokens, of those that min_p keeps, and down to two depths
-    constexpr int kDepth1 = 6 * kBinsPerUnit, kDepth2 = 12 * kBinsPerUnit;  // bins
+    // masses: of all tokens, of those that min_p keeps, and in fp32 down to some
+    // depths (the likely ends of a prefix: the histogram need not go deeper)
+    constexpr int kDepths[4] = {5 * kBinsPerUnit, 7 * kBinsPerUnit, 17 * kBinsPerUnit / 2, 21 * kBinsPerUnit / 2};  // bins
     const bool usual = warm && best < INFINITY && weigh.inv < INFINITY;
-    uint64_t to_depth[2] = {0, 0};
+    float to_depth[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // in units of the best token's weight
     {
-        if (tid < 64) {
-            const float least = r.least_of_bins(tid < 32 ? kDepth1 - 1 : kDepth2 - 1);
-            if ((tid & 31) == 0) sm.edge[tid >> 5] = least;
+        if (tid < 128) {
+            const int i = tid >> 5;
+            const float least = r.least_of_bins((i == 0 ? kDepths[0] : i == 1 ? kDepths[1] : i == 2 ? kDepths[2] : kDepths[3]) - 1);
+            if ((tid & 31) == 0) sm.edge[i] = least;
         }
         __syncthreads();
-        const float edge1 = sm.edge[0], edge2 = sm.edge[1];
-        uint64_t s = 0, q = 0, d1 = 0, d2 = 0;
+        const float edge[4] = {sm.edge[0], sm.edge[1], sm.edge[2], sm.edge[3]};
+        uint64_t s = 0, q = 0;
         if (usual) {
             // w in two halves of 20 bits, each an addition that cuts off what is
             // below 2^-20 (2^-40); a thread's at most 520 values leave their sums below 2^32
             const float least_e = static_cast<float>(least_w) * 9.094947017729282e-13f;  // 2^-40
-            uint32_t hi[4] = {}, lo[4] = {};
-            r.each([&](float z, int) {
+            uint32_t hi[2] = {}, lo[2] = {};
+            const auto add = [&](float z, bool for_min_p) {
                 const float e = fmaxf(expf((z - best) * weigh.inv), 0.0f);  // (NaN: 0)
                 const float t = __fadd_rz(e, 8.0f), t2 = __fadd_rz(e - (t - 8.0f), 7.62939453125e-06f);  // 2^-17
                 const uint32_t h = __float_as_uint(t) - 0x41000000u, l = __float_as_uint(t2) - 0x37000000u;
                 hi[0] += h, lo[0] += l;
-                if (e >= least_e) hi[1] += h, lo[1] += l;
-                if (z >= edge1) hi[2] += h, lo[2] += l;
-                if (z >= edge2) hi[3] += h, lo[3] += l;
-            });
-            auto whole_of = [&](int i) { return (static_cast<uint64_t>(hi[i]) << 20) + lo[i]; };
-            s = whole_of(0), q = whole_of(1), d1 = whole_of(2), d2 = whole_of(3);
+                if (for_min_p && e >= least_e) hi[1] += h, lo[1] += l;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (z >= edge[i]) to_depth[i] += e;
+            };
+            if (least_w > 0) r.each([&](float z, int) { add(z, true); });
+            else r.each([&](float z, int) { add(z, false); });
+            s = (static_cast<uint64_t>(hi[0]) << 20) + lo[0];
+            q = least_w > 0 ? (static_cast<uint64_t>(hi[1]) << 20) + lo[1] : s;
         } else {
             r.each([&](float z, int) {
                 const uint64_t w = weigh(z);
                 s += w;
                 q += w >= least_w ? w : 0;
-                d1 += z >= edge1 ? w : 0;
-                d2 += z >= edge2 ? w : 0;
+                const float e = static_cast<float>(w) * 9.094947017729282e-13f;  // 2^-40
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (z >= edge[i]) to_depth[i] += e;
             });
         }
-        s = r.block_sum(s), q = r.block_sum(q), d1 = r.block_sum(d1), d2 = r.block_sum(d2);
-        r.exchange(s, q, d1, d2);
+        s = r.block_sum(s), q = r.block_sum(q);
+        const float4 d = block_sum<kSampleThreads>(make_float4(to_depth[0], to_depth[1], to_depth[2], to_depth[3]), sm.depth_sums);
+        auto pair = [](float a, float b) { return static_cast<uint64_t>(__float_as_uint(b)) << 32 | __float_as_uint(a); };
+        r.exchange(s, q, pair(d.x, d.y), pair(d.z, d.w));
         if (whole) S = r.sum_all(0);
         Q = r.sum_all(1);
-        to_depth[0] = r.sum_all(2), to_depth[1] = r.sum_all(3);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            to_depth[i] = 0.0f;
+            for (int x = 0; x < r.slices; ++x)
+                to_depth[i] += __uint_as_float(static_cast<uint32_t>(sm.slots[r.turn][x][2 + i / 2] >> (32 * (i & 1))));
+        }
     }
-    // the histogram down to a depth that holds `most`
+    // The histogram down to a depth that holds `most`.  The sums above are off by
+    // 600 roundings at most, so a ten-thousandth is taken off them.
     auto join_masses = [&](uint64_t most) {
-        const int depth = most <= to_depth[0] ? kDepth1 : (most <= to_depth[1] ? kDepth2 : kBins);
-        const float least = depth == kBins ? r.least_of_bins(kBins - 1) : sm.edge[depth == kDepth2];
+        const float share = static_cast<float>(most) * 9.094947017729282e-13f * 1.0001f;
+        int depth = 4;
+#pragma unroll
+        for (int i = 3; i >= 0; --i)
+            if (share <= to_depth[i]) depth = i;
+        const float least = depth == 4 ? r.least_of_bins(kBins - 1) : sm.edge[depth];
         r.each_above_in_turn(least, [&](float z) {
             const float d = weigh.depth(z);
             r.count_mass(Weigh::bin_of(d), Weigh::of_depth(d));
@@ -764,6 +804,49 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
     bool joined = false;
     if (cuts_p && least_of(S) < M) {
         join_masses(least_of(S));
+        // P's bin bounds M, and with it the draw: where both bounds draw from
+        // one bin, the tokens of the two bins are all that is needed
+        uint64_t bins = 0, before_p = 0, before_t = 0;
+        if (rank == 0) {
+            r.find_bin(least_of(S));
+            const uint64_t bin_p = sm.found[0], end_p = bin_p + 1 < kBins ? sm.before[bin_p + 1] : sm.total;
+            before_p = sm.found[1];
+            r.find_bin(share_of(max(min(M, end_p), kOne), u24, &rest) + 1);
+            const uint64_t bin_t = sm.found[0];
+            before_t = sm.found[1];
+            r.find_bin(share_of(max(min(M, before_p + 1), kOne), u24, &rest) + 1);
+            bins = bin_p | bin_t << 16 | static_cast<uint64_t>(sm.found[0] == bin_t) << 32;
+        }
+        r.tell(&bins, &before_p, &before_t);
+        if (bins >> 32) {
+            const int bin_p = static_cast<int>(bins & 0xFFFF), bin_t = static_cast<int>(bins >> 16 & 0xFFFF);
+            typename SampleRow<T>::Range of_p, of_t;
+            r.ranges_of(bin_p, bin_t, &of_p, &of_t);
+            r.gather_two(of_p, of_t);
+            r.sync();
+            const uint32_t n = *cluster_peer(&sm.cand_count, 0);
+            cluster_arrive_relaxed();  // the first CTA stays until all have read how many there are
+            if (n <= kCap) {
+                if (rank == 0) {
+                    const int all = static_cast<int>(n);
+                    r.rank_candidates(all);
+                    int drawn = 0;  // tokens of the draw's bin, the better ones
+                    for (int i0 = 0; i0 < all; i0 += kSampleThreads)
+                        drawn += __syncthreads_count(i0 + tid < all && of_t.has(key_value(sm.cand[min(i0 + tid, all - 1)])));
+                    uint64_t mass;
+                    r.end_of_prefix(bin_p == bin_t ? 0 : drawn, all, before_p, least_of(S), &mass);
+                    M = max(min(M, mass), kOne);
+                    const int at = r.end_of_prefix(0, drawn, before_t, share_of(M, u24, &rest) + 1, &mass);
+                    if (tid == 0) {
+                        a.token[row] = key_index(sm.cand[at]);
+                        a.prob[row] = static_cast<float>(r.weight_of(sm.cand[at])) / static_cast<float>(M);
+                    }
+                }
+                cluster_wait();
+                return;
+            }
+            cluster_wait();
+        }
         M = min(M, r.shortest_prefix(false, least_of(S)).mass);
         if (r.crowded) {
             r.sync();  // (the histograms are read)
@@ -787,7 +870,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
             return;
         }
         r.rank_candidates(static_cast<int>(n));
-        const uint64_t last = sm.cand[r.end_of_prefix(static_cast<int>(n), before, target, &mass)];
+        const uint64_t last = sm.cand[r.end_of_prefix(0, static_cast<int>(n), before, target, &mass)];
         key = static_cast<uint32_t>(last >> 32);
         if (tid == 0) a.token[row] = key_index(last);
         cluster_wait();
