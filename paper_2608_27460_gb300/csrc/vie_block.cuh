@@ -40,17 +40,6 @@ __device__ __forceinline__ float block_max(float v, float (&scratch)[NT / 32]) {
     for (int o = NT / 64; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
     return v;
 }
-template <int NT>
-__device__ __forceinline__ float block_sum(float v, float (&scratch)[NT / 32]) {
-    const int lane = threadIdx.x & 31;
-    v = warp_sum(v);
-    if (lane == 0) scratch[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = scratch[lane & (NT / 32 - 1)];
-#pragma unroll
-    for (int o = NT / 64; o >= 1; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-    return v;
-}
 __device__ __forceinline__ float4 shfl_xor_add(float4 v, int o) {
     v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
     v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);

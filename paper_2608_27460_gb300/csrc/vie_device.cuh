@@ -108,11 +108,6 @@ __device__ __forceinline__ void named_barrier_sync(int id, int count) {
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(count) : "memory");
 }
 
-// The same without waiting: this warp's part of the barrier is done.
-__device__ __forceinline__ void named_barrier_arrive(int id, int count) {
-    asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(count) : "memory");
-}
-
 // Programmatic dependent launch: a kernel launched with programmatic stream
 // serialisation may start while the previous kernel on the stream still
 // runs; griddep_wait() blocks until that kernel has finished and its writes

@@ -38,7 +38,9 @@ struct DistillParams {
     uint32_t *flag;
 };
 
-constexpr int kSlices = 8, kMaxSlices = 16;  // per row: as many as clusters may have everywhere, and for a few rows alone
+// Slices per row: up to 8; up to 16 for a few rows alone (clusters of 16 find
+// fewer places to run: 64 rows of 151936 take 18.9 us with them, 13.5 with 8).
+constexpr int kSlices = 8, kMaxSlices = 16;
 constexpr int kFewRows = 8;
 
 // exp2((z - m) c) = exp((z - m) / T), with c = log2(e) / T.  The difference comes
@@ -96,9 +98,9 @@ struct GradSlice {
 };
 
 template <typename T>
-__device__ __forceinline__ void clear_gradient(const Slice<T> &sl, const GradSlice<T> &out, int threads) {
+__device__ __forceinline__ void clear_gradient(const Slice<T> &sl, const GradSlice<T> &out) {
     const float zero[Slice<T>::kVec] = {};
-    for (int i = sl.lo + threadIdx.x; i < sl.hi; i += threads) out.store(i, zero);
+    for (int i = sl.lo + threadIdx.x; i < sl.hi; i += kDistillThreads) out.store(i, zero);
     if (sl.has_edge()) out.store_values(sl.edge(), zero);
 }
 
@@ -139,13 +141,8 @@ struct Teacher {
     bool repeats;
 
     __device__ __forceinline__ Teacher(int k_, int warps_, int me_, int32_t *list, float *z_, int32_t *seen_)
-        : z(z_), seen(seen_), k(k_), warps(warps_), me(me_), repeats(false) {
-        point_at(list);
-    }
-    __device__ __forceinline__ void point_at(int32_t *list) {
-        idx = list;
-        p = reinterpret_cast<float *>(list + k);
-    }
+        : idx(list), p(reinterpret_cast<float *>(list + k_)), z(z_), seen(seen_), k(k_), warps(warps_), me(me_),
+          repeats(false) {}
     __device__ __forceinline__ bool mine() const { return me >= 0; }
     __device__ __forceinline__ int step() const { return 32 * warps; }
     __device__ __forceinline__ void barrier() const {
@@ -158,12 +155,12 @@ struct Teacher {
         idx[j] = -1;
         return false;
     }
-    // The student's logits at the entries from value e0 to e1 of the row; slice[0] is value e0.
+    // The student's logits at the entries from value e0 (which may be below 0) to e1 of the row.
     template <typename T>
-    __device__ __forceinline__ void read_logits(const T *slice, int e0, int e1) const {
+    __device__ __forceinline__ void read_logits(const T *row, int e0, int e1) const {
 #pragma unroll 4
         for (int j = me; j < k; j += step())
-            if (idx[j] >= e0 && idx[j] < e1) z[j] = load_value(slice + (idx[j] - e0));
+            if (idx[j] >= max(e0, 0) && idx[j] < e1) z[j] = load_value(row + idx[j]);
     }
     // p: from logits to the softmax.
     __device__ __forceinline__ void softmax(DistillSmem &sm, float inv_T) const {
@@ -291,8 +288,23 @@ __device__ __forceinline__ void write_row(const DistillParams &a, int64_t row, f
     }
 }
 
-// Loss and statistics (FWD) or the gradient (BWD) or both, one row per cluster,
-// its slices read from global memory, twice for both.
+// Loss and statistics (FWD) or the gradient (BWD) or both.
+//
+// A row is a cluster's, a slice of it a CTA's; each thread keeps eight 16-byte
+// vectors in flight, its running maximum and sum, and the slices' (m, s) go to
+// all CTAs of the row by asynchronous stores that count on their mbarriers (a
+// cluster barrier with release would wait for the gradients written before).
+// The teacher's softmax is worked out meanwhile.  For both, the slice is read
+// again, from L2: with four CTAs per SM the rows in progress take 46 MB or less.
+// (Keeping slices in shared memory measured the same at 50 entries per row, and
+// twice the time at 1000, where too few threads were left for the teacher.)
+//
+// Bound by bytes.  Measured on bf16 logits, and as a share of the time that a
+// copy of the bytes read and written once would take:
+//   loss and statistics  262144 x 2048: 152 us (0.94)
+//   gradient             128256 x 2048: 155 us (0.95)
+//   both                 151936 x 4096: 466 us (0.75), 262144 x 1024: 198 (0.76),
+//                        fp32 128256 x 1024: 190 (0.77); 32000 x 4096: 112 (0.66)
 // Dynamic shared memory: the teacher's entries (indices, logits, the student's
 // logits there), the hash table (BWD).
 template <typename T, bool FWD, bool BWD>
@@ -325,7 +337,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
     const GradSlice<T> out(a, row, sl);
     if (FWD) cluster_wait();
     if (!has) {
-        if (BWD) clear_gradient(sl, out, NT);
+        if (BWD) clear_gradient(sl, out);
         if (FWD && rank == 0 && tid == 0) write_row(a, row, 0.0f, 0.0f, 0.0f);
         return;
     }
@@ -335,7 +347,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
     // The entries' logits, before a gradient may overwrite them; the loss (rank
     // 0) needs those of the whole row.
     const bool whole = FWD && rank == 0;
-    if (tea.mine()) tea.read_logits(whole ? sl.z : sl.z + sl.e0, whole ? 0 : sl.e0, whole ? a.V : sl.e1);
+    if (tea.mine() && (BWD || whole)) tea.read_logits(sl.z, whole ? 0 : sl.e0, whole ? a.V : sl.e1);
     float m, s;
     if (FWD) {
         m = -INFINITY, s = 0.0f;  // of this thread, then of the CTA, then of the row
@@ -374,7 +386,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         if (lane == 0) sm.part[warp] = make_float2(m, s);
         __syncthreads();
         if (warp == 0) send_partial(sm, slices, rank, c);
-        if (tea.mine()) tea.softmax(sm, inv_T);
+        if (tea.mine() && (BWD || rank == 0)) tea.softmax(sm, inv_T);  // while the partials travel
         join_partials(a, sm, slices, c, &m, &s);
         if (rank == 0 && tea.mine()) {
             const float loss = tea.loss(sm, a.T, inv_T, m, s);
@@ -453,7 +465,9 @@ static cudaError_t start_distill(const DistillParams &p, int64_t n, int slices, 
     return cudaLaunchKernelEx(&l.cfg, kernel, p, log2_of(slices));
 }
 
-// Bytes of a slice that one CTA takes, at most, while a cluster can have more CTAs.
+// Bytes of a slice that one CTA takes, at most, while a cluster can have more
+// CTAs.  (Gradient, 128256 x 2048: 164 us in slices of 64 KB, 155 of 128, 163 of 256;
+// each CTA reads the teacher's entries.)
 constexpr int64_t kSliceBytes = 128 * 1024;
 
 template <bool FWD, bool BWD>

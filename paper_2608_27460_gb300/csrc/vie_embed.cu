@@ -5,6 +5,12 @@
 //   lookup    out[i, :] = scale * table[token_i, :]
 //   gradient  G[v, :] (+)= scale * sum over i with token_i = v of g[i, :]
 //
+// Bound by the bytes of the rows.  Measured: lookup of 16384 rows of 1024 bf16
+// 8.9 us (a copy of the distinct rows' and the output's bytes would take 7.0), of 32
+// rows 2.1; gradient table of 262144 x 640 fp32 from 8192 rows 101 us (100 to
+// write it), 16384 rows of 1024 bf16 added to fp32 33 us (12.9; 8 of it to sort
+// the tokens, and three launches).
+//
 // Products and sums are fp32, each result is rounded once.  The gradient's
 // sums run in the order of the positions i: the tokens are sorted (stably),
 // and each run of equal tokens is summed by itself, so results do not change

@@ -226,3 +226,21 @@ def test_offsets_beyond_32_bits(vie):
     vie.embed_grad(tok, rows[torch.tensor([2, 0, 1, 2], device="cuda")], V, out=table)
     assert torch.equal(table[-3:-1], rows[:2]) and torch.equal(table[-1].float(), 2 * rows[2].float())
     assert not table[:-3].any()
+
+
+@pytest.mark.parametrize("n", [131072, 131073, 200003])
+def test_gradient_of_long_batches(vie, n):
+    """Either side of the number of tokens from which the whole array is sorted,
+    with most of them one token."""
+    g = torch.Generator().manual_seed(n)
+    tok = torch.where(torch.rand(n, generator=g) < 0.7, torch.full((n,), 12345), torch.randint(0, 50000, (n,), generator=g)).int()
+    _check_grad(vie, tok, torch.randn(n, 24, generator=g), 50000, 1.0, torch.float32)
+
+
+def test_gradient_of_one_bucket(vie):
+    """Tokens that are all alike modulo 128: one CTA sorts them, beyond its shared memory."""
+    g = torch.Generator().manual_seed(3)
+    tok = (torch.randint(0, 2000, (30000,), generator=g) * 128 + 5).int()
+    _check_grad(vie, tok, torch.randn(30000, 16, generator=g), 262144, 1.0, torch.float32)
+    _check_grad(vie, tok[1:], torch.randn(29999, 16, generator=g), 262144, 1.0, torch.bfloat16,
+                torch.zeros(262144, 16, dtype=torch.bfloat16, device="cuda"))

@@ -227,3 +227,28 @@ def test_offsets_beyond_32_bits(vie):
     got = vie.sample_logits(big, u)[0]
     assert torch.equal(got[-2:], vie.sample_logits(z, u[-2:].contiguous())[0])
     np.testing.assert_array_equal(got[:-2].cpu().numpy(), ((u[:-2].double() * 2 ** 24).long() * V >> 24).cpu().numpy())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("b,V,spread", [(6, 60000, 2.0), (3, 262144, 0.05), (4, 262144, 3.0), (700, 3000, 1.0)])
+def test_large_top_k(vie, dtype, b, V, spread):
+    """More tokens than are ranked at once, and than there are threads."""
+    g = torch.Generator().manual_seed(V + b)
+    z = (spread * torch.randn(b, V, generator=g)).to(DT[dtype])
+    u, T, k, p, m = _settings(b, seed=b)
+    k = (V * torch.rand(b, generator=g) ** 3).int() + 1
+    _check(vie, z, u, torch.where(T > 0, T, torch.ones(b)), k, p, m)
+
+
+def test_the_split_of_a_row_does_not_matter(vie):
+    """The same row alone, among few and among many others: the same draw."""
+    V = 100000
+    z = 2.0 * torch.randn(1, V, generator=torch.Generator().manual_seed(9)).cuda()
+    for top_k, top_p, min_p in ((0, 0.9, 0.0), (40, 1.0, 0.0), (0, 1.0, 0.02), (20000, 0.7, 0.0), (0, 0.9, 0.001)):
+        got = set()
+        for b in (1, 5, 40, 300, 800):
+            row = lambda x, dt=torch.float32: torch.full((b,), x, dtype=dt, device="cuda")  # noqa: E731
+            tok, prob = vie.sample_logits(z.expand(b, V).contiguous(), row(0.37), row(0.9), row(top_k, torch.int32),
+                                          row(top_p), row(min_p))
+            got |= set(zip(tok.tolist(), prob.tolist()))
+        assert len(got) == 1, got
