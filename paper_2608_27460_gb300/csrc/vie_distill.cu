@@ -54,8 +54,12 @@ __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0
 
 constexpr int kDistillThreads = 256;
 constexpr int kDistillWarps = kDistillThreads / 32;
-constexpr int kUnroll = 8;  // vectors in flight per thread
-static_assert(VIE_K_MAX <= 128 * kDistillWarps, "a warp for every 128 entries of a teacher");
+// Vectors in flight per thread: eight, but for loss and gradient on bf16 logits,
+// where a thread's 64 registers hold six (151936 x 4096: 450 us; 497 with eight).
+template <typename T, bool FWD, bool BWD>
+constexpr int kUnroll = FWD && BWD && sizeof(T) == 2 ? 6 : 8;
+constexpr int kTeacherEntries = 4;  // of a teacher, per thread of the warps that deal with it
+static_assert(VIE_K_MAX <= 32 * kTeacherEntries * kDistillWarps, "warps for all entries");
 
 struct DistillSmem {
     float2 gathered[kMaxSlices];    // per slice of the row: max z and the sum of exp((z - max z) / T)
@@ -155,12 +159,21 @@ struct Teacher {
         idx[j] = -1;
         return false;
     }
-    // The student's logits at the entries from value e0 (which may be below 0) to e1 of the row.
+    // The student's logits at the entries from value e0 (which may be below 0) to
+    // e1 of the row: read into registers, which nothing waits for, and kept in z.
     template <typename T>
-    __device__ __forceinline__ void read_logits(const T *row, int e0, int e1) const {
-#pragma unroll 4
-        for (int j = me; j < k; j += step())
-            if (idx[j] >= max(e0, 0) && idx[j] < e1) z[j] = load_value(row + idx[j]);
+    __device__ __forceinline__ void read_logits(const T *row, int e0, int e1, T (&raw)[kTeacherEntries]) const {
+#pragma unroll
+        for (int u = 0; u < kTeacherEntries; ++u) {
+            const int j = me + u * step(), i = j < k ? idx[j] : -1;
+            if (i >= max(e0, 0) && i < e1) raw[u] = row[i];
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void keep_logits(const T (&raw)[kTeacherEntries]) const {
+#pragma unroll
+        for (int u = 0; u < kTeacherEntries; ++u)
+            if (me + u * step() < k) z[me + u * step()] = load_value(&raw[u]);
     }
     // p: from logits to the softmax.
     __device__ __forceinline__ void softmax(DistillSmem &sm, float inv_T) const {
@@ -299,22 +312,25 @@ __device__ __forceinline__ void write_row(const DistillParams &a, int64_t row, f
 // (Keeping slices in shared memory measured the same at 50 entries per row, and
 // twice the time at 1000, where too few threads were left for the teacher.)
 //
-// Bound by bytes.  Measured on bf16 logits, and as a share of the time that a
-// copy of the bytes read and written once would take:
-//   loss and statistics  262144 x 2048: 152 us (0.94)
+// Bound by bytes.  Measured on bf16 logits, 50 to 64 entries per row, and as a
+// share of the time that a copy of the bytes read and written once would take:
+//   loss and statistics  262144 x 2048: 149 us (0.96)
 //   gradient             128256 x 2048: 155 us (0.95)
-//   both                 151936 x 4096: 466 us (0.75), 262144 x 1024: 198 (0.76),
-//                        fp32 128256 x 1024: 190 (0.77); 32000 x 4096: 112 (0.66)
+//   both                 151936 x 4096: 453 us (0.77), 262144 x 1024: 197 (0.77), 32000 x 4096:
+//                        104 (0.71); fp32 128256 x 1024: 173 (0.85)
+// What is left in the last: a row's exchange and its entries, which the CTAs'
+// other rows hide only in part (61 % of issue slots used, DRAM 55 % busy).
 // Dynamic shared memory: the teacher's entries (indices, logits, the student's
 // logits there), the hash table (BWD).
 template <typename T, bool FWD, bool BWD>
 __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const DistillParams a, int log2_slices) {
-    constexpr int NT = kDistillThreads, U = kUnroll;
+    constexpr int NT = kDistillThreads, U = kUnroll<T, FWD, BWD>;
     extern __shared__ __align__(16) unsigned char distill_smem[];
     __shared__ DistillSmem sm;
     int32_t *const list = reinterpret_cast<int32_t *>(distill_smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int t_warps = (a.k + 127) / 128;  // the first ones, besides their part of the row
+    // the first warps deal with the teacher, besides their part of the row
+    const int t_warps = (a.k + 32 * kTeacherEntries - 1) / (32 * kTeacherEntries);
     Teacher tea(a.k, t_warps, tid < 32 * t_warps ? tid : -1, list, reinterpret_cast<float *>(list + 2 * a.k),
                 list + 3 * a.k);
     const int slices = 1 << log2_slices, rank = blockIdx.x & (slices - 1);
@@ -347,7 +363,9 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
     // The entries' logits, before a gradient may overwrite them; the loss (rank
     // 0) needs those of the whole row.
     const bool whole = FWD && rank == 0;
-    if (tea.mine() && (BWD || whole)) tea.read_logits(sl.z, whole ? 0 : sl.e0, whole ? a.V : sl.e1);
+    T z_entries[kTeacherEntries] = {};
+    const bool keeps = tea.mine() && (BWD || whole);
+    if (keeps) tea.read_logits(sl.z, whole ? 0 : sl.e0, whole ? a.V : sl.e1, z_entries);
     float m, s;
     if (FWD) {
         m = -INFINITY, s = 0.0f;  // of this thread, then of the CTA, then of the row
@@ -384,17 +402,15 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         raise(warp_max(m));
         s = warp_sum(s);
         if (lane == 0) sm.part[warp] = make_float2(m, s);
+        if (keeps) tea.keep_logits(z_entries);
         __syncthreads();
         if (warp == 0) send_partial(sm, slices, rank, c);
-        if (tea.mine() && (BWD || rank == 0)) tea.softmax(sm, inv_T);  // while the partials travel
+        if (keeps) tea.softmax(sm, inv_T);  // while the partials travel
         join_partials(a, sm, slices, c, &m, &s);
-        if (rank == 0 && tea.mine()) {
-            const float loss = tea.loss(sm, a.T, inv_T, m, s);
-            if (tid == 0) write_row(a, row, loss, m, s);
-        }
     } else {
         m = a.stats_in[2 * row];
         s = a.stats_in[2 * row + 1];
+        if (keeps) tea.keep_logits(z_entries);
         __syncthreads();  // (grad may be logits: the entries' logits are read before it is written)
     }
     if (BWD) {
@@ -418,12 +434,16 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
             gradient_of<T>(e, coef, sl.load_edge(), v);
             out.store_values(sl.edge(), v);
         }
-        if (tea.mine()) {
+        if (keeps) {
             if (!FWD) tea.softmax(sm, inv_T);
             tea.find_repeats(sm, sl.e0, sl.e1);
         }
         __syncthreads();
-        if (tea.mine()) tea.store_gradient(out.g, sl.e0, sl.e1, e, cg, inv);
+        if (keeps) tea.store_gradient(out.g, sl.e0, sl.e1, e, cg, inv);
+    }
+    if (FWD && rank == 0 && tea.mine()) {
+        const float loss = tea.loss(sm, a.T, inv_T, m, s);
+        if (tid == 0) write_row(a, row, loss, m, s);
     }
 }
 
@@ -465,10 +485,12 @@ static cudaError_t start_distill(const DistillParams &p, int64_t n, int slices, 
     return cudaLaunchKernelEx(&l.cfg, kernel, p, log2_of(slices));
 }
 
-// Bytes of a slice that one CTA takes, at most, while a cluster can have more
-// CTAs.  (Gradient, 128256 x 2048: 164 us in slices of 64 KB, 155 of 128, 163 of 256;
-// each CTA reads the teacher's entries.)
+// Bytes of a slice that one CTA takes, at most.  Gradient alone (128256 x 2048):
+// 155 us in slices of 128 KB, 163 of 256; each CTA reads the teacher's entries.
 constexpr int64_t kSliceBytes = 128 * 1024;
+// Loss and gradient, while a cluster can have more CTAs (fp32 128256 x 1024: 174 us in
+// slices of 64 KB, 186 of 128; bf16 151936 x 4096: 450 in slices of 76 KB, 556 of 38).
+constexpr int64_t kSliceStep = 80 * 1024;
 
 template <bool FWD, bool BWD>
 static cudaError_t launch_distill(const DistillParams &p, vie_dtype dtype, int64_t n, cudaStream_t s) {
@@ -478,7 +500,7 @@ static cudaError_t launch_distill(const DistillParams &p, vie_dtype dtype, int64
         while (bytes / slices > kSliceBytes && n * slices < (1 << 30)) slices *= 2;
     } else {
         if (BWD)
-            while (slices < kSlices && bytes / slices > kSliceBytes) slices *= 2;
+            while (slices < kSlices && bytes / slices > kSliceStep) slices *= 2;
         // enough CTAs for the chip, of 32 KB of the row or more
         while (slices < (n <= kFewRows ? kMaxSlices : kSlices) && n * slices < 1024 && bytes / slices > 32768) slices *= 2;
     }
