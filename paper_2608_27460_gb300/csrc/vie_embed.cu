@@ -389,28 +389,44 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortPass
     a.counts[static_cast<size_t>(threadIdx.x) * a.blocks + blockIdx.x] = count[threadIdx.x];
 }
 
-// Exclusive prefix sums over counts[0 .. total), in place; one CTA.
+// Exclusive prefix sums over counts[0 .. total), in place; one CTA, eight
+// counters per thread at a time (total is a multiple of 8, counts 16-byte aligned).
 __global__ void __launch_bounds__(1024) sort_scan_kernel(uint32_t *counts, uint32_t total) {
     __shared__ uint32_t part[32];
     uint32_t base = 0;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (uint32_t i0 = 0; i0 < total; i0 += 1024) {
-        const uint32_t i = i0 + threadIdx.x;
-        const uint32_t v = i < total ? counts[i] : 0;
-        uint32_t incl = v;
+    for (uint32_t i0 = 0; i0 < total; i0 += 8 * 1024) {
+        const uint32_t i = i0 + 8 * threadIdx.x;
+        uint4 x[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+        if (i < total) {
+            x[0] = reinterpret_cast<const uint4 *>(counts + i)[0];
+            x[1] = reinterpret_cast<const uint4 *>(counts + i)[1];
+        }
+        const uint32_t v[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
+        uint32_t sum = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += v[k];
+        uint32_t incl = sum;
+#pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-            if (lane >= o) incl += x;
+            const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += y;
         }
         if (lane == 31) part[warp] = incl;
         __syncthreads();
-        uint32_t before = 0, all = 0;
-        for (int w = 0; w < 32; ++w) {
-            before += w < warp ? part[w] : 0;
-            all += part[w];
+        const uint32_t p = part[lane];
+        uint32_t run = base + __reduce_add_sync(0xFFFFFFFFu, lane < warp ? p : 0) + incl - sum;
+        base += __reduce_add_sync(0xFFFFFFFFu, p);
+        uint32_t w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            w[k] = run;
+            run += v[k];
         }
-        if (i < total) counts[i] = base + before + incl - v;
-        base += all;
+        if (i < total) {
+            reinterpret_cast<uint4 *>(counts + i)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            reinterpret_cast<uint4 *>(counts + i)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
         __syncthreads();
     }
 }
