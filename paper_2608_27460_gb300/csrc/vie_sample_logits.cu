@@ -20,19 +20,20 @@
 // times more from L2:
 //   1. the maximum.  With a top_k, the threads' own maxima give a logit that at
 //      least top_k tokens reach: those that do go to the first CTA, which
-//      ranks them and does the rest.
+//      does the rest.
 //   2. the masses S and Q, and about those of the tokens down to four depths
 //      (max z - z) / T;
 //   3. a histogram of masses over 1024 steps of depth, of the tokens in the least of
 //      these ranges that holds the prefix; the bin in which it ends follows;
-//   4. the tokens of that bin go to the first CTA, which ranks them and finds
-//      the prefix exactly.
+//   4. the tokens of that bin go to the first CTA, which finds the prefix's last
+//      one exactly, by finer histograms and comparisons (sorting them all took 10 us
+//      more for bins of a thousand).
 // A bin of more tokens than fit is cut further by the logits' ranking keys.
 //
 // Reading a row once would take 10 us for 64 fp32 rows of 262144; measured there:
-// 32 us if all rows have a top_k of 50, 62 to 135 with other settings (the
-// exponentials of all values, 28 instructions each, then the histogram), 81 for a
-// mixture.  One row of 151936: 11 to 32 us, a chain of seven exchanges between
+// 33 us if all rows have a top_k of 50, 64 to 110 with other settings (the
+// exponentials of all values, 28 instructions each, then the histogram), 56 for a
+// mixture.  One row of 151936: 11 to 25 us, a chain of seven exchanges between
 // its CTAs of about a microsecond each.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -51,16 +52,17 @@ struct SampleLogitsParams {
     const int32_t *top_k;
     int32_t *token;
     float *prob;
-    int64_t ld;
+    int64_t ld, batch;
     int V;
+    bool by_work;  // rows of more work first
 };
 
 constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
 constexpr int kBins = 1024;       // two per thread
 constexpr int kBinsPerUnit = 36;  // bins per unit of (max z - z) / T: weights are 0 from 27.8 units on
 constexpr int kCap = 4096;        // tokens that the first CTA ranks
-constexpr int kByCount = 256;     // tokens that are ranked by counting; more are sorted
-static_assert(kByCount <= kSampleThreads, "a thread per token");
+constexpr int kFew = 256;         // tokens that are compared with each other
+static_assert(kFew <= kSampleThreads, "a thread per token");
 constexpr int kMaxSplit = 16;     // CTAs per row, at most
 constexpr uint64_t kOne = 1ull << 40;  // the best token's weight
 static_assert(kBins == 2 * kSampleThreads, "two bins per thread");
@@ -98,6 +100,7 @@ struct Weigh {
 
 struct SampleSmem {
     uint64_t cand[kCap];         // of the first CTA: tokens to rank, as ranking keys
+    uint64_t few[kFew], few_mass[kFew];
     uint64_t before[kBins];      // of the first CTA: what the bins before this one amount to
     uint32_t hist[3][kBins];     // counts in [0], or masses in parts: their low 14 bits, the next 14, the rest
     uint64_t slots[2][kMaxSplit][4];
@@ -107,21 +110,164 @@ struct SampleSmem {
     float4 depth_sums[kSampleWarps];
     uint64_t told[2][3];         // of the first CTA: what it has found, for all
     uint64_t found[2], total;    // of the first CTA: what its threads have found, and all bins' amount
-    uint32_t cand_count;
+    uint32_t cand_count, few_count, place;
 };
+
+// What a CTA does by itself.
+struct SampleBlock {
+    SampleSmem &sm;
+    Weigh weigh;
+
+    __device__ __forceinline__ SampleBlock(SampleSmem &sm_, const Weigh &weigh_) : sm(sm_), weigh(weigh_) {}
+
+    __device__ __forceinline__ uint64_t weight_of(uint64_t key) const { return key == 0 ? 0 : weigh(key_value(key)); }
+    __device__ __forceinline__ uint64_t block_sum(uint64_t v) const {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) v += shfl_xor_u64(v, o);
+        __syncthreads();
+        if (lane == 0) sm.warp_sums[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = lane < kSampleWarps ? sm.warp_sums[lane] : 0;
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) v += shfl_xor_u64(v, o);
+        return v;
+    }
+    // Sum of the threads before this one; *total: of all.
+    __device__ __forceinline__ uint64_t block_before(uint64_t v, uint64_t *total) const {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        uint64_t incl = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint64_t x = shfl_up_u64(incl, o);
+            if (lane >= o) incl += x;
+        }
+        __syncthreads();
+        if (lane == 31) sm.warp_sums[warp] = incl;
+        __syncthreads();
+        uint64_t run = incl - v, all = 0;
+#pragma unroll
+        for (int w = 0; w < kSampleWarps; ++w) {
+            run += w < warp ? sm.warp_sums[w] : 0;
+            all += sm.warp_sums[w];
+        }
+        *total = all;
+        return run;
+    }
+    __device__ __forceinline__ uint64_t block_max_u64(uint64_t v) const {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) v = max(v, shfl_xor_u64(v, o));
+        __syncthreads();
+        if (lane == 0) sm.warp_sums[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = lane < kSampleWarps ? sm.warp_sums[lane] : 0;
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) v = max(v, shfl_xor_u64(v, o));
+        return v;
+    }
+    __device__ __forceinline__ void forget() const {  // what is looked for is always there; never an index of chance
+        __syncthreads();
+        if (threadIdx.x == 0) sm.found[0] = sm.found[1] = 0, sm.few_count = 0;
+        __syncthreads();
+    }
+    __device__ __forceinline__ void clear_hist() const {
+        for (int b = threadIdx.x; b < kBins; b += kSampleThreads) sm.hist[0][b] = sm.hist[1][b] = sm.hist[2][b] = 0;
+        __syncthreads();
+    }
+    // A slice has at most 2^18 values, and w is at most 2^40: the sums of the
+    // parts stay below 2^32 (2^18 (2^14 - 1), and 2^18 2^12).
+    __device__ __forceinline__ void count_mass(int bin, uint64_t w) const {
+        const uint32_t a = static_cast<uint32_t>(w) & 0x3FFFu, b = static_cast<uint32_t>(w >> 14) & 0x3FFFu;
+        const uint32_t c = static_cast<uint32_t>(w >> 28);
+        if (a) atomicAdd(&sm.hist[0][bin], a);
+        if (b) atomicAdd(&sm.hist[1][bin], b);
+        if (c) atomicAdd(&sm.hist[2][bin], c);
+    }
+};
+
+// First CTA: of its n candidates those with keys low .. high, best first: the
+// key of the first one at which the running mass (or number), from `before`
+// on, reaches target, and that mass, in all threads; they have that much.
+// Nothing is sorted: histograms over the keys leave a few candidates, which are
+// compared with each other.  (Keys differ, so this ends.)
+__device__ __forceinline__ uint64_t first_to_reach(SampleSmem &sm, Weigh weigh, bool by_count, int n, uint64_t low, uint64_t high,
+                                                uint64_t before, uint64_t target, uint64_t *mass) {
+    const SampleBlock block(sm, weigh);
+    const int tid = threadIdx.x;
+    auto in = [&](uint64_t key) { return key >= low && key <= high; };
+    auto mass_of = [&](uint64_t key) { return by_count ? static_cast<uint64_t>(1) : block.weight_of(key); };
+    const uint64_t *few = sm.cand;
+    int left = n;
+    while (left > kFew) {
+        const int bits = 64 - __clzll(static_cast<long long>(high - low)), shift = bits > 10 ? bits - 10 : 0;
+        block.forget();
+        block.clear_hist();
+        for (int i = tid; i < n; i += kSampleThreads) {
+            const uint64_t key = sm.cand[i];
+            if (!in(key)) continue;
+            const int b = static_cast<int>((high - key) >> shift);
+            if (by_count) atomicAdd(&sm.hist[0][b], 1u);
+            else block.count_mass(b, mass_of(key));
+        }
+        __syncthreads();
+        uint64_t v[2], total;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int b = 2 * tid + x;
+            v[x] = sm.hist[0][b] + (static_cast<uint64_t>(sm.hist[1][b]) << 14) + (static_cast<uint64_t>(sm.hist[2][b]) << 28);
+        }
+        uint64_t run = before + block.block_before(v[0] + v[1], &total);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            if (run < target && target <= run + v[x]) sm.found[0] = 2 * tid + x, sm.found[1] = run;
+            run += v[x];
+        }
+        __syncthreads();
+        before = sm.found[1];
+        high -= sm.found[0] << shift;
+        const uint64_t width = (static_cast<uint64_t>(1) << shift) - 1;
+        if (high - low > width) low = high - width;
+        for (int i = tid; i < n; i += kSampleThreads) {
+            const uint64_t key = sm.cand[i];
+            if (!in(key)) continue;
+            const uint32_t at = atomicAdd(&sm.few_count, 1u);
+            if (at < kFew) sm.few[at] = key;
+        }
+        __syncthreads();
+        left = static_cast<int>(sm.few_count);
+        few = sm.few;
+    }
+    block.forget();
+    uint64_t own = 0, mine = 0;
+    if (tid < left) {
+        own = few[tid];
+        mine = in(own) ? mass_of(own) : 0;
+        sm.few_mass[tid] = mine;
+    }
+    __syncthreads();
+    if (tid < left) {
+        uint64_t after = before;
+#pragma unroll 8
+        for (int x = 0; x < left; ++x) after += few[x] >= own ? sm.few_mass[x] : 0;
+        if (after - mine < target && target <= after) sm.found[0] = tid, sm.found[1] = after;
+    }
+    __syncthreads();
+    *mass = sm.found[1];
+    return few[sm.found[0]];
+}
 
 // What all CTAs of a row know and do together.
 template <typename T>
-struct SampleRow {
-    SampleSmem &sm;
+struct SampleRow : SampleBlock {
     const Slice<T> sl;
-    Weigh weigh;
     int slices, rank;
     int turn, tale;  // of the exchanges, and of what the first CTA tells
     bool crowded;    // the last prefix has taken the histograms
+    uint64_t key_low, key_high;
 
     __device__ __forceinline__ SampleRow(SampleSmem &sm_, const T *row, int V, int log2_slices, int rank_)
-        : sm(sm_), sl(row, V, log2_slices, rank_), weigh{0.0f, 0.0f, false}, slices(1 << log2_slices), rank(rank_), turn(0), tale(0), crowded(false) {}
+        : SampleBlock(sm_, Weigh{0.0f, 0.0f, false}), sl(row, V, log2_slices, rank_), slices(1 << log2_slices), rank(rank_), turn(0), tale(0), crowded(false), key_low(0), key_high(0) {}
 
     __device__ __forceinline__ void sync() const {
         __syncwarp();
@@ -263,54 +409,7 @@ struct SampleRow {
         for (int r = 0; r < slices; ++r) s = max(s, sm.slots[turn][r][which]);
         return s;
     }
-    __device__ __forceinline__ uint64_t block_sum(uint64_t v) const {
-        const int lane = threadIdx.x & 31;
-#pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) v += shfl_xor_u64(v, o);
-        __syncthreads();
-        if (lane == 0) sm.warp_sums[threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = lane < kSampleWarps ? sm.warp_sums[lane] : 0;
-#pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) v += shfl_xor_u64(v, o);
-        return v;
-    }
-    // Sum of the threads before this one; *total: of all.
-    __device__ __forceinline__ uint64_t block_before(uint64_t v, uint64_t *total) const {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        uint64_t incl = v;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint64_t x = shfl_up_u64(incl, o);
-            if (lane >= o) incl += x;
-        }
-        __syncthreads();
-        if (lane == 31) sm.warp_sums[warp] = incl;
-        __syncthreads();
-        uint64_t run = incl - v, all = 0;
-#pragma unroll
-        for (int w = 0; w < kSampleWarps; ++w) {
-            run += w < warp ? sm.warp_sums[w] : 0;
-            all += sm.warp_sums[w];
-        }
-        *total = all;
-        return run;
-    }
-
     // ---- histograms
-    __device__ __forceinline__ void clear_hist() const {
-        for (int b = threadIdx.x; b < kBins; b += kSampleThreads) sm.hist[0][b] = sm.hist[1][b] = sm.hist[2][b] = 0;
-        __syncthreads();
-    }
-    // A slice has at most 2^18 values, and w is at most 2^40: the sums of the
-    // parts stay below 2^32 (2^18 (2^14 - 1), and 2^18 2^12).
-    __device__ __forceinline__ void count_mass(int bin, uint64_t w) const {
-        const uint32_t a = static_cast<uint32_t>(w) & 0x3FFFu, b = static_cast<uint32_t>(w >> 14) & 0x3FFFu;
-        const uint32_t c = static_cast<uint32_t>(w >> 28);
-        if (a) atomicAdd(&sm.hist[0][bin], a);
-        if (b) atomicAdd(&sm.hist[1][bin], b);
-        if (c) atomicAdd(&sm.hist[2][bin], c);
-    }
     // sm.before of the first CTA, from the histograms of all CTAs (complete, after
     // a sync): each CTA adds up its share of the bins, the first one the
     // running values.  All CTAs call; the candidates' memory is used.
@@ -360,11 +459,6 @@ struct SampleRow {
         if (threadIdx.x == 0) sm.cand_count = 0;
         __syncthreads();
     }
-    __device__ __forceinline__ void forget() const {  // what is looked for is always there; never an index of chance
-        __syncthreads();
-        if (threadIdx.x == 0) sm.found[0] = sm.found[1] = 0;
-        __syncthreads();
-    }
     // What the first CTA's threads have (a, b, c there), in all CTAs: two
     // buffers, so that a CTA may still read the last while the next is written.
     __device__ __forceinline__ void tell(uint64_t *a, uint64_t *b, uint64_t *c) {
@@ -386,19 +480,19 @@ struct SampleRow {
     }
 
     // ---- tokens to rank
-    // The slice's values of `least` and more, and below `limit` (NaN: no limit), go
-    // to the first CTA, unless they are too many.
-    __device__ __forceinline__ void gather(float least, float limit) const {
-        uint32_t *const count = cluster_peer(&sm.cand_count, 0);
-        uint64_t *const cand = cluster_peer(&sm.cand[0], 0);
-        each_above(least, limit, [&](float z, int index) {
-            const uint32_t at = atomicAdd(count, 1u);
-            if (at < kCap) cand[at] = make_key(z, static_cast<uint32_t>(index));
-        });
-    }
-    // The same for the values of two ranges.
-    template <typename R>
-    __device__ __forceinline__ void gather_two(const R &r0, const R &r1) const {
+    // The logits of a bin: `least` and more, and below `limit` (NaN: no limit).
+    struct Range {
+        float least, limit;
+        __device__ __forceinline__ bool has(float z) const { return z >= least && !(z >= limit); }
+        // their ranking keys' ends
+        __device__ __forceinline__ uint64_t low() const { return static_cast<uint64_t>(order_f32(least)) << 32; }
+        __device__ __forceinline__ uint64_t high() const {
+            return isnan(limit) ? ~0ull : (static_cast<uint64_t>(order_f32(limit)) << 32) - 1;
+        }
+    };
+    // The slice's values in one of two ranges go to the first CTA, unless they are
+    // too many.
+    __device__ __forceinline__ void gather(const Range &r0, const Range &r1) const {
         uint32_t *const count = cluster_peer(&sm.cand_count, 0);
         uint64_t *const cand = cluster_peer(&sm.cand[0], 0);
         each_above(fminf(r0.least, r1.least), __int_as_float(0x7FC00000), [&](float z, int index) {
@@ -407,11 +501,14 @@ struct SampleRow {
             if (at < kCap) cand[at] = make_key(z, static_cast<uint32_t>(index));
         });
     }
-    // The logits of a bin: `least` and more, and below `limit` (NaN: no limit).
-    struct Range {
-        float least, limit;
-        __device__ __forceinline__ bool has(float z) const { return z >= least && !(z >= limit); }
-    };
+    __device__ __forceinline__ void gather(const Range &range) const { gather(range, range); }
+    // How many they are, after a sync.  No thread has a read of the first CTA's
+    // memory in flight afterwards.
+    __device__ __forceinline__ uint32_t gathered() const {
+        if (threadIdx.x == 0) sm.place = *cluster_peer(&sm.cand_count, 0);
+        __syncthreads();
+        return sm.place;
+    }
     // Those of two bins, in all threads of the CTA.
     __device__ __forceinline__ void ranges_of(int bin0, int bin1, Range *r0, Range *r1) const {
         __syncthreads();
@@ -425,57 +522,9 @@ struct SampleRow {
         *r0 = Range{sm.bin_edge[0], sm.bin_edge[1]};
         *r1 = Range{sm.bin_edge[2], sm.bin_edge[3]};
     }
-    // First CTA: the candidates, best first.
-    __device__ __forceinline__ void rank_candidates(int n) const {
-        if (n <= kByCount) {  // a token's rank is the number of better ones
-            __syncthreads();
-            uint64_t own = 0;
-            int place = 0;
-            if (threadIdx.x < n) {
-                own = sm.cand[threadIdx.x];
-#pragma unroll 8
-                for (int x = 0; x < n; ++x) place += sm.cand[x] > own;
-            }
-            __syncthreads();
-            if (threadIdx.x < n) sm.cand[place] = own;
-            __syncthreads();
-            return;
-        }
-        int size = 32;
-        while (size < n) size <<= 1;
-        for (int i = n + threadIdx.x; i < size; i += kSampleThreads) sm.cand[i] = 0;
-        __syncthreads();
-        for (int k = 2; k <= size; k <<= 1)
-            for (int j = k >> 1; j > 0; j >>= 1) {
-                for (int i = threadIdx.x; i < size / 2; i += kSampleThreads) {
-                    const int a = 2 * i - (i & (j - 1)), b = a + j;  // a: bit j clear
-                    const uint64_t x = sm.cand[a], y = sm.cand[b];
-                    if ((x < y) == ((a & k) == 0)) sm.cand[a] = y, sm.cand[b] = x;
-                }
-                __syncthreads();
-            }
-    }
-    __device__ __forceinline__ uint64_t weight_of(uint64_t key) const { return key == 0 ? 0 : weigh(key_value(key)); }
-    // First CTA: position of the first of the ranked candidates first .. n - 1
-    // whose running mass (from `before` on) reaches target, and that mass, in
-    // all threads; they have that much.
-    __device__ __forceinline__ int end_of_prefix(int first, int n, uint64_t before, uint64_t target, uint64_t *mass) const {
-        const int per = (n - first + kSampleThreads - 1) / kSampleThreads;
-        const int lo = min(first + static_cast<int>(threadIdx.x) * per, n), hi = min(lo + per, n);
-        forget();
-        uint64_t own = 0, total;
-        for (int i = lo; i < hi; ++i) own += weight_of(sm.cand[i]);
-        uint64_t run = before + block_before(own, &total);
-        for (int i = lo; i < hi; ++i) {
-            const uint64_t after = run + weight_of(sm.cand[i]);
-            if (run < target && target <= after) sm.found[0] = i, sm.found[1] = after;
-            run = after;
-        }
-        __syncthreads();
-        const int at = static_cast<int>(sm.found[0]);
-        *mass = sm.found[1];
-        __syncthreads();
-        return at;
+    __device__ __forceinline__ uint64_t first_of(bool by_count, int n, uint64_t low, uint64_t high, uint64_t before,
+                                                 uint64_t target, uint64_t *mass) const {
+        return first_to_reach(sm, weigh, by_count, n, low, high, before, target, mass);
     }
 
     // ---- a prefix in all of the row
@@ -487,16 +536,18 @@ struct SampleRow {
     };
     // The tokens among which the shortest prefix with `target` tokens or mass
     // ends go to the first CTA, which has joined the histograms of it: how many
-    // they are, what is before them (and, if they are one key too many to rank, that key).
+    // they are, what is before them (and, if they are one key too many to rank,
+    // that key); their keys lie in key_low .. key_high.
     __device__ __forceinline__ uint32_t collect(bool by_count, uint64_t target, uint64_t *before, uint32_t *only_key) {
         uint64_t bin = 0;
         crowded = false;
         find_bin_for_all(target, &bin, before);
         Range range, same;
         ranges_of(static_cast<int>(bin), static_cast<int>(bin), &range, &same);
-        gather(range.least, range.limit);
+        gather(range);
+        key_low = range.low(), key_high = range.high();
         sync();
-        uint32_t n = *cluster_peer(&sm.cand_count, 0);
+        uint32_t n = gathered();
         if (n <= kCap) return n;
         // a crowded bin: cut by keys, low .. high are left
         crowded = true;
@@ -527,9 +578,10 @@ struct SampleRow {
             high -= static_cast<uint32_t>(b) << shift;
             const uint32_t width = (1u << shift) - 1u;
             if (high - low > width) low = high - width;
-            gather(unorder_f32(low), unorder_f32(high + 1));  // (above +inf: NaN)
+            gather(Range{unorder_f32(low), unorder_f32(high + 1)});  // (above +inf: NaN)
+            key_low = static_cast<uint64_t>(low) << 32, key_high = static_cast<uint64_t>(high) << 32 | 0xFFFFFFFFu;
             sync();
-            n = *cluster_peer(&sm.cand_count, 0);
+            n = gathered();
         }
         *only_key = high;
         return n;
@@ -547,32 +599,14 @@ struct SampleRow {
         const uint32_t n = collect(by_count, target, &before, &only_key);
         if (n > kCap) return of_ties(by_count, target, before, only_key);
         if (rank == 0) {
-            rank_candidates(static_cast<int>(n));
-            const int at = by_count ? static_cast<int>(min(max(target - before, static_cast<uint64_t>(1)), static_cast<uint64_t>(kCap))) - 1
-                                    : end_of_prefix(0, static_cast<int>(n), before, target, &mass);
-            last = sm.cand[at];
-            int lo = 0, hi = at;  // the first candidate with this key
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if ((sm.cand[mid] >> 32) == (last >> 32)) hi = mid;
-                else lo = mid + 1;
-            }
-            ties = static_cast<uint64_t>(at - lo + 1);
+            last = first_of(by_count, static_cast<int>(n), key_low, key_high, before, target, &mass);
+            uint64_t same = 0;  // candidates with its logit, down to it
+            for (uint32_t i = threadIdx.x; i < n; i += kSampleThreads)
+                same += (sm.cand[i] >> 32) == (last >> 32) && sm.cand[i] >= last;
+            ties = block_sum(same);
         }
         tell(&last, &mass, &ties);
         return Prefix{static_cast<uint32_t>(last >> 32), ties, mass, key_index(last)};
-    }
-    __device__ __forceinline__ uint64_t block_max_u64(uint64_t v) const {
-        const int lane = threadIdx.x & 31;
-#pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) v = max(v, shfl_xor_u64(v, o));
-        __syncthreads();
-        if (lane == 0) sm.warp_sums[threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = lane < kSampleWarps ? sm.warp_sums[lane] : 0;
-#pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) v = max(v, shfl_xor_u64(v, o));
-        return v;
     }
     // The index of the ties-th token (from 1) with this key, written by the CTA that has it.
     __device__ __forceinline__ void write_tie(uint32_t key, uint64_t ties, int32_t *token) {
@@ -598,15 +632,42 @@ struct SampleRow {
     }
 };
 
+// The row of a cluster where not all run at once: within blocks of kSampleThreads
+// rows those without a top_k, several times the work, come first (64 rows of 262144, a
+// third of them without: 70 us, 81 in the batch's order).
+__device__ __forceinline__ int64_t row_by_work(const SampleLogitsParams &a, SampleSmem &sm, int64_t turn) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t base = turn / kSampleThreads * kSampleThreads;
+    const bool is_row = base + tid < a.batch;
+    bool long_row = false;
+    if (is_row) {
+        const int k = a.top_k[base + tid];
+        long_row = !(k > 0 && k < a.V) && (a.temperature == nullptr || a.temperature[base + tid] > 0.0f);
+    }
+    const uint32_t mask = __ballot_sync(0xFFFFFFFFu, long_row);
+    if (lane == 0) sm.slots[0][warp][0] = static_cast<uint64_t>(__popc(mask));
+    __syncthreads();
+    int before = __popc(mask & ((1u << lane) - 1u)), all = 0;  // long rows
+    for (int w = 0; w < kSampleWarps; ++w) {
+        const int in_warp = static_cast<int>(sm.slots[0][w][0]);
+        all += in_warp;
+        before += w < warp ? in_warp : 0;
+    }
+    if (is_row && (long_row ? before : all + tid - before) == turn - base) sm.place = tid;
+    __syncthreads();
+    return base + sm.place;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const SampleLogitsParams a, int log2_slices) {
     extern __shared__ __align__(16) unsigned char sample_smem[];
     SampleSmem &sm = *reinterpret_cast<SampleSmem *>(sample_smem);
     const int rank = blockIdx.x & ((1 << log2_slices) - 1), tid = threadIdx.x;
-    const int64_t row = blockIdx.x >> log2_slices;
+    const int64_t turn = blockIdx.x >> log2_slices;
     cluster_arrive_relaxed();  // all CTAs of the cluster run, before their memory is written
     griddep_launch_dependents();
     griddep_wait();  // the inputs may come from the kernel before this one
+    const int64_t row = a.by_work ? row_by_work(a, sm, turn) : turn;
     SampleRow<T> r(sm, static_cast<const T *>(a.logits) + row * a.ld, a.V, log2_slices, rank);
     const float temp = a.temperature != nullptr ? a.temperature[row] : 1.0f;
     const float top_p = a.top_p != nullptr ? a.top_p[row] : 1.0f, min_p = a.min_p != nullptr ? a.min_p[row] : 0.0f;
@@ -640,27 +701,30 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
 
     // The first CTA has all tokens from some depth up, n of them and top_k at
     // least: the row's token.
-    auto finish_top_k = [&](int n) {
-        r.rank_candidates(n);
+    auto finish_top_k = [&](int n, float least) {
+        const uint64_t high = static_cast<uint64_t>(order_f32(best)) << 32 | 0xFFFFFFFFu;
+        uint64_t low = static_cast<uint64_t>(order_f32(least)) << 32, mass;
+        if (n > top_k) low = r.first_of(true, n, low, high, 0, static_cast<uint64_t>(top_k), &mass);
         uint64_t s = 0, q = 0;
-        for (int i = tid; i < top_k; i += kSampleThreads) {
-            const uint64_t w = r.weight_of(sm.cand[i]);
+        for (int i = tid; i < n; i += kSampleThreads) {
+            const uint64_t key = sm.cand[i], w = key >= low ? r.weight_of(key) : 0;
             s += w;
             q += w >= least_w ? w : 0;
         }
         const uint64_t S = r.block_sum(s), Q = r.block_sum(q);
-        uint64_t M = min(S, Q), mass;
+        uint64_t M = min(S, Q);
         if (cuts_p && least_of(S) < M) {
-            r.end_of_prefix(0, top_k, 0, least_of(S), &mass);
+            r.first_of(false, n, low, high, 0, least_of(S), &mass);
             M = min(M, mass);
         }
         M = max(M, kOne);
-        const int at = r.end_of_prefix(0, top_k, 0, share_of(M, u24, &rest) + 1, &mass);
+        const uint64_t key = r.first_of(false, n, low, high, 0, share_of(M, u24, &rest) + 1, &mass);
         if (tid == 0) {
-            a.token[row] = key_index(sm.cand[at]);
-            a.prob[row] = static_cast<float>(r.weight_of(sm.cand[at])) / static_cast<float>(M);
+            a.token[row] = key_index(key);
+            a.prob[row] = static_cast<float>(r.weight_of(key)) / static_cast<float>(M);
         }
     };
+    using Range = typename SampleRow<T>::Range;
     const float kNoLimit = __int_as_float(0x7FC00000);
     uint64_t S = 0, Q = 0;
     bool whole = true;  // all tokens of a weight are in
@@ -681,12 +745,12 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
             r.tell(&last, &none, &enough);
             if (last < kBins) {
                 const float least = r.least_of_bins(static_cast<int>(last));
-                r.gather(least, kNoLimit);
+                r.gather(Range{least, kNoLimit});
                 r.sync();
-                const uint32_t n = *cluster_peer(&sm.cand_count, 0);
+                const uint32_t n = r.gathered();
                 cluster_arrive_relaxed();  // the first CTA stays until all have read how many there are
                 if (n <= kCap) {
-                    if (rank == 0) finish_top_k(static_cast<int>(n));
+                    if (rank == 0) finish_top_k(static_cast<int>(n), least);
                     cluster_wait();
                     return;
                 }
@@ -714,9 +778,10 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
             const uint64_t end = bin + 1 < kBins ? firsts[bin + 1] : positive;
             if (end <= kCap) {
                 // all tokens down to that bin: the first CTA does the rest
-                r.gather(r.least_of_bins(static_cast<int>(bin)), kNoLimit);
+                const float least = r.least_of_bins(static_cast<int>(bin));
+                r.gather(Range{least, kNoLimit});
                 r.sync();
-                if (rank == 0) finish_top_k(static_cast<int>(end));
+                if (rank == 0) finish_top_k(static_cast<int>(end), least);
                 return;
             }
             // too many to rank: their last one's key, and the mass down to it
@@ -827,26 +892,22 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
         r.tell(&bins, &before_p, &before_t);
         if (bins >> 32) {
             const int bin_p = static_cast<int>(bins & 0xFFFF), bin_t = static_cast<int>(bins >> 16 & 0xFFFF);
-            typename SampleRow<T>::Range of_p, of_t;
+            Range of_p, of_t;
             r.ranges_of(bin_p, bin_t, &of_p, &of_t);
-            r.gather_two(of_p, of_t);
+            r.gather(of_p, of_t);
             r.sync();
-            const uint32_t n = *cluster_peer(&sm.cand_count, 0);
+            const uint32_t n = r.gathered();
             cluster_arrive_relaxed();  // the first CTA stays until all have read how many there are
             if (n <= kCap) {
                 if (rank == 0) {
                     const int all = static_cast<int>(n);
-                    r.rank_candidates(all);
-                    int drawn = 0;  // tokens of the draw's bin, the better ones
-                    for (int i0 = 0; i0 < all; i0 += kSampleThreads)
-                        drawn += __syncthreads_count(i0 + tid < all && of_t.has(key_value(sm.cand[min(i0 + tid, all - 1)])));
                     uint64_t mass;
-                    r.end_of_prefix(bin_p == bin_t ? 0 : drawn, all, before_p, least_of(S), &mass);
+                    r.first_of(false, all, of_p.low(), of_p.high(), before_p, least_of(S), &mass);
                     M = max(min(M, mass), kOne);
-                    const int at = r.end_of_prefix(0, drawn, before_t, share_of(M, u24, &rest) + 1, &mass);
+                    const uint64_t key = r.first_of(false, all, of_t.low(), of_t.high(), before_t, share_of(M, u24, &rest) + 1, &mass);
                     if (tid == 0) {
-                        a.token[row] = key_index(sm.cand[at]);
-                        a.prob[row] = static_cast<float>(r.weight_of(sm.cand[at])) / static_cast<float>(M);
+                        a.token[row] = key_index(key);
+                        a.prob[row] = static_cast<float>(r.weight_of(key)) / static_cast<float>(M);
                     }
                 }
                 cluster_wait();
@@ -876,8 +937,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
             cluster_wait();
             return;
         }
-        r.rank_candidates(static_cast<int>(n));
-        const uint64_t last = sm.cand[r.end_of_prefix(0, static_cast<int>(n), before, target, &mass)];
+        const uint64_t last = r.first_of(false, static_cast<int>(n), r.key_low, r.key_high, before, target, &mass);
         key = static_cast<uint32_t>(last >> 32);
         if (tid == 0) a.token[row] = key_index(last);
         cluster_wait();
@@ -890,11 +950,13 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
 constexpr int64_t kCtas = 608;
 
 template <typename T>
-static cudaError_t start_sample(const SampleLogitsParams &p, int64_t batch, cudaStream_t s) {
+static cudaError_t start_sample(SampleLogitsParams p, cudaStream_t s) {
+    const int64_t batch = p.batch;
     // CTAs per row: enough for the chip, of 8192 values or more; 2^18 values at most
     int log2_slices = 0;
     while (((p.V - 1) >> log2_slices) >= (1 << 18)) ++log2_slices;
     while (log2_slices < (batch <= 8 ? 4 : 3) && (batch << (log2_slices + 1)) <= kCtas && (p.V >> log2_slices) >= 16384) ++log2_slices;
+    p.by_work = p.top_k != nullptr && (batch << log2_slices) > kCtas / 2;
     auto kernel = sample_logits_kernel<T>;
     static PerDevice prepared;
     const cudaError_t e = prepared.once([&] {
@@ -942,8 +1004,8 @@ extern "C" vie_status vie_sample_logits(const void *logits, vie_dtype dtype, int
     if (batch == 0) return VIE_OK;
     SampleLogitsParams p = {};
     p.logits = logits, p.u = u, p.temperature = temperature, p.top_p = top_p, p.min_p = min_p, p.top_k = top_k;
-    p.token = out_token, p.prob = out_prob, p.ld = ld, p.V = static_cast<int>(V);
+    p.token = out_token, p.prob = out_prob, p.ld = ld, p.batch = batch, p.V = static_cast<int>(V);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = dtype == VIE_DTYPE_BF16 ? start_sample<__nv_bfloat16>(p, batch, s) : start_sample<float>(p, batch, s);
+    const cudaError_t e = dtype == VIE_DTYPE_BF16 ? start_sample<__nv_bfloat16>(p, s) : start_sample<float>(p, s);
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
