@@ -98,6 +98,14 @@ struct Weigh {
     }
 };
 
+// floor(2^40 e) = 2^20 high + low for 0 <= e <= 1: two additions that cut off what
+// is below 2^-20 and 2^-40.
+__device__ __forceinline__ void split_weight(float e, uint32_t *high, uint32_t *low) {
+    const float t = __fadd_rz(e, 8.0f), t2 = __fadd_rz(e - (t - 8.0f), 7.62939453125e-06f);  // 2^-17
+    *high = __float_as_uint(t) - 0x41000000u;
+    *low = __float_as_uint(t2) - 0x37000000u;
+}
+
 struct SampleSmem {
     uint64_t cand[kCap];         // of the first CTA: tokens to rank, as ranking keys
     uint64_t few[kFew], few_mass[kFew];
@@ -181,6 +189,15 @@ struct SampleBlock {
         const uint32_t a = static_cast<uint32_t>(w) & 0x3FFFu, b = static_cast<uint32_t>(w >> 14) & 0x3FFFu;
         const uint32_t c = static_cast<uint32_t>(w >> 28);
         if (a) atomicAdd(&sm.hist[0][bin], a);
+        if (b) atomicAdd(&sm.hist[1][bin], b);
+        if (c) atomicAdd(&sm.hist[2][bin], c);
+    }
+    // The same for the weight of an exponential (fewer instructions).
+    __device__ __forceinline__ void count_weight(int bin, float e) const {
+        uint32_t high, low;
+        split_weight(e, &high, &low);
+        const uint32_t b = (low >> 14 | high << 6) & 0x3FFFu, c = high >> 8;
+        atomicAdd(&sm.hist[0][bin], low & 0x3FFFu);
         if (b) atomicAdd(&sm.hist[1][bin], b);
         if (c) atomicAdd(&sm.hist[2][bin], c);
     }
@@ -277,7 +294,7 @@ struct SampleRow : SampleBlock {
     // f(z, index) for the slice's values, in no order.
     template <typename F>
     __device__ __forceinline__ void each(const F &f) const {
-        constexpr int kVec = Slice<T>::kVec, U = 4;
+        constexpr int kVec = Slice<T>::kVec, U = 2;
         const uint4 *const zv = sl.vectors();
         auto of_vector = [&](const uint4 &raw, int i) {
             float v[kVec];
@@ -814,14 +831,13 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
         const float edge[4] = {sm.edge[0], sm.edge[1], sm.edge[2], sm.edge[3]};
         uint64_t s = 0, q = 0;
         if (usual) {
-            // w in two halves of 20 bits, each an addition that cuts off what is
-            // below 2^-20 (2^-40); a thread's at most 520 values leave their sums below 2^32
+            // w in two halves of 20 bits: a thread's at most 520 values leave their sums below 2^32
             const float least_e = static_cast<float>(least_w) * 9.094947017729282e-13f;  // 2^-40
             uint32_t hi[2] = {}, lo[2] = {};
             const auto add = [&](float z, bool for_min_p) {
                 const float e = fmaxf(expf((z - best) * weigh.inv), 0.0f);  // (NaN: 0)
-                const float t = __fadd_rz(e, 8.0f), t2 = __fadd_rz(e - (t - 8.0f), 7.62939453125e-06f);  // 2^-17
-                const uint32_t h = __float_as_uint(t) - 0x41000000u, l = __float_as_uint(t2) - 0x37000000u;
+                uint32_t h, l;
+                split_weight(e, &h, &l);
                 hi[0] += h, lo[0] += l;
                 if (for_min_p && e >= least_e) hi[1] += h, lo[1] += l;
 #pragma unroll
@@ -867,7 +883,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
         const float least = depth == 4 ? r.least_of_bins(kBins - 1) : sm.edge[depth];
         r.each_above_in_turn(least, [&](float z) {
             const float d = weigh.depth(z);
-            r.count_mass(Weigh::bin_of(d), Weigh::of_depth(d));
+            r.count_weight(Weigh::bin_of(d), expf(-d));
         });
         r.sync();
         r.join_hists(false);
@@ -948,14 +964,19 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
 // CTAs of a launch, about: twice what runs at once (two per SM), since rows differ in their work (64 rows of
 // 262144: 106 us; 304 CTAs: 121).
 constexpr int64_t kCtas = 608;
+// Bytes of a row per CTA, at most: what runs at once is read again from L2 then
+// (1000 rows of 151936 fp32: 325 us in two slices, 335 in one; without a top_k 444 and 507; four: 400 and more).
+constexpr int64_t kSliceBytes = 384 << 10;
 
 template <typename T>
 static cudaError_t start_sample(SampleLogitsParams p, cudaStream_t s) {
     const int64_t batch = p.batch;
-    // CTAs per row: enough for the chip, of 8192 values or more; 2^18 values at most
+    // CTAs per row: enough for the chip, of 8192 values or more, or so that slices
+    // stay in L2; 2^18 values each at most
     int log2_slices = 0;
     while (((p.V - 1) >> log2_slices) >= (1 << 18)) ++log2_slices;
     while (log2_slices < (batch <= 8 ? 4 : 3) && (batch << (log2_slices + 1)) <= kCtas && (p.V >> log2_slices) >= 16384) ++log2_slices;
+    while (log2_slices < 3 && (p.V * static_cast<int64_t>(sizeof(T))) >> log2_slices > kSliceBytes) ++log2_slices;
     p.by_work = p.top_k != nullptr && (batch << log2_slices) > kCtas / 2;
     auto kernel = sample_logits_kernel<T>;
     static PerDevice prepared;
