@@ -252,3 +252,28 @@ def test_the_split_of_a_row_does_not_matter(vie):
                                           row(top_p), row(min_p))
             got |= set(zip(tok.tolist(), prob.tolist()))
         assert len(got) == 1, got
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_batches_of_rows_that_differ_in_work(vie, dtype):
+    """Rows without a top-k go first in large batches: the draws are those of small ones."""
+    b, V = 1100, 3001
+    z = (2 * torch.randn(b, V, generator=torch.Generator().manual_seed(12))).to(DT[dtype]).cuda()
+    u, T, k, p, m = (x.cuda() for x in _settings(b, 13))
+    tok, prob = vie.sample_logits(z, u, T, k, p, m)
+    for lo in range(0, b, 50):
+        rows = slice(lo, min(lo + 50, b))
+        one = vie.sample_logits(z[rows], u[rows], T[rows], k[rows], p[rows], m[rows])
+        assert torch.equal(tok[rows], one[0]) and torch.equal(prob[rows], one[1])
+    no_k = vie.sample_logits(z, u, T, None, p, m)
+    zero = vie.sample_logits(z, u, T, torch.zeros_like(k), p, m)
+    assert torch.equal(no_k[0], zero[0]) and torch.equal(no_k[1], zero[1])
+
+
+@pytest.mark.parametrize("V,step", [(5000, 0.0), (5000, 1e-6), (20000, 1e-7), (3000, 0.01)])
+def test_many_candidates_that_differ_little(vie, V, step):
+    """Hundreds to thousands of tokens of one bin: few keys, each of many tokens or of one."""
+    b = 24
+    z = -step * torch.randint(0, 40, (b, V), generator=torch.Generator().manual_seed(V)).float()
+    _check(vie, z, *_settings(b, 14))
+    _check(vie, z.bfloat16(), *_settings(b, 15))
