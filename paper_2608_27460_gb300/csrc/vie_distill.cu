@@ -314,9 +314,9 @@ __device__ __forceinline__ void write_row(const DistillParams &a, int64_t row, f
 //
 // Bound by bytes.  Measured on bf16 logits, 50 to 64 entries per row, and as a
 // share of the time that a copy of the bytes read and written once would take:
-//   loss and statistics  262144 x 2048: 149 us (0.96)
-//   gradient             128256 x 2048: 155 us (0.95)
-//   both                 151936 x 4096: 453 us (0.77), 262144 x 1024: 197 (0.77), 32000 x 4096:
+//   loss and statistics  262144 x 2048: 147 us (0.97)
+//   gradient             128256 x 2048: 154 us (0.96)
+//   both                 151936 x 4096: 450 us (0.78), 262144 x 1024: 197 (0.77), 32000 x 4096:
 //                        104 (0.71); fp32 128256 x 1024: 173 (0.85)
 // What is left in the last: a row's exchange and its entries, which the CTAs'
 // other rows hide only in part (61 % of issue slots used, DRAM 55 % busy).

@@ -7,8 +7,8 @@
 //
 // Bound by the bytes of the rows.  Measured: lookup of 16384 rows of 1024 bf16
 // 8.9 us (a copy of the distinct rows' and the output's bytes would take 7.0), of 32
-// rows 2.1; gradient table of 262144 x 640 fp32 from 8192 rows 101 us (100 to
-// write it), 16384 rows of 1024 bf16 added to fp32 33 us (12.9; 8 of it to sort
+// rows 1.4; gradient table of 262144 x 640 fp32 from 8192 rows 101 us (100 to
+// write it), 16384 rows of 1024 bf16 added to fp32 34 us (12.9; 8 of it to sort
 // the tokens, and three launches).
 //
 // Products and sums are fp32, each result is rounded once.  The gradient's
@@ -744,9 +744,10 @@ static cudaError_t start_embed(const EmbedParams &p, cudaStream_t s) {
     return chain(embed_kernel<TI, TO, kW, kVector>, grid, kEmbedThreads, s, p);
 }
 
-// How rows of two matrices are read and written: 8 values per lane (one 16-byte
-// vector of bf16, two of fp32) if asked for and rows are wide enough for a warp, 4 otherwise; value by
-// value where addresses do not allow either.
+// How rows of two matrices are read and written: 8 values per lane (a 16-byte
+// vector) if both are bf16 and rows are wide enough for a warp, 4 otherwise (60000 rows of
+// 1024, bf16 to fp32: 43 us; 62 with 8, whose two fp32 vectors per lane lie 32
+// bytes apart); value by value where addresses do not allow either.
 enum class Access { kWide, kNarrow, kValues };
 static Access access_of(const void *a, vie_dtype ta, int64_t lda, const void *b, vie_dtype tb, int64_t ldb, int d,
                         bool wide) {
@@ -800,7 +801,7 @@ vie_status vie_embed(const void *table, vie_dtype dtype, int64_t V, int32_t d, i
     p.scale = scale;
     cudaError_t e = device_flag_word(&p.flag);
     if (e != cudaSuccess) return fail_cuda(e, fn);
-    e = VIE_BY_TYPES(start_embed, dtype, out_dtype, access_of(table, dtype, ld, out, out_dtype, ld_out, d, dtype == VIE_DTYPE_BF16 || out_dtype == VIE_DTYPE_BF16), p,
+    e = VIE_BY_TYPES(start_embed, dtype, out_dtype, access_of(table, dtype, ld, out, out_dtype, ld_out, d, dtype == VIE_DTYPE_BF16 && out_dtype == VIE_DTYPE_BF16), p,
                      static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }

@@ -31,8 +31,8 @@
 // A bin of more tokens than fit is cut further by the logits' ranking keys.
 //
 // Reading a row once would take 10 us for 64 fp32 rows of 262144; measured there:
-// 33 us if all rows have a top_k of 50, 64 to 110 with other settings (the
-// exponentials of all values, 28 instructions each, then the histogram), 56 for a
+// 32 us if all rows have a top_k of 50, 63 to 107 with other settings (the
+// exponentials of all values, 28 instructions each, then the histogram), 55 for a
 // mixture.  One row of 151936: 11 to 25 us, a chain of seven exchanges between
 // its CTAs of about a microsecond each.
 #include <cuda_bf16.h>
@@ -961,8 +961,9 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_logits_kernel(const 
     if (rank == 0 && tid == 0) a.prob[row] = static_cast<float>(weigh(unorder_f32(key))) / static_cast<float>(M);
 }
 
-// CTAs of a launch, about: twice what runs at once (two per SM), since rows differ in their work (64 rows of
-// 262144: 106 us; 304 CTAs: 121).
+// CTAs of a launch, about: twice what runs at once (two per SM), since rows differ
+// in their work (64 rows of 262144 with settings of their own: 55 us, 78 with 304
+// CTAs; where all rows are alike 32 to 107, 21 to 91 with 304).
 constexpr int64_t kCtas = 608;
 // Bytes of a row per CTA, at most: what runs at once is read again from L2 then
 // (1000 rows of 151936 fp32: 325 us in two slices, 335 in one; without a top_k 444 and 507; four: 400 and more).
