@@ -448,7 +448,9 @@ vie_status vie_head_topk_noalloc(const void *W_out, int64_t V, int32_t d, const 
  *   n, V        0 <= n <= VIE_MANY_MAX;  1 <= V <= VIE_DISTILL_V_MAX.
  *   t_idx, t_logits  device, int32 / fp32 [n, k], in any order;
  *               1 <= k <= VIE_K_MAX.
- *   temperature > 0 and finite.
+ *   temperature > 0 and finite.  The loss is made of differences of fp32
+ *               logarithms, times T^2: their roundings, some 2^-20 T^2, are what
+ *               a large T leaves of a small loss.
  *   out_loss    device, fp32 [n].
  *   out_stats   device, fp32 [n, 2]: max z and sum_v exp((z_v - max z) / T), what
  *               vie_distill_topk_grad needs; may be NULL.

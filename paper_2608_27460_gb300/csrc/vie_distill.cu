@@ -227,20 +227,22 @@ struct Teacher {
         repeats = sm.repeats != 0;
     }
     // T^2 sum p (log p - log q) over all entries, in all of the warps; m, s: the student's statistics.
-    __device__ __forceinline__ float loss(DistillSmem &sm, float T, float inv_T, float m, float s) const {
-        float kl = 0.0f;
+    // One T is taken into the sum, log q = (z - m) / T - log s: neither T^2 nor a
+    // difference of logits over T need be within fp32, and +inf stays +inf.
+    __device__ __forceinline__ float loss(DistillSmem &sm, float T, float m, float s) const {
+        float cost = 0.0f;
         const float log_s = logf(s), m0 = finite_max(m);
 #pragma unroll 4
         for (int j = me; j < k; j += step())
-            if (p[j] != 0.0f) kl += p[j] * (logf(p[j]) - (z[j] - m0) * inv_T + log_s);
-        kl = warp_sum(kl);
+            if (p[j] != 0.0f) cost += p[j] * (T * (logf(p[j]) + log_s) - (z[j] - m0));
+        cost = warp_sum(cost);
         if (warps > 1) {
-            if ((me & 31) == 0) sm.teacher[me >> 5].z = kl;
+            if ((me & 31) == 0) sm.teacher[me >> 5].z = cost;
             barrier();
-            kl = 0.0f;
-            for (int w = 0; w < warps; ++w) kl += sm.teacher[w].z;
+            cost = 0.0f;
+            for (int w = 0; w < warps; ++w) cost += sm.teacher[w].z;
         }
-        return s == 0.0f ? INFINITY : T * T * kl;  // (no softmax: no logit above -inf)
+        return s == 0.0f ? INFINITY : T * cost;  // (no softmax: no logit above -inf)
     }
     // q - p over what the slice's loop has written at its entries; the first
     // entry of an index takes off the sum of all.
@@ -442,7 +444,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         if (keeps) tea.store_gradient(out.g, sl.e0, sl.e1, e, cg, inv);
     }
     if (FWD && rank == 0 && tea.mine()) {
-        const float loss = tea.loss(sm, a.T, inv_T, m, s);
+        const float loss = tea.loss(sm, a.T, m, s);
         if (tid == 0) write_row(a, row, loss, m, s);
     }
 }

@@ -270,3 +270,33 @@ def test_offsets_beyond_32_bits(vie):
     loss, grad = vie.distill_topk_step(big, idx_all, t_all, gl_all, out_grad=big)
     assert torch.equal(loss[-2:], want[0]) and torch.equal(grad[-2:], want[1])
     assert (loss[:-2] == 0).all() and not grad[:-2].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1e-38, 1e-30, 1e-24, 1e-20, 1e18, 1e20, 1e30])
+def test_temperatures_whose_square_leaves_fp32(vie, dtype, T):
+    """Any positive finite temperature: T^2 is 0 or infinite in fp32 at most of
+    these, the loss (about T times a difference of logits where T is small) is not.
+    Where T^2 times the roundings' error is beyond fp32, only its sign of NaN is looked at."""
+    T = float(torch.tensor(T, dtype=torch.float32))
+    n, V = 4, 64
+    z, idx, t, gl = _inputs(n, V, V, dtype, seed=41)
+    z[1, idx[1, t[1].argmax()].long()] = -math.inf  # the teacher wants a masked token: +inf
+    idx[2, 5:] = -1
+    t[3] = z[3, idx[3].long()].float()              # the same distribution
+    want_loss, _, want_grad, loss_tol, _, grad_tol = ref.distill(z, idx, t, T, gl)
+    zc, ic, tc, gc = z.cuda(), idx.cuda(), t.cuda(), gl.cuda()
+    least = 2.0 ** -149  # spacing of the smallest fp32 values
+    largest = torch.finfo(torch.float32).max
+    for loss, grad in (vie.distill_topk_step(zc, ic, tc, gc, temperature=T),
+                       (vie.distill_topk(zc, ic, tc, temperature=T)[0], None)):
+        loss = loss.double().cpu()
+        assert not torch.isnan(loss).any() and loss[1] == math.inf
+        for r in (0, 2, 3):
+            want = float(want_loss[r].float())  # (+inf where the loss itself is beyond fp32)
+            if float(loss_tol[r]) < largest:
+                assert float(loss[r]) == want or abs(float(loss[r]) - want) <= float(loss_tol[r]) + 2 * least, r
+        if grad is not None:
+            grad = grad.double().cpu()
+            tol = grad_tol + (ref.out_round(z.dtype) + ref.U) * want_grad.abs() + 2 * least
+            assert ((grad - want_grad).abs() <= tol).all()
