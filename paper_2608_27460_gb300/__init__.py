@@ -414,6 +414,8 @@ class _on:
     def __init__(self, x, stream):
         self.ctx = [_torch.cuda.device(x.get_device())]
         if stream is not None:
+            if stream.device.index != x.get_device():
+                raise ValueError(f"stream belongs to {stream.device}, the tensors to cuda:{x.get_device()}")
             self.ctx.append(_torch.cuda.stream(stream))
 
     def __enter__(self):

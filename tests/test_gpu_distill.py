@@ -300,3 +300,11 @@ def test_temperatures_whose_square_leaves_fp32(vie, dtype, T):
             grad = grad.double().cpu()
             tol = grad_tol + (ref.out_round(z.dtype) + ref.U) * want_grad.abs() + 2 * least
             assert ((grad - want_grad).abs() <= tol).all()
+
+
+def test_a_stream_of_another_device_is_refused(vie):
+    if torch.cuda.device_count() < 2:
+        pytest.skip("one GPU")
+    z, idx, t, _ = (x.cuda(0) for x in _inputs(4, 100, 5, "f32", seed=31))
+    with pytest.raises(ValueError, match="stream"):
+        vie.distill_topk(z, idx, t, stream=torch.cuda.Stream(device=1))

@@ -127,3 +127,27 @@ def test_limits_and_types_match_the_header():
     text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "vie_head.h")).read()
     assert re.search(r"#define\s+VIE_SAMPLE_V_MAX\s+\(1 << 22\)", text) and vie.VIE_SAMPLE_V_MAX == 1 << 22
     assert re.search(r"VIE_DTYPE_F32\s*=\s*1", text) and vie.VIE_DTYPE_F32 == 1
+
+
+class _Tensor:
+    """A tensor of device 0, as far as the binding asks before it launches."""
+    is_cuda, dtype = True, torch.float32
+
+    def get_device(self):
+        return 0
+
+
+class _Stream:
+    def __init__(self, index):
+        self.device, self.cuda_stream = torch.device("cuda", index), 0
+
+
+def test_binding_refuses_a_stream_of_another_device(monkeypatch):
+    """Not to run on a stream that the caller has not named."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    x, y = _Tensor(), _Tensor()
+    for call in (lambda s: vie.distill_topk(x, y, y, stream=s), lambda s: vie.distill_topk_grad(x, y, y, y, y, stream=s),
+                 lambda s: vie.distill_topk_step(x, y, y, y, stream=s), lambda s: vie.embed(x, y, stream=s),
+                 lambda s: vie.embed_grad(y, x, 10, stream=s), lambda s: vie.sample_logits(x, y, stream=s)):
+        with pytest.raises(ValueError, match="stream"):
+            call(_Stream(1))
