@@ -392,6 +392,11 @@ def _stream_ptr(stream) -> int:
 # ---- training and sampling around the head (torch tensors) ------------------
 # Small calls are bound by the host, so their checks are cheap ones: device
 # numbers instead of device objects, no context managers unless one is needed.
+# Autograd does not see these calls: tensors are read as plain values, whether
+# they require a gradient or not, and results have no graph.  A call that
+# changes what it reads (a gradient in place of the logits, an addition to a
+# gradient table) says so, and a graph that has saved that tensor refuses to go
+# on as after any change in place.
 
 _torch = None
 
@@ -490,6 +495,11 @@ def _matrix_output(x, name, shape, dtype, like):
     return x, ld
 
 
+def _changed(x):
+    """Counts a change in place of x, which autograd checks what it has saved by."""
+    _torch.autograd.graph.increment_version(x)
+
+
 def _teacher(logits, t_idx, t_logits):
     """The checked arguments that the distillation calls share: logits and
     their pitch, the teacher's lists and their width."""
@@ -505,7 +515,8 @@ def distill_topk(logits, t_idx, t_logits, temperature: float = 1.0, out_loss=Non
     """Loss of a student's logits [n, V] (bf16 or fp32) against a teacher's
     top-k logits (int32 / float32 [n, k], as :meth:`Head.topk_many` returns
     them; negative indices are empty slots): T^2 KL(teacher || student) per
-    row.  Returns (loss [n], stats [n, 2]); stats go to distill_topk_grad."""
+    row.  Returns (loss [n], stats [n, 2]); stats go to distill_topk_grad, which
+    an autograd program calls in its backward pass: the loss has no graph."""
     if not _here(logits, "logits") or stream is not None:
         with _on(logits, stream):
             return distill_topk(logits, t_idx, t_logits, temperature, out_loss, out_stats)
@@ -522,7 +533,8 @@ def distill_topk(logits, t_idx, t_logits, temperature: float = 1.0, out_loss=Non
 def distill_topk_grad(logits, t_idx, t_logits, stats, grad_loss, temperature: float = 1.0, out_grad=None,
                       stream=None):
     """Gradient of sum(grad_loss * loss) with respect to the student's logits,
-    in their type; `stats` come from distill_topk.  out_grad may be logits."""
+    in their type; `stats` come from distill_topk.  out_grad may be logits.
+    (logits.backward(gradient) takes it on through the graph that made them.)"""
     if not _here(logits, "logits") or stream is not None:
         with _on(logits, stream):
             return distill_topk_grad(logits, t_idx, t_logits, stats, grad_loss, temperature, out_grad)
@@ -534,6 +546,8 @@ def distill_topk_grad(logits, t_idx, t_logits, stats, grad_loss, temperature: fl
     check(vie_distill_topk_grad(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
                                 t_logits.data_ptr(), k, temperature, stats.data_ptr(), grad_loss.data_ptr(),
                                 out_grad.data_ptr(), ld_grad, _stream_ptr(None)))
+    if out_grad.data_ptr() == logits.data_ptr():
+        _changed(out_grad)
     return out_grad
 
 
@@ -541,7 +555,7 @@ def distill_topk_step(logits, t_idx, t_logits, grad_loss, temperature: float = 1
                       stream=None):
     """distill_topk and distill_topk_grad in one call: (loss [n], gradient
     [n, V]).  grad_loss [n] is the weight of each row's loss; out_grad may be
-    logits."""
+    logits.  The loss has no graph: logits.backward(gradient) goes on from here."""
     if not _here(logits, "logits") or stream is not None:
         with _on(logits, stream):
             return distill_topk_step(logits, t_idx, t_logits, grad_loss, temperature, out_loss, out_grad)
@@ -553,13 +567,16 @@ def distill_topk_step(logits, t_idx, t_logits, grad_loss, temperature: float = 1
     check(vie_distill_topk_step(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
                                 t_logits.data_ptr(), k, temperature, grad_loss.data_ptr(), out_loss.data_ptr(), 0,
                                 out_grad.data_ptr(), ld_grad, _stream_ptr(None)))
+    if out_grad.data_ptr() == logits.data_ptr():
+        _changed(out_grad)
     return out_loss, out_grad
 
 
 def embed(table, tokens, scale: float = 1.0, out=None, out_dtype=None, stream=None):
     """scale * table[tokens] (table [V, d] and out [n, d] bf16 or fp32, tokens
     int32 [n]); negative tokens give zeros.  out_dtype (of a new `out`)
-    defaults to the table's type; float32 rows are what a Head takes."""
+    defaults to the table's type; float32 rows are what a Head takes.  The rows
+    have no graph: embed_grad is the table's gradient."""
     if not _here(table, "table") or stream is not None:
         with _on(table, stream):
             return embed(table, tokens, scale, out, out_dtype)
@@ -602,6 +619,8 @@ def embed_grad(tokens, grad, V: int, scale: float = 1.0, out=None, accumulate: b
     check(vie_embed_grad(tokens.data_ptr(), n, grad.data_ptr(), _dtype_code(grad, "grad"), ld_grad, scale, V, d,
                          out.data_ptr(), _dtype_code(out, "out"), ld, 1 if accumulate else 0, workspace.data_ptr(),
                          workspace.numel(), _stream_ptr(None)))
+    if accumulate:
+        _changed(out)
     return out
 
 

@@ -308,3 +308,28 @@ def test_a_stream_of_another_device_is_refused(vie):
     z, idx, t, _ = (x.cuda(0) for x in _inputs(4, 100, 5, "f32", seed=31))
     with pytest.raises(ValueError, match="stream"):
         vie.distill_topk(z, idx, t, stream=torch.cuda.Stream(device=1))
+
+
+def test_changes_in_place_are_counted(vie):
+    """A gradient in place of the logits is a change that autograd has to know
+    of: a graph that has saved them refuses to go on.  Other calls change none."""
+    _, idx, t, gl = (x.cuda() for x in _inputs(4, 100, 5, "f32", seed=43))
+    leaf = torch.randn(4, 100, device="cuda", requires_grad=True)
+    for form in ("step", "apart"):
+        z = leaf * 1.0
+        square = (z * z).sum()  # saves z
+        before = z._version
+        stats = vie.distill_topk(z, idx, t)[1]
+        vie.distill_topk_step(z, idx, t, gl, out_grad=torch.empty_like(z))
+        assert z._version == before
+        own = z.detach()
+        if form == "step":
+            vie.distill_topk_step(own, idx, t, gl, out_grad=own)
+        else:
+            vie.distill_topk_grad(own, idx, t, stats, gl, out_grad=own)
+        assert z._version > before
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            square.backward()
+    with torch.inference_mode():  # such tensors have no count
+        z = torch.randn(4, 100, device="cuda")
+        vie.distill_topk_step(z, idx, t, gl, out_grad=z)

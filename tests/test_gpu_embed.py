@@ -244,3 +244,20 @@ def test_gradient_of_one_bucket(vie):
     _check_grad(vie, tok, torch.randn(30000, 16, generator=g), 262144, 1.0, torch.float32)
     _check_grad(vie, tok[1:], torch.randn(29999, 16, generator=g), 262144, 1.0, torch.bfloat16,
                 torch.zeros(262144, 16, dtype=torch.bfloat16, device="cuda"))
+
+
+def test_additions_in_place_are_counted(vie):
+    """What a call adds to has changed, and autograd can tell."""
+    tok, rows = torch.tensor([1, 1, 3], dtype=torch.int32, device="cuda"), torch.ones(3, 8, device="cuda")
+    table = torch.ones(5, 8, device="cuda")
+    weight = torch.ones(5, 8, device="cuda", requires_grad=True)
+    product = (weight * table).sum()  # saves table
+    before = table._version
+    vie.embed(table, tok)
+    assert table._version == before
+    vie.embed_grad(tok, rows, 5, out=table, accumulate=True)
+    assert table._version > before
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        product.backward()
+    with torch.inference_mode():
+        vie.embed_grad(tok, rows, 5, out=torch.ones(5, 8, device="cuda"), accumulate=True)
