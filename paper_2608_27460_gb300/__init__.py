@@ -552,21 +552,26 @@ def distill_topk_grad(logits, t_idx, t_logits, stats, grad_loss, temperature: fl
 
 
 def distill_topk_step(logits, t_idx, t_logits, grad_loss, temperature: float = 1.0, out_loss=None, out_grad=None,
-                      stream=None):
+                      stream=None, out_stats=None):
     """distill_topk and distill_topk_grad in one call: (loss [n], gradient
     [n, V]).  grad_loss [n] is the weight of each row's loss; out_grad may be
-    logits.  The loss has no graph: logits.backward(gradient) goes on from here."""
+    logits.  out_stats (float32 [n, 2]) takes distill_topk's statistics, if given.
+    The loss has no graph: logits.backward(gradient) goes on from here."""
     if not _here(logits, "logits") or stream is not None:
         with _on(logits, stream):
-            return distill_topk_step(logits, t_idx, t_logits, grad_loss, temperature, out_loss, out_grad)
+            return distill_topk_step(logits, t_idx, t_logits, grad_loss, temperature, out_loss, out_grad,
+                                     out_stats=out_stats)
     logits, ld, t_idx, t_logits, k = _teacher(logits, t_idx, t_logits)
     n, V = logits.shape
     grad_loss = _given(grad_loss, "grad_loss", (n,), _torch.float32, logits)
     out_loss = _contiguous_output(out_loss, "out_loss", (n,), _torch.float32, logits)
+    if out_stats is not None:
+        out_stats = _contiguous_output(out_stats, "out_stats", (n, 2), _torch.float32, logits)
     out_grad, ld_grad = _matrix_output(out_grad, "out_grad", (n, V), logits.dtype, logits)
     check(vie_distill_topk_step(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
-                                t_logits.data_ptr(), k, temperature, grad_loss.data_ptr(), out_loss.data_ptr(), 0,
-                                out_grad.data_ptr(), ld_grad, _stream_ptr(None)))
+                                t_logits.data_ptr(), k, temperature, grad_loss.data_ptr(), out_loss.data_ptr(),
+                                0 if out_stats is None else out_stats.data_ptr(), out_grad.data_ptr(), ld_grad,
+                                _stream_ptr(None)))
     if out_grad.data_ptr() == logits.data_ptr():
         _changed(out_grad)
     return out_loss, out_grad

@@ -333,3 +333,24 @@ def test_changes_in_place_are_counted(vie):
     with torch.inference_mode():  # such tensors have no count
         z = torch.randn(4, 100, device="cuda")
         vie.distill_topk_step(z, idx, t, gl, out_grad=z)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_step_hands_out_its_statistics(vie, dtype):
+    z, idx, t, gl = _inputs(5, 3001, 20, dtype, seed=47)
+    idx[2] = -1
+    _, want_stats, want_grad, _, s_tol, grad_tol = ref.distill(z, idx, t, 1.5, gl)
+    zc, ic, tc, gc = z.cuda(), idx.cuda(), t.cuda(), gl.cuda()
+    out = torch.full((5, 2), 7.0, device="cuda")
+    loss, grad = vie.distill_topk_step(zc, ic, tc, gc, temperature=1.5, out_stats=out)
+    plain = vie.distill_topk_step(zc, ic, tc, gc, temperature=1.5)
+    assert torch.equal(loss, plain[0]) and torch.equal(grad, plain[1])
+    got = out.double().cpu()
+    assert torch.equal(got[:, 0], want_stats[:, 0]) and ((got[:, 1] - want_stats[:, 1]).abs() <= s_tol).all()
+    again = vie.distill_topk_grad(zc, ic, tc, out, gc, temperature=1.5)  # what they are for
+    tol = grad_tol + (ref.out_round(z.dtype) + ref.U) * want_grad.abs()
+    assert ((again.double().cpu() - want_grad).abs() <= tol).all()
+    for bad in (torch.empty(5, 3, device="cuda"), torch.empty(5, 2, dtype=torch.float64, device="cuda"),
+                torch.empty(5, 2), torch.empty(2, 5, device="cuda").t()):
+        with pytest.raises(ValueError, match="out_stats"):
+            vie.distill_topk_step(zc, ic, tc, gc, out_stats=bad)
