@@ -32,16 +32,15 @@ constexpr int kEmbedThreads = 256;
 constexpr int kEmbedWarps = kEmbedThreads / 32;
 constexpr int kEmbedBlocks = 4;  // blocks of columns that a lookup's warp has in flight
 
-// kW values of a row per lane, as loaded.  kVector: a run of kW at 16-byte (or
-// 8-byte) addresses; otherwise 32 apart, value by value: rows of any width,
+// kW values of a row per lane, as loaded.  kVector: one vector of kW at a 16-byte
+// (or 8-byte) address; otherwise 32 apart, value by value: rows of any width,
 // pitch and alignment.  Loads do not branch: a lane beyond the row reads the
 // row's first values.
 template <typename T, int kW, bool kVector>
 struct LaneRow {
     using Word = typename std::conditional<!kVector, T, typename std::conditional<sizeof(T) * kW == 8, uint2, uint4>::type>::type;
-    static constexpr int kWords = sizeof(T) * kW / sizeof(Word);
-    static constexpr int kApart = kVector ? sizeof(Word) / sizeof(T) : 32;  // columns from word to word
-    static constexpr int kBlock = 32 * kW;                                  // columns per warp
+    static constexpr int kWords = kVector ? 1 : kW;
+    static_assert(sizeof(Word) * kWords == sizeof(T) * kW, "all values of a lane");
     Word r[kWords];
 
     __device__ __forceinline__ static int column(int lane) { return kVector ? lane * kW : lane; }
@@ -49,14 +48,14 @@ struct LaneRow {
     __device__ __forceinline__ void load(const T *row, int c, int d) {
 #pragma unroll
         for (int x = 0; x < kWords; ++x) {
-            const int at = c + x * kApart;
+            const int at = c + 32 * x;
             r[x] = *reinterpret_cast<const Word *>(row + (at < d ? at : 0));
         }
     }
     __device__ __forceinline__ void store(T *row, int c, int d) const {
 #pragma unroll
         for (int x = 0; x < kWords; ++x)
-            if (c + x * kApart < d) *reinterpret_cast<Word *>(row + c + x * kApart) = r[x];
+            if (c + 32 * x < d) *reinterpret_cast<Word *>(row + c + 32 * x) = r[x];
     }
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -494,15 +493,15 @@ __device__ __forceinline__ void put_row(const GradParams &a, T *row, int c, cons
     float v[kW];
     if constexpr (kAddsInL2<T>) {
         if (a.accumulate) {
+            if constexpr (kVector) {
+                static_assert(kW == 4, "a vector of fp32");
+                if (c < a.d)
+                    atomicAdd(reinterpret_cast<float4 *>(row + c), make_float4(a.scale * sum[0], a.scale * sum[1],
+                                                                              a.scale * sum[2], a.scale * sum[3]));
+            } else {
 #pragma unroll
-            for (int w = 0; w < kW; w += kVector ? 4 : 1) {
-                const int at = kVector ? c + w : c + 32 * w;
-                if (at >= a.d) continue;
-                if constexpr (kVector)
-                    atomicAdd(reinterpret_cast<float4 *>(row + at), make_float4(a.scale * sum[w], a.scale * sum[w + 1],
-                                                                               a.scale * sum[w + 2], a.scale * sum[w + 3]));
-                else
-                    atomicAdd(row + at, a.scale * sum[w]);
+                for (int w = 0; w < kW; ++w)
+                    if (c + 32 * w < a.d) atomicAdd(row + c + 32 * w, a.scale * sum[w]);
             }
             return;
         }
@@ -749,27 +748,25 @@ static cudaError_t start_embed(const EmbedParams &p, cudaStream_t s) {
 // 1024, bf16 to fp32: 43 us; 62 with 8, whose two fp32 vectors per lane lie 32
 // bytes apart); value by value where addresses do not allow either.
 enum class Access { kWide, kNarrow, kValues };
-static Access access_of(const void *a, vie_dtype ta, int64_t lda, const void *b, vie_dtype tb, int64_t ldb, int d,
-                        bool wide) {
+static Access access_of(const void *a, vie_dtype ta, int64_t lda, const void *b, vie_dtype tb, int64_t ldb, int d) {
     auto fits = [&](const void *p, vie_dtype t, int64_t ld, int w) {
-        const int bytes = w * dtype_size(t) < 16 ? w * dtype_size(t) : 16;
+        const int bytes = w * dtype_size(t);
         return aligned_to(p, static_cast<uintptr_t>(bytes)) && ld * dtype_size(t) % bytes == 0 && d % w == 0;
     };
-    if (wide && d > 128 && fits(a, ta, lda, 8) && fits(b, tb, ldb, 8))
+    if (ta == VIE_DTYPE_BF16 && tb == VIE_DTYPE_BF16 && d > 128 && fits(a, ta, lda, 8) && fits(b, tb, ldb, 8))
         return Access::kWide;
     return fits(a, ta, lda, 4) && fits(b, tb, ldb, 4) ? Access::kNarrow : Access::kValues;
 }
 
-#define VIE_BY_ACCESS(f, TI, TO, access, ...)                                \
-    ((access) == Access::kWide     ? f<TI, TO, 8, true>(__VA_ARGS__)         \
-     : (access) == Access::kNarrow ? f<TI, TO, 4, true>(__VA_ARGS__)         \
-                                   : f<TI, TO, 4, false>(__VA_ARGS__))
 // f<TI, TO, kW, kVector>(...) for two storage types and how rows are accessed.
-#define VIE_BY_TYPES(f, in, out, access, ...)                                                          \
-    ((in) == VIE_DTYPE_BF16                                                                            \
+#define VIE_BY_ACCESS(f, TI, TO, access, ...) \
+    ((access) == Access::kNarrow ? f<TI, TO, 4, true>(__VA_ARGS__) : f<TI, TO, 4, false>(__VA_ARGS__))
+#define VIE_BY_TYPES(f, in, out, access, ...)                                                       \
+    ((access) == Access::kWide  ? f<__nv_bfloat16, __nv_bfloat16, 8, true>(__VA_ARGS__)             \
+     : (in) == VIE_DTYPE_BF16                                                                       \
          ? ((out) == VIE_DTYPE_BF16 ? VIE_BY_ACCESS(f, __nv_bfloat16, __nv_bfloat16, access, __VA_ARGS__) \
-                                    : VIE_BY_ACCESS(f, __nv_bfloat16, float, access, __VA_ARGS__))     \
-         : ((out) == VIE_DTYPE_BF16 ? VIE_BY_ACCESS(f, float, __nv_bfloat16, access, __VA_ARGS__)      \
+                                    : VIE_BY_ACCESS(f, __nv_bfloat16, float, access, __VA_ARGS__))  \
+         : ((out) == VIE_DTYPE_BF16 ? VIE_BY_ACCESS(f, float, __nv_bfloat16, access, __VA_ARGS__)   \
                                     : VIE_BY_ACCESS(f, float, float, access, __VA_ARGS__)))
 
 static vie_status check_embed(const char *fn, const int32_t *tokens, int64_t n, int64_t V, int32_t d) {
@@ -801,8 +798,8 @@ vie_status vie_embed(const void *table, vie_dtype dtype, int64_t V, int32_t d, i
     p.scale = scale;
     cudaError_t e = device_flag_word(&p.flag);
     if (e != cudaSuccess) return fail_cuda(e, fn);
-    e = VIE_BY_TYPES(start_embed, dtype, out_dtype, access_of(table, dtype, ld, out, out_dtype, ld_out, d, dtype == VIE_DTYPE_BF16 && out_dtype == VIE_DTYPE_BF16), p,
-                     static_cast<cudaStream_t>(stream));
+    const Access access = access_of(table, dtype, ld, out, out_dtype, ld_out, d);
+    e = VIE_BY_TYPES(start_embed, dtype, out_dtype, access, p, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
 
@@ -875,7 +872,8 @@ vie_status vie_embed_grad(const int32_t *tokens, int64_t n, const void *grad, vi
     p.sorted = entries[sorted], p.grad = grad, p.out = out, p.parts = reinterpret_cast<float *>(ws + w.parts);
     p.ld_grad = ld_grad, p.ld = ld, p.n = static_cast<uint32_t>(n), p.V = static_cast<uint32_t>(V), p.chunk = w.chunk;
     p.d = d, p.accumulate = accumulate != 0, p.scale = scale;
-    e = VIE_BY_TYPES(start_sums, dtype, out_dtype, access_of(grad, dtype, ld_grad, out, out_dtype, ld, d, dtype == VIE_DTYPE_BF16 && out_dtype == VIE_DTYPE_BF16), p, w.chunks, s);
+    const Access access = access_of(grad, dtype, ld_grad, out, out_dtype, ld, d);
+    e = VIE_BY_TYPES(start_sums, dtype, out_dtype, access, p, w.chunks, s);
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
 
