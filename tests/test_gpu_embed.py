@@ -261,3 +261,37 @@ def test_additions_in_place_are_counted(vie):
         product.backward()
     with torch.inference_mode():
         vie.embed_grad(tok, rows, 5, out=torch.ones(5, 8, device="cuda"), accumulate=True)
+
+
+@pytest.mark.parametrize("V,passes", [(2 ** 19 + 3, 3), (2 ** 25 + 9, 4)])
+def test_gradient_of_grouped_tokens_with_many_digits(vie, V, passes):
+    """Up to 131072 tokens are spread over 128 lists by their low 7 bits, and each
+    list is sorted 6 bits at a time: both parities of the number of passes, with
+    lists that fit shared memory (2048 entries) and lists that do not."""
+    assert -(-((V - 1) >> 7).bit_length() // 6) == passes
+    g = torch.Generator().manual_seed(V)
+    n, top = 12000, (V - 1) >> 7
+    tok = torch.randint(0, V, (n,), generator=g)
+    tok[::3] = torch.randint(0, top, (n // 3,), generator=g) * 128 + 77      # a list of about 4000
+    tok[1::3] = (torch.randint(0, top >> 6, (n // 3,), generator=g) << 13) + 5  # ids that differ in the upper digits only
+    tok[2::3] %= V - 128                                                     # the other lists hold about 30
+    tok[2::300] = V - 1
+    tok[5], tok[8] = 0, (1 << (V - 1).bit_length() - 1)                      # the top digit alone
+    tok = tok.int()
+    tok[11::50] = -1
+    assert (tok % 128 == 77).sum() > 2048 and (tok % 128 == 5).sum() > 2048
+    _check_grad(vie, tok, torch.randn(n, 2, generator=g), V, 1.0, torch.bfloat16)
+
+
+@pytest.mark.parametrize("n", [131072, 131073])
+def test_gradient_of_long_batches_with_large_ids(vie, n):
+    """Ids of more than 24 bits on either side of the number of tokens from which the
+    whole array is sorted: a fourth pass of 8 bits there, a fourth of 6 here."""
+    V = 2 ** 25 + 9
+    g = torch.Generator().manual_seed(n)
+    tok = torch.randint(0, V, (n,), generator=g)
+    tok[::4] = (torch.randint(0, 2, (tok[::4].numel(),), generator=g) << 24) + 3  # the top digit alone
+    tok[1::4] = torch.randint(V - 50, V, (tok[1::4].numel(),), generator=g)
+    tok = tok.int()
+    tok[2::40] = -1
+    _check_grad(vie, tok, torch.randn(n, 1, generator=g), V, 1.0, torch.bfloat16)

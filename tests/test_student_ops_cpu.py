@@ -151,3 +151,13 @@ def test_binding_refuses_a_stream_of_another_device(monkeypatch):
                  lambda s: vie.embed_grad(y, x, 10, stream=s), lambda s: vie.sample_logits(x, y, stream=s)):
         with pytest.raises(ValueError, match="stream"):
             call(_Stream(1))
+
+
+def test_embed_grad_workspace_where_the_sort_changes():
+    """From 131073 tokens on the whole array is sorted, with counters of its own:
+    no workspace there is smaller than one for fewer tokens."""
+    for V, d in ((262144, 1), (262144, 1024), (2 ** 31 - 2, vie.VIE_D_MAX)):
+        need = [vie.vie_embed_grad_workspace(n, V, d) for n in range(131000, 131200)]
+        assert all(st == vie.VIE_OK for st, _ in need)
+        sizes = [b for _, b in need]
+        assert sizes == sorted(sizes) and sizes[73] > sizes[72]  # 131073 and 131072
