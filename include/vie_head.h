@@ -543,10 +543,11 @@ vie_status vie_embed_grad(const int32_t *tokens, int64_t n, const void *grad, vi
  *   min_p keeps the tokens with w >= min_p 2^40 (0 or less: all);
  *   the shortest of these prefixes is kept, the best token always; mass M;
  *   the token is the first one whose running mass exceeds u M.
- * Weights are whole numbers, so their sums are exact in any order: the same
- * inputs give the same tokens on any device.  u and top_p count in steps of
- * 2^-24 (u rounded down and held in [0, 1), top_p rounded up).  T of 0 (or
- * anything not above 0) takes the best token.  Logits of -inf and NaN are
+ * Weights are whole numbers, so their sums are exact in any order: a row's
+ * token does not depend on how its work is split, nor on the rows beside it.
+ * (A weight's last bits are those of the device's exp.)  u and top_p count in
+ * steps of 2^-24 (u rounded down and held in [0, 1), top_p rounded up).  T of 0
+ * (or anything not above 0) takes the best token.  Logits of -inf and NaN are
  * never drawn; a row that has no others gives token -1 and probability 0.
  * Logits of +inf share the whole mass.
  *

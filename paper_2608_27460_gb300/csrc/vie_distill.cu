@@ -305,21 +305,25 @@ __device__ __forceinline__ void write_row(const DistillParams &a, int64_t row, f
 
 // Loss and statistics (FWD) or the gradient (BWD) or both.
 //
-// A row is a cluster's, a slice of it a CTA's; each thread keeps eight 16-byte
+// A row is a cluster's, a slice of it a CTA's; each thread keeps kUnroll 16-byte
 // vectors in flight, its running maximum and sum, and the slices' (m, s) go to
 // all CTAs of the row by asynchronous stores that count on their mbarriers (a
 // cluster barrier with release would wait for the gradients written before).
 // The teacher's softmax is worked out meanwhile.  For both, the slice is read
-// again, from L2: with four CTAs per SM the rows in progress take 46 MB or less.
+// again: from L2, as long as the slices in progress, four CTAs per SM of them,
+// fit it.  They are 80 KB or less each up to rows of 640 KB, 50 MB in all, and an
+// eighth of the row beyond: 80 MB at 262144 fp32 values (0.83 below); at a million
+// 300 MB, which do not fit (0.61).
 // (Keeping slices in shared memory measured the same at 50 entries per row, and
 // twice the time at 1000, where too few threads were left for the teacher.)
 //
 // Bound by bytes.  Measured on bf16 logits, 50 to 64 entries per row, and as a
 // share of the time that a copy of the bytes read and written once would take:
-//   loss and statistics  262144 x 2048: 147 us (0.97)
-//   gradient             128256 x 2048: 154 us (0.96)
-//   both                 151936 x 4096: 450 us (0.78), 262144 x 1024: 197 (0.77), 32000 x 4096:
-//                        104 (0.71); fp32 128256 x 1024: 173 (0.85)
+//   loss and statistics  262144 x 2048: 151 us (0.94)
+//   gradient             128256 x 2048: 154 us (0.95)
+//   both                 151936 x 4096: 450 us (0.78), 262144 x 1024: 196 (0.77), 32000 x 4096:
+//                        104 (0.71); fp32 128256 x 1024: 173 (0.85), 262144 x 1024: 363 (0.83),
+//                        1000003 x 128: 235 (0.61)
 // What is left in the last: a row's exchange and its entries, which the CTAs'
 // other rows hide only in part (61 % of issue slots used, DRAM 55 % busy).
 // Dynamic shared memory: the teacher's entries (indices, logits, the student's

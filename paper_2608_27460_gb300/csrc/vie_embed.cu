@@ -7,7 +7,7 @@
 //
 // Bound by the bytes of the rows.  Measured: lookup of 16384 rows of 1024 bf16
 // 8.9 us (a copy of the distinct rows' and the output's bytes would take 7.0), of 32
-// rows 1.4; gradient table of 262144 x 640 fp32 from 8192 rows 101 us (100 to
+// rows 1.5; gradient table of 262144 x 640 fp32 from 8192 rows 101 us (100 to
 // write it), 16384 rows of 1024 bf16 added to fp32 34 us (12.9; 8 of it to sort
 // the tokens, and three launches).
 //
