@@ -227,14 +227,15 @@ struct Teacher {
         repeats = sm.repeats != 0;
     }
     // T^2 sum p (log p - log q) over all entries, in all of the warps; m, s: the student's statistics.
-    // One T is taken into the sum, log q = (z - m) / T - log s: neither T^2 nor a
-    // difference of logits over T need be within fp32, and +inf stays +inf.
+    // One T is taken into the sum, log q = (z - m) / T - log s, and the other if it
+    // is below 1: neither T^2 nor a difference of logits over T need be within fp32
+    // (masks of the type's lowest value), and +inf stays +inf.
     __device__ __forceinline__ float loss(DistillSmem &sm, float T, float m, float s) const {
         float cost = 0.0f;
-        const float log_s = logf(s), m0 = finite_max(m);
+        const float log_s = logf(s), m0 = finite_max(m), inside = fminf(T, 1.0f);
 #pragma unroll 4
         for (int j = me; j < k; j += step())
-            if (p[j] != 0.0f) cost += p[j] * (T * (logf(p[j]) + log_s) - (z[j] - m0));
+            if (p[j] != 0.0f) cost += p[j] * (inside * (T * (logf(p[j]) + log_s) - (z[j] - m0)));
         cost = warp_sum(cost);
         if (warps > 1) {
             if ((me & 31) == 0) sm.teacher[me >> 5].z = cost;
@@ -242,7 +243,7 @@ struct Teacher {
             cost = 0.0f;
             for (int w = 0; w < warps; ++w) cost += sm.teacher[w].z;
         }
-        return s == 0.0f ? INFINITY : T * cost;  // (no softmax: no logit above -inf)
+        return s == 0.0f ? INFINITY : fmaxf(T, 1.0f) * cost;  // (no softmax: no logit above -inf)
     }
     // q - p over what the slice's loop has written at its entries; the first
     // entry of an index takes off the sum of all.

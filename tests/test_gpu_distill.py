@@ -354,3 +354,18 @@ def test_the_step_hands_out_its_statistics(vie, dtype):
                 torch.empty(5, 2), torch.empty(2, 5, device="cuda").t()):
         with pytest.raises(ValueError, match="out_stats"):
             vie.distill_topk_step(zc, ic, tc, gc, out_stats=bad)
+
+
+@pytest.mark.parametrize("T", [0.01, 0.1, 0.5, 0.9])
+def test_teachers_of_nothing_but_masked_tokens(vie, T):
+    """All of a teacher's tokens at the type's lowest value: a loss of about T times
+    that, within fp32, though the lowest value over T is not."""
+    n, V, k = 200, 300, 40
+    z, idx, t, gl = _inputs(n, V, k, "f32", seed=53)
+    z.scatter_(1, idx.long(), torch.finfo(torch.float32).min)
+    T = float(torch.tensor(T, dtype=torch.float32))
+    want, _, _, tol, _, _ = ref.distill(z, idx, t, T, gl)
+    assert float(want.max()) < 0.95 * torch.finfo(torch.float32).max
+    for loss in (vie.distill_topk(z.cuda(), idx.cuda(), t.cuda(), temperature=T)[0],
+                 vie.distill_topk_step(z.cuda(), idx.cuda(), t.cuda(), gl.cuda(), temperature=T)[0]):
+        assert ((loss.double().cpu() - want).abs() <= tol).all()
