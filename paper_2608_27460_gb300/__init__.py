@@ -543,10 +543,10 @@ def distill_topk_grad(logits, t_idx, t_logits, stats, grad_loss, temperature: fl
     stats = _given(stats, "stats", (n, 2), _torch.float32, logits)
     grad_loss = _given(grad_loss, "grad_loss", (n,), _torch.float32, logits)
     out_grad, ld_grad = _matrix_output(out_grad, "out_grad", (n, V), logits.dtype, logits)
-    check(vie_distill_topk_grad(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
-                                t_logits.data_ptr(), k, temperature, stats.data_ptr(), grad_loss.data_ptr(),
-                                out_grad.data_ptr(), ld_grad, _stream_ptr(None)))
-    if out_grad.data_ptr() == logits.data_ptr():
+    z, dz = logits.data_ptr(), out_grad.data_ptr()
+    check(vie_distill_topk_grad(z, _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(), t_logits.data_ptr(), k,
+                                temperature, stats.data_ptr(), grad_loss.data_ptr(), dz, ld_grad, _stream_ptr(None)))
+    if dz == z:
         _changed(out_grad)
     return out_grad
 
@@ -565,14 +565,15 @@ def distill_topk_step(logits, t_idx, t_logits, grad_loss, temperature: float = 1
     n, V = logits.shape
     grad_loss = _given(grad_loss, "grad_loss", (n,), _torch.float32, logits)
     out_loss = _contiguous_output(out_loss, "out_loss", (n,), _torch.float32, logits)
+    stats = 0
     if out_stats is not None:
-        out_stats = _contiguous_output(out_stats, "out_stats", (n, 2), _torch.float32, logits)
+        stats = _contiguous_output(out_stats, "out_stats", (n, 2), _torch.float32, logits).data_ptr()
     out_grad, ld_grad = _matrix_output(out_grad, "out_grad", (n, V), logits.dtype, logits)
-    check(vie_distill_topk_step(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(),
-                                t_logits.data_ptr(), k, temperature, grad_loss.data_ptr(), out_loss.data_ptr(),
-                                0 if out_stats is None else out_stats.data_ptr(), out_grad.data_ptr(), ld_grad,
+    z, dz = logits.data_ptr(), out_grad.data_ptr()
+    check(vie_distill_topk_step(z, _dtype_code(logits, "logits"), n, V, ld, t_idx.data_ptr(), t_logits.data_ptr(), k,
+                                temperature, grad_loss.data_ptr(), out_loss.data_ptr(), stats, dz, ld_grad,
                                 _stream_ptr(None)))
-    if out_grad.data_ptr() == logits.data_ptr():
+    if dz == z:
         _changed(out_grad)
     return out_loss, out_grad
 
