@@ -238,11 +238,11 @@ def prepare(case, seed):
     else:
         s["z"], s["tok"], s["weight"] = _row_inputs(case, g)
         exactly = _statistics(s["z"], s["tok"], case["T"])
-        s["stats"] = exactly[:, 1:].float().contiguous()  # what a forward pass has left, or room for it
+        s["stats"] = exactly[:, 1:].float().contiguous()  # what a forward pass has left, as s["lp"], or room for it
         if kind.startswith("policy"):
             s["old"], s["adv"], s["ref"] = _policy_inputs(case, exactly[:, 0], g)
             s["loss"] = empty((case["n"],), torch.float32)
-        s["lp"] = empty((case["n"],), torch.float32)
+        s["lp"] = exactly[:, 0].float()
         if kind.endswith(("grad", "step")):
             s["to"] = torch.empty_like(s["z"])
     return s
@@ -251,7 +251,7 @@ def prepare(case, seed):
 # ---- the plain forms --------------------------------------------------------
 
 def _plain_softmax(s, forward):
-    """lp, m, s of each row (from the statistics that it was given, if not forward), exp((z - m) / T) and live rows."""
+    """lp, m, s of each row (those of the forward pass, if this is not one), exp((z - m) / T), tokens and live rows."""
     z, T = s["z"].float(), s["T"]
     tok = s["tok"].long()
     live = (tok >= 0) & (tok < s["V"])
@@ -259,7 +259,7 @@ def _plain_softmax(s, forward):
     e = torch.exp((z - m[:, None]) / T)
     total = e.sum(1) if forward else s["stats"][:, 1]
     tok = torch.where(live, tok, torch.zeros_like(tok))
-    lp = (z.gather(1, tok[:, None])[:, 0] - m) / T - torch.log(total)
+    lp = (z.gather(1, tok[:, None])[:, 0] - m) / T - torch.log(total) if forward else s["lp"]
     return torch.where(live, lp, torch.zeros_like(lp)), m, total, e, tok, live
 
 
@@ -405,8 +405,8 @@ def run(s):
         return vie.policy_loss(s["z"], s["tok"], s["old"], s["adv"], out_loss=s["loss"], out_logprob=s["lp"],
                                out_stats=s["stats"], **how)
     if kind == "policy_grad":
-        return (vie.policy_loss_grad(s["z"], s["tok"], s["old"], s["adv"], s["stats"], s["weight"], out_grad=s["to"],
-                                     **how),)
+        return (vie.policy_loss_grad(s["z"], s["tok"], s["old"], s["adv"], s["lp"], s["stats"], s["weight"],
+                                     out_grad=s["to"], **how),)
     return vie.policy_loss_step(s["z"], s["tok"], s["old"], s["adv"], s["weight"], out_loss=s["loss"],
                                 out_logprob=s["lp"], out_grad=s["to"], **how)
 
@@ -429,7 +429,7 @@ def work(case):
     live = 0.9 * n  # rows without a token need not be read
     if kind in ("logprob", "policy"):
         return {"bytes": live * V * size + 28 * n, "flops": 4 * live * V}
-    return {"bytes": (live + n) * V * size + 28 * n, "flops": 6 * live * V}
+    return {"bytes": (live + n) * V * size + 32 * n, "flops": 6 * live * V}
 
 
 # ---- the same in 64 bits ----------------------------------------------------
