@@ -20,6 +20,7 @@
 #include "vie_api.h"
 #include "vie_block.cuh"
 #include "vie_device.cuh"
+#include "vie_row_softmax.cuh"
 
 namespace vie {
 
@@ -38,35 +39,12 @@ struct DistillParams {
     uint32_t *flag;
 };
 
-// Slices per row: up to 8; up to 16 for a few rows alone (clusters of 16 find
-// fewer places to run: 64 rows of 151936 take 18.9 us with them, 13.5 with 8).
-constexpr int kSlices = 8, kMaxSlices = 16;
-constexpr int kFewRows = 8;
-
-// exp2((z - m) c) = exp((z - m) / T), with c = log2(e) / T.  The difference comes
-// first: the type's lowest value is a usual mask, and z c - m c overflows there.
-struct Exponent {
-    float m, c;
-    __device__ __forceinline__ float operator()(float z) const { return exp2_approx((z - m) * c); }
-};
-// The maximum that exponents are taken from: 0 where no logit is above -inf.
-__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
-
-constexpr int kDistillThreads = 256;
-constexpr int kDistillWarps = kDistillThreads / 32;
-// Vectors in flight per thread: eight, but for loss and gradient on bf16 logits,
-// where a thread's 64 registers hold six (151936 x 4096: 450 us; 497 with eight).
-template <typename T, bool FWD, bool BWD>
-constexpr int kUnroll = FWD && BWD && sizeof(T) == 2 ? 6 : 8;
 constexpr int kTeacherEntries = 4;  // of a teacher, per thread of the warps that deal with it
-static_assert(VIE_K_MAX <= 32 * kTeacherEntries * kDistillWarps, "warps for all entries");
+static_assert(VIE_K_MAX <= 32 * kTeacherEntries * kRowWarps, "warps for all entries");
 
-struct DistillSmem {
-    float2 gathered[kMaxSlices];    // per slice of the row: max z and the sum of exp((z - max z) / T)
-    uint64_t gather_bar;
-    float2 part[kDistillWarps];     // the same per warp of a slice
-    float3 teacher[kDistillWarps];  // per teacher warp: max t, the sum of exp((t - max t) / T), part of the loss
-    int repeats, abort;
+struct DistillSmem : RowSmem {
+    float3 teacher[kRowWarps];  // per teacher warp: max t, the sum of exp((t - max t) / T), part of the loss
+    int repeats;
 };
 
 // Slots of the hash table of a slice's entries: a power of two, at least
@@ -76,62 +54,6 @@ __host__ __device__ inline int seen_slots(int k) {
     while (slots < 2 * k) slots <<= 1;
     return slots;
 }
-
-// Where a slice's gradient goes: by vectors if its rows lie to 16-byte
-// addresses as the logits' do, else value by value.
-template <typename T>
-struct GradSlice {
-    static constexpr int kVec = Vec16<T>::kVec;
-    T *g;
-    int e0, V;
-    bool by_vector;
-
-    __device__ __forceinline__ GradSlice(const DistillParams &a, int64_t row, const Slice<T> &sl)
-        : g(static_cast<T *>(a.grad) + row * a.ld_grad), e0(sl.e0), V(sl.V),
-          by_vector(((reinterpret_cast<uintptr_t>(sl.z) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0) {}
-    __device__ __forceinline__ void store_values(int i, const float *v) const {  // those inside the row
-        const int e = e0 + i * kVec;
-#pragma unroll
-        for (int x = 0; x < kVec; ++x)
-            if (e + x >= 0 && e + x < V) store_value(g + e + x, v[x]);
-    }
-    __device__ __forceinline__ void store(int i, const float *v) const {
-        if (by_vector) reinterpret_cast<uint4 *>(g + e0)[i] = Vec16<T>::pack(v);
-        else store_values(i, v);
-    }
-};
-
-template <typename T>
-__device__ __forceinline__ void clear_gradient(const Slice<T> &sl, const GradSlice<T> &out) {
-    const float zero[Slice<T>::kVec] = {};
-    for (int i = sl.lo + threadIdx.x; i < sl.hi; i += kDistillThreads) out.store(i, zero);
-    if (sl.has_edge()) out.store_values(sl.edge(), zero);
-}
-
-template <typename T>
-__device__ __forceinline__ void gradient_of(const Exponent &e, float coef, const uint4 &raw, float *v) {
-    Vec16<T>::unpack(raw, v);
-#pragma unroll
-    for (int x = 0; x < Slice<T>::kVec; ++x) v[x] = coef * e(v[x]);
-}
-// Running sums of exponentials, one per position of a vector: chains that do
-// not wait for one another.
-template <typename T>
-struct Sums {
-    float v[Slice<T>::kVec] = {};
-    __device__ __forceinline__ void add(const Exponent &e, const uint4 &raw) {
-        float x[Slice<T>::kVec];
-        Vec16<T>::unpack(raw, x);
-#pragma unroll
-        for (int i = 0; i < Slice<T>::kVec; ++i) v[i] += e(x[i]);
-    }
-    __device__ __forceinline__ float total() const {
-        float s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < Slice<T>::kVec; i += 2) s += v[i] + v[i + 1];
-        return s;
-    }
-};
 
 // The teacher's entries of a row in shared memory, and the warps of the CTA that
 // deal with them: `me` is a thread's number among theirs, below 0 in the
@@ -267,35 +189,6 @@ struct Teacher {
     }
 };
 
-// One warp: the maximum and sum of this CTA's slice, joined from its warps'
-// (sm.part, written before the last barrier), to all CTAs of the row.
-__device__ __forceinline__ void send_partial(DistillSmem &sm, int slices, int rank, float c) {
-    const int lane = threadIdx.x & 31;
-    const float2 part = lane < kDistillWarps ? sm.part[lane] : make_float2(-INFINITY, 0.0f);
-    const float m = warp_max(part.x);
-    const float s = warp_sum(part.y != 0.0f ? part.y * Exponent{finite_max(m), c}(finite_max(part.x)) : 0.0f);
-    if (lane == 0) mbar_arrive_expect_tx(&sm.gather_bar, 8u * slices);
-    if (lane < slices)
-        cluster_send(cluster_addr(&sm.gathered[rank], lane), make_float2(m, s),
-                     cluster_addr(&sm.gather_bar, lane));
-    __syncwarp();
-}
-// The row's, from those of all its slices, in the same order in every warp.
-__device__ __forceinline__ void join_partials(const DistillParams &a, DistillSmem &sm, int slices, float c, float *m,
-                                              float *s) {
-    if (!mbar_wait(&sm.gather_bar, 0, &sm.abort) && threadIdx.x == 0) atomicOr(a.flag, kErrWaitTimeout);
-    const int lane = threadIdx.x & 31;
-    const float2 part = lane < slices ? sm.gathered[lane] : make_float2(-INFINITY, 0.0f);
-    *m = warp_max(part.x);
-    *s = warp_sum(part.y != 0.0f ? part.y * Exponent{finite_max(*m), c}(finite_max(part.x)) : 0.0f);
-}
-
-__device__ __forceinline__ void init_smem(DistillSmem &sm) {
-    sm.abort = 0;
-    mbar_init(&sm.gather_bar, 1);
-    fence_mbar_init();
-}
-
 __device__ __forceinline__ void write_row(const DistillParams &a, int64_t row, float loss, float m, float s) {
     a.loss[row] = loss;
     if (a.stats_out != nullptr) {
@@ -330,12 +223,12 @@ __device__ __forceinline__ void write_row(const DistillParams &a, int64_t row, f
 // Dynamic shared memory: the teacher's entries (indices, logits, the student's
 // logits there), the hash table (BWD).
 template <typename T, bool FWD, bool BWD>
-__global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const DistillParams a, int log2_slices) {
-    constexpr int NT = kDistillThreads, U = kUnroll<T, FWD, BWD>;
+__global__ void __launch_bounds__(kRowThreads, 4) distill_kernel(const DistillParams a, int log2_slices) {
+    constexpr int NT = kRowThreads, U = kUnroll<T, FWD, BWD>;
     extern __shared__ __align__(16) unsigned char distill_smem[];
     __shared__ DistillSmem sm;
     int32_t *const list = reinterpret_cast<int32_t *>(distill_smem);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, warp = tid >> 5;
     // the first warps deal with the teacher, besides their part of the row
     const int t_warps = (a.k + 32 * kTeacherEntries - 1) / (32 * kTeacherEntries);
     Teacher tea(a.k, t_warps, tid < 32 * t_warps ? tid : -1, list, reinterpret_cast<float *>(list + 2 * a.k),
@@ -343,7 +236,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
     const int slices = 1 << log2_slices, rank = blockIdx.x & (slices - 1);
     const int64_t row = blockIdx.x >> log2_slices;
     if (FWD) {
-        if (tid == 0) init_smem(sm);
+        if (tid == 0) sm.init();
         __syncwarp();
         cluster_arrive_relaxed();  // all CTAs of the cluster run and wait, before their memory is written
     }
@@ -357,7 +250,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
     }
     const bool has = __syncthreads_or(any);
     const Slice<T> sl(static_cast<const T *>(a.logits) + row * a.ld, a.V, log2_slices, rank);
-    const GradSlice<T> out(a, row, sl);
+    const GradSlice<T> out(static_cast<T *>(a.grad) + row * a.ld_grad, sl);
     if (FWD) cluster_wait();
     if (!has) {
         if (BWD) clear_gradient(sl, out);
@@ -365,8 +258,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
         return;
     }
     const float inv_T = fminf(1.0f / a.T, 3.4e38f);
-    const float c = fminf(1.44269504f / a.T, 3.4e38f);  // log2 e / T
-    const uint4 *const zv = sl.vectors();
+    const float c = exponent_factor(a.T);
     // The entries' logits, before a gradient may overwrite them; the loss (rank
     // 0) needs those of the whole row.
     const bool whole = FWD && rank == 0;
@@ -375,45 +267,12 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
     if (keeps) tea.read_logits(sl.z, whole ? 0 : sl.e0, whole ? a.V : sl.e1, z_entries);
     float m, s;
     if (FWD) {
-        m = -INFINITY, s = 0.0f;  // of this thread, then of the CTA, then of the row
-        auto raise = [&](float mx) {  // the thread's maximum, and its sum with it
-            if (s != 0.0f) s *= Exponent{finite_max(mx), c}(finite_max(m));
-            m = mx;
-        };
-        for (int i = sl.lo + tid; i < sl.hi; i += U * NT) {
-            uint4 raw[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i + u * NT < sl.hi) raw[u] = BWD ? __ldcg(zv + i + u * NT) : __ldcs(zv + i + u * NT);
-            typename Vec16<T>::Max top;
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i + u * NT < sl.hi) top.add(raw[u]);
-            raise(fmaxf(m, top.top()));
-            Sums<T> part;
-            const Exponent e{finite_max(m), c};
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i + u * NT < sl.hi) part.add(e, raw[u]);
-            s += part.total();
-        }
-        if (sl.has_edge()) {
-            const uint4 raw = sl.load_edge();
-            typename Vec16<T>::Max top;
-            top.add(raw);
-            raise(fmaxf(m, top.top()));
-            Sums<T> part;
-            part.add(Exponent{finite_max(m), c}, raw);
-            s += part.total();
-        }
-        raise(warp_max(m));
-        s = warp_sum(s);
-        if (lane == 0) sm.part[warp] = make_float2(m, s);
+        slice_statistics<T, U, BWD>(sl, c, sm);
         if (keeps) tea.keep_logits(z_entries);
         __syncthreads();
         if (warp == 0) send_partial(sm, slices, rank, c);
         if (keeps) tea.softmax(sm, inv_T);  // while the partials travel
-        join_partials(a, sm, slices, c, &m, &s);
+        join_partials(a.flag, sm, slices, c, &m, &s);
     } else {
         m = a.stats_in[2 * row];
         s = a.stats_in[2 * row + 1];
@@ -423,24 +282,7 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
     if (BWD) {
         const Exponent e{finite_max(m), c};
         const float cg = a.T * a.grad_loss[row], inv = s == 0.0f ? 0.0f : 1.0f / s, coef = cg * inv;
-        for (int i = sl.lo + tid; i < sl.hi; i += U * NT) {
-            uint4 raw[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i + u * NT < sl.hi) raw[u] = __ldcs(zv + i + u * NT);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i + u * NT < sl.hi) {
-                    float v[Slice<T>::kVec];
-                    gradient_of<T>(e, coef, raw[u], v);
-                    out.store(i + u * NT, v);
-                }
-        }
-        if (sl.has_edge()) {
-            float v[Slice<T>::kVec];
-            gradient_of<T>(e, coef, sl.load_edge(), v);
-            out.store_values(sl.edge(), v);
-        }
+        store_softmax<T, U>(sl, out, e, coef);
         if (keeps) {
             if (!FWD) tea.softmax(sm, inv_T);
             tea.find_repeats(sm, sl.e0, sl.e1);
@@ -454,29 +296,6 @@ __global__ void __launch_bounds__(kDistillThreads, 4) distill_kernel(const Disti
     }
 }
 
-static int log2_of(int slices) {
-    int l = 0;
-    while ((1 << l) < slices) ++l;
-    return l;
-}
-
-struct DistillLaunch {
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[2];
-    DistillLaunch(int threads, int slices, bool cluster, size_t smem, cudaStream_t s) {
-        cfg.blockDim = dim3(static_cast<unsigned>(threads));
-        cfg.dynamicSmemBytes = smem;
-        cfg.stream = s;
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = static_cast<unsigned>(slices);
-        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = cluster ? 2 : 1;
-    }
-};
-
 template <typename T, bool FWD, bool BWD>
 static cudaError_t start_distill(const DistillParams &p, int64_t n, int slices, cudaStream_t s) {
     auto kernel = distill_kernel<T, FWD, BWD>;
@@ -487,30 +306,13 @@ static cudaError_t start_distill(const DistillParams &p, int64_t n, int slices, 
             prepared.once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); });
         if (e != cudaSuccess) return e;
     }
-    DistillLaunch l(kDistillThreads, slices, FWD, smem, s);
-    l.cfg.gridDim = dim3(static_cast<unsigned>(n * slices));
+    RowLaunch l(n * slices, FWD ? slices : 0, smem, s);
     return cudaLaunchKernelEx(&l.cfg, kernel, p, log2_of(slices));
 }
 
-// Bytes of a slice that one CTA takes, at most.  Gradient alone (128256 x 2048):
-// 155 us in slices of 128 KB, 163 of 256; each CTA reads the teacher's entries.
-constexpr int64_t kSliceBytes = 128 * 1024;
-// Loss and gradient, while a cluster can have more CTAs (fp32 128256 x 1024: 174 us in
-// slices of 64 KB, 186 of 128; bf16 151936 x 4096: 450 in slices of 76 KB, 556 of 38).
-constexpr int64_t kSliceStep = 80 * 1024;
-
 template <bool FWD, bool BWD>
 static cudaError_t launch_distill(const DistillParams &p, vie_dtype dtype, int64_t n, cudaStream_t s) {
-    const int64_t bytes = static_cast<int64_t>(p.V) * dtype_size(dtype);
-    int slices = 1;
-    if (!FWD) {  // no partials to join
-        while (bytes / slices > kSliceBytes && n * slices < (1 << 30)) slices *= 2;
-    } else {
-        if (BWD)
-            while (slices < kSlices && bytes / slices > kSliceStep) slices *= 2;
-        // enough CTAs for the chip, of 32 KB of the row or more
-        while (slices < (n <= kFewRows ? kMaxSlices : kSlices) && n * slices < 1024 && bytes / slices > 32768) slices *= 2;
-    }
+    const int slices = slices_of(FWD, BWD, static_cast<int64_t>(p.V) * dtype_size(dtype), n);
     return dtype == VIE_DTYPE_BF16 ? start_distill<__nv_bfloat16, FWD, BWD>(p, n, slices, s)
                                    : start_distill<float, FWD, BWD>(p, n, slices, s);
 }
