@@ -63,6 +63,8 @@ typedef enum {
 #define VIE_RECALL_M_MAX (1 << 20) /* largest candidate count m             */
 #define VIE_DISTILL_V_MAX (1 << 30) /* largest V of vie_distill_topk*       */
 #define VIE_SAMPLE_V_MAX (1 << 22) /* largest V of vie_sample_logits        */
+#define VIE_PREFERENCE_N_MAX (1 << 30) /* most tokens of vie_preference_loss* */
+#define VIE_E2M1_N_MAX (1 << 28)   /* most rows of an e2m1 matrix           */
 
 /* Read-only facts about a handle (for callers that size buffers or report). */
 typedef struct {
@@ -564,6 +566,204 @@ vie_status vie_embed_grad(const int32_t *tokens, int64_t n, const void *grad, vi
 vie_status vie_sample_logits(const void *logits, vie_dtype dtype, int64_t batch, int64_t V, int64_t ld, const float *u,
                              const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
                              int32_t *out_token, float *out_prob, vie_stream stream);
+
+/*
+ * vie_token_logprobs - log-probabilities of given tokens under full logits, e.g.
+ * of tokens that vie_sample_logits has drawn.  Per row, z its V logits, t its
+ * token, T the temperature:
+ *   m = max z,  s = sum_v exp((z_v - m) / T),  logprob = (z_t - m) / T - log s.
+ * Negative tokens are empty slots (a prompt's, padding): logprob 0 and stats
+ * (0, 0), and the row's logits are not read.  A token of V or more is taken as
+ * one and sets the device flag that vie_device_status reports.  A token whose
+ * logit is -inf has logprob -inf, whatever the other logits.  NaN or +inf
+ * logits give a NaN in their row only.
+ *
+ *   logits      device, dtype [n, V], row pitch ld.
+ *   n, V        0 <= n <= VIE_MANY_MAX;  1 <= V <= VIE_DISTILL_V_MAX.
+ *   tokens      device, int32 [n].
+ *   temperature > 0 and finite.
+ *   out_logprob device, fp32 [n].
+ *   out_stats   device, fp32 [n, 2]: m and s, what the gradients need; may be NULL.
+ *
+ * Errors: VIE_ERR_INVALID_ARG, VIE_ERR_UNSUPPORTED (dtype), VIE_ERR_CUDA.
+ */
+vie_status vie_token_logprobs(const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                              const int32_t *tokens, float temperature, float *out_logprob, float *out_stats,
+                              vie_stream stream);
+
+/*
+ * vie_token_logprobs_grad - the gradient of sum_i grad_logprob[i] logprob[i] with
+ * respect to the logits, q = softmax(z / T) (0 where no logit is above -inf):
+ *   out_grad[i, v] = grad_logprob[i] ([v = t] - q_v) / T,
+ * 0 in empty rows and in rows whose grad_logprob is 0, whose logits are not read.
+ * Arguments as for vie_token_logprobs, and
+ *   stats        device, fp32 [n, 2]: out_stats on the same logits and temperature.
+ *   grad_logprob device, fp32 [n].
+ *   out_grad     device, dtype [n, V], row pitch ld_grad; may be logits itself
+ *                (with ld_grad = ld), but not overlap it in any other way.
+ */
+vie_status vie_token_logprobs_grad(const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                                   const int32_t *tokens, float temperature, const float *stats,
+                                   const float *grad_logprob, void *out_grad, int64_t ld_grad, vie_stream stream);
+
+/*
+ * vie_policy_loss - clipped policy loss of drawn tokens with a KL term against a
+ * reference policy.  Per row, lp as of vie_token_logprobs, A the advantage:
+ *   r    = exp(lp - old_logprob)
+ *   loss = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)
+ *          + kl_coef (exp(x) - x - 1),  x = ref_logprob - lp.
+ * Empty rows (a token outside [0, V)) have loss, logprob and stats 0, and nothing
+ * of them is read.  An advantage of 0 has no first term, whatever r; the second
+ * is +inf where x is infinite.
+ *
+ *   logits, dtype, n, V, ld, tokens, temperature  as for vie_token_logprobs.
+ *   old_logprob, advantage  device, fp32 [n]: of the policy that drew the tokens.
+ *   ref_logprob device, fp32 [n]; may be NULL with a kl_coef of 0, which does not
+ *               read it.
+ *   clip_low    in [0, 1];  clip_high, kl_coef: finite, not negative.
+ *   out_loss, out_logprob  device, fp32 [n].
+ *   out_stats   as for vie_token_logprobs.
+ *
+ * Errors: VIE_ERR_INVALID_ARG, VIE_ERR_UNSUPPORTED (dtype), VIE_ERR_CUDA.
+ */
+vie_status vie_policy_loss(const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                           const int32_t *tokens, float temperature, const float *old_logprob, const float *advantage,
+                           const float *ref_logprob, float clip_low, float clip_high, float kl_coef, float *out_loss,
+                           float *out_logprob, float *out_stats, vie_stream stream);
+
+/*
+ * vie_policy_loss_grad - the gradient of sum_i grad_loss[i] loss[i] with respect
+ * to the logits:
+ *   slope = -A r where r A is the smaller one (also where both are the same),
+ *           else 0, + kl_coef (1 - exp(x));
+ *   out_grad[i, v] = grad_loss[i] slope ([v = t] - q_v) / T,
+ * 0 in empty rows, where grad_loss is 0 and where slope is 0 (a clipped token
+ * without a KL term); the logits of those are not read.  It is not finite where
+ * slope is not.
+ * Arguments as for vie_policy_loss, and
+ *   logprob, stats  device, fp32 [n] and [n, 2]: out_logprob and out_stats of
+ *               vie_policy_loss on the same logits and temperature.
+ *   grad_loss   device, fp32 [n].
+ *   out_grad    as for vie_token_logprobs_grad.
+ */
+vie_status vie_policy_loss_grad(const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                                const int32_t *tokens, float temperature, const float *old_logprob,
+                                const float *advantage, const float *ref_logprob, float clip_low, float clip_high,
+                                float kl_coef, const float *logprob, const float *stats, const float *grad_loss,
+                                void *out_grad, int64_t ld_grad, vie_stream stream);
+
+/*
+ * vie_policy_loss_step - vie_policy_loss and vie_policy_loss_grad in one call, for
+ * programs that know grad_loss beforehand.  Arguments as for those two;
+ * out_stats may be NULL.
+ */
+vie_status vie_policy_loss_step(const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                                const int32_t *tokens, float temperature, const float *old_logprob,
+                                const float *advantage, const float *ref_logprob, float clip_low, float clip_high,
+                                float kl_coef, const float *grad_loss, float *out_loss, float *out_logprob,
+                                float *out_stats, void *out_grad, int64_t ld_grad, vie_stream stream);
+
+/*
+ * vie_preference_loss - loss of preferred over rejected sequences from their
+ * tokens' log-probabilities (vie_token_logprobs).  Sequence j holds the tokens
+ * offsets[j] to offsets[j + 1] - 1 and may be empty; D_j is its sum of logprob -
+ * ref_logprob.  Pair p is sequence 2p, the chosen one, and 2p + 1, the rejected:
+ *   margin = beta (D_2p - D_2p+1)
+ *   loss   = -(1 - label_smoothing) log sigmoid(margin) - label_smoothing log sigmoid(-margin).
+ * Sums are fp32, in an order that depends on the sequence's place and length, n
+ * and pairs alone: the same call gives the same bits.
+ *
+ *   logprob     device, fp32 [n];  0 <= n <= VIE_PREFERENCE_N_MAX.
+ *   ref_logprob device, fp32 [n], or NULL (no reference: 0).
+ *   offsets     device, int32 [2 pairs + 1], 0 <= offsets[0] <= offsets[1] ... <= n;
+ *               tokens before the first and from the last on belong to no
+ *               sequence.  Offsets that decrease or leave [0, n] are held inside
+ *               (the results of their pairs are unspecified) and set the device
+ *               flag that vie_device_status reports.
+ *   pairs       0 <= pairs <= VIE_MANY_MAX.
+ *   beta        finite;  label_smoothing in [0, 1].
+ *   out_loss, out_margin  device, fp32 [pairs].
+ *
+ * Errors: VIE_ERR_INVALID_ARG, VIE_ERR_CUDA.
+ */
+vie_status vie_preference_loss(const float *logprob, const float *ref_logprob, int64_t n, const int32_t *offsets,
+                               int64_t pairs, float beta, float label_smoothing, float *out_loss, float *out_margin,
+                               vie_stream stream);
+
+/*
+ * vie_preference_loss_grad - the gradient of sum_p grad_loss[p] loss[p] with
+ * respect to each token's logprob: beta grad_loss (label_smoothing -
+ * sigmoid(-margin)) for the tokens of a chosen sequence, the negative for those
+ * of a rejected one, 0 for the others (all n are written).  It is what
+ * vie_token_logprobs_grad takes as grad_logprob.
+ *   margin      device, fp32 [pairs]: out_margin.
+ *   grad_loss   device, fp32 [pairs].
+ *   out_grad    device, fp32 [n]; must not overlap the inputs.
+ * The other arguments as for vie_preference_loss.
+ */
+vie_status vie_preference_loss_grad(const float *margin, int64_t n, const int32_t *offsets, int64_t pairs, float beta,
+                                    float label_smoothing, const float *grad_loss, float *out_grad,
+                                    vie_stream stream);
+
+/* vie_preference_loss and vie_preference_loss_grad in one call. */
+vie_status vie_preference_loss_step(const float *logprob, const float *ref_logprob, int64_t n, const int32_t *offsets,
+                                    int64_t pairs, float beta, float label_smoothing, const float *grad_loss,
+                                    float *out_loss, float *out_margin, float *out_grad, vie_stream stream);
+
+/*
+ * Matrices in microscaled 4-bit floating point (e2m1), e.g. a head's rows: 4.5
+ * bits per value.  Each row x of d values has a power of two s = 2^E, E the least
+ * whole number (-126 at the least) with max |x| <= 2688 s; each block of 16 values
+ * has a scale sigma = e4m3(max |x| over the block / (6 s)); a value's code is
+ * e2m1(x / (s sigma)), at most 6 in magnitude (0 where sigma is 0), and stands for
+ * code * sigma * s.  Roundings are to nearest, ties to even.  A row that holds a
+ * NaN or an infinity has s = NaN and codes of 0: all that is made of it is NaN.
+ *   codes       uint8 [n, ceil(d / 32) * 16]: two codes to a byte, the even column
+ *               in the low four bits; columns from d on are 0.
+ *   scales      e4m3 [ceil(n / 128), ceil(d / 64), 32, 4, 4]: tiles of 128 rows by 4
+ *               blocks; element [a, b, c] of a tile belongs to its row 32 b + a and
+ *               block c.  Scales beyond the matrix are 0.
+ *   row_scales  fp32 [n]: s.
+ * vie_e2m1_bytes gives the sizes of codes and scales; both are 16-byte aligned.
+ * 0 <= n <= VIE_E2M1_N_MAX;  1 <= d <= VIE_D_MAX.
+ */
+vie_status vie_e2m1_bytes(int64_t n, int32_t d, int64_t *code_bytes, int64_t *scale_bytes);
+
+/*
+ * vie_e2m1_quantize - rows to e2m1.
+ *   x           device, dtype [n, d], row pitch ld.
+ *   out_codes, out_scales, out_row_scales  device, as above.
+ *   out_values  device, values_dtype [n, d], row pitch ld_values, or NULL: what the
+ *               codes stand for, e.g. the weights that a training step computes
+ *               with (exact in fp32, and in bf16 above its subnormal numbers); may
+ *               be x itself (with its type and pitch), but not overlap it in any
+ *               other way.
+ *
+ * Errors: VIE_ERR_INVALID_ARG, VIE_ERR_UNSUPPORTED (dtype), VIE_ERR_CUDA.
+ */
+vie_status vie_e2m1_quantize(const void *x, vie_dtype dtype, int64_t n, int32_t d, int64_t ld, void *out_codes,
+                             void *out_scales, float *out_row_scales, void *out_values, vie_dtype values_dtype,
+                             int64_t ld_values, vie_stream stream);
+
+/* vie_e2m1_dequantize - out[i, j] = what the codes stand for (out_dtype [n, d], row pitch ld_out). */
+vie_status vie_e2m1_dequantize(const void *codes, const void *scales, const float *row_scales, int64_t n, int32_t d,
+                               void *out, vie_dtype out_dtype, int64_t ld_out, vie_stream stream);
+
+/*
+ * vie_e2m1_logits - full logits of a head whose rows are e2m1, for hidden states
+ * that are e2m1 as well:
+ *   out[i, v] = sum_j x[i, j] w[v, j],
+ * products exact, sums fp32, rounded once to out_dtype.  (vie_sample_logits draws
+ * from them, vie_token_logprobs scores them.)
+ *   x_*         device, n rows of d values;  0 <= n <= VIE_MANY_MAX.
+ *   w_*         device, V rows of d values;  1 <= V <= VIE_E2M1_N_MAX.
+ *   out         device, out_dtype [n, V], row pitch ld_out.
+ *
+ * Errors: VIE_ERR_INVALID_ARG, VIE_ERR_UNSUPPORTED (dtype), VIE_ERR_CUDA.
+ */
+vie_status vie_e2m1_logits(const void *x_codes, const void *x_scales, const float *x_row_scales, int64_t n,
+                           const void *w_codes, const void *w_scales, const float *w_row_scales, int64_t V, int32_t d,
+                           void *out, vie_dtype out_dtype, int64_t ld_out, vie_stream stream);
 
 /*
  * vie_device_status - synchronises `stream`, then reads and clears the

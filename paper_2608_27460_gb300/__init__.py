@@ -36,6 +36,8 @@ VIE_RECALL_N_MAX = 1 << 28
 VIE_RECALL_M_MAX = 1 << 20
 VIE_DISTILL_V_MAX = 1 << 30
 VIE_SAMPLE_V_MAX = 1 << 22
+VIE_PREFERENCE_N_MAX = 1 << 30
+VIE_E2M1_N_MAX = 1 << 28
 
 # Launch options (vie_launch_option): tuning and test hooks, never results.
 VIE_OPT_STAGE_MIN_KB = 0
@@ -60,7 +62,10 @@ EXPORTS = ("vie_head_create", "vie_head_destroy", "vie_head_get_props", "vie_hea
            "vie_head_topk_noalloc", "vie_scatter_sparse_logits", "vie_device_status",
            "vie_head_device_status", "vie_last_error", "vie_set_launch_option", "vie_get_launch_option",
            "vie_distill_topk", "vie_distill_topk_grad", "vie_distill_topk_step", "vie_embed",
-           "vie_embed_grad_workspace", "vie_embed_grad", "vie_sample_logits")
+           "vie_embed_grad_workspace", "vie_embed_grad", "vie_sample_logits", "vie_token_logprobs",
+           "vie_token_logprobs_grad", "vie_policy_loss", "vie_policy_loss_grad", "vie_policy_loss_step",
+           "vie_preference_loss", "vie_preference_loss_grad", "vie_preference_loss_step", "vie_e2m1_bytes",
+           "vie_e2m1_quantize", "vie_e2m1_dequantize", "vie_e2m1_logits")
 
 
 class VieError(RuntimeError):
@@ -135,6 +140,21 @@ def load(path: str | None = None, build_if_missing: bool = True):
             "vie_embed_grad": ([P, I64, P, ctypes.c_int, I64, F32, I64, I32, P, ctypes.c_int, I64, I32, P, I64, P],
                                ctypes.c_int),
             "vie_sample_logits": ([P, ctypes.c_int, I64, I64, I64, P, P, P, P, P, P, P, P], ctypes.c_int),
+            "vie_token_logprobs": ([P, ctypes.c_int, I64, I64, I64, P, F32, P, P, P], ctypes.c_int),
+            "vie_token_logprobs_grad": ([P, ctypes.c_int, I64, I64, I64, P, F32, P, P, P, I64, P], ctypes.c_int),
+            "vie_policy_loss": ([P, ctypes.c_int, I64, I64, I64, P, F32, P, P, P, F32, F32, F32, P, P, P, P],
+                                ctypes.c_int),
+            "vie_policy_loss_grad": ([P, ctypes.c_int, I64, I64, I64, P, F32, P, P, P, F32, F32, F32, P, P, P, P, I64,
+                                      P], ctypes.c_int),
+            "vie_policy_loss_step": ([P, ctypes.c_int, I64, I64, I64, P, F32, P, P, P, F32, F32, F32, P, P, P, P, P,
+                                      I64, P], ctypes.c_int),
+            "vie_preference_loss": ([P, P, I64, P, I64, F32, F32, P, P, P], ctypes.c_int),
+            "vie_preference_loss_grad": ([P, I64, P, I64, F32, F32, P, P, P], ctypes.c_int),
+            "vie_preference_loss_step": ([P, P, I64, P, I64, F32, F32, P, P, P, P, P], ctypes.c_int),
+            "vie_e2m1_bytes": ([I64, I32, ctypes.POINTER(I64), ctypes.POINTER(I64)], ctypes.c_int),
+            "vie_e2m1_quantize": ([P, ctypes.c_int, I64, I32, I64, P, P, P, P, ctypes.c_int, I64, P], ctypes.c_int),
+            "vie_e2m1_dequantize": ([P, P, P, I64, I32, P, ctypes.c_int, I64, P], ctypes.c_int),
+            "vie_e2m1_logits": ([P, P, P, I64, P, P, P, I64, I32, P, ctypes.c_int, I64, P], ctypes.c_int),
         }
         for name, (args, res) in sig.items():
             fn = getattr(lib, name)
@@ -311,6 +331,86 @@ def vie_sample_logits(logits: int, dtype: int, batch: int, V: int, ld: int, u: i
                       top_p: int, min_p: int, out_token: int, out_prob: int, stream: int = 0) -> int:
     return load().vie_sample_logits(logits, dtype, batch, V, ld, u, temperature, top_k, top_p, min_p, out_token,
                                     out_prob, stream)
+
+
+def vie_token_logprobs(logits: int, dtype: int, n: int, V: int, ld: int, tokens: int, temperature: float,
+                       out_logprob: int, out_stats: int = 0, stream: int = 0) -> int:
+    return load().vie_token_logprobs(logits, dtype, n, V, ld, tokens, temperature, out_logprob, out_stats, stream)
+
+
+def vie_token_logprobs_grad(logits: int, dtype: int, n: int, V: int, ld: int, tokens: int, temperature: float,
+                            stats: int, grad_logprob: int, out_grad: int, ld_grad: int, stream: int = 0) -> int:
+    return load().vie_token_logprobs_grad(logits, dtype, n, V, ld, tokens, temperature, stats, grad_logprob, out_grad,
+                                          ld_grad, stream)
+
+
+def vie_policy_loss(logits: int, dtype: int, n: int, V: int, ld: int, tokens: int, temperature: float,
+                    old_logprob: int, advantage: int, ref_logprob: int, clip_low: float, clip_high: float,
+                    kl_coef: float, out_loss: int, out_logprob: int, out_stats: int = 0, stream: int = 0) -> int:
+    return load().vie_policy_loss(logits, dtype, n, V, ld, tokens, temperature, old_logprob, advantage, ref_logprob,
+                                  clip_low, clip_high, kl_coef, out_loss, out_logprob, out_stats, stream)
+
+
+def vie_policy_loss_grad(logits: int, dtype: int, n: int, V: int, ld: int, tokens: int, temperature: float,
+                         old_logprob: int, advantage: int, ref_logprob: int, clip_low: float, clip_high: float,
+                         kl_coef: float, logprob: int, stats: int, grad_loss: int, out_grad: int, ld_grad: int,
+                         stream: int = 0) -> int:
+    return load().vie_policy_loss_grad(logits, dtype, n, V, ld, tokens, temperature, old_logprob, advantage,
+                                       ref_logprob, clip_low, clip_high, kl_coef, logprob, stats, grad_loss, out_grad,
+                                       ld_grad, stream)
+
+
+def vie_policy_loss_step(logits: int, dtype: int, n: int, V: int, ld: int, tokens: int, temperature: float,
+                         old_logprob: int, advantage: int, ref_logprob: int, clip_low: float, clip_high: float,
+                         kl_coef: float, grad_loss: int, out_loss: int, out_logprob: int, out_stats: int,
+                         out_grad: int, ld_grad: int, stream: int = 0) -> int:
+    return load().vie_policy_loss_step(logits, dtype, n, V, ld, tokens, temperature, old_logprob, advantage,
+                                       ref_logprob, clip_low, clip_high, kl_coef, grad_loss, out_loss, out_logprob,
+                                       out_stats, out_grad, ld_grad, stream)
+
+
+def vie_preference_loss(logprob: int, ref_logprob: int, n: int, offsets: int, pairs: int, beta: float,
+                        label_smoothing: float, out_loss: int, out_margin: int, stream: int = 0) -> int:
+    return load().vie_preference_loss(logprob, ref_logprob, n, offsets, pairs, beta, label_smoothing, out_loss,
+                                      out_margin, stream)
+
+
+def vie_preference_loss_grad(margin: int, n: int, offsets: int, pairs: int, beta: float, label_smoothing: float,
+                             grad_loss: int, out_grad: int, stream: int = 0) -> int:
+    return load().vie_preference_loss_grad(margin, n, offsets, pairs, beta, label_smoothing, grad_loss, out_grad,
+                                           stream)
+
+
+def vie_preference_loss_step(logprob: int, ref_logprob: int, n: int, offsets: int, pairs: int, beta: float,
+                             label_smoothing: float, grad_loss: int, out_loss: int, out_margin: int, out_grad: int,
+                             stream: int = 0) -> int:
+    return load().vie_preference_loss_step(logprob, ref_logprob, n, offsets, pairs, beta, label_smoothing, grad_loss,
+                                           out_loss, out_margin, out_grad, stream)
+
+
+def vie_e2m1_bytes(n: int, d: int):
+    """Returns (status, bytes of codes, bytes of scales)."""
+    c, s = ctypes.c_int64(0), ctypes.c_int64(0)
+    st = load().vie_e2m1_bytes(n, d, ctypes.byref(c), ctypes.byref(s))
+    return st, c.value, s.value
+
+
+def vie_e2m1_quantize(x: int, dtype: int, n: int, d: int, ld: int, out_codes: int, out_scales: int,
+                      out_row_scales: int, out_values: int = 0, values_dtype: int = VIE_DTYPE_F32, ld_values: int = 0,
+                      stream: int = 0) -> int:
+    return load().vie_e2m1_quantize(x, dtype, n, d, ld, out_codes, out_scales, out_row_scales, out_values,
+                                    values_dtype, ld_values, stream)
+
+
+def vie_e2m1_dequantize(codes: int, scales: int, row_scales: int, n: int, d: int, out: int, out_dtype: int,
+                        ld_out: int, stream: int = 0) -> int:
+    return load().vie_e2m1_dequantize(codes, scales, row_scales, n, d, out, out_dtype, ld_out, stream)
+
+
+def vie_e2m1_logits(x_codes: int, x_scales: int, x_row_scales: int, n: int, w_codes: int, w_scales: int,
+                    w_row_scales: int, V: int, d: int, out: int, out_dtype: int, ld_out: int, stream: int = 0) -> int:
+    return load().vie_e2m1_logits(x_codes, x_scales, x_row_scales, n, w_codes, w_scales, w_row_scales, V, d, out,
+                                  out_dtype, ld_out, stream)
 
 
 def vie_scatter_sparse_logits(idx: int, logits: int, batch: int, k: int, V: int, out: int,
@@ -659,6 +759,315 @@ def sample_logits(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
                             0 if min_p is None else min_p.data_ptr(), out_token.data_ptr(), out_prob.data_ptr(),
                             _stream_ptr(None)))
     return out_token, out_prob
+
+
+def _drawn(logits, tokens):
+    """The checked arguments that the calls on drawn tokens share: logits and their pitch, tokens."""
+    logits, ld = _matrix(logits, "logits")
+    return logits, ld, _given(tokens, "tokens", (logits.shape[0],), _torch.int32, logits)
+
+
+def token_logprobs(logits, tokens, temperature: float = 1.0, out_logprob=None, out_stats=None, stream=None):
+    """Log-probabilities of tokens (int32 [n], negative: empty slots) under the
+    softmax of logits / temperature ([n, V], bf16 or fp32).  Returns (logprob
+    [n], stats [n, 2]); stats go to token_logprobs_grad, which an autograd
+    program calls in its backward pass: the results have no graph."""
+    if not _here(logits, "logits") or stream is not None:
+        with _on(logits, stream):
+            return token_logprobs(logits, tokens, temperature, out_logprob, out_stats)
+    logits, ld, tokens = _drawn(logits, tokens)
+    n, V = logits.shape
+    out_logprob = _contiguous_output(out_logprob, "out_logprob", (n,), _torch.float32, logits)
+    out_stats = _contiguous_output(out_stats, "out_stats", (n, 2), _torch.float32, logits)
+    check(vie_token_logprobs(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, tokens.data_ptr(),
+                             temperature, out_logprob.data_ptr(), out_stats.data_ptr(), _stream_ptr(None)))
+    return out_logprob, out_stats
+
+
+def token_logprobs_grad(logits, tokens, stats, grad_logprob, temperature: float = 1.0, out_grad=None, stream=None):
+    """Gradient of sum(grad_logprob * logprob) with respect to the logits, in
+    their type; `stats` come from token_logprobs (or policy_loss).  out_grad may
+    be logits.  (logits.backward(gradient) takes it on through the graph that
+    made them.)"""
+    if not _here(logits, "logits") or stream is not None:
+        with _on(logits, stream):
+            return token_logprobs_grad(logits, tokens, stats, grad_logprob, temperature, out_grad)
+    logits, ld, tokens = _drawn(logits, tokens)
+    n, V = logits.shape
+    stats = _given(stats, "stats", (n, 2), _torch.float32, logits)
+    grad_logprob = _given(grad_logprob, "grad_logprob", (n,), _torch.float32, logits)
+    out_grad, ld_grad = _matrix_output(out_grad, "out_grad", (n, V), logits.dtype, logits)
+    z, dz = logits.data_ptr(), out_grad.data_ptr()
+    check(vie_token_logprobs_grad(z, _dtype_code(logits, "logits"), n, V, ld, tokens.data_ptr(), temperature,
+                                  stats.data_ptr(), grad_logprob.data_ptr(), dz, ld_grad, _stream_ptr(None)))
+    if dz == z:
+        _changed(out_grad)
+    return out_grad
+
+
+def _policy(logits, old_logprob, advantage, ref_logprob, kl_coef):
+    """The policy calls' checked terms and their addresses."""
+    n = (logits.shape[0],)
+    old_logprob = _given(old_logprob, "old_logprob", n, _torch.float32, logits)
+    advantage = _given(advantage, "advantage", n, _torch.float32, logits)
+    if ref_logprob is not None:
+        ref_logprob = _given(ref_logprob, "ref_logprob", n, _torch.float32, logits)
+    elif kl_coef != 0.0:
+        raise ValueError("kl_coef needs the reference's log-probabilities (ref_logprob)")
+    return (old_logprob, advantage, ref_logprob), (old_logprob.data_ptr(), advantage.data_ptr(),
+                                                   0 if ref_logprob is None else ref_logprob.data_ptr())
+
+
+def policy_loss(logits, tokens, old_logprob, advantage, ref_logprob=None, clip_low: float = 0.2,
+                clip_high: float = 0.2, kl_coef: float = 0.0, temperature: float = 1.0, out_loss=None,
+                out_logprob=None, out_stats=None, stream=None):
+    """Clipped policy loss of drawn tokens with a KL term, per row: with r =
+    exp(logprob - old_logprob) and x = ref_logprob - logprob,
+    -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(x) - x - 1).
+    logits, tokens and temperature as for token_logprobs; old_logprob,
+    advantage and ref_logprob float32 [n].  Returns (loss [n], logprob [n],
+    stats [n, 2]); the last two go to policy_loss_grad: the loss has no graph."""
+    if not _here(logits, "logits") or stream is not None:
+        with _on(logits, stream):
+            return policy_loss(logits, tokens, old_logprob, advantage, ref_logprob, clip_low, clip_high, kl_coef,
+                               temperature, out_loss, out_logprob, out_stats)
+    logits, ld, tokens = _drawn(logits, tokens)
+    n, V = logits.shape
+    keep, terms = _policy(logits, old_logprob, advantage, ref_logprob, kl_coef)
+    out_loss = _contiguous_output(out_loss, "out_loss", (n,), _torch.float32, logits)
+    out_logprob = _contiguous_output(out_logprob, "out_logprob", (n,), _torch.float32, logits)
+    out_stats = _contiguous_output(out_stats, "out_stats", (n, 2), _torch.float32, logits)
+    check(vie_policy_loss(logits.data_ptr(), _dtype_code(logits, "logits"), n, V, ld, tokens.data_ptr(), temperature,
+                          *terms, clip_low, clip_high, kl_coef, out_loss.data_ptr(), out_logprob.data_ptr(),
+                          out_stats.data_ptr(), _stream_ptr(None)))
+    return out_loss, out_logprob, out_stats
+
+
+def policy_loss_grad(logits, tokens, old_logprob, advantage, logprob, stats, grad_loss, ref_logprob=None,
+                     clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0, temperature: float = 1.0,
+                     out_grad=None, stream=None):
+    """Gradient of sum(grad_loss * loss) with respect to the logits, in their
+    type; `logprob` and `stats` come from policy_loss.  out_grad may be logits."""
+    if not _here(logits, "logits") or stream is not None:
+        with _on(logits, stream):
+            return policy_loss_grad(logits, tokens, old_logprob, advantage, logprob, stats, grad_loss, ref_logprob,
+                                    clip_low, clip_high, kl_coef, temperature, out_grad)
+    logits, ld, tokens = _drawn(logits, tokens)
+    n, V = logits.shape
+    keep, terms = _policy(logits, old_logprob, advantage, ref_logprob, kl_coef)
+    logprob = _given(logprob, "logprob", (n,), _torch.float32, logits)
+    stats = _given(stats, "stats", (n, 2), _torch.float32, logits)
+    grad_loss = _given(grad_loss, "grad_loss", (n,), _torch.float32, logits)
+    out_grad, ld_grad = _matrix_output(out_grad, "out_grad", (n, V), logits.dtype, logits)
+    z, dz = logits.data_ptr(), out_grad.data_ptr()
+    check(vie_policy_loss_grad(z, _dtype_code(logits, "logits"), n, V, ld, tokens.data_ptr(), temperature, *terms,
+                               clip_low, clip_high, kl_coef, logprob.data_ptr(), stats.data_ptr(),
+                               grad_loss.data_ptr(), dz, ld_grad, _stream_ptr(None)))
+    if dz == z:
+        _changed(out_grad)
+    return out_grad
+
+
+def policy_loss_step(logits, tokens, old_logprob, advantage, grad_loss, ref_logprob=None, clip_low: float = 0.2,
+                     clip_high: float = 0.2, kl_coef: float = 0.0, temperature: float = 1.0, out_loss=None,
+                     out_logprob=None, out_grad=None, out_stats=None, stream=None):
+    """policy_loss and policy_loss_grad in one call: (loss [n], logprob [n],
+    gradient [n, V]).  grad_loss [n] is the weight of each row's loss; out_grad
+    may be logits.  out_stats (float32 [n, 2]) takes the statistics, if given."""
+    if not _here(logits, "logits") or stream is not None:
+        with _on(logits, stream):
+            return policy_loss_step(logits, tokens, old_logprob, advantage, grad_loss, ref_logprob, clip_low,
+                                    clip_high, kl_coef, temperature, out_loss, out_logprob, out_grad, out_stats)
+    logits, ld, tokens = _drawn(logits, tokens)
+    n, V = logits.shape
+    keep, terms = _policy(logits, old_logprob, advantage, ref_logprob, kl_coef)
+    grad_loss = _given(grad_loss, "grad_loss", (n,), _torch.float32, logits)
+    out_loss = _contiguous_output(out_loss, "out_loss", (n,), _torch.float32, logits)
+    out_logprob = _contiguous_output(out_logprob, "out_logprob", (n,), _torch.float32, logits)
+    stats = 0
+    if out_stats is not None:
+        stats = _contiguous_output(out_stats, "out_stats", (n, 2), _torch.float32, logits).data_ptr()
+    out_grad, ld_grad = _matrix_output(out_grad, "out_grad", (n, V), logits.dtype, logits)
+    z, dz = logits.data_ptr(), out_grad.data_ptr()
+    check(vie_policy_loss_step(z, _dtype_code(logits, "logits"), n, V, ld, tokens.data_ptr(), temperature, *terms,
+                               clip_low, clip_high, kl_coef, grad_loss.data_ptr(), out_loss.data_ptr(),
+                               out_logprob.data_ptr(), stats, dz, ld_grad, _stream_ptr(None)))
+    if dz == z:
+        _changed(out_grad)
+    return out_loss, out_logprob, out_grad
+
+
+def _sequences(logprob, offsets):
+    """The preference calls' checked log-probabilities (or what else has one value
+    per token), offsets and number of pairs."""
+    if logprob.dim() != 1 or offsets.dim() != 1 or offsets.numel() % 2 != 1:
+        raise ValueError("log-probabilities [n] and offsets [2 pairs + 1] must be 1-D tensors")
+    m = offsets.numel()
+    return _given(offsets, "offsets", (m,), _torch.int32, logprob), m // 2
+
+
+def preference_loss(logprob, offsets, ref_logprob=None, beta: float = 0.1, label_smoothing: float = 0.0,
+                    out_loss=None, out_margin=None, stream=None):
+    """Loss of preferred over rejected sequences from their tokens'
+    log-probabilities (float32 [n], as token_logprobs returns them): with
+    sequence j at tokens offsets[j] to offsets[j + 1] - 1 (int32 [2 pairs + 1]),
+    D_j its sum of logprob - ref_logprob and margin = beta (D_2p - D_2p+1),
+    -(1 - label_smoothing) log sigmoid(margin) - label_smoothing log
+    sigmoid(-margin).  Returns (loss [pairs], margin [pairs]), without a graph."""
+    if not _here(logprob, "logprob") or stream is not None:
+        with _on(logprob, stream):
+            return preference_loss(logprob, offsets, ref_logprob, beta, label_smoothing, out_loss, out_margin)
+    offsets, pairs = _sequences(logprob, offsets)
+    n = (logprob.shape[0],)
+    logprob = _given(logprob, "logprob", n, _torch.float32, logprob)
+    if ref_logprob is not None:
+        ref_logprob = _given(ref_logprob, "ref_logprob", n, _torch.float32, logprob)
+    out_loss = _contiguous_output(out_loss, "out_loss", (pairs,), _torch.float32, logprob)
+    out_margin = _contiguous_output(out_margin, "out_margin", (pairs,), _torch.float32, logprob)
+    check(vie_preference_loss(logprob.data_ptr(), 0 if ref_logprob is None else ref_logprob.data_ptr(), n[0],
+                              offsets.data_ptr(), pairs, beta, label_smoothing, out_loss.data_ptr(),
+                              out_margin.data_ptr(), _stream_ptr(None)))
+    return out_loss, out_margin
+
+
+def preference_loss_grad(margin, offsets, grad_loss, n: int, beta: float = 0.1, label_smoothing: float = 0.0,
+                         out_grad=None, stream=None):
+    """Gradient of sum(grad_loss * loss) with respect to the n tokens'
+    log-probabilities (float32 [n], what token_logprobs_grad takes); `margin`
+    comes from preference_loss."""
+    if not _here(margin, "margin") or stream is not None:
+        with _on(margin, stream):
+            return preference_loss_grad(margin, offsets, grad_loss, n, beta, label_smoothing, out_grad)
+    offsets, pairs = _sequences(margin, offsets)
+    margin = _given(margin, "margin", (pairs,), _torch.float32, margin)
+    grad_loss = _given(grad_loss, "grad_loss", (pairs,), _torch.float32, margin)
+    out_grad = _contiguous_output(out_grad, "out_grad", (n,), _torch.float32, margin)
+    check(vie_preference_loss_grad(margin.data_ptr(), n, offsets.data_ptr(), pairs, beta, label_smoothing,
+                                   grad_loss.data_ptr(), out_grad.data_ptr(), _stream_ptr(None)))
+    return out_grad
+
+
+def preference_loss_step(logprob, offsets, grad_loss, ref_logprob=None, beta: float = 0.1,
+                         label_smoothing: float = 0.0, out_loss=None, out_margin=None, out_grad=None, stream=None):
+    """preference_loss and preference_loss_grad in one call: (loss [pairs],
+    margin [pairs], gradient [n])."""
+    if not _here(logprob, "logprob") or stream is not None:
+        with _on(logprob, stream):
+            return preference_loss_step(logprob, offsets, grad_loss, ref_logprob, beta, label_smoothing, out_loss,
+                                        out_margin, out_grad)
+    offsets, pairs = _sequences(logprob, offsets)
+    n = (logprob.shape[0],)
+    logprob = _given(logprob, "logprob", n, _torch.float32, logprob)
+    if ref_logprob is not None:
+        ref_logprob = _given(ref_logprob, "ref_logprob", n, _torch.float32, logprob)
+    grad_loss = _given(grad_loss, "grad_loss", (pairs,), _torch.float32, logprob)
+    out_loss = _contiguous_output(out_loss, "out_loss", (pairs,), _torch.float32, logprob)
+    out_margin = _contiguous_output(out_margin, "out_margin", (pairs,), _torch.float32, logprob)
+    out_grad = _contiguous_output(out_grad, "out_grad", n, _torch.float32, logprob)
+    check(vie_preference_loss_step(logprob.data_ptr(), 0 if ref_logprob is None else ref_logprob.data_ptr(), n[0],
+                                   offsets.data_ptr(), pairs, beta, label_smoothing, grad_loss.data_ptr(),
+                                   out_loss.data_ptr(), out_margin.data_ptr(), out_grad.data_ptr(),
+                                   _stream_ptr(None)))
+    return out_loss, out_margin, out_grad
+
+
+class E2m1:
+    """A matrix in microscaled 4-bit floating point: n rows of d values in
+    `codes` (uint8 [n, ceil(d / 32) * 16], two to a byte), `scales` (e4m3 bits,
+    uint8 [ceil(n / 128), ceil(d / 64), 32, 4, 4], one per 16 values) and
+    `row_scales` (float32 [n], powers of two), as e2m1_quantize makes them."""
+
+    __slots__ = ("codes", "scales", "row_scales", "d")
+
+    def __init__(self, codes, scales, row_scales, d: int):
+        self.codes, self.scales, self.row_scales, self.d = codes, scales, row_scales, d
+
+    @classmethod
+    def empty(cls, n: int, d: int, device="cuda"):
+        """Room for n rows of d values."""
+        import torch
+        return cls(torch.empty((n, (d + 31) // 32 * 16), dtype=torch.uint8, device=device),
+                   torch.empty(((n + 127) // 128, (d + 63) // 64, 32, 4, 4), dtype=torch.uint8, device=device),
+                   torch.empty((n,), dtype=torch.float32, device=device), d)
+
+    @property
+    def shape(self):
+        return (self.codes.shape[0], self.d)
+
+    def _pointers(self, name, shape, like):
+        """Addresses of the parts of a matrix of this shape on like's device."""
+        n, d = shape
+        c, s, r = self.codes, self.scales, self.row_scales
+        if d != self.d or c.shape != (n, (d + 31) // 32 * 16) or c.dtype is not _torch.uint8 or                 s.numel() != (n + 127) // 128 * ((d + 63) // 64) * 512 or s.element_size() != 1 or                 r.shape != (n,) or r.dtype is not _torch.float32:
+            raise ValueError(f"{name} must be an E2m1 of {n} rows of {d} values")
+        for x in (c, s, r):
+            if not x.is_contiguous() or not x.is_cuda or x.get_device() != like.get_device():
+                raise ValueError(f"{name} must hold contiguous tensors on {like.device}")
+        return c.data_ptr(), s.data_ptr(), r.data_ptr()
+
+
+def e2m1_quantize(x, out=None, out_values=None, stream=None):
+    """The rows of x [n, d] (bf16 or fp32) in 4 bits, an E2m1 (`out`, if given).
+    out_values (bf16 or fp32 [n, d]) takes what the codes stand for; it may be x."""
+    if not _here(x, "x") or stream is not None:
+        with _on(x, stream):
+            return e2m1_quantize(x, out, out_values)
+    x, ld = _matrix(x, "x")
+    n, d = x.shape
+    if out is None:
+        out = E2m1.empty(n, d, x.device)
+    codes, scales, row_scales = out._pointers("out", (n, d), x)
+    values, values_dtype, ld_values = 0, VIE_DTYPE_F32, 0
+    if out_values is not None:
+        out_values, ld_values = _matrix_output(out_values, "out_values", (n, d), out_values.dtype, x)
+        values, values_dtype = out_values.data_ptr(), _dtype_code(out_values, "out_values")
+    check(vie_e2m1_quantize(x.data_ptr(), _dtype_code(x, "x"), n, d, ld, codes, scales, row_scales, values,
+                            values_dtype, ld_values, _stream_ptr(None)))
+    if values and values == x.data_ptr():
+        _changed(out_values)
+    return out
+
+
+def e2m1_dequantize(q, out=None, out_dtype=None, stream=None):
+    """What the codes of an E2m1 stand for, [n, d]; out_dtype (of a new `out`)
+    defaults to float32."""
+    like = q.codes
+    if not _here(like, "codes") or stream is not None:
+        with _on(like, stream):
+            return e2m1_dequantize(q, out, out_dtype)
+    n, d = q.shape
+    codes, scales, row_scales = q._pointers("q", (n, d), like)
+    if out_dtype is None:
+        out_dtype = _torch.float32 if out is None else out.dtype
+    out, ld = _matrix_output(out, "out", (n, d), out_dtype, like)
+    check(vie_e2m1_dequantize(codes, scales, row_scales, n, d, out.data_ptr(), _dtype_code(out, "out"), ld,
+                              _stream_ptr(None)))
+    return out
+
+
+def e2m1_logits(x, weights, out=None, out_dtype=None, x_quantized=None, stream=None):
+    """Full logits [n, V] (bf16 or fp32) of a head whose rows are an E2m1 of V
+    rows of d values.  x: hidden states [n, d] in bf16 or fp32, which the call
+    quantises as well (into x_quantized, an E2m1 of n rows of d values that a
+    program keeps, if given), or an E2m1.  out_dtype (of a new `out`) defaults
+    to float32.  The logits have no graph."""
+    like = weights.codes
+    if not _here(like, "weights") or stream is not None:
+        with _on(like, stream):
+            return e2m1_logits(x, weights, out, out_dtype, x_quantized)
+    V, d = weights.shape
+    if not isinstance(x, E2m1):
+        if x.dim() != 2 or x.shape[1] != d or not x.is_cuda or x.get_device() != like.get_device():
+            raise ValueError(f"x must be a tensor [n, {d}] on {like.device}")
+        x = e2m1_quantize(x, out=x_quantized)
+    n = x.shape[0]
+    xp = x._pointers("x", (n, d), like)
+    wp = weights._pointers("weights", (V, d), like)
+    if out_dtype is None:
+        out_dtype = _torch.float32 if out is None else out.dtype
+    out, ld = _matrix_output(out, "out", (n, V), out_dtype, like)
+    check(vie_e2m1_logits(*xp, n, *wp, V, d, out.data_ptr(), _dtype_code(out, "out"), ld, _stream_ptr(None)))
+    return out
 
 
 class Head:

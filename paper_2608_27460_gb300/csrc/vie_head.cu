@@ -1137,9 +1137,10 @@ vie_status vie_device_status(vie_stream stream) {
     const uint32_t zero = 0;
     e = cudaMemcpyToSymbol(g_dev_err, &zero, sizeof zero);
     if (e != cudaSuccess) return fail_cuda(e, "vie_device_status: clear flag");
-    return fail(VIE_ERR_DEVICE, "device flag 0x%x:%s%s%s", w,
+    return fail(VIE_ERR_DEVICE, "device flag 0x%x:%s%s%s%s", w,
                 (w & vie::kErrScatterIndex) ? " scatter index outside [0, V)" : "",
                 (w & vie::kErrTokenIndex) ? " token at or above V" : "",
+                (w & vie::kErrOffsets) ? " sequence offsets decrease or leave [0, n]" : "",
                 (w & vie::kErrWaitTimeout) ? " pipeline wait timed out" : "");
 }
 

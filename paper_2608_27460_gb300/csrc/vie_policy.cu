@@ -1,0 +1,458 @@
+// vie_policy.cu - what a model learns from tokens that were drawn: their
+// log-probabilities under full logits, a clipped policy loss with a KL term and
+// a loss of preferred over rejected sequences, each with its gradient.
+//
+// Per row of logits, z the V values, t the row's token, T the temperature:
+//   m  = max z,  s = sum_v exp((z_v - m) / T)
+//   lp = (z_t - m) / T - log s
+//   q  = softmax(z / T),  d lp / d z_v = ([v = t] - q_v) / T
+// A row whose token is outside [0, V) has results 0 and its logits are not read.
+// All arithmetic is fp32; a bf16 gradient is rounded once.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "vie_api.h"
+#include "vie_block.cuh"
+#include "vie_device.cuh"
+#include "vie_row_softmax.cuh"
+
+namespace vie {
+
+// Terms of the policy loss; `old` NULL: log-probabilities alone.
+struct PolicyTerms {
+    const float *old_lp, *advantage, *ref_lp;
+    float low, high, kl;
+};
+
+struct PolicyParams {
+    const void *logits;
+    const int32_t *tokens;
+    const float *lp_in, *stats_in;  // backward alone: log-probability, m and s of each row
+    const float *grad;              // backward: weight of each row's loss, or gradient of its log-probability
+    float *loss;                    // forward of a policy loss
+    float *lp_out;                  // forward
+    float *stats_out;               // forward, or NULL
+    void *grad_logits;              // backward
+    PolicyTerms terms;
+    int64_t ld, ld_grad;
+    int V;
+    float T;
+    uint32_t *flag;
+};
+
+// The loss of one token and its derivative by lp:
+//   r = exp(lp - old), A the advantage,
+//   loss  = -min(r A, clip(r, 1 - low, 1 + high) A) + kl (exp(ref - lp) - (ref - lp) - 1)
+//   slope = -A r if r A is the smaller one, else 0, + kl (1 - exp(ref - lp))
+// No advantage, no first term, whatever the ratio; the second is +inf where one
+// of the two policies alone rules the token out.
+__device__ __forceinline__ float2 policy_terms(const PolicyTerms &a, int64_t row, float lp) {
+    const float r = expf(lp - a.old_lp[row]), A = a.advantage[row];
+    const float held = r < 1.0f - a.low ? 1.0f - a.low : r > 1.0f + a.high ? 1.0f + a.high : r;  // (NaN stays)
+    const float free_ = A == 0.0f ? 0.0f : r * A, bound = A == 0.0f ? 0.0f : held * A;
+    float loss = free_ <= bound ? -free_ : -bound, slope = free_ > bound ? 0.0f : -free_;
+    if (a.kl != 0.0f) {
+        const float x = a.ref_lp[row] - lp, e = expm1f(x);
+        loss += a.kl * (e == INFINITY ? INFINITY : e - x);
+        slope -= a.kl * e;
+    }
+    return make_float2(loss, slope);
+}
+
+// Log-probabilities and statistics (FWD) or the gradient (BWD) or both, of the
+// log-probabilities themselves or of the policy loss.
+//
+// A row is a cluster's, a slice of it a CTA's; for both, the slice is read again,
+// from L2 as long as the slices in progress fit it (vie_row_softmax.cuh).
+template <typename T, bool FWD, bool BWD>
+__global__ void __launch_bounds__(kRowThreads, 4) policy_kernel(const PolicyParams a, int log2_slices) {
+    constexpr int U = kUnroll<T, FWD, BWD>;
+    __shared__ RowSmem sm;
+    const int tid = threadIdx.x, warp = tid >> 5;
+    const int slices = 1 << log2_slices, rank = blockIdx.x & (slices - 1);
+    const int64_t row = blockIdx.x >> log2_slices;
+    if (FWD) {
+        if (tid == 0) sm.init();
+        __syncthreads();
+        cluster_arrive_relaxed();  // all CTAs of the cluster run and wait, before their memory is written
+    }
+    griddep_launch_dependents();
+    griddep_wait();  // the inputs may come from the kernel before this one
+
+    const int token = a.tokens[row];
+    const bool live = token >= 0 && token < a.V;
+    if (token >= a.V && rank == 0 && tid == 0) atomicOr(a.flag, kErrTokenIndex);
+    const Slice<T> sl(static_cast<const T *>(a.logits) + row * a.ld, a.V, log2_slices, rank);
+    const GradSlice<T> out(static_cast<T *>(a.grad_logits) + row * a.ld_grad, sl);
+    const bool policy = a.terms.old_lp != nullptr;
+    auto write_row = [&](float loss, float lp, float m, float s) {
+        if (policy) a.loss[row] = loss;
+        a.lp_out[row] = lp;
+        if (a.stats_out != nullptr) {
+            a.stats_out[2 * row] = m;
+            a.stats_out[2 * row + 1] = s;
+        }
+    };
+    if (FWD) cluster_wait();
+    if (!live) {
+        if (BWD) clear_gradient(sl, out);
+        if (FWD && rank == 0 && tid == 0) write_row(0.0f, 0.0f, 0.0f, 0.0f);
+        return;
+    }
+    const float c = exponent_factor(a.T);
+    // The thread that the token's vector is: it reads the token's logit before it
+    // writes a gradient there (which may be the same place), and afterwards
+    // replaces what the loop has written.
+    const int at = token - sl.e0, vec = at >= 0 ? at / Slice<T>::kVec : -1;
+    const bool here = vec >= 0 && vec < sl.nv &&
+                      tid == (vec < sl.lo ? 0 : vec >= sl.hi ? (sl.nv > 1 ? 1 : 0) : (vec - sl.lo) % kRowThreads);
+    float m, s, z_token = 0.0f, lp;
+    if (FWD) {
+        T raw;  // read while the slice is, and consumed before the row's slices meet
+        if (tid == 0 || here) raw = sl.z[token];
+        slice_statistics<T, U, BWD>(sl, c, sm);
+        if (tid == 0 || here) z_token = load_value(&raw);
+        __shared__ float z_shared;
+        if (tid == 0) z_shared = z_token;
+        __syncthreads();
+        if (warp == 0) send_partial(sm, slices, rank, c);
+        join_partials(a.flag, sm, slices, c, &m, &s);
+        z_token = z_shared;
+        lp = s == 0.0f ? -INFINITY : (z_token - m) / a.T - logf(s);
+    } else {
+        m = a.stats_in[2 * row];
+        s = a.stats_in[2 * row + 1];
+        if (here) z_token = load_value(sl.z + token);
+        lp = policy ? a.lp_in[row] : 0.0f;
+    }
+    float2 terms = make_float2(0.0f, 1.0f);
+    if (policy) terms = policy_terms(a.terms, row, lp);
+    if (BWD) {
+        const Exponent e{finite_max(m), c};
+        const float weight = a.grad[row];  // (one of 0 masks a row, whatever its slope)
+        const float slope = weight == 0.0f ? 0.0f : weight * terms.y / a.T, inv = s == 0.0f ? 0.0f : 1.0f / s;
+        if (slope == 0.0f) clear_gradient(sl, out);
+        else store_softmax<T, U>(sl, out, e, -slope * inv);
+        if (here && slope != 0.0f) store_value(out.g + token, slope * (1.0f - e(z_token) * inv));
+    }
+    if (FWD && rank == 0 && tid == 0) write_row(terms.x, lp, m, s);
+}
+
+template <typename T, bool FWD, bool BWD>
+static cudaError_t start_policy(const PolicyParams &p, int64_t n, int slices, cudaStream_t s) {
+    auto kernel = policy_kernel<T, FWD, BWD>;
+    if (FWD && slices > kSlices) {
+        static PerDevice prepared;
+        const cudaError_t e =
+            prepared.once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); });
+        if (e != cudaSuccess) return e;
+    }
+    RowLaunch l(n * slices, FWD ? slices : 0, 0, s);
+    return cudaLaunchKernelEx(&l.cfg, kernel, p, log2_of(slices));
+}
+
+template <bool FWD, bool BWD>
+static vie_status launch_policy(const char *fn, PolicyParams &p, vie_dtype dtype, int64_t n, vie_stream stream) {
+    if (n == 0) return VIE_OK;
+    cudaError_t e = device_flag_word(&p.flag);
+    if (e != cudaSuccess) return fail_cuda(e, fn);
+    const int slices = slices_of(FWD, BWD, static_cast<int64_t>(p.V) * dtype_size(dtype), n);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    e = dtype == VIE_DTYPE_BF16 ? start_policy<__nv_bfloat16, FWD, BWD>(p, n, slices, s)
+                                : start_policy<float, FWD, BWD>(p, n, slices, s);
+    return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
+}
+
+static vie_status check_rows(const char *fn, const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                             const int32_t *tokens, float T) {
+    if (n < 0 || n > VIE_MANY_MAX)
+        return fail(VIE_ERR_INVALID_ARG, "%s: n=%lld outside [0, %d]", fn, static_cast<long long>(n), VIE_MANY_MAX);
+    if (V < 1 || V > VIE_DISTILL_V_MAX)
+        return fail(VIE_ERR_INVALID_ARG, "%s: V=%lld outside [1, %d]", fn, static_cast<long long>(V), VIE_DISTILL_V_MAX);
+    if (!(T > 0.0f) || std::isinf(T))
+        return fail(VIE_ERR_INVALID_ARG, "%s: temperature=%g must be positive and finite", fn, static_cast<double>(T));
+    if (n > 0 && tokens == nullptr) return fail(VIE_ERR_INVALID_ARG, "%s: NULL buffer", fn);
+    if (!aligned_to(tokens, 4)) return fail(VIE_ERR_INVALID_ARG, "%s: buffers must be 4-byte aligned", fn);
+    return check_matrix(fn, "logits", logits, dtype, n, V, ld);
+}
+
+static vie_status check_floats(const char *fn, int64_t n, const float *p, bool may_be_null = false) {
+    if (p == nullptr && n > 0 && !may_be_null) return fail(VIE_ERR_INVALID_ARG, "%s: NULL buffer", fn);
+    if (!aligned_to(p, 4)) return fail(VIE_ERR_INVALID_ARG, "%s: buffers must be 4-byte aligned", fn);
+    return VIE_OK;
+}
+
+static vie_status check_terms(const char *fn, int64_t n, const PolicyTerms &t) {
+    vie_status st = check_floats(fn, n, t.old_lp);
+    if (st == VIE_OK) st = check_floats(fn, n, t.advantage);
+    if (st == VIE_OK) st = check_floats(fn, n, t.ref_lp, true);
+    if (st != VIE_OK) return st;
+    if (!(t.low >= 0.0f && t.low <= 1.0f) || !(t.high >= 0.0f) || std::isinf(t.high))
+        return fail(VIE_ERR_INVALID_ARG, "%s: clip_low=%g outside [0, 1] or clip_high=%g not finite or negative", fn,
+                    static_cast<double>(t.low), static_cast<double>(t.high));
+    if (!(t.kl >= 0.0f) || std::isinf(t.kl))
+        return fail(VIE_ERR_INVALID_ARG, "%s: kl_coef=%g must be finite and not negative", fn, static_cast<double>(t.kl));
+    if (t.kl != 0.0f && t.ref_lp == nullptr && n > 0)
+        return fail(VIE_ERR_INVALID_ARG, "%s: kl_coef=%g needs ref_logprob", fn, static_cast<double>(t.kl));
+    return VIE_OK;
+}
+
+static PolicyParams rows_of(const void *logits, int64_t V, int64_t ld, const int32_t *tokens, float T) {
+    PolicyParams p = {};
+    p.logits = logits, p.tokens = tokens, p.ld = ld, p.V = static_cast<int>(V), p.T = T;
+    return p;
+}
+
+// ---- preference loss ---------------------------------------------------------
+//
+// Sequence j holds the tokens offsets[j] to offsets[j + 1] - 1; D_j is its sum of
+// lp - ref.  Pair p is sequence 2p, the chosen one, and 2p + 1:
+//   h    = beta (D_2p - D_2p+1)
+//   loss = (1 - e) softplus(-h) + e softplus(h),  e the label smoothing
+//   d loss / d lp = beta (e - sigmoid(-h)) for chosen tokens, the negative for
+//                   rejected ones, 0 for tokens of no sequence.
+
+struct PreferenceParams {
+    const float *lp, *ref;     // forward; ref may be NULL
+    const int32_t *offsets;
+    const float *margin_in;    // backward alone
+    const float *grad_loss;    // backward
+    float *loss, *margin_out;  // forward
+    float *grad;               // backward
+    int64_t n;
+    int pairs;
+    float beta, smoothing;
+    uint32_t *flag;
+};
+
+constexpr int kPairThreads = 256;
+
+// One CTA per pair.
+template <bool FWD, bool BWD>
+__global__ void __launch_bounds__(kPairThreads) preference_kernel(const PreferenceParams a) {
+    constexpr int NT = kPairThreads;
+    __shared__ float4 sums[NT / 32];
+    const int tid = threadIdx.x, p = blockIdx.x;
+    griddep_launch_dependents();
+    griddep_wait();
+    int o[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) o[i] = a.offsets[2 * p + i];
+    const int n = static_cast<int>(a.n);
+    if (tid == 0 && (o[0] < 0 || o[1] < o[0] || o[2] < o[1] || o[2] > n)) atomicOr(a.flag, kErrOffsets);
+    o[0] = min(max(o[0], 0), n);
+    o[1] = min(max(o[1], o[0]), n);
+    o[2] = min(max(o[2], o[1]), n);
+    float h;
+    if (FWD) {
+        float4 d = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int i = o[0] + tid; i < o[1]; i += NT) d.x += a.lp[i] - (a.ref != nullptr ? a.ref[i] : 0.0f);
+        for (int i = o[1] + tid; i < o[2]; i += NT) d.y += a.lp[i] - (a.ref != nullptr ? a.ref[i] : 0.0f);
+        d = block_sum<NT>(d, sums);
+        h = a.beta * (d.x - d.y);
+    } else {
+        h = a.margin_in[p];
+    }
+    if (FWD && tid == 0) {
+        const float both = log1pf(expf(-fabsf(h)));  // softplus(x) = both + max(x, 0)
+        float loss = 0.0f;  // (h may be infinite: no product of it with 0)
+        if (a.smoothing != 1.0f) loss += (1.0f - a.smoothing) * (h < 0.0f ? both - h : both);
+        if (a.smoothing != 0.0f) loss += a.smoothing * (h > 0.0f ? both + h : both);
+        a.loss[p] = loss;
+        a.margin_out[p] = h;
+    }
+    if (BWD) {
+        const float slope = a.beta * a.grad_loss[p] * (a.smoothing - 1.0f / (1.0f + expf(h)));
+        for (int i = o[0] + tid; i < o[2]; i += NT) a.grad[i] = i < o[1] ? slope : -slope;
+        // tokens of no sequence, shared among all CTAs
+        const int first = min(max(a.offsets[0], 0), n), last = min(max(a.offsets[2 * a.pairs], 0), n);
+        for (int64_t i = static_cast<int64_t>(p) * NT + tid; i < first; i += static_cast<int64_t>(a.pairs) * NT) a.grad[i] = 0.0f;
+        for (int64_t i = last + static_cast<int64_t>(p) * NT + tid; i < n; i += static_cast<int64_t>(a.pairs) * NT) a.grad[i] = 0.0f;
+    }
+}
+
+template <bool FWD, bool BWD>
+static vie_status launch_preference(const char *fn, PreferenceParams &p, vie_stream stream) {
+    cudaError_t e = device_flag_word(&p.flag);
+    if (e != cudaSuccess) return fail_cuda(e, fn);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (p.pairs == 0) {
+        if (BWD && p.n > 0) e = cudaMemsetAsync(p.grad, 0, sizeof(float) * static_cast<size_t>(p.n), s);
+        return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    cfg.gridDim = dim3(static_cast<unsigned>(p.pairs));
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.stream = s;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, preference_kernel<FWD, BWD>, p);
+    return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
+}
+
+static vie_status check_pairs(const char *fn, int64_t n, const int32_t *offsets, int64_t pairs, float beta,
+                              float smoothing) {
+    if (n < 0 || n > VIE_PREFERENCE_N_MAX)
+        return fail(VIE_ERR_INVALID_ARG, "%s: n=%lld outside [0, %d]", fn, static_cast<long long>(n),
+                    VIE_PREFERENCE_N_MAX);
+    if (pairs < 0 || pairs > VIE_MANY_MAX)
+        return fail(VIE_ERR_INVALID_ARG, "%s: pairs=%lld outside [0, %d]", fn, static_cast<long long>(pairs),
+                    VIE_MANY_MAX);
+    if (!std::isfinite(beta)) return fail(VIE_ERR_INVALID_ARG, "%s: beta=%g must be finite", fn, static_cast<double>(beta));
+    if (!(smoothing >= 0.0f && smoothing <= 1.0f))
+        return fail(VIE_ERR_INVALID_ARG, "%s: label_smoothing=%g outside [0, 1]", fn, static_cast<double>(smoothing));
+    if (pairs > 0 && offsets == nullptr) return fail(VIE_ERR_INVALID_ARG, "%s: NULL buffer", fn);
+    if (!aligned_to(offsets, 4)) return fail(VIE_ERR_INVALID_ARG, "%s: buffers must be 4-byte aligned", fn);
+    return VIE_OK;
+}
+
+static PreferenceParams pairs_of(int64_t n, const int32_t *offsets, int64_t pairs, float beta, float smoothing) {
+    PreferenceParams p = {};
+    p.n = n, p.offsets = offsets, p.pairs = static_cast<int>(pairs), p.beta = beta, p.smoothing = smoothing;
+    return p;
+}
+
+}  // namespace vie
+
+using namespace vie;
+
+extern "C" {
+
+vie_status vie_token_logprobs(const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                              const int32_t *tokens, float temperature, float *out_logprob, float *out_stats,
+                              vie_stream stream) {
+    const char *fn = "vie_token_logprobs";
+    vie_status st = check_rows(fn, logits, dtype, n, V, ld, tokens, temperature);
+    if (st == VIE_OK) st = check_floats(fn, n, out_logprob);
+    if (st == VIE_OK) st = check_floats(fn, n, out_stats, true);
+    if (st != VIE_OK) return st;
+    PolicyParams p = rows_of(logits, V, ld, tokens, temperature);
+    p.lp_out = out_logprob, p.stats_out = out_stats;
+    return launch_policy<true, false>(fn, p, dtype, n, stream);
+}
+
+vie_status vie_token_logprobs_grad(const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                                   const int32_t *tokens, float temperature, const float *stats,
+                                   const float *grad_logprob, void *out_grad, int64_t ld_grad, vie_stream stream) {
+    const char *fn = "vie_token_logprobs_grad";
+    vie_status st = check_rows(fn, logits, dtype, n, V, ld, tokens, temperature);
+    if (st == VIE_OK) st = check_floats(fn, n, stats);
+    if (st == VIE_OK) st = check_floats(fn, n, grad_logprob);
+    if (st == VIE_OK) st = check_matrix(fn, "out_grad", out_grad, dtype, n, V, ld_grad);
+    if (st != VIE_OK) return st;
+    PolicyParams p = rows_of(logits, V, ld, tokens, temperature);
+    p.stats_in = stats, p.grad = grad_logprob, p.grad_logits = out_grad, p.ld_grad = ld_grad;
+    return launch_policy<false, true>(fn, p, dtype, n, stream);
+}
+
+vie_status vie_policy_loss(const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                           const int32_t *tokens, float temperature, const float *old_logprob, const float *advantage,
+                           const float *ref_logprob, float clip_low, float clip_high, float kl_coef, float *out_loss,
+                           float *out_logprob, float *out_stats, vie_stream stream) {
+    const char *fn = "vie_policy_loss";
+    PolicyParams p = rows_of(logits, V, ld, tokens, temperature);
+    p.terms = {old_logprob, advantage, ref_logprob, clip_low, clip_high, kl_coef};
+    vie_status st = check_rows(fn, logits, dtype, n, V, ld, tokens, temperature);
+    if (st == VIE_OK) st = check_terms(fn, n, p.terms);
+    if (st == VIE_OK) st = check_floats(fn, n, out_loss);
+    if (st == VIE_OK) st = check_floats(fn, n, out_logprob);
+    if (st == VIE_OK) st = check_floats(fn, n, out_stats, true);
+    if (st != VIE_OK) return st;
+    p.loss = out_loss, p.lp_out = out_logprob, p.stats_out = out_stats;
+    return launch_policy<true, false>(fn, p, dtype, n, stream);
+}
+
+vie_status vie_policy_loss_grad(const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                                const int32_t *tokens, float temperature, const float *old_logprob,
+                                const float *advantage, const float *ref_logprob, float clip_low, float clip_high,
+                                float kl_coef, const float *logprob, const float *stats, const float *grad_loss,
+                                void *out_grad, int64_t ld_grad, vie_stream stream) {
+    const char *fn = "vie_policy_loss_grad";
+    PolicyParams p = rows_of(logits, V, ld, tokens, temperature);
+    p.terms = {old_logprob, advantage, ref_logprob, clip_low, clip_high, kl_coef};
+    vie_status st = check_rows(fn, logits, dtype, n, V, ld, tokens, temperature);
+    if (st == VIE_OK) st = check_terms(fn, n, p.terms);
+    if (st == VIE_OK) st = check_floats(fn, n, logprob);
+    if (st == VIE_OK) st = check_floats(fn, n, stats);
+    if (st == VIE_OK) st = check_floats(fn, n, grad_loss);
+    if (st == VIE_OK) st = check_matrix(fn, "out_grad", out_grad, dtype, n, V, ld_grad);
+    if (st != VIE_OK) return st;
+    p.lp_in = logprob, p.stats_in = stats, p.grad = grad_loss, p.grad_logits = out_grad, p.ld_grad = ld_grad;
+    return launch_policy<false, true>(fn, p, dtype, n, stream);
+}
+
+vie_status vie_policy_loss_step(const void *logits, vie_dtype dtype, int64_t n, int64_t V, int64_t ld,
+                                const int32_t *tokens, float temperature, const float *old_logprob,
+                                const float *advantage, const float *ref_logprob, float clip_low, float clip_high,
+                                float kl_coef, const float *grad_loss, float *out_loss, float *out_logprob,
+                                float *out_stats, void *out_grad, int64_t ld_grad, vie_stream stream) {
+    const char *fn = "vie_policy_loss_step";
+    PolicyParams p = rows_of(logits, V, ld, tokens, temperature);
+    p.terms = {old_logprob, advantage, ref_logprob, clip_low, clip_high, kl_coef};
+    vie_status st = check_rows(fn, logits, dtype, n, V, ld, tokens, temperature);
+    if (st == VIE_OK) st = check_terms(fn, n, p.terms);
+    if (st == VIE_OK) st = check_floats(fn, n, grad_loss);
+    if (st == VIE_OK) st = check_floats(fn, n, out_loss);
+    if (st == VIE_OK) st = check_floats(fn, n, out_logprob);
+    if (st == VIE_OK) st = check_floats(fn, n, out_stats, true);
+    if (st == VIE_OK) st = check_matrix(fn, "out_grad", out_grad, dtype, n, V, ld_grad);
+    if (st != VIE_OK) return st;
+    p.grad = grad_loss, p.loss = out_loss, p.lp_out = out_logprob, p.stats_out = out_stats;
+    p.grad_logits = out_grad, p.ld_grad = ld_grad;
+    return launch_policy<true, true>(fn, p, dtype, n, stream);
+}
+
+vie_status vie_preference_loss(const float *logprob, const float *ref_logprob, int64_t n, const int32_t *offsets,
+                               int64_t pairs, float beta, float label_smoothing, float *out_loss, float *out_margin,
+                               vie_stream stream) {
+    const char *fn = "vie_preference_loss";
+    vie_status st = check_pairs(fn, n, offsets, pairs, beta, label_smoothing);
+    if (st == VIE_OK) st = check_floats(fn, n, logprob);
+    if (st == VIE_OK) st = check_floats(fn, n, ref_logprob, true);
+    if (st == VIE_OK) st = check_floats(fn, pairs, out_loss);
+    if (st == VIE_OK) st = check_floats(fn, pairs, out_margin);
+    if (st != VIE_OK) return st;
+    PreferenceParams p = pairs_of(n, offsets, pairs, beta, label_smoothing);
+    p.lp = logprob, p.ref = ref_logprob, p.loss = out_loss, p.margin_out = out_margin;
+    return launch_preference<true, false>(fn, p, stream);
+}
+
+vie_status vie_preference_loss_grad(const float *margin, int64_t n, const int32_t *offsets, int64_t pairs, float beta,
+                                    float label_smoothing, const float *grad_loss, float *out_grad,
+                                    vie_stream stream) {
+    const char *fn = "vie_preference_loss_grad";
+    vie_status st = check_pairs(fn, n, offsets, pairs, beta, label_smoothing);
+    if (st == VIE_OK) st = check_floats(fn, pairs, margin);
+    if (st == VIE_OK) st = check_floats(fn, pairs, grad_loss);
+    if (st == VIE_OK) st = check_floats(fn, n, out_grad);
+    if (st != VIE_OK) return st;
+    PreferenceParams p = pairs_of(n, offsets, pairs, beta, label_smoothing);
+    p.margin_in = margin, p.grad_loss = grad_loss, p.grad = out_grad;
+    return launch_preference<false, true>(fn, p, stream);
+}
+
+vie_status vie_preference_loss_step(const float *logprob, const float *ref_logprob, int64_t n, const int32_t *offsets,
+                                    int64_t pairs, float beta, float label_smoothing, const float *grad_loss,
+                                    float *out_loss, float *out_margin, float *out_grad, vie_stream stream) {
+    const char *fn = "vie_preference_loss_step";
+    vie_status st = check_pairs(fn, n, offsets, pairs, beta, label_smoothing);
+    if (st == VIE_OK) st = check_floats(fn, n, logprob);
+    if (st == VIE_OK) st = check_floats(fn, n, ref_logprob, true);
+    if (st == VIE_OK) st = check_floats(fn, pairs, grad_loss);
+    if (st == VIE_OK) st = check_floats(fn, pairs, out_loss);
+    if (st == VIE_OK) st = check_floats(fn, pairs, out_margin);
+    if (st == VIE_OK) st = check_floats(fn, n, out_grad);
+    if (st != VIE_OK) return st;
+    PreferenceParams p = pairs_of(n, offsets, pairs, beta, label_smoothing);
+    p.lp = logprob, p.ref = ref_logprob, p.grad_loss = grad_loss;
+    p.loss = out_loss, p.margin_out = out_margin, p.grad = out_grad;
+    return launch_preference<true, true>(fn, p, stream);
+}
+
+}  // extern "C"

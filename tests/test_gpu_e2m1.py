@@ -1,0 +1,260 @@
+"""GPU parity of 4-bit rows (e2m1_quantize, e2m1_dequantize, e2m1_logits) against
+their definitions in 64 bits (tests/policy_ref.py).  Quantisation and its values
+are exact; a logit is a sum of exact products in fp32, at most one rounding per
+product, and is rounded once more to its type."""
+import math
+
+import pytest
+import torch
+
+import policy_ref as ref
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _rows(n, d, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(n, d, generator=g) * torch.exp(2.0 * torch.randn(n, 1, generator=g))
+    x[torch.rand(n, d, generator=g) < 0.05] = 0.0
+    return x.to(DT[dtype])
+
+
+def _check_rows(vie, x, xc=None, q=None):
+    n, d = x.shape
+    code, byte, s, values = ref.quantize(x.cpu())
+    values_out = torch.empty((n, d), device="cuda")
+    q = vie.e2m1_quantize(x.cuda() if xc is None else xc, out=q, out_values=values_out)
+    codes, scales, row = ref.unpack(q)
+    good = torch.isfinite(s)
+    got = ref.VALUES[codes.long()]  # (a zero may have a sign)
+    assert torch.equal(got[:, :d][good], ref.VALUES[code][good])
+    assert not codes[:, d:].any() and not codes[~good].any()
+    blocks = byte.shape[1]
+    assert torch.equal(scales[:n, :blocks][good], byte[good])
+    assert not scales[n:].any() and not scales[:, blocks:].any() and not scales[:n][~good].any()
+    assert torch.equal(torch.isnan(row), ~good) and torch.equal(row[good].double(), s[good])
+    assert torch.equal(values_out.double().cpu().nan_to_num(9.0), values.float().double().nan_to_num(9.0))
+    for dt in (torch.float32, torch.bfloat16):
+        got = vie.e2m1_dequantize(q, out_dtype=dt).cpu().nan_to_num(9.0)
+        assert torch.equal(got, values.to(dt).nan_to_num(9.0))
+    return q, values
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,d", [(1, 1), (1, 16), (3, 17), (2, 31), (5, 64), (127, 33), (128, 65), (129, 100),
+                                 (300, 640), (33, 1152), (260, 257), (4, 5000), (9, 16384), (1000, 48)])
+def test_sizes(vie, dtype, n, d):
+    _check_rows(vie, _rows(n, d, dtype, seed=n + d))
+
+
+def test_ties_and_borders(vie):
+    """Values on and beside the midpoints of codes and of scales, in blocks whose scale is known."""
+    g = torch.Generator().manual_seed(3)
+    mids = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 5.9, 0.5, 3.0])
+    rows = []
+    for sigma in (1.0, 1.125, 1.25, 1.375, 1.5, 1.625, 1.75, 1.875, 0.0625, 448.0, 13.0):
+        v = mids[torch.randint(0, len(mids), (4, 64), generator=g)] * sigma
+        v = v * torch.where(torch.rand(4, 64, generator=g) < 0.5, -1.0, 1.0)
+        v[:, ::16] = 6.0 * sigma
+        up, down = torch.nextafter(v, v * 2), torch.nextafter(v, v * 0)
+        pick = torch.randint(0, 3, v.shape, generator=g)
+        v = torch.where(pick == 0, v, torch.where(pick == 1, up, down))
+        v[:, ::16] = 6.0 * sigma
+        v[:, 48] = 2688.0  # the row's power of two is 1
+        rows.append(v)
+    x = torch.cat(rows)
+    _check_rows(vie, x)
+    _check_rows(vie, x.bfloat16())
+    # largest magnitudes around the midpoints of scales, and around 2688 powers of two
+    top = torch.tensor([6.375, 6.125, 7.125, 11.625, 2688.0, 2687.9998, 2688.0002, 1344.0001, 1344.0, 5376.0])
+    x = torch.zeros(len(top) * 3, 48)
+    for i, t in enumerate(top):
+        for j, v in enumerate((t, torch.nextafter(t, t * 2), torch.nextafter(t, t * 0))):
+            x[3 * i + j, 5], x[3 * i + j, 20] = -v, 2000.0 if i < 4 else 1.0
+            x[3 * i + j, 21] = v / 3
+    _check_rows(vie, x)
+
+
+def test_ranges(vie):
+    """Rows from subnormal numbers to the largest ones, rows of zeros, blocks that vanish beside others."""
+    x = _rows(60, 96, "f32", seed=5)
+    x = x / x.abs().amax(1, keepdim=True) * (2.0 ** torch.linspace(-149, 127.9, 60).double()[:, None]).float()
+    x[7] = 0.0
+    x[8] = -0.0
+    x[9, :90] = 0.0
+    _check_rows(vie, x)
+    y = _rows(40, 64, "f32", seed=7)
+    y[:, 16:32] *= 2.0 ** -torch.arange(40.0)[:, None]
+    y[:, 40] = 2.0 ** torch.arange(40.0) * 10
+    _check_rows(vie, y)
+    x = torch.full((3, 20), torch.finfo(torch.float32).max)
+    _check_rows(vie, x)
+    _check_rows(vie, torch.full((3, 20), torch.finfo(torch.bfloat16).max, dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_that_are_not_finite(vie, dtype):
+    x = _rows(6, 100, dtype, seed=9)
+    x[1, 99], x[3, 0], x[4, 50] = float("nan"), math.inf, -math.inf
+    q, values = _check_rows(vie, x)
+    assert torch.isnan(values[[1, 3, 4]]).all() and torch.isfinite(values[[0, 2, 5]]).all()
+    w = vie.e2m1_quantize(_rows(70, 100, dtype, seed=10).cuda())
+    out = vie.e2m1_logits(q, w)
+    assert torch.isnan(out[[1, 3, 4]]).all() and torch.isfinite(out[[0, 2, 5]]).all()
+    out = vie.e2m1_logits(w, q)
+    assert torch.isnan(out[:, [1, 3, 4]]).all() and torch.isfinite(out[:, [0, 2, 5]]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strides_places_and_values_in_place(vie, dtype):
+    n, d = 37, 99
+    x = _rows(n, d, dtype, seed=11)
+    for off, ld in ((0, 104), (1, 99), (3, 101), (8, 128)):
+        big = torch.full((off + n * ld,), float("nan"), dtype=DT[dtype], device="cuda")
+        xc = big[off:].view(n, ld)[:, :d]
+        xc.copy_(x)
+        _check_rows(vie, x, xc=xc)
+        out = torch.full((n * ld + 16,), 7.0, dtype=DT[dtype], device="cuda")
+        view = out[off:off + n * ld].view(n, ld)[:, :d]
+        vie.e2m1_quantize(xc, out_values=view)
+        want = ref.quantize(x)[3].to(DT[dtype])
+        assert torch.equal(view.cpu(), want)
+        view.fill_(7.0)
+        assert (out == 7.0).all()
+    own = x.cuda().clone()
+    before = own._version
+    vie.e2m1_quantize(own, out_values=own)
+    assert torch.equal(own.cpu(), ref.quantize(x)[3].to(DT[dtype])) and own._version > before
+    _check_rows(vie, x, xc=x.t().contiguous().cuda().t())
+    # codes and scales that were something else before
+    q = vie.E2m1.empty(n, d)
+    q.codes.fill_(255)
+    q.scales.fill_(255)
+    _check_rows(vie, x, q=q)
+
+
+def _whole(n, d, seed):
+    """Rows whose codes are their values times a power of two, each block's another:
+    all products and sums are whole numbers below 2^24."""
+    g = torch.Generator().manual_seed(seed)
+    v = torch.tensor([0.0, 1.0, 2.0, 3.0, 4.0, 6.0, -1.0, -2.0, -3.0, -4.0, -6.0])
+    x = v[torch.randint(0, len(v), (n, d), generator=g)]
+    blocks = (d + 15) // 16
+    x[:, ::16] = 6.0
+    power = 2.0 ** torch.randint(0, 2, (n, blocks), generator=g).float()
+    return x * power.repeat_interleave(16, 1)[:, :d] * 2.0 ** torch.randint(-9, 9, (n, 1), generator=g).float()
+
+
+SHAPES = [(1, 1, 1), (3, 7, 5), (16, 128, 64), (17, 129, 65), (33, 300, 100), (64, 1000, 640), (65, 515, 1152),
+          (8, 4096, 128), (129, 2048, 257), (257, 4099, 300), (5, 20011, 96), (300, 384, 4096), (2, 257, 16384),
+          (100, 40000, 192), (1, 30000, 1000), (513, 1024, 512), (1030, 3001, 64)]
+
+
+@pytest.mark.parametrize("n,V,d", SHAPES)
+def test_logits_of_whole_numbers_are_exact(vie, n, V, d):
+    x, w = _whole(n, d, seed=n), _whole(V, d, seed=V + 1)
+    want = x.cuda().double() @ w.cuda().double().t()
+    wq, xq = vie.e2m1_quantize(w.cuda()), vie.e2m1_quantize(x.cuda())
+    assert torch.equal(vie.e2m1_dequantize(wq).cpu(), w) and torch.equal(vie.e2m1_dequantize(xq).cpu(), x)
+    assert torch.equal(vie.e2m1_logits(xq, wq).double(), want)
+    assert torch.equal(vie.e2m1_logits(x.cuda(), wq, out_dtype=torch.bfloat16), want.float().bfloat16())
+    assert vie.vie_device_status() == vie.VIE_OK
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V,d", SHAPES[:14])
+def test_logits_of_any_rows(vie, dtype, n, V, d):
+    x, w = _rows(n, d, dtype, seed=n + d), _rows(V, d, "bf16", seed=V)
+    wq = vie.e2m1_quantize(w.cuda())
+    room = vie.E2m1.empty(n, d)
+    got = vie.e2m1_logits(x.cuda(), wq, x_quantized=room)
+    assert torch.equal(got, vie.e2m1_logits(room, wq))
+    xv, wv = vie.e2m1_dequantize(room).double(), vie.e2m1_dequantize(wq).double()
+    want, mass = xv @ wv.t(), xv.abs() @ wv.abs().t()
+    tol = (d + 2) * ref.U * mass
+    assert ((got.double() - want).abs() <= tol).all()
+    got = vie.e2m1_logits(x.cuda(), wq, out_dtype=torch.bfloat16)
+    assert ((got.double() - want).abs() <= tol + (ref.HALF[torch.bfloat16] + ref.U) * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_logits_into_rows_with_a_pitch(vie, dtype):
+    n, V, d = 19, 333, 80
+    x, w = _whole(n, d, seed=1).cuda(), _whole(V, d, seed=2).cuda()
+    wq = vie.e2m1_quantize(w)
+    want = vie.e2m1_logits(x, wq, out_dtype=DT[dtype])
+    for off, ld in ((0, 333), (1, 336), (3, 341), (8, 512)):
+        buf = torch.full((off + n * ld + 40,), 7.0, dtype=DT[dtype], device="cuda")
+        view = buf[off:off + n * ld].view(n, ld)[:, :V]
+        got = vie.e2m1_logits(x, wq, out=view)
+        assert got.data_ptr() == view.data_ptr() and torch.equal(got, want)
+        view.fill_(7.0)
+        assert (buf == 7.0).all()
+
+
+def test_the_same_bits_again_on_streams_and_in_a_graph(vie):
+    n, V, d = 40, 30011, 640
+    x, w = _rows(n, d, "f32", seed=21).cuda(), _rows(V, d, "bf16", seed=22).cuda()
+    wq = vie.e2m1_quantize(w)
+    want = vie.e2m1_logits(x, wq)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(3):
+        for s in streams:  # two calls at once
+            got.append(vie.e2m1_logits(x, wq, stream=s))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want) for y in got)
+    out, room = torch.empty_like(want), vie.E2m1.empty(n, d)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        vie.e2m1_logits(x, wq, out=out, x_quantized=room)
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
+def test_rows_beyond_32_bits(vie):
+    """Codes of more than 2^31 values, and logits of more than 2^31 values."""
+    d = 16384
+    n = 2 ** 31 // d + 130
+    x = torch.zeros((n, d), dtype=torch.bfloat16, device="cuda")
+    x[-3:] = _rows(3, d, "bf16", seed=31).cuda()
+    q = vie.e2m1_quantize(x)
+    want = vie.e2m1_quantize(x[-3:].clone())
+    assert torch.equal(q.codes[-3:], want.codes) and torch.equal(q.row_scales[-3:], want.row_scales)
+    assert torch.equal(vie.e2m1_dequantize(q, out_dtype=torch.bfloat16)[-3:],
+                       vie.e2m1_dequantize(want, out_dtype=torch.bfloat16))
+    y = vie.e2m1_quantize(_rows(2, d, "f32", seed=32).cuda())
+    assert torch.equal(vie.e2m1_logits(y, q)[:, -3:], vie.e2m1_logits(y, want))
+    del x, q
+    V, n = 262144, 2 ** 31 // 262144 + 3
+    w, h = vie.e2m1_quantize(_whole(V, 64, seed=33).cuda()), vie.e2m1_quantize(_whole(n, 64, seed=34).cuda())
+    out = vie.e2m1_logits(h, w, out_dtype=torch.bfloat16)
+    last = vie.e2m1_quantize(vie.e2m1_dequantize(h)[-2:])
+    assert torch.equal(out[-2:], vie.e2m1_logits(last, w, out_dtype=torch.bfloat16))
+
+
+def test_no_rows_and_refusals(vie):
+    x, w = _rows(4, 50, "f32", seed=41).cuda(), _rows(60, 50, "f32", seed=42).cuda()
+    q = vie.e2m1_quantize(x[:0])
+    assert q.shape == (0, 50) and vie.e2m1_dequantize(q).shape == (0, 50)
+    wq = vie.e2m1_quantize(w)
+    assert vie.e2m1_logits(q, wq).shape == (0, 60) and vie.e2m1_logits(x[:0], wq).shape == (0, 60)
+    for call in (lambda: vie.e2m1_quantize(x.half()), lambda: vie.e2m1_quantize(x[0]), lambda: vie.e2m1_quantize(x.cpu()),
+                 lambda: vie.e2m1_quantize(x, out=vie.E2m1.empty(5, 50)),
+                 lambda: vie.e2m1_quantize(x, out=vie.E2m1.empty(4, 51)),
+                 lambda: vie.e2m1_quantize(x, out=vie.E2m1.empty(4, 50, device="cpu")),
+                 lambda: vie.e2m1_quantize(x, out_values=x[:3]), lambda: vie.e2m1_quantize(x, out_values=x.t()),
+                 lambda: vie.e2m1_quantize(x, out_values=x.half()),
+                 lambda: vie.e2m1_logits(x[:, :49], wq), lambda: vie.e2m1_logits(x.cpu(), wq),
+                 lambda: vie.e2m1_logits(vie.e2m1_quantize(x[:, :48]), wq),
+                 lambda: vie.e2m1_logits(x, wq, x_quantized=vie.E2m1.empty(5, 50)),
+                 lambda: vie.e2m1_logits(x, wq, out=torch.empty(4, 61, device="cuda")),
+                 lambda: vie.e2m1_logits(x, wq, out=torch.empty(4, 60, device="cuda", dtype=torch.float16)),
+                 lambda: vie.e2m1_logits(x, wq, out=torch.empty(60, 4, device="cuda").t())):
+        with pytest.raises(ValueError):
+            call()
