@@ -10,6 +10,7 @@
 #include "vie_block.cuh"
 #include "vie_device.cuh"
 #include "vie_e2m1.cuh"
+#include "vie_e2m1_logits.h"
 
 namespace vie {
 
@@ -125,49 +126,6 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const E2m1Matrix q, int
         if (b * 16 + j < d) store_value(out + r * ld + b * 16 + j, v[j] * s);
 }
 
-// out[i, v] = sum over columns of x[i] w[v]: 64 x 64 results per CTA, 64 columns at
-// a time decoded to shared memory.
-template <typename T>
-__global__ void __launch_bounds__(256) e2m1_logits_kernel(const E2m1Matrix x, const E2m1Matrix w, int d, T *out,
-                                                          int64_t ld) {
-    __shared__ float xs[64][65], ws[64][65];
-    const int tid = threadIdx.x;
-    const int64_t v0 = static_cast<int64_t>(blockIdx.x) * 64, i0 = static_cast<int64_t>(blockIdx.y) * 64;
-    griddep_launch_dependents();
-    griddep_wait();
-    float acc[4][4] = {};
-    for (int c0 = 0; c0 < d; c0 += 64) {
-        const int r = tid >> 2, b = c0 / 16 + (tid & 3);
-        float v[16] = {};
-        if (i0 + r < x.n && b * 16 < d) e2m1_block(x, i0 + r, b, d, v);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) xs[r][(tid & 3) * 16 + j] = v[j];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = 0.0f;
-        if (v0 + r < w.n && b * 16 < d) e2m1_block(w, v0 + r, b, d, v);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) ws[r][(tid & 3) * 16 + j] = v[j];
-        __syncthreads();
-        for (int k = 0; k < 64; ++k) {
-            float p[4], q[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) p[j] = xs[(tid >> 4) + 16 * j][k], q[j] = ws[(tid & 15) + 16 * j][k];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(p[i], q[j], acc[i][j]);
-        }
-        __syncthreads();
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t r = i0 + (tid >> 4) + 16 * i, v = v0 + (tid & 15) + 16 * j;
-            if (r < x.n && v < w.n) store_value(out + r * ld + v, acc[i][j] * x.row_scales[r] * w.row_scales[v]);
-        }
-}
-
 template <typename... P, typename... A>
 static cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t s, A... args) {
     cudaLaunchConfig_t cfg = {};
@@ -275,18 +233,12 @@ vie_status vie_e2m1_logits(const void *x_codes, const void *x_scales, const floa
     if (st != VIE_OK || n == 0) return st;
     const E2m1Matrix x = {static_cast<const uint8_t *>(x_codes), static_cast<const uint8_t *>(x_scales), x_row_scales, n};
     const E2m1Matrix w = {static_cast<const uint8_t *>(w_codes), static_cast<const uint8_t *>(w_scales), w_row_scales, V};
-    const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e = cudaSuccess;
-    const int64_t step = 65535 * 64;  // rows of x that one grid's second dimension covers
-    for (int64_t i = 0; i < n && e == cudaSuccess; i += step) {
-        E2m1Matrix part = {x.codes + i * e2m1_pitch(d), x.scales + i / kE2m1TileRows * e2m1_tiles(d) * kE2m1TileBytes,
-                           x.row_scales + i, n - i < step ? n - i : step};
-        const dim3 grid(static_cast<unsigned>((V + 63) / 64), static_cast<unsigned>((part.n + 63) / 64));
-        e = out_dtype == VIE_DTYPE_BF16
-                ? launch(e2m1_logits_kernel<__nv_bfloat16>, grid, 256, s, part, w, d,
-                         static_cast<__nv_bfloat16 *>(out) + i * ld_out, ld_out)
-                : launch(e2m1_logits_kernel<float>, grid, 256, s, part, w, d, static_cast<float *>(out) + i * ld_out, ld_out);
-    }
+    E2m1Product p = {};
+    cudaError_t e = device_flag_word(&p.flag);
+    if (e != cudaSuccess) return fail_cuda(e, fn);
+    p.x_scales = x.scales, p.w_scales = w.scales, p.x_row_scales = x.row_scales, p.w_row_scales = w.row_scales;
+    p.out = out, p.ld = ld_out, p.n = n, p.V = V, p.d = d;
+    e = launch_e2m1_logits(p, x.codes, w.codes, out_dtype, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
 

@@ -1,0 +1,319 @@
+// vie_e2m1_logits.cu - full logits of a 4-bit head on the tensor cores.
+//
+//   out[i, v] = s_i t_v sum_b sigma_ib tau_vb sum_(j in b) x_ij w_vj
+//
+// with codes x, w (e2m1), block scales sigma, tau (e4m3, 16 columns each) and row
+// scales s, t (powers of two): block-scaled MMAs of 128 vocabulary rows by up to
+// 256 rows of x and 64 columns, scales and accumulators in TMEM.
+//
+// A persistent CTA per SM takes tiles of 128 vocabulary rows by BN rows of x.  A
+// producer thread fills a ring of stages of 256 columns each: codes by TMA boxes
+// of 128 bytes a row (columns and rows beyond the matrix read as 0), scales by bulk
+// copies of their 512-byte tiles, which lie in memory as TMEM wants them.  An
+// issuing thread copies a stage's scales to the stage's own columns of TMEM and
+// runs its MMAs; that a stage is full again says that its MMAs are over, so the
+// columns are free.  Epilogue warps scale the accumulators and write them.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+#include <cstdint>
+
+#include "vie_api.h"
+#include "vie_block.cuh"
+#include "vie_device.cuh"
+#include "vie_e2m1.cuh"
+#include "vie_e2m1_logits.h"
+#include "vie_launch.h"
+#include "vie_tcgen05.cuh"
+
+namespace vie {
+
+constexpr int kE2m1Kb = 256;                      // columns per stage: 128 bytes of codes a row
+constexpr int kE2m1KbTiles = kE2m1Kb / 64;        // scale tiles per stage, and MMAs
+constexpr int kE2m1StageScales = kE2m1KbTiles * kE2m1TileBytes;
+
+template <int BN>
+struct E2m1Shape {
+    static constexpr int kXTiles = BN > 128 ? 2 : 1;              // tiles of 128 rows of x
+    static constexpr int kStageW = kE2m1TileRows * 128, kStageX = BN * 128;
+    static constexpr int kStageBytes = kStageW + kStageX + (1 + kXTiles) * kE2m1StageScales;
+    static constexpr int kBuffers = BN > 128 ? 1 : 2;             // accumulators
+    static constexpr int kScaleCols = 4 * kE2m1KbTiles * (1 + kXTiles);  // TMEM columns of a stage's scales
+    static constexpr int kScaleBase = (kBuffers * BN + 31) / 32 * 32;
+    static constexpr int kByMemory = (232448 - 1024 - 2048) / kStageBytes, kByTmem = (512 - kScaleBase) / kScaleCols;
+    static constexpr int kStages = kByMemory < kByTmem ? kByMemory : kByTmem;
+    static constexpr int kEpilogueWarps = BN >= 128 ? 8 : 4;
+    static constexpr int kWarpCols = BN * 4 / kEpilogueWarps;     // columns that an epilogue warp writes
+    static constexpr int kThreads = 32 * (4 + kEpilogueWarps);
+    static constexpr int kSmem = 1024 + kStages * kStageBytes;  // 1024: the ring starts at a multiple of it
+    static_assert(kStages >= 2 && kStages <= 16, "ring");
+};
+
+template <int BN>
+struct E2m1Smem {
+    uint64_t full[16], empty[16], acc_full[2], acc_empty[2], final_bar;
+    uint32_t tmem_base;
+    int abort;
+    float x_scale[E2m1Shape<BN>::kEpilogueWarps][E2m1Shape<BN>::kWarpCols];  // (no barrier between warps: one may give up)
+};
+
+// Ends a wait that ran out: the flag for the host, `abort` for the other roles.
+__device__ __forceinline__ void give_up(uint32_t *flag, int *abort) {
+    atomicOr(flag, kErrWaitTimeout);
+    *static_cast<volatile int *>(abort) = 1;
+}
+
+template <int BN, typename T>
+__global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
+    e2m1_logits_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+                       const E2m1Product p, int v_tiles, int x_tiles) {
+    using Sh = E2m1Shape<BN>;
+    constexpr int S = Sh::kStages;
+    extern __shared__ unsigned char e2m1_smem[];
+    __shared__ E2m1Smem<BN> sm;
+    unsigned char *const ring =
+        reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(e2m1_smem) + 1023) & ~uintptr_t(1023));
+    unsigned char *const ring_x = ring + S * Sh::kStageW;
+    unsigned char *const ring_s = ring_x + S * Sh::kStageX;  // per stage: scales of W, then of x
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tiles64 = e2m1_tiles(p.d), n_kb = (tiles64 + kE2m1KbTiles - 1) / kE2m1KbTiles;
+    const int64_t total = static_cast<int64_t>(v_tiles) * x_tiles;
+    volatile int *const abort = &sm.abort;
+    volatile int never = 0;
+
+    if (tid == 0) {
+        tma_prefetch_map(&map_w);
+        tma_prefetch_map(&map_x);
+        for (int s = 0; s < S; ++s) {
+            mbar_init(&sm.full[s], 1);
+            mbar_init(&sm.empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&sm.acc_full[b], 1);
+            mbar_init(&sm.acc_empty[b], Sh::kEpilogueWarps);
+        }
+        mbar_init(&sm.final_bar, 1);
+        sm.abort = 0;
+        fence_mbar_init();
+    }
+    if (warp == 2) {
+        tmem_alloc(&sm.tmem_base, 512);
+        tmem_relinquish();
+        tc_fence_before_sync();
+    }
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = sm.tmem_base;
+    griddep_launch_dependents();
+    griddep_wait();  // the inputs may come from the kernels before this one
+
+    // Tiles: x fastest, so that the CTAs that share rows of W run together.
+    if (warp == 0) {
+        // ---------------- producer ----------------
+        if (lane == 0) {
+            const uint64_t once = l2_evict_first_policy(), keep = l2_evict_last_policy();
+            const uint64_t w_policy = x_tiles == 1 ? once : keep;
+            int s = 0, issued = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            for (int64_t t = blockIdx.x; ok && t < total; t += gridDim.x) {
+                const int64_t vt = t / x_tiles;
+                const int xt = static_cast<int>(t % x_tiles);
+                for (int kb = 0; kb < n_kb; ++kb) {
+                    if (issued >= S && !mbar_wait(&sm.empty[s], ph ^ 1u, abort)) {
+                        ok = false;
+                        break;
+                    }
+                    const int steps = min(kE2m1KbTiles, tiles64 - kb * kE2m1KbTiles);
+                    const uint32_t scale_bytes = static_cast<uint32_t>(steps * kE2m1TileBytes);
+                    mbar_arrive_expect_tx(&sm.full[s], Sh::kStageW + Sh::kStageX + (1 + Sh::kXTiles) * scale_bytes);
+                    tma_load_2d(ring + s * Sh::kStageW, &map_w, kb * 128, static_cast<int>(vt * kE2m1TileRows),
+                                &sm.full[s], w_policy);
+                    tma_load_2d(ring_x + s * Sh::kStageX, &map_x, kb * 128, xt * BN, &sm.full[s], keep);
+                    unsigned char *const sc = ring_s + s * (1 + Sh::kXTiles) * kE2m1StageScales;
+                    bulk_g2s(sc, p.w_scales + (vt * tiles64 + kb * kE2m1KbTiles) * kE2m1TileBytes, scale_bytes,
+                             &sm.full[s], w_policy);
+#pragma unroll
+                    for (int i = 0; i < Sh::kXTiles; ++i) {
+                        // a tile beyond the last is not stored: any scales do for it
+                        const int64_t rt = min(static_cast<int64_t>(xt) * BN / kE2m1TileRows + i,
+                                               (p.n - 1) / kE2m1TileRows);
+                        bulk_g2s(sc + (1 + i) * kE2m1StageScales,
+                                 p.x_scales + (rt * tiles64 + kb * kE2m1KbTiles) * kE2m1TileBytes, scale_bytes,
+                                 &sm.full[s], keep);
+                    }
+                    ++issued;
+                    if (++s == S) {
+                        s = 0;
+                        ph ^= 1u;
+                    }
+                }
+            }
+            if (!ok) {
+                give_up(p.flag, &sm.abort);
+                for (int i = max(0, issued - S); i < issued; ++i)  // copies in flight land before the CTA ends
+                    mbar_wait(&sm.full[i % S], (i / S) & 1, &never);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---------------- MMA issuer ----------------
+        if (lane == 0) {
+            constexpr uint32_t idesc = umma_idesc_e2m1_f32(kE2m1TileRows, BN);
+            int s = 0, ti = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            for (int64_t t = blockIdx.x; ok && t < total; t += gridDim.x, ++ti) {
+                const int b = ti % Sh::kBuffers, ub = ti / Sh::kBuffers;
+                if (ub > 0 && !mbar_wait(&sm.acc_empty[b], (ub - 1) & 1, abort)) {
+                    ok = false;
+                    break;
+                }
+                const uint32_t acc = tmem + static_cast<uint32_t>(b * BN);
+                for (int kb = 0; kb < n_kb; ++kb) {
+                    if (!mbar_wait(&sm.full[s], ph, abort)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after_sync();
+                    const int steps = min(kE2m1KbTiles, tiles64 - kb * kE2m1KbTiles);
+                    const unsigned char *const sc = ring_s + s * (1 + Sh::kXTiles) * kE2m1StageScales;
+                    const uint32_t sfa = tmem + Sh::kScaleBase + s * Sh::kScaleCols;
+                    const uint32_t sfb = sfa + 4 * kE2m1KbTiles;
+                    const uint64_t ad = umma_desc_k_sw128(ring + s * Sh::kStageW);
+                    const uint64_t bd = umma_desc_k_sw128(ring_x + s * Sh::kStageX);
+                    for (int k = 0; k < steps; ++k) {
+                        tmem_cp_32x128b(sfa + 4 * k, tmem_cp_desc(sc + k * kE2m1TileBytes));
+#pragma unroll
+                        for (int i = 0; i < Sh::kXTiles; ++i)
+                            tmem_cp_32x128b(sfb + 4 * (Sh::kXTiles * k + i),
+                                            tmem_cp_desc(sc + (1 + i) * kE2m1StageScales + k * kE2m1TileBytes));
+                    }
+                    for (int k = 0; k < steps; ++k)
+                        umma_e2m1(acc, ad + 2 * k, bd + 2 * k, idesc, sfa + 4 * k, sfb + 4 * Sh::kXTiles * k,
+                                  (kb | k) != 0 ? 1u : 0u);
+                    umma_commit(&sm.empty[s]);
+                    if (++s == S) {
+                        s = 0;
+                        ph ^= 1u;
+                    }
+                }
+                if (ok) umma_commit(&sm.acc_full[b]);
+            }
+            if (!ok) give_up(p.flag, &sm.abort);
+            umma_commit(&sm.final_bar);  // every MMA has finished before TMEM is freed
+            mbar_wait(&sm.final_bar, 0, &never);
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        // ---------------- epilogue ----------------
+        constexpr int kCols = Sh::kWarpCols, kChunk = kCols < 32 ? kCols : 32;
+        const int quarter = warp & 3, c0 = (warp - 4) / 4 * kCols;
+        float *const x_scale = sm.x_scale[warp - 4];
+        T *const out = static_cast<T *>(p.out);
+        int ti = 0, last_xt = -1;
+        for (int64_t t = blockIdx.x; t < total; t += gridDim.x, ++ti) {
+            const int b = ti % Sh::kBuffers, ub = ti / Sh::kBuffers;
+            const int64_t vt = t / x_tiles;
+            const int xt = static_cast<int>(t % x_tiles);
+            const int64_t i0 = static_cast<int64_t>(xt) * BN, v = vt * kE2m1TileRows + 32 * quarter + lane;
+            if (xt != last_xt) {
+                __syncwarp();  // the scales of the last tile have been read
+                for (int c = lane; c < kCols; c += 32) x_scale[c] = i0 + c0 + c < p.n ? p.x_row_scales[i0 + c0 + c] : 0.0f;
+                __syncwarp();
+                last_xt = xt;
+            }
+            const float tv = v < p.V ? p.w_row_scales[v] : 0.0f;
+            if (!mbar_wait(&sm.acc_full[b], ub & 1, abort)) {
+                if (lane == 0) give_up(p.flag, &sm.abort);
+                break;
+            }
+            tc_fence_after_sync();
+            const uint32_t acc = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + b * BN + c0;
+            uint32_t r[kCols];
+#pragma unroll
+            for (int c = 0; c < kCols; c += kChunk) {
+                if constexpr (kChunk == 32) tmem_ld_32x32b_x32(acc + c, reinterpret_cast<uint32_t(&)[32]>(r[c]));
+                else tmem_ld_32x32b_x16(acc + c, reinterpret_cast<uint32_t(&)[16]>(r[c]));
+            }
+            tmem_wait_ld();
+            tc_fence_before_sync();
+            if (lane == 0) mbar_arrive(&sm.acc_empty[b]);
+            const int rows = static_cast<int>(min(static_cast<int64_t>(kCols), p.n - i0 - c0));
+            if (v < p.V) {
+                T *o = out + (i0 + c0) * p.ld + v;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c, o += p.ld)
+                    if (c < rows) store_value(o, __uint_as_float(r[c]) * x_scale[c] * tv);
+            }
+        }
+    }
+    __syncthreads();
+    if (warp == 2) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// SMs of the current device.
+static cudaError_t sm_count(int *sms) {
+    static std::atomic<int> known[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 64 && (*sms = known[dev].load(std::memory_order_relaxed)) > 0) return cudaSuccess;
+    e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess && dev < 64) known[dev].store(*sms, std::memory_order_relaxed);
+    return e;
+}
+
+template <int BN, typename T>
+static cudaError_t start_e2m1_logits(const E2m1Product &p, const uint8_t *x_codes, const uint8_t *w_codes,
+                                     cudaStream_t stream) {
+    using Sh = E2m1Shape<BN>;
+    auto kernel = e2m1_logits_kernel<BN, T>;
+    static PerDevice prepared;
+    cudaError_t e = prepared.once(
+        [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem); });
+    int sms = 0;
+    if (e == cudaSuccess) e = sm_count(&sms);
+    if (e != cudaSuccess) return e;
+    const uint64_t pitch = static_cast<uint64_t>(e2m1_pitch(p.d));
+    CUtensorMap map_w, map_x;
+    if (!make_map_u8(&map_w, const_cast<uint8_t *>(w_codes), static_cast<uint64_t>(p.V), pitch, pitch, kE2m1TileRows) ||
+        !make_map_u8(&map_x, const_cast<uint8_t *>(x_codes), static_cast<uint64_t>(p.n), pitch, pitch, BN))
+        return cudaErrorInvalidValue;
+    const int v_tiles = static_cast<int>((p.V + kE2m1TileRows - 1) / kE2m1TileRows);
+    const int x_tiles = static_cast<int>((p.n + BN - 1) / BN);
+    const int64_t total = static_cast<int64_t>(v_tiles) * x_tiles;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    cfg.gridDim = dim3(static_cast<unsigned>(total < sms ? total : sms));
+    cfg.blockDim = dim3(Sh::kThreads);
+    cfg.dynamicSmemBytes = Sh::kSmem;
+    cfg.stream = stream;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, map_w, map_x, p, v_tiles, x_tiles);
+}
+
+template <typename T>
+static cudaError_t start_by_rows(const E2m1Product &p, const uint8_t *x_codes, const uint8_t *w_codes,
+                                 cudaStream_t stream) {
+    if (p.n <= 16) return start_e2m1_logits<16, T>(p, x_codes, w_codes, stream);
+    if (p.n <= 32) return start_e2m1_logits<32, T>(p, x_codes, w_codes, stream);
+    if (p.n <= 64) return start_e2m1_logits<64, T>(p, x_codes, w_codes, stream);
+    if (p.n <= 128) return start_e2m1_logits<128, T>(p, x_codes, w_codes, stream);
+    return start_e2m1_logits<256, T>(p, x_codes, w_codes, stream);
+}
+
+cudaError_t launch_e2m1_logits(const E2m1Product &p, const uint8_t *x_codes, const uint8_t *w_codes, vie_dtype dtype,
+                               cudaStream_t stream) {
+    return dtype == VIE_DTYPE_BF16 ? start_by_rows<__nv_bfloat16>(p, x_codes, w_codes, stream)
+                                   : start_by_rows<float>(p, x_codes, w_codes, stream);
+}
+
+}  // namespace vie

@@ -371,9 +371,11 @@ EncodeTiledFn encode_tiled() {
     return fn;
 }
 
+}  // namespace
+
 // 2-D uint8 tensor map [rows][cols] (cols contiguous, pitch bytes), box
 // box_rows x 128 columns, 128-byte swizzle, out-of-range elements read as 0.
-bool make_map_u8(CUtensorMap *m, void *base, uint64_t rows, uint64_t cols, uint64_t pitch,
+bool vie::make_map_u8(CUtensorMap *m, void *base, uint64_t rows, uint64_t cols, uint64_t pitch,
                  uint32_t box_rows) {
     EncodeTiledFn fn = encode_tiled();
     if (fn == nullptr) return false;
@@ -385,6 +387,8 @@ bool make_map_u8(CUtensorMap *m, void *base, uint64_t rows, uint64_t cols, uint6
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+namespace {
 
 // 2-D bf16 tensor map [rows][cols] (cols contiguous, pitch bytes), box
 // box_rows x 64 columns, 128-byte swizzle, out-of-range elements read as 0.
@@ -565,9 +569,9 @@ static vie_status create_head(const void *W_out, int64_t V, int32_t d, vie_dtype
     if (e4m3) {  // kind::f8f6f4 maps: codes [V][d_pad] and the query pieces, 128-byte rows
         const uint64_t pitch8 = static_cast<uint64_t>(hd->d_pad);
         hd->tc_ready = hd->d_pad >= 128 &&
-                       make_map_u8(&hd->mapW, hd->W, static_cast<uint64_t>(V), hd->d_pad, pitch8, vie::kTcTile);
+                       vie::make_map_u8(&hd->mapW, hd->W, static_cast<uint64_t>(V), hd->d_pad, pitch8, vie::kTcTile);
         for (int i = 0; i < 4 && hd->tc_ready; ++i)
-            hd->tc_ready = make_map_u8(&hd->mapH[i], hd->hB, vie::kTcHRows, hd->d_pad, pitch8, 16u << i);
+            hd->tc_ready = vie::make_map_u8(&hd->mapH[i], hd->hB, vie::kTcHRows, hd->d_pad, pitch8, 16u << i);
         *out = hd;
         return VIE_OK;
     }

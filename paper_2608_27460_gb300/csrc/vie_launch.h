@@ -34,6 +34,10 @@ cudaError_t launch_stream_topk_e4m3_nb8(int r, const StreamTopkParams &p, int gr
                                         uint32_t smem, cudaStream_t stream);
 
 
+// Tensor map of bytes [rows][cols] (cols contiguous, rows pitch apart) for boxes of
+// box_rows x 128 with the 128-byte swizzle; bytes out of range read as 0.
+bool make_map_u8(CUtensorMap *m, void *base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows);
+
 // ---- tensor-core head (vie_tc_topk.cu, vie_tc_many.cu) ----
 struct TcParams;
 struct MnParams;

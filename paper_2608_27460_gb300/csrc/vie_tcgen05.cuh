@@ -81,6 +81,42 @@ __device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t adesc, uint6
         : "memory");
 }
 
+// Instruction descriptor of tcgen05.mma.kind::mxf4nvf4: fp32 accumulator, e2m1 A
+// and B (format code 1 for both), both K-major, unsigned e4m3 scales (type 0) from
+// the first byte of their TMEM words (ids 0), shape M x N x 64.
+__host__ __device__ constexpr uint32_t umma_idesc_e2m1_f32(int M, int N) {
+    return (1u << 7)                                   // A: e2m1
+           | (1u << 10)                                // B: e2m1
+           | (static_cast<uint32_t>(N >> 3) << 17)     // N / 8
+           | (static_cast<uint32_t>(M >> 7) << 27);    // M / 128
+}
+
+// D[tmem] (+)= (A scaled)[smem] * (B scaled)[smem]^T on 4-bit floats, K = 64 per
+// instruction (32 bytes of each row), a scale per 16 of them: sfa holds word
+// (scales of four blocks) of row i in lane i % 32, column i / 32, sfb likewise.
+__device__ __forceinline__ void umma_e2m1(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                          uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
+            d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
+}
+
+// 32 rows of 16 bytes, consecutive in shared memory, to four columns of TMEM, the
+// same in each of the four 32-lane quarters.  In order with this thread's later MMAs.
+__device__ __forceinline__ uint64_t tmem_cp_desc(const void *smem_ptr) {
+    const uint64_t addr = smem_addr(smem_ptr);
+    uint64_t d = (addr >> 4) & 0x3FFFull;  // start address; no swizzle
+    d |= (128ull >> 4) << 32;              // stride byte offset of 8 rows
+    d |= 1ull << 46;                       // descriptor version
+    return d;
+}
+__device__ __forceinline__ void tmem_cp_32x128b(uint32_t taddr, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
 // Arrive once on `bar` when every tcgen05 operation this thread issued so
 // far has completed.
 __device__ __forceinline__ void umma_commit(uint64_t *bar) {
@@ -127,6 +163,17 @@ __device__ __forceinline__ void tmem_ld_32x32b_x16(uint32_t taddr, uint32_t (&r)
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
           "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
           "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld_32x32b_x32(uint32_t taddr, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
+        "%22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_wait_ld() {
