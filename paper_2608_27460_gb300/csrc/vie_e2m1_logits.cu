@@ -9,10 +9,15 @@
 // A persistent CTA per SM takes tiles of 128 vocabulary rows by BN rows of x.  A
 // producer thread fills a ring of stages of 256 columns each: codes by TMA boxes
 // of 128 bytes a row (columns and rows beyond the matrix read as 0), scales by bulk
-// copies of their 512-byte tiles, which lie in memory as TMEM wants them.  An
-// issuing thread copies a stage's scales to the stage's own columns of TMEM and
-// runs its MMAs; that a stage is full again says that its MMAs are over, so the
-// columns are free.  Epilogue warps scale the accumulators and write them.
+// copies of their 512-byte tiles, which lie in memory as TMEM wants them.  Four
+// warps take a stage's scales to the stage's own columns of TMEM, each to its
+// quarter of the lanes (all four hold the same); an issuing thread runs the MMAs.
+// That a stage is full again says that its MMAs are over, so its columns are free.
+// Epilogue warps scale the accumulators and write them.
+//
+// (tcgen05.cp, which takes scales to TMEM without registers, runs in order with
+// the MMAs, some 100 cycles a copy of 512 bytes: 51 us for one row of x on 262144 x
+// 1152.)
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -45,14 +50,15 @@ struct E2m1Shape {
     static constexpr int kStages = kByMemory < kByTmem ? kByMemory : kByTmem;
     static constexpr int kEpilogueWarps = BN >= 128 ? 8 : 4;
     static constexpr int kWarpCols = BN * 4 / kEpilogueWarps;     // columns that an epilogue warp writes
-    static constexpr int kThreads = 32 * (4 + kEpilogueWarps);
+    static constexpr int kScaleWarp = 4 + kEpilogueWarps;         // the first of four
+    static constexpr int kThreads = 32 * (kScaleWarp + 4);
     static constexpr int kSmem = 1024 + kStages * kStageBytes;  // 1024: the ring starts at a multiple of it
     static_assert(kStages >= 2 && kStages <= 16, "ring");
 };
 
 template <int BN>
 struct E2m1Smem {
-    uint64_t full[16], empty[16], acc_full[2], acc_empty[2], final_bar;
+    uint64_t full[16], scaled[16], empty[16], acc_full[2], acc_empty[2], final_bar;
     uint32_t tmem_base;
     int abort;
     float x_scale[E2m1Shape<BN>::kEpilogueWarps][E2m1Shape<BN>::kWarpCols];  // (no barrier between warps: one may give up)
@@ -64,7 +70,58 @@ __device__ __forceinline__ void give_up(uint32_t *flag, int *abort) {
     *static_cast<volatile int *>(abort) = 1;
 }
 
-template <int BN, typename T>
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// Where an epilogue lane writes its vocabulary row v: columns c and c + 1 of a
+// tile (rows of the output, ld apart) at a time, in ascending order; all lanes of
+// the warp call.  WORDS (bf16): lanes trade, an even lane writes its own and its
+// neighbour's value of column c in one word, the odd one those of column c + 1.  It
+// needs even V and ld and rows that start at such words, and is a parameter of the
+// kernel because a branch per store costs more than the stores (151936 x 1024 for
+// 2048 rows: 357 us; 213 value by value, 193 by words).
+template <typename T, bool WORDS>
+struct ColumnStore {
+    T *o;
+    int64_t ld;
+    int rows;  // of this lane, columns counted from its first
+    __device__ __forceinline__ ColumnStore(T *out, int64_t ld_, int64_t v, int64_t V, int rows_) : ld(ld_) {
+        const int odd = WORDS ? static_cast<int>(v & 1) : 0;  // (a tile's first row is even: the lane is odd as well)
+        o = out + odd * ld + (v - odd);
+        rows = v < V ? rows_ - odd : 0;
+    }
+    __device__ __forceinline__ void pair(int c, uint32_t both) {  // of bf16
+        if constexpr (WORDS) {
+            const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, both, 1);
+            const uint32_t w = (threadIdx.x & 1) == 0 ? __byte_perm(both, other, 0x5410) : __byte_perm(other, both, 0x7632);
+            if (c < rows) *reinterpret_cast<uint32_t *>(o) = w;
+            o += 2 * ld;
+        } else {
+            put(c, static_cast<uint16_t>(both));
+            put(c + 1, static_cast<uint16_t>(both >> 16));
+        }
+    }
+    __device__ __forceinline__ void pair(int c, float a, float b) {
+        if constexpr (sizeof(T) == 2) {
+            pair(c, pack_bf16(a, b));
+        } else {
+            put(c, a);
+            put(c + 1, b);
+        }
+    }
+
+  private:
+    template <typename V>
+    __device__ __forceinline__ void put(int c, V value) {
+        static_assert(sizeof(V) == sizeof(T), "one value");
+        if (c < rows) *reinterpret_cast<V *>(o) = value;
+        o += ld;
+    }
+};
+
+template <int BN, typename T, bool WORDS>
 __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
     e2m1_logits_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                        const E2m1Product p, int v_tiles, int x_tiles) {
@@ -87,6 +144,7 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
         tma_prefetch_map(&map_x);
         for (int s = 0; s < S; ++s) {
             mbar_init(&sm.full[s], 1);
+            mbar_init(&sm.scaled[s], 4);
             mbar_init(&sm.empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -172,24 +230,16 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
                 }
                 const uint32_t acc = tmem + static_cast<uint32_t>(b * BN);
                 for (int kb = 0; kb < n_kb; ++kb) {
-                    if (!mbar_wait(&sm.full[s], ph, abort)) {
+                    if (!mbar_wait(&sm.full[s], ph, abort) || !mbar_wait(&sm.scaled[s], ph, abort)) {
                         ok = false;
                         break;
                     }
                     tc_fence_after_sync();
                     const int steps = min(kE2m1KbTiles, tiles64 - kb * kE2m1KbTiles);
-                    const unsigned char *const sc = ring_s + s * (1 + Sh::kXTiles) * kE2m1StageScales;
                     const uint32_t sfa = tmem + Sh::kScaleBase + s * Sh::kScaleCols;
                     const uint32_t sfb = sfa + 4 * kE2m1KbTiles;
                     const uint64_t ad = umma_desc_k_sw128(ring + s * Sh::kStageW);
                     const uint64_t bd = umma_desc_k_sw128(ring_x + s * Sh::kStageX);
-                    for (int k = 0; k < steps; ++k) {
-                        tmem_cp_32x128b(sfa + 4 * k, tmem_cp_desc(sc + k * kE2m1TileBytes));
-#pragma unroll
-                        for (int i = 0; i < Sh::kXTiles; ++i)
-                            tmem_cp_32x128b(sfb + 4 * (Sh::kXTiles * k + i),
-                                            tmem_cp_desc(sc + (1 + i) * kE2m1StageScales + k * kE2m1TileBytes));
-                    }
                     for (int k = 0; k < steps; ++k)
                         umma_e2m1(acc, ad + 2 * k, bd + 2 * k, idesc, sfa + 4 * k, sfb + 4 * Sh::kXTiles * k,
                                   (kb | k) != 0 ? 1u : 0u);
@@ -206,12 +256,52 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
             mbar_wait(&sm.final_bar, 0, &never);
         }
         __syncwarp();
+    } else if (warp >= Sh::kScaleWarp) {
+        // ---------------- scales: shared memory -> TMEM ----------------
+        const uint32_t cols = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + Sh::kScaleBase;
+        int s = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+        for (int64_t t = blockIdx.x; ok && t < total; t += gridDim.x) {
+            for (int kb = 0; kb < n_kb; ++kb) {
+                if (!mbar_wait(&sm.full[s], ph, abort)) {
+                    if (lane == 0) give_up(p.flag, &sm.abort);
+                    ok = false;
+                    break;
+                }
+                // (what lies behind the matrix's last scales is not used by an MMA)
+                const uint4 *const sc =
+                    reinterpret_cast<const uint4 *>(ring_s + s * (1 + Sh::kXTiles) * kE2m1StageScales) + lane;
+                constexpr int kTile = kE2m1TileBytes / 16, kSet = kE2m1StageScales / 16;
+                const uint32_t at = cols + s * Sh::kScaleCols;
+                uint32_t r[16];
+                auto gather = [&](int j, const uint4 &w) { r[j] = w.x, r[j + 1] = w.y, r[j + 2] = w.z, r[j + 3] = w.w; };
+#pragma unroll
+                for (int k = 0; k < 4; ++k) gather(4 * k, sc[k * kTile]);
+                tmem_st_32x32b_x16(at, r);
+#pragma unroll
+                for (int h = 0; h < Sh::kXTiles; ++h) {  // x: columns of step 0 of each tile of rows, step 1, ...
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int k = (4 * h + j) / Sh::kXTiles, i = (4 * h + j) % Sh::kXTiles;
+                        gather(4 * j, sc[(1 + i) * kSet + k * kTile]);
+                    }
+                    tmem_st_32x32b_x16(at + 16 * (1 + h), r);
+                }
+                tmem_wait_st();
+                tc_fence_before_sync();
+                if (lane == 0) mbar_arrive(&sm.scaled[s]);
+                if (++s == S) {
+                    s = 0;
+                    ph ^= 1u;
+                }
+            }
+        }
     } else if (warp >= 4) {
         // ---------------- epilogue ----------------
         constexpr int kCols = Sh::kWarpCols, kChunk = kCols < 32 ? kCols : 32;
         const int quarter = warp & 3, c0 = (warp - 4) / 4 * kCols;
         float *const x_scale = sm.x_scale[warp - 4];
-        T *const out = static_cast<T *>(p.out);
         int ti = 0, last_xt = -1;
         for (int64_t t = blockIdx.x; t < total; t += gridDim.x, ++ti) {
             const int b = ti % Sh::kBuffers, ub = ti / Sh::kBuffers;
@@ -231,21 +321,52 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
             }
             tc_fence_after_sync();
             const uint32_t acc = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + b * BN + c0;
-            uint32_t r[kCols];
-#pragma unroll
-            for (int c = 0; c < kCols; c += kChunk) {
-                if constexpr (kChunk == 32) tmem_ld_32x32b_x32(acc + c, reinterpret_cast<uint32_t(&)[32]>(r[c]));
-                else tmem_ld_32x32b_x16(acc + c, reinterpret_cast<uint32_t(&)[16]>(r[c]));
-            }
-            tmem_wait_ld();
-            tc_fence_before_sync();
-            if (lane == 0) mbar_arrive(&sm.acc_empty[b]);
+            // The accumulator is handed back as soon as its last columns are in registers:
+            // 64 of fp32, or 128 rounded to bf16.
             const int rows = static_cast<int>(min(static_cast<int64_t>(kCols), p.n - i0 - c0));
-            if (v < p.V) {
-                T *o = out + (i0 + c0) * p.ld + v;
+            ColumnStore<T, WORDS> put(static_cast<T *>(p.out) + (i0 + c0) * p.ld, p.ld, v, p.V, rows);
+            auto scaled = [&](uint32_t bits, int c) { return __uint_as_float(bits) * x_scale[c] * tv; };
+            auto hand_back = [&] {
+                tc_fence_before_sync();
+                if (lane == 0) mbar_arrive(&sm.acc_empty[b]);
+            };
+            if constexpr (sizeof(T) == 2 && kCols == 128) {
+                uint32_t r[64];
 #pragma unroll
-                for (int c = 0; c < kCols; ++c, o += p.ld)
-                    if (c < rows) store_value(o, __uint_as_float(r[c]) * x_scale[c] * tv);
+                for (int c = 0; c < kCols; c += 32) {
+                    uint32_t part[32];
+                    tmem_ld_32x32b_x32(acc + c, part);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2)
+                        r[(c + j) / 2] = pack_bf16(scaled(part[j], c + j), scaled(part[j + 1], c + j + 1));
+                }
+                hand_back();
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2) put.pair(c, r[c / 2]);
+            } else {
+                constexpr int kHeld = kCols < 64 ? kCols : 64, kFirst = kCols - kHeld;
+#pragma unroll
+                for (int c = 0; c < kFirst; c += 32) {
+                    uint32_t part[32];
+                    tmem_ld_32x32b_x32(acc + c, part);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2)
+                        put.pair(c + j, scaled(part[j], c + j), scaled(part[j + 1], c + j + 1));
+                }
+                uint32_t r[kHeld];
+#pragma unroll
+                for (int c = 0; c < kHeld; c += kChunk) {
+                    const uint32_t at = acc + kFirst + c;
+                    if constexpr (kChunk == 32) tmem_ld_32x32b_x32(at, reinterpret_cast<uint32_t(&)[32]>(r[c]));
+                    else tmem_ld_32x32b_x16(at, reinterpret_cast<uint32_t(&)[16]>(r[c]));
+                }
+                tmem_wait_ld();
+                hand_back();
+#pragma unroll
+                for (int c = 0; c < kHeld; c += 2)
+                    put.pair(kFirst + c, scaled(r[c], kFirst + c), scaled(r[c + 1], kFirst + c + 1));
             }
         }
     }
@@ -268,11 +389,11 @@ static cudaError_t sm_count(int *sms) {
     return e;
 }
 
-template <int BN, typename T>
+template <int BN, typename T, bool WORDS>
 static cudaError_t start_e2m1_logits(const E2m1Product &p, const uint8_t *x_codes, const uint8_t *w_codes,
                                      cudaStream_t stream) {
     using Sh = E2m1Shape<BN>;
-    auto kernel = e2m1_logits_kernel<BN, T>;
+    auto kernel = e2m1_logits_kernel<BN, T, WORDS>;
     static PerDevice prepared;
     cudaError_t e = prepared.once(
         [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem); });
@@ -300,20 +421,22 @@ static cudaError_t start_e2m1_logits(const E2m1Product &p, const uint8_t *x_code
     return cudaLaunchKernelEx(&cfg, kernel, map_w, map_x, p, v_tiles, x_tiles);
 }
 
-template <typename T>
+template <typename T, bool WORDS>
 static cudaError_t start_by_rows(const E2m1Product &p, const uint8_t *x_codes, const uint8_t *w_codes,
                                  cudaStream_t stream) {
-    if (p.n <= 16) return start_e2m1_logits<16, T>(p, x_codes, w_codes, stream);
-    if (p.n <= 32) return start_e2m1_logits<32, T>(p, x_codes, w_codes, stream);
-    if (p.n <= 64) return start_e2m1_logits<64, T>(p, x_codes, w_codes, stream);
-    if (p.n <= 128) return start_e2m1_logits<128, T>(p, x_codes, w_codes, stream);
-    return start_e2m1_logits<256, T>(p, x_codes, w_codes, stream);
+    if (p.n <= 16) return start_e2m1_logits<16, T, WORDS>(p, x_codes, w_codes, stream);
+    if (p.n <= 32) return start_e2m1_logits<32, T, WORDS>(p, x_codes, w_codes, stream);
+    if (p.n <= 64) return start_e2m1_logits<64, T, WORDS>(p, x_codes, w_codes, stream);
+    if (p.n <= 128) return start_e2m1_logits<128, T, WORDS>(p, x_codes, w_codes, stream);
+    return start_e2m1_logits<256, T, WORDS>(p, x_codes, w_codes, stream);
 }
 
 cudaError_t launch_e2m1_logits(const E2m1Product &p, const uint8_t *x_codes, const uint8_t *w_codes, vie_dtype dtype,
                                cudaStream_t stream) {
-    return dtype == VIE_DTYPE_BF16 ? start_by_rows<__nv_bfloat16>(p, x_codes, w_codes, stream)
-                                   : start_by_rows<float>(p, x_codes, w_codes, stream);
+    if (dtype == VIE_DTYPE_F32) return start_by_rows<float, false>(p, x_codes, w_codes, stream);
+    const bool words = p.V % 2 == 0 && (p.n == 1 || p.ld % 2 == 0) && aligned_to(p.out, 4);
+    return words ? start_by_rows<__nv_bfloat16, true>(p, x_codes, w_codes, stream)
+                 : start_by_rows<__nv_bfloat16, false>(p, x_codes, w_codes, stream);
 }
 
 }  // namespace vie

@@ -104,19 +104,6 @@ __device__ __forceinline__ void umma_e2m1(uint32_t d_tmem, uint64_t adesc, uint6
         : "memory");
 }
 
-// 32 rows of 16 bytes, consecutive in shared memory, to four columns of TMEM, the
-// same in each of the four 32-lane quarters.  In order with this thread's later MMAs.
-__device__ __forceinline__ uint64_t tmem_cp_desc(const void *smem_ptr) {
-    const uint64_t addr = smem_addr(smem_ptr);
-    uint64_t d = (addr >> 4) & 0x3FFFull;  // start address; no swizzle
-    d |= (128ull >> 4) << 32;              // stride byte offset of 8 rows
-    d |= 1ull << 46;                       // descriptor version
-    return d;
-}
-__device__ __forceinline__ void tmem_cp_32x128b(uint32_t taddr, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-}
-
 // Arrive once on `bar` when every tcgen05 operation this thread issued so
 // far has completed.
 __device__ __forceinline__ void umma_commit(uint64_t *bar) {
@@ -175,6 +162,18 @@ __device__ __forceinline__ void tmem_ld_32x32b_x32(uint32_t taddr, uint32_t (&r)
           "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr));
+}
+// The same 16 columns from registers; complete after tmem_wait_st.
+__device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() {
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void tmem_wait_ld() {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
