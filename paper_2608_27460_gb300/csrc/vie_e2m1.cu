@@ -5,6 +5,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "vie_api.h"
 #include "vie_block.cuh"
@@ -24,74 +25,170 @@ struct QuantizeParams {
 };
 
 constexpr int kQuantizeThreads = 256;
+constexpr int kQuantizeWarps = kQuantizeThreads / 32;
 
-// Block b of a row, 0 beyond it.
+// Eight values of a row as they are stored, 0 beyond it.
 template <typename T>
-__device__ __forceinline__ void load_block(const T *row, int b, int d, float (&v)[16]) {
+struct Raw8;
+template <>
+struct Raw8<__nv_bfloat16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p, int left, bool vectors) {
+        if (vectors && left >= 8) {
+            const uint4 a = *reinterpret_cast<const uint4 *>(p);
+            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+            return;
+        }
+        const uint16_t *q = reinterpret_cast<const uint16_t *>(p);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = b * 16 + i < d ? load_value(row + b * 16 + i) : 0.0f;
+        for (int i = 0; i < 4; ++i)
+            w[i] = (2 * i < left ? q[2 * i] : 0u) | (2 * i + 1 < left ? static_cast<uint32_t>(q[2 * i + 1]) << 16 : 0u);
+    }
+    // The largest magnitude, as the bits of an fp32 value (NaN above infinity).
+    __device__ __forceinline__ uint32_t top() const {
+        const uint32_t m = 0x7FFF7FFFu;
+        const uint32_t t = __vmaxu2(__vmaxu2(w[0] & m, w[1] & m), __vmaxu2(w[2] & m, w[3] & m));
+        return max(t << 16, t & 0xFFFF0000u);
+    }
+    __device__ __forceinline__ float value(int i) const { return i % 2 == 0 ? bf16_lo(w[i / 2]) : bf16_hi(w[i / 2]); }
+};
+template <>
+struct Raw8<float> {
+    uint32_t w[8];
+    __device__ __forceinline__ void load(const float *p, int left, bool vectors) {
+        if (vectors && left >= 8) {
+            const uint4 a = reinterpret_cast<const uint4 *>(p)[0], b = reinterpret_cast<const uint4 *>(p)[1];
+            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = i < left ? __float_as_uint(p[i]) : 0u;
+    }
+    __device__ __forceinline__ uint32_t top() const {
+        uint32_t t = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t = max(t, w[i] & 0x7FFFFFFFu);
+        return t;
+    }
+    __device__ __forceinline__ float value(int i) const { return __uint_as_float(w[i]); }
+};
+
+// a / b rounded to nearest from r = 1 / b rounded to nearest, without over- or
+// underflow in between: one correction of a r by its remainder (Markstein,
+// "Computation of elementary functions on the IBM RISC System/6000 processor", 1990).
+__device__ __forceinline__ float quotient(float a, float b, float r) {
+    const float q = a * r;
+    return fmaf(fmaf(-q, b, a), r, q);
 }
 
-// A warp per row, a block of 16 values per lane, twice: for the row's largest
-// magnitude, and for its codes.
-template <typename T, typename TV>
+template <typename T>
+__device__ __forceinline__ void store8(T *p, const float *v, int left, bool vectors) {
+    if (vectors && left >= 8) {
+        reinterpret_cast<uint4 *>(p)[0] = Vec16<T>::pack(v);
+        if constexpr (sizeof(T) == 4) reinterpret_cast<uint4 *>(p)[1] = Vec16<T>::pack(v + 4);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left) store_value(p + i, v[i]);
+}
+
+struct None {};  // no values wanted
+
+// Rows to codes and scales, in two passes over a row: its largest magnitude, then
+// the codes (the second time from L1 or L2).  A lane takes eight values at a time,
+// two lanes a block.
+//
+// ROW_WARPS 1: a warp per row, a CTA for 32 rows of a tile, 8 at a time: the four
+// rows of each of its warps are those whose scales lie side by side, so that the
+// CTA's scales (gathered in shared memory) are written 128 bytes at a time.
+// ROW_WARPS 8: a CTA per row, for the latency of few rows.
+template <typename T, typename TV, int ROW_WARPS>
 __global__ void __launch_bounds__(kQuantizeThreads) quantize_kernel(const QuantizeParams a) {
-    const int lane = threadIdx.x & 31;
-    const int64_t r = (static_cast<int64_t>(blockIdx.x) * kQuantizeThreads + threadIdx.x) >> 5;
-    const int tiles = e2m1_tiles(a.d), code_blocks = 2 * ((a.d + 31) / 32);
+    constexpr bool kMany = ROW_WARPS == 1;
+    constexpr int kRowLanes = 32 * ROW_WARPS, kRounds = kMany ? 4 : 1;
+    extern __shared__ __align__(16) uint32_t scale_words[];  // kMany: [tiles][row % 8 of 32][row / 32]
+    __shared__ uint32_t warp_top[kQuantizeWarps];
+    const int warp = threadIdx.x >> 5, at = kMany ? threadIdx.x & 31 : threadIdx.x;
+    const int tiles = e2m1_tiles(a.d);
+    const int64_t pitch = e2m1_pitch(a.d);
+    const bool vectors = (reinterpret_cast<uintptr_t>(a.x) & 15u) == 0 && a.ld * sizeof(T) % 16 == 0;
+    constexpr bool kValues = !std::is_same<TV, None>::value;
     griddep_launch_dependents();
     griddep_wait();
-    const bool real = r < a.n;
-    const T *row = static_cast<const T *>(a.x) + r * a.ld;
-    uint32_t top = 0;
-    if (real)
-        for (int b = lane; b * 16 < a.d; b += 32) {
-            float v[16];
-            load_block(row, b, a.d, v);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    // CTA c of kMany takes rows 8 (c % 4) + 0 .. 7 of each 32 of tile c / 4
+    const int64_t first = kMany ? static_cast<int64_t>(blockIdx.x / 4) * kE2m1TileRows + 8 * (blockIdx.x % 4) + warp
+                                : static_cast<int64_t>(blockIdx.x);
+#pragma unroll 1
+    for (int round = 0; round < kRounds; ++round) {
+        const int64_t r = first + 32 * round;
+        const bool real = r < a.n;
+        const T *const row = static_cast<const T *>(a.x) + (real ? r : 0) * a.ld;
+        const int width = real ? a.d : 0;  // rows beyond the last have scales of 0 and nothing else
+        uint32_t top = 0;
+#pragma unroll 4
+        for (int j = 8 * at; j < width; j += 8 * kRowLanes) {
+            Raw8<T> raw;
+            raw.load(row + j, width - j, vectors);
+            top = max(top, raw.top());
         }
-    top = __reduce_max_sync(0xFFFFFFFFu, top);
-    const bool finite = top < 0x7F800000u;
-    const int E = e2m1_exponent(finite ? top : 0u);
-    const float scale = power_of_two(E), inv = power_of_two(-E);
-    for (int b = lane; b < 4 * tiles; b += 32) {
-        float v[16];
-        uint32_t sigma8 = 0;
-        float sigma = 0.0f;
-        uint32_t codes[2] = {0, 0};
-        const bool inside = real && b * 16 < a.d;
-        if (inside && finite) {
-            load_block(row, b, a.d, v);
-            float m = 0.0f;
+        top = __reduce_max_sync(0xFFFFFFFFu, top);
+        if (!kMany) {
+            if ((threadIdx.x & 31) == 0) warp_top[warp] = top;
+            __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                v[i] *= inv;
-                m = fmaxf(m, fabsf(v[i]));
-            }
-            sigma8 = to_e4m3(__fdiv_rn(m, 6.0f));
-            sigma = from_e4m3(sigma8);
+            for (int w = 0; w < kQuantizeWarps; ++w) top = max(top, warp_top[w]);
+        }
+        const bool finite = top < 0x7F800000u;
+        const int E = e2m1_exponent(finite ? top : 0u);
+        const float scale = power_of_two(E), inv = power_of_two(-E);
+        if (at == 0 && real) a.row_scales[r] = finite ? scale : NAN;
+        const int steps = (8 * tiles + kRowLanes - 1) / kRowLanes;  // the same for all lanes: they exchange
+#pragma unroll 2
+        for (int s = 0; s < steps; ++s) {
+            const int vec = s * kRowLanes + at, j = 8 * vec, left = width - j;
+            Raw8<T> raw = {};
+            if (left > 0) raw.load(row + j, left, vectors);
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = finite ? raw.value(i) * inv : 0.0f;
+            uint32_t block_top = finite ? raw.top() : 0u;
+            block_top = max(block_top, __shfl_xor_sync(0xFFFFFFFFu, block_top, 1));
+            const uint32_t sigma8 = to_e4m3(quotient(__uint_as_float(block_top) * inv, 6.0f, 1.0f / 6.0f));
+            const float sigma = from_e4m3(sigma8);
+            uint32_t codes = 0;
             if (sigma8 != 0) {
+                const float back = __frcp_rn(sigma);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = __fdiv_rn(v[i], sigma);
-                codes[0] = to_e2m1(v);
-                codes[1] = to_e2m1(v + 8);
+                for (int i = 0; i < 8; ++i) v[i] = quotient(v[i], sigma, back);
+                codes = to_e2m1(v);
             }
-        }
-        if (r < (a.n + kE2m1TileRows - 1) / kE2m1TileRows * kE2m1TileRows)
-            a.scales[e2m1_scale_at(r, b, tiles)] = static_cast<uint8_t>(sigma8);
-        if (real && b < code_blocks)
-            *reinterpret_cast<uint2 *>(a.codes + r * e2m1_pitch(a.d) + b * 8) = make_uint2(codes[0], codes[1]);
-        if (a.values != nullptr && inside) {
-            TV *out = static_cast<TV *>(a.values) + r * a.ld_values + b * 16;
-            from_e2m1(codes[0], v);
-            from_e2m1(codes[1], v + 8);
+            // the four scales of a tile's row from the lanes 0, 2, 4 and 6 of each eight
+            uint32_t word = sigma8 | __shfl_down_sync(0xFFFFFFFFu, sigma8, 2) << 8;
+            word |= __shfl_down_sync(0xFFFFFFFFu, word, 4) << 16;
+            if (vec % 8 == 0 && vec < 8 * tiles) {
+                if (kMany) scale_words[((vec / 8) * 8 + warp) * 4 + round] = word;
+                else *reinterpret_cast<uint32_t *>(a.scales + e2m1_scale_at(r, vec / 2, tiles)) = word;
+            }
+            if (real && vec * 4 < pitch) *reinterpret_cast<uint32_t *>(a.codes + r * pitch + vec * 4) = codes;
+            if constexpr (kValues) {
+                if (left > 0) {
+                    from_e2m1(codes, v);
+                    const float unit = finite ? sigma * scale : NAN;
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (b * 16 + i < a.d) store_value(out + i, finite ? v[i] * sigma * scale : NAN);
+                    for (int i = 0; i < 8; ++i) v[i] *= unit;
+                    TV *const out = static_cast<TV *>(a.values) + r * a.ld_values + j;
+                    store8(out, v, left, (reinterpret_cast<uintptr_t>(out) & 15u) == 0);
+                }
+            }
         }
     }
-    if (lane == 0 && real) a.row_scales[r] = finite ? scale : NAN;
+    if (kMany) {
+        __syncthreads();
+        uint4 *const out = reinterpret_cast<uint4 *>(a.scales + e2m1_scale_at(first - warp, 0, tiles));
+        for (int i = threadIdx.x; i < 8 * tiles; i += kQuantizeThreads)
+            out[(i / 8) * (kE2m1TileBytes / 16) + i % 8] = reinterpret_cast<const uint4 *>(scale_words)[i];
+    }
 }
 
 struct E2m1Matrix {
@@ -127,11 +224,12 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const E2m1Matrix q, int
 }
 
 template <typename... P, typename... A>
-static cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t s, A... args) {
+static cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     cfg.gridDim = grid;
     cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -157,12 +255,22 @@ static vie_status check_e2m1(const char *fn, int64_t n, const void *codes, const
     return VIE_OK;
 }
 
+// Rows from which on a warp takes each: CTAs of 32 rows for most of the chip.
+constexpr int64_t kQuantizeManyRows = 4096;
+
+template <typename T, typename TV>
+static cudaError_t start_quantize(const QuantizeParams &p, cudaStream_t s) {
+    const int64_t rows = (p.n + kE2m1TileRows - 1) / kE2m1TileRows * kE2m1TileRows;  // with those that have scales alone
+    if (p.n < kQuantizeManyRows)
+        return launch(quantize_kernel<T, TV, kQuantizeWarps>, dim3(static_cast<unsigned>(rows)), kQuantizeThreads, 0, s, p);
+    const size_t smem = static_cast<size_t>(e2m1_tiles(p.d)) * 128;  // 32 KB at most
+    return launch(quantize_kernel<T, TV, 1>, dim3(static_cast<unsigned>(rows / 32)), kQuantizeThreads, smem, s, p);
+}
+
 template <typename T>
 static cudaError_t start_quantize(const QuantizeParams &p, vie_dtype values_dtype, cudaStream_t s) {
-    const int64_t rows = (p.n + kE2m1TileRows - 1) / kE2m1TileRows * kE2m1TileRows;
-    const dim3 grid(static_cast<unsigned>(rows * 32 / kQuantizeThreads));
-    return values_dtype == VIE_DTYPE_BF16 ? launch(quantize_kernel<T, __nv_bfloat16>, grid, kQuantizeThreads, s, p)
-                                          : launch(quantize_kernel<T, float>, grid, kQuantizeThreads, s, p);
+    if (p.values == nullptr) return start_quantize<T, None>(p, s);
+    return values_dtype == VIE_DTYPE_BF16 ? start_quantize<T, __nv_bfloat16>(p, s) : start_quantize<T, float>(p, s);
 }
 
 }  // namespace vie
@@ -195,7 +303,6 @@ vie_status vie_e2m1_quantize(const void *x, vie_dtype dtype, int64_t n, int32_t 
     p.x = x, p.n = n, p.d = d, p.ld = ld;
     p.codes = static_cast<uint8_t *>(out_codes), p.scales = static_cast<uint8_t *>(out_scales);
     p.row_scales = out_row_scales, p.values = out_values, p.ld_values = ld_values;
-    if (out_values == nullptr) values_dtype = VIE_DTYPE_F32;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = dtype == VIE_DTYPE_BF16 ? start_quantize<__nv_bfloat16>(p, values_dtype, s)
                                                   : start_quantize<float>(p, values_dtype, s);
@@ -214,8 +321,8 @@ vie_status vie_e2m1_dequantize(const void *codes, const void *scales, const floa
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e =
         out_dtype == VIE_DTYPE_BF16
-            ? launch(dequantize_kernel<__nv_bfloat16>, grid, 256, s, q, d, static_cast<__nv_bfloat16 *>(out), ld_out)
-            : launch(dequantize_kernel<float>, grid, 256, s, q, d, static_cast<float *>(out), ld_out);
+            ? launch(dequantize_kernel<__nv_bfloat16>, grid, 256, 0, s, q, d, static_cast<__nv_bfloat16 *>(out), ld_out)
+            : launch(dequantize_kernel<float>, grid, 256, 0, s, q, d, static_cast<float *>(out), ld_out);
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
 
