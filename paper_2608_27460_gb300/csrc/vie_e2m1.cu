@@ -27,6 +27,26 @@ struct QuantizeParams {
 constexpr int kQuantizeThreads = 256;
 constexpr int kQuantizeWarps = kQuantizeThreads / 32;
 
+// a / b from r = 1 / b to an ulp or two, without over- or underflow in between: one
+// correction of q = a r by its remainder (Markstein, "Computation of elementary
+// functions on the IBM RISC System/6000 processor", 1990).  With b of few bits the
+// remainder is exact and the result off by 2^-45 before its rounding: where a / b is a
+// midpoint of codes or scales it is that number, and where it is not (half an ulp
+// away or more, a having 24 bits) it is another.
+__device__ __forceinline__ float quotient(float a, float b, float r) {
+    const float q = a * r;
+    return fmaf(fmaf(-q, b, a), r, q);
+}
+__device__ __forceinline__ float reciprocal_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
 // Eight values of a row as they are stored, 0 beyond it.
 template <typename T>
 struct Raw8;
@@ -51,6 +71,18 @@ struct Raw8<__nv_bfloat16> {
         return max(t << 16, t & 0xFFFF0000u);
     }
     __device__ __forceinline__ float value(int i) const { return i % 2 == 0 ? bf16_lo(w[i / 2]) : bf16_hi(w[i / 2]); }
+    __device__ __forceinline__ void scale(float by) {  // a power of two that leaves them exact
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack_bf16(bf16_lo(w[i]) * by, bf16_hi(w[i]) * by);
+    }
+    // x_i / b as far as it decides codes, from r = 1 / b to an ulp or two.  Of x b^-1 with 8
+    // bits of x and 4 of b, what is not a midpoint of codes is 2^-10 or more from all of
+    // them: rounded to multiples of 2^-10 (the sum's last place), the others are exact.
+    __device__ __forceinline__ void quotients(float, float r, float *v) const {
+        constexpr float kShift = 12288.0f;  // 1.5 * 2^13
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(value(i), r, kShift) - kShift;
+    }
 };
 template <>
 struct Raw8<float> {
@@ -71,15 +103,15 @@ struct Raw8<float> {
         return t;
     }
     __device__ __forceinline__ float value(int i) const { return __uint_as_float(w[i]); }
+    __device__ __forceinline__ void scale(float by) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(value(i) * by);
+    }
+    __device__ __forceinline__ void quotients(float b, float r, float *v) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = quotient(value(i), b, r);
+    }
 };
-
-// a / b rounded to nearest from r = 1 / b rounded to nearest, without over- or
-// underflow in between: one correction of a r by its remainder (Markstein,
-// "Computation of elementary functions on the IBM RISC System/6000 processor", 1990).
-__device__ __forceinline__ float quotient(float a, float b, float r) {
-    const float q = a * r;
-    return fmaf(fmaf(-q, b, a), r, q);
-}
 
 template <typename T>
 __device__ __forceinline__ void store8(T *p, const float *v, int left, bool vectors) {
@@ -95,25 +127,25 @@ __device__ __forceinline__ void store8(T *p, const float *v, int left, bool vect
 
 struct None {};  // no values wanted
 
-// Rows to codes and scales, in two passes over a row: its largest magnitude, then
-// the codes (the second time from L1 or L2).  A lane takes eight values at a time,
-// two lanes a block.
+// Rows to codes and scales: a row in registers, its largest magnitude, its codes.  A
+// lane takes eight values at a time, two lanes a block.
 //
 // ROW_WARPS 1: a warp per row, a CTA for 32 rows of a tile, 8 at a time: the four
 // rows of each of its warps are those whose scales lie side by side, so that the
 // CTA's scales (gathered in shared memory) are written 128 bytes at a time.
-// ROW_WARPS 8: a CTA per row, for the latency of few rows.
-template <typename T, typename TV, int ROW_WARPS>
+// ROW_WARPS 8: a CTA per row, for the latency of few rows, and for long ones.
+// NV: vectors of eight values that a lane keeps.
+template <typename T, typename TV, int ROW_WARPS, int NV>
 __global__ void __launch_bounds__(kQuantizeThreads) quantize_kernel(const QuantizeParams a) {
     constexpr bool kMany = ROW_WARPS == 1;
     constexpr int kRowLanes = 32 * ROW_WARPS, kRounds = kMany ? 4 : 1;
-    extern __shared__ __align__(16) uint32_t scale_words[];  // kMany: [tiles][row % 8 of 32][row / 32]
+    constexpr bool kValues = !std::is_same<TV, None>::value;
+    extern __shared__ __align__(16) uint8_t scale_bytes[];  // kMany: [tiles][row % 8 of 32][row / 32][4]
     __shared__ uint32_t warp_top[kQuantizeWarps];
     const int warp = threadIdx.x >> 5, at = kMany ? threadIdx.x & 31 : threadIdx.x;
     const int tiles = e2m1_tiles(a.d);
     const int64_t pitch = e2m1_pitch(a.d);
     const bool vectors = (reinterpret_cast<uintptr_t>(a.x) & 15u) == 0 && a.ld * sizeof(T) % 16 == 0;
-    constexpr bool kValues = !std::is_same<TV, None>::value;
     griddep_launch_dependents();
     griddep_wait();
     // CTA c of kMany takes rows 8 (c % 4) + 0 .. 7 of each 32 of tile c / 4
@@ -125,12 +157,18 @@ __global__ void __launch_bounds__(kQuantizeThreads) quantize_kernel(const Quanti
         const bool real = r < a.n;
         const T *const row = static_cast<const T *>(a.x) + (real ? r : 0) * a.ld;
         const int width = real ? a.d : 0;  // rows beyond the last have scales of 0 and nothing else
-        uint32_t top = 0;
-#pragma unroll 4
-        for (int j = 8 * at; j < width; j += 8 * kRowLanes) {
-            Raw8<T> raw;
-            raw.load(row + j, width - j, vectors);
-            top = max(top, raw.top());
+        Raw8<T> raw[NV];
+        uint32_t tops[NV], top = 0;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int j = 8 * (k * kRowLanes + at);
+            raw[k] = {};
+            if (j < width) raw[k].load(row + j, width - j, vectors);
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            tops[k] = raw[k].top();
+            top = max(top, tops[k]);
         }
         top = __reduce_max_sync(0xFFFFFFFFu, top);
         if (!kMany) {
@@ -141,43 +179,40 @@ __global__ void __launch_bounds__(kQuantizeThreads) quantize_kernel(const Quanti
         }
         const bool finite = top < 0x7F800000u;
         const int E = e2m1_exponent(finite ? top : 0u);
-        const float scale = power_of_two(E), inv = power_of_two(-E);
+        float scale = power_of_two(E), inv = power_of_two(-E), unit = scale;  // of quotients, of values
         if (at == 0 && real) a.row_scales[r] = finite ? scale : NAN;
-        const int steps = (8 * tiles + kRowLanes - 1) / kRowLanes;  // the same for all lanes: they exchange
-#pragma unroll 2
-        for (int s = 0; s < steps; ++s) {
-            const int vec = s * kRowLanes + at, j = 8 * vec, left = width - j;
-            Raw8<T> raw = {};
-            if (left > 0) raw.load(row + j, left, vectors);
-            float v[8];
+        if (!finite || E < -100) {  // (sigma scale would be subnormal, its reciprocal infinite)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = finite ? raw.value(i) * inv : 0.0f;
-            uint32_t block_top = finite ? raw.top() : 0u;
-            block_top = max(block_top, __shfl_xor_sync(0xFFFFFFFFu, block_top, 1));
+            for (int k = 0; k < NV; ++k) {
+                raw[k].scale(finite ? inv : 0.0f);
+                if (!finite) raw[k] = {};
+                tops[k] = raw[k].top();
+            }
+            if (!finite) unit = NAN;
+            scale = inv = 1.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (k * kRowLanes >= 8 * tiles) break;  // (the same for all lanes: they exchange)
+            const int vec = k * kRowLanes + at, left = width - 8 * vec;
+            const uint32_t block_top = max(tops[k], __shfl_xor_sync(0xFFFFFFFFu, tops[k], 1));
             const uint32_t sigma8 = to_e4m3(quotient(__uint_as_float(block_top) * inv, 6.0f, 1.0f / 6.0f));
             const float sigma = from_e4m3(sigma8);
-            uint32_t codes = 0;
-            if (sigma8 != 0) {
-                const float back = __frcp_rn(sigma);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = quotient(v[i], sigma, back);
-                codes = to_e2m1(v);
-            }
-            // the four scales of a tile's row from the lanes 0, 2, 4 and 6 of each eight
-            uint32_t word = sigma8 | __shfl_down_sync(0xFFFFFFFFu, sigma8, 2) << 8;
-            word |= __shfl_down_sync(0xFFFFFFFFu, word, 4) << 16;
-            if (vec % 8 == 0 && vec < 8 * tiles) {
-                if (kMany) scale_words[((vec / 8) * 8 + warp) * 4 + round] = word;
-                else *reinterpret_cast<uint32_t *>(a.scales + e2m1_scale_at(r, vec / 2, tiles)) = word;
+            float v[8];
+            raw[k].quotients(sigma * scale, sigma8 != 0 ? reciprocal_approx(sigma) * inv : 0.0f, v);
+            const uint32_t codes = to_e2m1(v);
+            if (vec % 2 == 0 && vec < 8 * tiles) {
+                if (kMany) scale_bytes[(vec / 8) * 128 + warp * 16 + round * 4 + vec / 2 % 4] = static_cast<uint8_t>(sigma8);
+                else a.scales[e2m1_scale_at(r, vec / 2, tiles)] = static_cast<uint8_t>(sigma8);
             }
             if (real && vec * 4 < pitch) *reinterpret_cast<uint32_t *>(a.codes + r * pitch + vec * 4) = codes;
             if constexpr (kValues) {
                 if (left > 0) {
                     from_e2m1(codes, v);
-                    const float unit = finite ? sigma * scale : NAN;
+                    const float u = sigma * unit;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] *= unit;
-                    TV *const out = static_cast<TV *>(a.values) + r * a.ld_values + j;
+                    for (int i = 0; i < 8; ++i) v[i] *= u;
+                    TV *const out = static_cast<TV *>(a.values) + r * a.ld_values + 8 * vec;
                     store8(out, v, left, (reinterpret_cast<uintptr_t>(out) & 15u) == 0);
                 }
             }
@@ -187,7 +222,7 @@ __global__ void __launch_bounds__(kQuantizeThreads) quantize_kernel(const Quanti
         __syncthreads();
         uint4 *const out = reinterpret_cast<uint4 *>(a.scales + e2m1_scale_at(first - warp, 0, tiles));
         for (int i = threadIdx.x; i < 8 * tiles; i += kQuantizeThreads)
-            out[(i / 8) * (kE2m1TileBytes / 16) + i % 8] = reinterpret_cast<const uint4 *>(scale_words)[i];
+            out[(i / 8) * (kE2m1TileBytes / 16) + i % 8] = reinterpret_cast<const uint4 *>(scale_bytes)[i];
     }
 }
 
@@ -261,10 +296,17 @@ constexpr int64_t kQuantizeManyRows = 4096;
 template <typename T, typename TV>
 static cudaError_t start_quantize(const QuantizeParams &p, cudaStream_t s) {
     const int64_t rows = (p.n + kE2m1TileRows - 1) / kE2m1TileRows * kE2m1TileRows;  // with those that have scales alone
-    if (p.n < kQuantizeManyRows)
-        return launch(quantize_kernel<T, TV, kQuantizeWarps>, dim3(static_cast<unsigned>(rows)), kQuantizeThreads, 0, s, p);
-    const size_t smem = static_cast<size_t>(e2m1_tiles(p.d)) * 128;  // 32 KB at most
-    return launch(quantize_kernel<T, TV, 1>, dim3(static_cast<unsigned>(rows / 32)), kQuantizeThreads, smem, s, p);
+    constexpr int W = kQuantizeWarps, NT = kQuantizeThreads;
+    if (p.n >= kQuantizeManyRows && p.d <= 2048) {
+        const dim3 grid(static_cast<unsigned>(rows / 32));
+        const size_t smem = static_cast<size_t>(e2m1_tiles(p.d)) * 128;
+        return p.d <= 1024 ? launch(quantize_kernel<T, TV, 1, 4>, grid, NT, smem, s, p)
+                           : launch(quantize_kernel<T, TV, 1, 8>, grid, NT, smem, s, p);
+    }
+    const dim3 grid(static_cast<unsigned>(rows));
+    return p.d <= 2048   ? launch(quantize_kernel<T, TV, W, 1>, grid, NT, 0, s, p)
+           : p.d <= 4096 ? launch(quantize_kernel<T, TV, W, 2>, grid, NT, 0, s, p)
+                         : launch(quantize_kernel<T, TV, W, VIE_D_MAX / (8 * NT)>, grid, NT, 0, s, p);
 }
 
 template <typename T>
