@@ -566,7 +566,7 @@ def _matrix(x, name):
 
 def _given(x, name, shape, dtype, like):
     """A contiguous argument of this shape and type on like's device."""
-    if x.dtype is not dtype or x.shape != shape or not x.is_cuda or x.get_device() != like.get_device():
+    if x.dtype is not dtype or x.shape != shape or x.get_device() != like.get_device():  # (-1: a CPU tensor)
         raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {like.device}")
     return x if x.is_contiguous() else x.contiguous()
 
@@ -575,7 +575,7 @@ def _output(x, name, shape, dtype, like):
     """An output tensor: `x` if it fits, a new one if it is None."""
     if x is None:
         return _torch.empty(shape, dtype=dtype, device=like.device)
-    if x.dtype is not dtype or x.shape != shape or not x.is_cuda or x.get_device() != like.get_device():
+    if x.dtype is not dtype or x.shape != shape or x.get_device() != like.get_device():  # (-1: a CPU tensor)
         raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {like.device}")
     return x
 
@@ -994,15 +994,18 @@ class E2m1:
     def shape(self):
         return (self.codes.shape[0], self.d)
 
-    def _pointers(self, name, shape, like):
-        """Addresses of the parts of a matrix of this shape on like's device."""
-        n, d = shape
+    def _pointers(self, name, n, d, like):
+        """Addresses of the parts of a matrix of n rows of d values on like's device."""
         c, s, r = self.codes, self.scales, self.row_scales
-        if d != self.d or c.shape != (n, (d + 31) // 32 * 16) or c.dtype is not _torch.uint8 or                 s.numel() != (n + 127) // 128 * ((d + 63) // 64) * 512 or s.element_size() != 1 or                 r.shape != (n,) or r.dtype is not _torch.float32:
+        fits = d == self.d and c.shape == (n, (d + 31) // 32 * 16) and c.dtype is _torch.uint8 and \
+            s.numel() == (n + 127) // 128 * ((d + 63) // 64) * 512 and s.element_size() == 1 and \
+            r.shape == (n,) and r.dtype is _torch.float32
+        if not fits:
             raise ValueError(f"{name} must be an E2m1 of {n} rows of {d} values")
-        for x in (c, s, r):
-            if not x.is_contiguous() or not x.is_cuda or x.get_device() != like.get_device():
-                raise ValueError(f"{name} must hold contiguous tensors on {like.device}")
+        dev = like.get_device()
+        if not (c.is_contiguous() and s.is_contiguous() and r.is_contiguous() and c.get_device() == dev
+                and s.get_device() == dev and r.get_device() == dev):
+            raise ValueError(f"{name} must hold contiguous tensors on {like.device}")
         return c.data_ptr(), s.data_ptr(), r.data_ptr()
 
 
@@ -1016,7 +1019,7 @@ def e2m1_quantize(x, out=None, out_values=None, stream=None):
     n, d = x.shape
     if out is None:
         out = E2m1.empty(n, d, x.device)
-    codes, scales, row_scales = out._pointers("out", (n, d), x)
+    codes, scales, row_scales = out._pointers("out", n, d, x)
     values, values_dtype, ld_values = 0, VIE_DTYPE_F32, 0
     if out_values is not None:
         out_values, ld_values = _matrix_output(out_values, "out_values", (n, d), out_values.dtype, x)
@@ -1036,7 +1039,7 @@ def e2m1_dequantize(q, out=None, out_dtype=None, stream=None):
         with _on(like, stream):
             return e2m1_dequantize(q, out, out_dtype)
     n, d = q.shape
-    codes, scales, row_scales = q._pointers("q", (n, d), like)
+    codes, scales, row_scales = q._pointers("q", n, d, like)
     if out_dtype is None:
         out_dtype = _torch.float32 if out is None else out.dtype
     out, ld = _matrix_output(out, "out", (n, d), out_dtype, like)
@@ -1056,17 +1059,26 @@ def e2m1_logits(x, weights, out=None, out_dtype=None, x_quantized=None, stream=N
         with _on(like, stream):
             return e2m1_logits(x, weights, out, out_dtype, x_quantized)
     V, d = weights.shape
-    if not isinstance(x, E2m1):
-        if x.dim() != 2 or x.shape[1] != d or not x.is_cuda or x.get_device() != like.get_device():
-            raise ValueError(f"x must be a tensor [n, {d}] on {like.device}")
-        x = e2m1_quantize(x, out=x_quantized)
-    n = x.shape[0]
-    xp = x._pointers("x", (n, d), like)
-    wp = weights._pointers("weights", (V, d), like)
+    w = weights._pointers("weights", V, d, like)
+    stream = _stream_ptr(None)
+    given = isinstance(x, E2m1)
+    if given:
+        x_quantized, n = x, x.codes.shape[0]
+    else:
+        if x.get_device() != like.get_device() or x.dim() != 2 or x.shape[1] != d:
+            raise ValueError(f"x must be a CUDA tensor [n, {d}] on {like.device}")
+        n = x.shape[0]
+        x, ld_x = _matrix(x, "x")
+        if x_quantized is None:
+            x_quantized = E2m1.empty(n, d, like.device)
+    q = x_quantized._pointers("x" if given else "x_quantized", n, d, like)
     if out_dtype is None:
         out_dtype = _torch.float32 if out is None else out.dtype
     out, ld = _matrix_output(out, "out", (n, V), out_dtype, like)
-    check(vie_e2m1_logits(*xp, n, *wp, V, d, out.data_ptr(), _dtype_code(out, "out"), ld, _stream_ptr(None)))
+    to = _dtype_code(out, "out")
+    if not given:
+        check(vie_e2m1_quantize(x.data_ptr(), _dtype_code(x, "x"), n, d, ld_x, *q, 0, VIE_DTYPE_F32, 0, stream))
+    check(vie_e2m1_logits(*q, n, *w, V, d, out.data_ptr(), to, ld, stream))
     return out
 
 
