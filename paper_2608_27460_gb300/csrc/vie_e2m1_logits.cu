@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
         tma_prefetch_map(&map_w);
         tma_prefetch_map(&map_x);
         for (int s = 0; s < S; ++s) {
-            mbar_init(&sm.full[s], 1);
+            mbar_init(&sm.full[s], 2);
             mbar_init(&sm.scaled[s], 4);
             mbar_init(&sm.empty[s], 1);
         }
@@ -167,40 +167,48 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
     griddep_wait();  // the inputs may come from the kernels before this one
 
     // Tiles: x fastest, so that the CTAs that share rows of W run together.
-    if (warp == 0) {
-        // ---------------- producer ----------------
+    if (warp == 0 || warp == 3) {
+        // ---------------- producers: W (warp 0), x (warp 3) ----------------
+        // One thread alone would be what a stage waits for: a few hundred cycles for
+        // its wait, its expected bytes and four or five copies.
         if (lane == 0) {
-            const uint64_t once = l2_evict_first_policy(), keep = l2_evict_last_policy();
-            const uint64_t w_policy = x_tiles == 1 ? once : keep;
+            const bool of_w = warp == 0;
+            const uint64_t policy = of_w && x_tiles == 1 ? l2_evict_first_policy() : l2_evict_last_policy();
+            const CUtensorMap *const map = of_w ? &map_w : &map_x;
+            unsigned char *const codes = of_w ? ring : ring_x;
+            const int stage_codes = of_w ? Sh::kStageW : Sh::kStageX;
+            const int sets = of_w ? 1 : Sh::kXTiles;
+            const int last_steps = tiles64 - (n_kb - 1) * kE2m1KbTiles;
+            const int64_t last_x_tile = (p.n - 1) / kE2m1TileRows;
             int s = 0, issued = 0;
             uint32_t ph = 0;
             bool ok = true;
             for (int64_t t = blockIdx.x; ok && t < total; t += gridDim.x) {
                 const int64_t vt = t / x_tiles;
-                const int xt = static_cast<int>(t % x_tiles);
+                const int xt = static_cast<int>(t - vt * x_tiles);
+                const int y = of_w ? static_cast<int>(vt * kE2m1TileRows) : xt * BN;
+                const uint8_t *from[2];
+                if (of_w) {
+                    from[0] = from[1] = p.w_scales + vt * tiles64 * kE2m1TileBytes;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {  // a tile beyond the last is not stored: any scales do for it
+                        const int64_t rt = min(static_cast<int64_t>(xt) * BN / kE2m1TileRows + i, last_x_tile);
+                        from[i] = p.x_scales + rt * tiles64 * kE2m1TileBytes;
+                    }
+                }
                 for (int kb = 0; kb < n_kb; ++kb) {
                     if (issued >= S && !mbar_wait(&sm.empty[s], ph ^ 1u, abort)) {
                         ok = false;
                         break;
                     }
-                    const int steps = min(kE2m1KbTiles, tiles64 - kb * kE2m1KbTiles);
-                    const uint32_t scale_bytes = static_cast<uint32_t>(steps * kE2m1TileBytes);
-                    mbar_arrive_expect_tx(&sm.full[s], Sh::kStageW + Sh::kStageX + (1 + Sh::kXTiles) * scale_bytes);
-                    tma_load_2d(ring + s * Sh::kStageW, &map_w, kb * 128, static_cast<int>(vt * kE2m1TileRows),
-                                &sm.full[s], w_policy);
-                    tma_load_2d(ring_x + s * Sh::kStageX, &map_x, kb * 128, xt * BN, &sm.full[s], keep);
-                    unsigned char *const sc = ring_s + s * (1 + Sh::kXTiles) * kE2m1StageScales;
-                    bulk_g2s(sc, p.w_scales + (vt * tiles64 + kb * kE2m1KbTiles) * kE2m1TileBytes, scale_bytes,
-                             &sm.full[s], w_policy);
-#pragma unroll
-                    for (int i = 0; i < Sh::kXTiles; ++i) {
-                        // a tile beyond the last is not stored: any scales do for it
-                        const int64_t rt = min(static_cast<int64_t>(xt) * BN / kE2m1TileRows + i,
-                                               (p.n - 1) / kE2m1TileRows);
-                        bulk_g2s(sc + (1 + i) * kE2m1StageScales,
-                                 p.x_scales + (rt * tiles64 + kb * kE2m1KbTiles) * kE2m1TileBytes, scale_bytes,
-                                 &sm.full[s], keep);
-                    }
+                    const uint32_t bytes = static_cast<uint32_t>((kb == n_kb - 1 ? last_steps : kE2m1KbTiles) * kE2m1TileBytes);
+                    mbar_arrive_expect_tx(&sm.full[s], stage_codes + sets * bytes);
+                    tma_load_2d(codes + s * stage_codes, map, kb * 128, y, &sm.full[s], policy);
+                    unsigned char *const sc =
+                        ring_s + (s * (1 + Sh::kXTiles) + (of_w ? 0 : 1)) * kE2m1StageScales;
+                    bulk_g2s(sc, from[0] + kb * kE2m1StageScales, bytes, &sm.full[s], policy);
+                    if (sets > 1) bulk_g2s(sc + kE2m1StageScales, from[1] + kb * kE2m1StageScales, bytes, &sm.full[s], policy);
                     ++issued;
                     if (++s == S) {
                         s = 0;
@@ -240,9 +248,11 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
                     const uint32_t sfb = sfa + 4 * kE2m1KbTiles;
                     const uint64_t ad = umma_desc_k_sw128(ring + s * Sh::kStageW);
                     const uint64_t bd = umma_desc_k_sw128(ring_x + s * Sh::kStageX);
-                    for (int k = 0; k < steps; ++k)
-                        umma_e2m1(acc, ad + 2 * k, bd + 2 * k, idesc, sfa + 4 * k, sfb + 4 * Sh::kXTiles * k,
-                                  (kb | k) != 0 ? 1u : 0u);
+#pragma unroll
+                    for (int k = 0; k < kE2m1KbTiles; ++k)
+                        if (k < steps)
+                            umma_e2m1(acc, ad + 2 * k, bd + 2 * k, idesc, sfa + 4 * k, sfb + 4 * Sh::kXTiles * k,
+                                      (kb | k) != 0 ? 1u : 0u);
                     umma_commit(&sm.empty[s]);
                     if (++s == S) {
                         s = 0;
