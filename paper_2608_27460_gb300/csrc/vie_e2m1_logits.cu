@@ -7,7 +7,7 @@
 // 256 rows of x and 64 columns, scales and accumulators in TMEM.
 //
 // A persistent CTA per SM takes tiles of 128 vocabulary rows by BN rows of x.  A
-// producer thread fills a ring of stages of 256 columns each: codes by TMA boxes
+// producer threads fill a ring of stages of 256 or 512 columns: codes by TMA boxes
 // of 128 bytes a row (columns and rows beyond the matrix read as 0), scales by bulk
 // copies of their 512-byte tiles, which lie in memory as TMEM wants them.  Four
 // warps take a stage's scales to the stage's own columns of TMEM, each to its
@@ -34,17 +34,22 @@
 
 namespace vie {
 
-constexpr int kE2m1Kb = 256;                      // columns per stage: 128 bytes of codes a row
-constexpr int kE2m1KbTiles = kE2m1Kb / 64;        // scale tiles per stage, and MMAs
-constexpr int kE2m1StageScales = kE2m1KbTiles * kE2m1TileBytes;
+constexpr int kE2m1Kb = 256;                // columns of a K-block: 128 bytes of codes a row, a box
+constexpr int kE2m1KbTiles = kE2m1Kb / 64;  // its scale tiles, and MMAs
 
 template <int BN>
 struct E2m1Shape {
     static constexpr int kXTiles = BN > 128 ? 2 : 1;              // tiles of 128 rows of x
-    static constexpr int kStageW = kE2m1TileRows * 128, kStageX = BN * 128;
-    static constexpr int kStageBytes = kStageW + kStageX + (1 + kXTiles) * kE2m1StageScales;
+    // K-blocks per stage: what a stage costs besides its bytes (waits, arrivals) is paid for
+    // more of them where shared memory holds enough such stages.
+    static constexpr int kBlocks = BN > 64 ? 1 : 2;
+    static constexpr int kSteps = kBlocks * kE2m1KbTiles;         // scale tiles and MMAs of a stage
+    static constexpr int kBoxW = kE2m1TileRows * 128, kBoxX = BN * 128;
+    static constexpr int kStageW = kBlocks * kBoxW, kStageX = kBlocks * kBoxX;
+    static constexpr int kSet = kSteps * kE2m1TileBytes;          // a stage's scales of 128 rows
+    static constexpr int kStageBytes = kStageW + kStageX + (1 + kXTiles) * kSet;
     static constexpr int kBuffers = BN > 128 ? 1 : 2;             // accumulators
-    static constexpr int kScaleCols = 4 * kE2m1KbTiles * (1 + kXTiles);  // TMEM columns of a stage's scales
+    static constexpr int kScaleCols = 4 * kSteps * (1 + kXTiles);  // TMEM columns of a stage's scales
     static constexpr int kScaleBase = (kBuffers * BN + 31) / 32 * 32;
     static constexpr int kByMemory = (232448 - 1024 - 2048) / kStageBytes, kByTmem = (512 - kScaleBase) / kScaleCols;
     static constexpr int kStages = kByMemory < kByTmem ? kByMemory : kByTmem;
@@ -134,7 +139,7 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
     unsigned char *const ring_x = ring + S * Sh::kStageW;
     unsigned char *const ring_s = ring_x + S * Sh::kStageX;  // per stage: scales of W, then of x
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int tiles64 = e2m1_tiles(p.d), n_kb = (tiles64 + kE2m1KbTiles - 1) / kE2m1KbTiles;
+    const int tiles64 = e2m1_tiles(p.d), n_stages = (tiles64 + Sh::kSteps - 1) / Sh::kSteps;  // of a tile
     const int64_t total = static_cast<int64_t>(v_tiles) * x_tiles;
     volatile int *const abort = &sm.abort;
     volatile int never = 0;
@@ -178,7 +183,7 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
             unsigned char *const codes = of_w ? ring : ring_x;
             const int stage_codes = of_w ? Sh::kStageW : Sh::kStageX;
             const int sets = of_w ? 1 : Sh::kXTiles;
-            const int last_steps = tiles64 - (n_kb - 1) * kE2m1KbTiles;
+            const int box = of_w ? Sh::kBoxW : Sh::kBoxX;
             const int64_t last_x_tile = (p.n - 1) / kE2m1TileRows;
             int s = 0, issued = 0;
             uint32_t ph = 0;
@@ -197,18 +202,23 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
                         from[i] = p.x_scales + rt * tiles64 * kE2m1TileBytes;
                     }
                 }
-                for (int kb = 0; kb < n_kb; ++kb) {
+                for (int k = 0; k < n_stages; ++k) {
                     if (issued >= S && !mbar_wait(&sm.empty[s], ph ^ 1u, abort)) {
                         ok = false;
                         break;
                     }
-                    const uint32_t bytes = static_cast<uint32_t>((kb == n_kb - 1 ? last_steps : kE2m1KbTiles) * kE2m1TileBytes);
-                    mbar_arrive_expect_tx(&sm.full[s], stage_codes + sets * bytes);
-                    tma_load_2d(codes + s * stage_codes, map, kb * 128, y, &sm.full[s], policy);
-                    unsigned char *const sc =
-                        ring_s + (s * (1 + Sh::kXTiles) + (of_w ? 0 : 1)) * kE2m1StageScales;
-                    bulk_g2s(sc, from[0] + kb * kE2m1StageScales, bytes, &sm.full[s], policy);
-                    if (sets > 1) bulk_g2s(sc + kE2m1StageScales, from[1] + kb * kE2m1StageScales, bytes, &sm.full[s], policy);
+                    const int steps = min(Sh::kSteps, tiles64 - k * Sh::kSteps);
+                    const int boxes = (steps + kE2m1KbTiles - 1) / kE2m1KbTiles;
+                    const uint32_t bytes = static_cast<uint32_t>(steps * kE2m1TileBytes);
+                    mbar_arrive_expect_tx(&sm.full[s], boxes * box + sets * bytes);
+#pragma unroll
+                    for (int i = 0; i < Sh::kBlocks; ++i)
+                        if (i < boxes)
+                            tma_load_2d(codes + s * stage_codes + i * box, map, (k * Sh::kBlocks + i) * 128, y, &sm.full[s],
+                                        policy);
+                    unsigned char *const sc = ring_s + (s * (1 + Sh::kXTiles) + (of_w ? 0 : 1)) * Sh::kSet;
+                    bulk_g2s(sc, from[0] + k * Sh::kSet, bytes, &sm.full[s], policy);
+                    if (sets > 1) bulk_g2s(sc + Sh::kSet, from[1] + k * Sh::kSet, bytes, &sm.full[s], policy);
                     ++issued;
                     if (++s == S) {
                         s = 0;
@@ -237,22 +247,26 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
                     break;
                 }
                 const uint32_t acc = tmem + static_cast<uint32_t>(b * BN);
-                for (int kb = 0; kb < n_kb; ++kb) {
+                for (int k = 0; k < n_stages; ++k) {
                     if (!mbar_wait(&sm.full[s], ph, abort) || !mbar_wait(&sm.scaled[s], ph, abort)) {
                         ok = false;
                         break;
                     }
                     tc_fence_after_sync();
-                    const int steps = min(kE2m1KbTiles, tiles64 - kb * kE2m1KbTiles);
+                    const int steps = tiles64 - k * Sh::kSteps;  // of this stage and those behind it
                     const uint32_t sfa = tmem + Sh::kScaleBase + s * Sh::kScaleCols;
-                    const uint32_t sfb = sfa + 4 * kE2m1KbTiles;
+                    const uint32_t sfb = sfa + 4 * Sh::kSteps;
                     const uint64_t ad = umma_desc_k_sw128(ring + s * Sh::kStageW);
                     const uint64_t bd = umma_desc_k_sw128(ring_x + s * Sh::kStageX);
 #pragma unroll
-                    for (int k = 0; k < kE2m1KbTiles; ++k)
-                        if (k < steps)
-                            umma_e2m1(acc, ad + 2 * k, bd + 2 * k, idesc, sfa + 4 * k, sfb + 4 * Sh::kXTiles * k,
-                                      (kb | k) != 0 ? 1u : 0u);
+                    for (int j = 0; j < Sh::kSteps; ++j) {
+                        constexpr int kInBox = kE2m1KbTiles;  // steps of 32 bytes in a box of 128
+                        const uint64_t at_w = j / kInBox * (Sh::kBoxW >> 4) + j % kInBox * 2;
+                        const uint64_t at_x = j / kInBox * (Sh::kBoxX >> 4) + j % kInBox * 2;
+                        if (j < steps)
+                            umma_e2m1(acc, ad + at_w, bd + at_x, idesc, sfa + 4 * j, sfb + 4 * Sh::kXTiles * j,
+                                      (k | j) != 0 ? 1u : 0u);
+                    }
                     umma_commit(&sm.empty[s]);
                     if (++s == S) {
                         s = 0;
@@ -273,30 +287,32 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
         uint32_t ph = 0;
         bool ok = true;
         for (int64_t t = blockIdx.x; ok && t < total; t += gridDim.x) {
-            for (int kb = 0; kb < n_kb; ++kb) {
+            for (int k = 0; k < n_stages; ++k) {
                 if (!mbar_wait(&sm.full[s], ph, abort)) {
                     if (lane == 0) give_up(p.flag, &sm.abort);
                     ok = false;
                     break;
                 }
                 // (what lies behind the matrix's last scales is not used by an MMA)
-                const uint4 *const sc =
-                    reinterpret_cast<const uint4 *>(ring_s + s * (1 + Sh::kXTiles) * kE2m1StageScales) + lane;
-                constexpr int kTile = kE2m1TileBytes / 16, kSet = kE2m1StageScales / 16;
+                const uint4 *const sc = reinterpret_cast<const uint4 *>(ring_s + s * (1 + Sh::kXTiles) * Sh::kSet) + lane;
+                constexpr int kTile = kE2m1TileBytes / 16, kSet = Sh::kSet / 16;
                 const uint32_t at = cols + s * Sh::kScaleCols;
                 uint32_t r[16];
                 auto gather = [&](int j, const uint4 &w) { r[j] = w.x, r[j + 1] = w.y, r[j + 2] = w.z, r[j + 3] = w.w; };
 #pragma unroll
-                for (int k = 0; k < 4; ++k) gather(4 * k, sc[k * kTile]);
-                tmem_st_32x32b_x16(at, r);
+                for (int h = 0; h < Sh::kBlocks; ++h) {
 #pragma unroll
-                for (int h = 0; h < Sh::kXTiles; ++h) {  // x: columns of step 0 of each tile of rows, step 1, ...
+                    for (int j = 0; j < 4; ++j) gather(4 * j, sc[(4 * h + j) * kTile]);
+                    tmem_st_32x32b_x16(at + 16 * h, r);
+                }
+#pragma unroll
+                for (int h = 0; h < Sh::kBlocks * Sh::kXTiles; ++h) {  // x: step 0 of each tile of rows, step 1, ...
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const int k = (4 * h + j) / Sh::kXTiles, i = (4 * h + j) % Sh::kXTiles;
-                        gather(4 * j, sc[(1 + i) * kSet + k * kTile]);
+                        const int step = (4 * h + j) / Sh::kXTiles, i = (4 * h + j) % Sh::kXTiles;
+                        gather(4 * j, sc[(1 + i) * kSet + step * kTile]);
                     }
-                    tmem_st_32x32b_x16(at + 16 * (1 + h), r);
+                    tmem_st_32x32b_x16(at + 16 * (Sh::kBlocks + h), r);
                 }
                 tmem_wait_st();
                 tc_fence_before_sync();
