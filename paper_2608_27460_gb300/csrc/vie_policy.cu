@@ -228,37 +228,63 @@ struct PreferenceParams {
     uint32_t *flag;
 };
 
-constexpr int kPairThreads = 256;
+constexpr int kPairCtas = 8;  // of a pair, at most
 
-// One CTA per pair.
-template <bool FWD, bool BWD>
-__global__ void __launch_bounds__(kPairThreads) preference_kernel(const PreferenceParams a) {
-    constexpr int NT = kPairThreads;
+// The sum of lp - ref over tokens i, i + step, ... below end, as four running sums.
+__device__ __forceinline__ float sum_ratios(const PreferenceParams &a, int i, int end, int step) {
+    float s[4] = {};
+    for (; i + 3 * step < end; i += 4 * step) {
+        float v[4], r[4] = {};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = a.lp[i + u * step];
+        if (a.ref != nullptr) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) r[u] = a.ref[i + u * step];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s[u] += v[u] - r[u];
+    }
+    for (; i < end; i += step) s[0] += a.lp[i] - (a.ref != nullptr ? a.ref[i] : 0.0f);
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+// A cluster of CTAs of NT threads per pair, whose sums meet in shared memory.
+template <bool FWD, bool BWD, int NT>
+__global__ void __launch_bounds__(NT) preference_kernel(const PreferenceParams a, int ctas) {
     __shared__ float4 sums[NT / 32];
-    const int tid = threadIdx.x, p = blockIdx.x;
+    __shared__ float2 parts[kPairCtas];  // of the pair's CTAs
+    const int tid = threadIdx.x, p = blockIdx.x / ctas, rank = blockIdx.x % ctas;
+    const int first = rank * NT + tid, step = ctas * NT;  // this thread's place among the pair's
+    if (FWD && ctas > 1) cluster_arrive_relaxed();
     griddep_launch_dependents();
     griddep_wait();
     int o[3];
 #pragma unroll
     for (int i = 0; i < 3; ++i) o[i] = a.offsets[2 * p + i];
     const int n = static_cast<int>(a.n);
-    if (tid == 0 && (o[0] < 0 || o[1] < o[0] || o[2] < o[1] || o[2] > n)) atomicOr(a.flag, kErrOffsets);
+    if (first == 0 && (o[0] < 0 || o[1] < o[0] || o[2] < o[1] || o[2] > n)) atomicOr(a.flag, kErrOffsets);
     o[0] = min(max(o[0], 0), n);
     o[1] = min(max(o[1], o[0]), n);
     o[2] = min(max(o[2], o[1]), n);
     float h;
     if (FWD) {
-        float4 d = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int i = o[0] + tid; i < o[1]; i += NT) d.x += a.lp[i] - (a.ref != nullptr ? a.ref[i] : 0.0f);
-        for (int i = o[1] + tid; i < o[2]; i += NT) d.y += a.lp[i] - (a.ref != nullptr ? a.ref[i] : 0.0f);
+        float4 d = make_float4(sum_ratios(a, o[0] + first, o[1], step), sum_ratios(a, o[1] + first, o[2], step), 0.0f, 0.0f);
         d = block_sum<NT>(d, sums);
+        if (ctas > 1) {
+            cluster_wait();  // all CTAs of the pair run, before their memory is written
+            if (tid < ctas) *cluster_peer(&parts[rank], tid) = make_float2(d.x, d.y);
+            cluster_arrive();
+            cluster_wait();
+            d.x = d.y = 0.0f;
+            for (int i = 0; i < ctas; ++i) d.x += parts[i].x, d.y += parts[i].y;
+        }
         h = a.beta * (d.x - d.y);
     } else {
         h = a.margin_in[p];
     }
-    if (FWD && tid == 0) {
+    if (FWD && first == 0) {
         const float both = log1pf(expf(-fabsf(h)));  // softplus(x) = both + max(x, 0)
-        float loss = 0.0f;  // (h may be infinite: no product of it with 0)
+        float loss = 0.0f;                           // (h may be infinite: no product of it with 0)
         if (a.smoothing != 1.0f) loss += (1.0f - a.smoothing) * (h < 0.0f ? both - h : both);
         if (a.smoothing != 0.0f) loss += a.smoothing * (h > 0.0f ? both + h : both);
         a.loss[p] = loss;
@@ -266,11 +292,13 @@ __global__ void __launch_bounds__(kPairThreads) preference_kernel(const Preferen
     }
     if (BWD) {
         const float slope = a.beta * a.grad_loss[p] * (a.smoothing - 1.0f / (1.0f + expf(h)));
-        for (int i = o[0] + tid; i < o[2]; i += NT) a.grad[i] = i < o[1] ? slope : -slope;
-        // tokens of no sequence, shared among all CTAs
-        const int first = min(max(a.offsets[0], 0), n), last = min(max(a.offsets[2 * a.pairs], 0), n);
-        for (int64_t i = static_cast<int64_t>(p) * NT + tid; i < first; i += static_cast<int64_t>(a.pairs) * NT) a.grad[i] = 0.0f;
-        for (int64_t i = last + static_cast<int64_t>(p) * NT + tid; i < n; i += static_cast<int64_t>(a.pairs) * NT) a.grad[i] = 0.0f;
+        for (int i = o[0] + first; i < o[2]; i += step) a.grad[i] = i < o[1] ? slope : -slope;
+        // tokens of no sequence, shared among all pairs
+        const int begin = min(max(a.offsets[0], 0), n), end = min(max(a.offsets[2 * a.pairs], 0), n);
+        const int64_t all = static_cast<int64_t>(a.pairs) * step;
+        const int64_t mine = static_cast<int64_t>(p) * step + first;
+        for (int64_t i = mine; i < begin; i += all) a.grad[i] = 0.0f;
+        for (int64_t i = end + mine; i < n; i += all) a.grad[i] = 0.0f;
     }
 }
 
@@ -283,16 +311,26 @@ static vie_status launch_preference(const char *fn, PreferenceParams &p, vie_str
         if (BWD && p.n > 0) e = cudaMemsetAsync(p.grad, 0, sizeof(float) * static_cast<size_t>(p.n), s);
         return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
     }
+    // Threads for about 8 tokens each where pairs are few: up to eight CTAs, of 1024
+    // threads where those of 256 would have more than 32 tokens each left.
+    const int64_t mean = p.n / p.pairs;
+    int ctas = 1;
+    while (ctas < kPairCtas && static_cast<int64_t>(p.pairs) * ctas < 256 && mean > ctas * 8 * 256) ctas *= 2;
+    const bool wide = p.pairs <= 64 && mean > kPairCtas * 32 * 256;
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    cfg.gridDim = dim3(static_cast<unsigned>(p.pairs));
-    cfg.blockDim = dim3(kPairThreads);
+    cudaLaunchAttribute attr[2];
+    cfg.gridDim = dim3(static_cast<unsigned>(p.pairs * ctas));
+    cfg.blockDim = dim3(wide ? 1024 : 256);
     cfg.stream = s;
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(ctas);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, preference_kernel<FWD, BWD>, p);
+    cfg.numAttrs = ctas > 1 ? 2 : 1;
+    e = wide ? cudaLaunchKernelEx(&cfg, preference_kernel<FWD, BWD, 1024>, p, ctas)
+             : cudaLaunchKernelEx(&cfg, preference_kernel<FWD, BWD, 256>, p, ctas);
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
 
