@@ -622,7 +622,7 @@ vie_status vie_token_logprobs_grad(const void *logits, vie_dtype dtype, int64_t 
  *               read it.
  *   clip_low    in [0, 1];  clip_high, kl_coef: finite, not negative.
  *   out_loss, out_logprob  device, fp32 [n].
- *   out_stats   as for vie_token_logprobs.
+ *   out_stats   as for vie_token_logprobs.  Results do not overlap the terms.
  *
  * Errors: VIE_ERR_INVALID_ARG, VIE_ERR_UNSUPPORTED (dtype), VIE_ERR_CUDA.
  */
@@ -753,8 +753,9 @@ vie_status vie_e2m1_dequantize(const void *codes, const void *scales, const floa
  * vie_e2m1_logits - full logits of a head whose rows are e2m1, for hidden states
  * that are e2m1 as well:
  *   out[i, v] = sum_j x[i, j] w[v, j],
- * products exact, sums fp32, rounded once to out_dtype.  (vie_sample_logits draws
- * from them, vie_token_logprobs scores them.)
+ * products exact, sums fp32, rounded once to out_dtype.  (Where the product of the
+ * rows' powers of two s is below 2^-149 or above 2^127, results are 0 or infinite.)
+ * vie_sample_logits draws from them, vie_token_logprobs scores them.
  *   x_*         device, n rows of d values;  0 <= n <= VIE_MANY_MAX.
  *   w_*         device, V rows of d values;  1 <= V <= VIE_E2M1_N_MAX.
  *   out         device, out_dtype [n, V], row pitch ld_out.

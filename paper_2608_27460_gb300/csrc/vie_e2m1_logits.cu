@@ -357,7 +357,8 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
             // 64 of fp32, or 128 rounded to bf16.
             const int rows = static_cast<int>(min(static_cast<int64_t>(kCols), p.n - i0 - c0));
             ColumnStore<T, WORDS> put(static_cast<T *>(p.out) + (i0 + c0) * p.ld, p.ld, v, p.V, rows);
-            auto scaled = [&](uint32_t bits, int c) { return __uint_as_float(bits) * x_scale[c] * tv; };
+            // (the powers of two first: of large rows with small ones neither product overflows)
+            auto scaled = [&](uint32_t bits, int c) { return __uint_as_float(bits) * (x_scale[c] * tv); };
             auto hand_back = [&] {
                 tc_fence_before_sync();
                 if (lane == 0) mbar_arrive(&sm.acc_empty[b]);

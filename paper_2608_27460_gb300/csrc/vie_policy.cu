@@ -13,6 +13,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "vie_api.h"
 #include "vie_block.cuh"
@@ -197,6 +198,19 @@ static vie_status check_terms(const char *fn, int64_t n, const PolicyTerms &t) {
         return fail(VIE_ERR_INVALID_ARG, "%s: kl_coef=%g must be finite and not negative", fn, static_cast<double>(t.kl));
     if (t.kl != 0.0f && t.ref_lp == nullptr && n > 0)
         return fail(VIE_ERR_INVALID_ARG, "%s: kl_coef=%g needs ref_logprob", fn, static_cast<double>(t.kl));
+    return VIE_OK;
+}
+
+// What is written per row while other CTAs may still read the terms of that row.
+static vie_status check_results(const char *fn, int64_t n, const PolicyTerms &t, const float *out_loss,
+                                const float *out_logprob, const float *out_stats) {
+    vie_status st = check_floats(fn, n, out_loss);
+    if (st == VIE_OK) st = check_floats(fn, n, out_logprob);
+    if (st == VIE_OK) st = check_floats(fn, n, out_stats, true);
+    if (st != VIE_OK || n == 0) return st;
+    for (const float *out : {out_loss, out_logprob, out_stats})
+        if (out != nullptr && (out == t.old_lp || out == t.advantage || out == t.ref_lp))
+            return fail(VIE_ERR_INVALID_ARG, "%s: a result in place of old_logprob, advantage or ref_logprob", fn);
     return VIE_OK;
 }
 
@@ -398,9 +412,7 @@ vie_status vie_policy_loss(const void *logits, vie_dtype dtype, int64_t n, int64
     p.terms = {old_logprob, advantage, ref_logprob, clip_low, clip_high, kl_coef};
     vie_status st = check_rows(fn, logits, dtype, n, V, ld, tokens, temperature);
     if (st == VIE_OK) st = check_terms(fn, n, p.terms);
-    if (st == VIE_OK) st = check_floats(fn, n, out_loss);
-    if (st == VIE_OK) st = check_floats(fn, n, out_logprob);
-    if (st == VIE_OK) st = check_floats(fn, n, out_stats, true);
+    if (st == VIE_OK) st = check_results(fn, n, p.terms, out_loss, out_logprob, out_stats);
     if (st != VIE_OK) return st;
     p.loss = out_loss, p.lp_out = out_logprob, p.stats_out = out_stats;
     return launch_policy<true, false>(fn, p, dtype, n, stream);
@@ -436,9 +448,7 @@ vie_status vie_policy_loss_step(const void *logits, vie_dtype dtype, int64_t n, 
     vie_status st = check_rows(fn, logits, dtype, n, V, ld, tokens, temperature);
     if (st == VIE_OK) st = check_terms(fn, n, p.terms);
     if (st == VIE_OK) st = check_floats(fn, n, grad_loss);
-    if (st == VIE_OK) st = check_floats(fn, n, out_loss);
-    if (st == VIE_OK) st = check_floats(fn, n, out_logprob);
-    if (st == VIE_OK) st = check_floats(fn, n, out_stats, true);
+    if (st == VIE_OK) st = check_results(fn, n, p.terms, out_loss, out_logprob, out_stats);
     if (st == VIE_OK) st = check_matrix(fn, "out_grad", out_grad, dtype, n, V, ld_grad);
     if (st != VIE_OK) return st;
     p.grad = grad_loss, p.loss = out_loss, p.lp_out = out_logprob, p.stats_out = out_stats;

@@ -193,6 +193,28 @@ def test_logits_into_rows_with_a_pitch(vie, dtype):
         assert (buf == 7.0).all()
 
 
+def test_logits_of_far_powers(vie):
+    """Rows near the ends of fp32 whose products are within it, and products beyond it.
+    A sum of codes and block scales, at most d 2688^2, is multiplied with s t, the product
+    of the rows' powers of two, which is exact but where it is below 2^-149: there it
+    becomes 0, and what is lost is less than d 2688^2 2^-149."""
+    x, w = _whole(5, 96, seed=51), _whole(40, 96, seed=52)
+    x = x / x.abs().amax(1, keepdim=True) * 6
+    w = w / w.abs().amax(1, keepdim=True) * 6
+    a = 2.0 ** torch.tensor([120.0, -120.0, 60.0, 0.0, -140.0])
+    b = 2.0 ** torch.tensor([-120.0, 120.0, 100.0, -20.0]).repeat(10)
+    x, w = x * a[:, None], w * b[:, None]
+    want = (x.double() @ w.double().t()).float()
+    got = vie.e2m1_logits(x.cuda(), vie.e2m1_quantize(w.cuda())).cpu()
+    values = ref.quantize(x)[3].double() @ ref.quantize(w)[3].double().t()  # (subnormal rows lose digits)
+    st = ref.quantize(x)[2][:, None] * ref.quantize(w)[2]
+    lost = torch.where(st < 2.0 ** -149, 96 * 2688.0 ** 2 * 2.0 ** -149, 0.0)
+    far = torch.isinf(want) | torch.isinf(got)
+    assert torch.equal(got[far], values.float()[far])
+    scale = (x.double().abs() @ w.double().abs().t()).float()
+    assert ((got - values).abs()[~far] <= 98 * ref.U * scale[~far] + 2.0 ** -148 + lost[~far]).all()
+
+
 def test_the_same_bits_again_on_streams_and_in_a_graph(vie):
     n, V, d = 40, 30011, 640
     x, w = _rows(n, d, "f32", seed=21).cuda(), _rows(V, d, "bf16", seed=22).cuda()

@@ -56,6 +56,17 @@ def test_row_refusals(name):
     assert _call(fn, ok, n=0, **none) == vie.VIE_OK  # nothing to do: no buffer is looked at
 
 
+@pytest.mark.parametrize("name", ["vie_policy_loss", "vie_policy_loss_step"])
+def test_results_in_place_of_terms_are_refused(name):
+    """Other CTAs of a row may still read them."""
+    fn = getattr(vie, name)
+    ok = dict(FORMS[name], out_loss=P + 16, out_logprob=P + 32, out_stats=P + 64)
+    for out in ("out_loss", "out_logprob", "out_stats"):
+        for term in ("old_logprob", "advantage", "ref_logprob"):
+            bad = dict(ok, **{term: P + 128, out: P + 128})
+            assert _call(fn, bad) == INVALID and "in place" in vie.vie_last_error()
+
+
 PAIRS = dict(n=20, offsets=P, pairs=2, beta=0.1, label_smoothing=0.0)
 PREFERENCE = {
     "vie_preference_loss": dict(dict(logprob=P, ref_logprob=P), **PAIRS, out_loss=P, out_margin=P),
