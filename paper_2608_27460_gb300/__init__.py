@@ -557,6 +557,8 @@ def _matrix(x, name):
     rows is copied."""
     if x.dim() != 2:
         raise ValueError(f"{name} must be a 2-D CUDA tensor")
+    if x.is_contiguous():
+        return x, max(x.shape[1], 1)
     ld = _pitch(x)
     if ld:
         return x, ld
@@ -571,25 +573,21 @@ def _given(x, name, shape, dtype, like):
     return x if x.is_contiguous() else x.contiguous()
 
 
-def _output(x, name, shape, dtype, like):
+def _contiguous_output(x, name, shape, dtype, like):
     """An output tensor: `x` if it fits, a new one if it is None."""
     if x is None:
         return _torch.empty(shape, dtype=dtype, device=like.device)
-    if x.dtype is not dtype or x.shape != shape or x.get_device() != like.get_device():  # (-1: a CPU tensor)
-        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {like.device}")
-    return x
-
-
-def _contiguous_output(x, name, shape, dtype, like):
-    x = _output(x, name, shape, dtype, like)
-    if not x.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+    if x.dtype is not dtype or x.shape != shape or x.get_device() != like.get_device() or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {like.device}")
     return x
 
 
 def _matrix_output(x, name, shape, dtype, like):
-    x = _output(x, name, shape, dtype, like)
-    ld = _pitch(x)
+    if x is None:
+        return _torch.empty(shape, dtype=dtype, device=like.device), max(shape[1], 1)
+    if x.dtype is not dtype or x.shape != shape or x.get_device() != like.get_device():
+        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {like.device}")
+    ld = max(shape[1], 1) if x.is_contiguous() else _pitch(x)
     if not ld:
         raise ValueError(f"{name} must be laid out by rows")
     return x, ld

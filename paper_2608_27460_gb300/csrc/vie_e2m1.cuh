@@ -16,10 +16,8 @@
 
 namespace vie {
 
-constexpr int kE2m1Block = 16;        // values per scale
 constexpr int kE2m1TileRows = 128;    // rows of a tile of scales
 constexpr int kE2m1TileBytes = 512;   // 128 rows x 4 scales
-constexpr float kE2m1RowTop = 2688.0f;  // 6 * 448
 
 // Bytes of a row of codes: two to a byte, the even column in the low half.
 __host__ __device__ inline int64_t e2m1_pitch(int d) { return static_cast<int64_t>((d + 31) / 32) * 16; }
