@@ -767,6 +767,17 @@ vie_status vie_e2m1_logits(const void *x_codes, const void *x_scales, const floa
                            void *out, vie_dtype out_dtype, int64_t ld_out, vie_stream stream);
 
 /*
+ * vie_e2m1_quantize_logits - vie_e2m1_quantize of x (device, dtype [n, d], row pitch
+ * ld) into x_* and vie_e2m1_logits of those, in one call: the head's rows are
+ * fetched while x is quantised.  x_* do not overlap w_*.  Arguments and errors as
+ * for those two.
+ */
+vie_status vie_e2m1_quantize_logits(const void *x, vie_dtype dtype, int64_t n, int64_t ld, void *x_codes,
+                                    void *x_scales, float *x_row_scales, const void *w_codes, const void *w_scales,
+                                    const float *w_row_scales, int64_t V, int32_t d, void *out, vie_dtype out_dtype,
+                                    int64_t ld_out, vie_stream stream);
+
+/*
  * vie_device_status - synchronises `stream`, then reads and clears the
  * library's device-side flag word of the current device.  Returns VIE_OK when
  * no kernel recorded a problem, VIE_ERR_DEVICE otherwise (vie_last_error()

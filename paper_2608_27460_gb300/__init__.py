@@ -65,7 +65,7 @@ EXPORTS = ("vie_head_create", "vie_head_destroy", "vie_head_get_props", "vie_hea
            "vie_embed_grad_workspace", "vie_embed_grad", "vie_sample_logits", "vie_token_logprobs",
            "vie_token_logprobs_grad", "vie_policy_loss", "vie_policy_loss_grad", "vie_policy_loss_step",
            "vie_preference_loss", "vie_preference_loss_grad", "vie_preference_loss_step", "vie_e2m1_bytes",
-           "vie_e2m1_quantize", "vie_e2m1_dequantize", "vie_e2m1_logits")
+           "vie_e2m1_quantize", "vie_e2m1_dequantize", "vie_e2m1_logits", "vie_e2m1_quantize_logits")
 
 
 class VieError(RuntimeError):
@@ -155,6 +155,8 @@ def load(path: str | None = None, build_if_missing: bool = True):
             "vie_e2m1_quantize": ([P, ctypes.c_int, I64, I32, I64, P, P, P, P, ctypes.c_int, I64, P], ctypes.c_int),
             "vie_e2m1_dequantize": ([P, P, P, I64, I32, P, ctypes.c_int, I64, P], ctypes.c_int),
             "vie_e2m1_logits": ([P, P, P, I64, P, P, P, I64, I32, P, ctypes.c_int, I64, P], ctypes.c_int),
+            "vie_e2m1_quantize_logits": ([P, ctypes.c_int, I64, I64, P, P, P, P, P, P, I64, I32, P, ctypes.c_int, I64,
+                                          P], ctypes.c_int),
         }
         for name, (args, res) in sig.items():
             fn = getattr(lib, name)
@@ -411,6 +413,13 @@ def vie_e2m1_logits(x_codes: int, x_scales: int, x_row_scales: int, n: int, w_co
                     w_row_scales: int, V: int, d: int, out: int, out_dtype: int, ld_out: int, stream: int = 0) -> int:
     return load().vie_e2m1_logits(x_codes, x_scales, x_row_scales, n, w_codes, w_scales, w_row_scales, V, d, out,
                                   out_dtype, ld_out, stream)
+
+
+def vie_e2m1_quantize_logits(x: int, dtype: int, n: int, ld: int, x_codes: int, x_scales: int, x_row_scales: int,
+                             w_codes: int, w_scales: int, w_row_scales: int, V: int, d: int, out: int, out_dtype: int,
+                             ld_out: int, stream: int = 0) -> int:
+    return load().vie_e2m1_quantize_logits(x, dtype, n, ld, x_codes, x_scales, x_row_scales, w_codes, w_scales,
+                                           w_row_scales, V, d, out, out_dtype, ld_out, stream)
 
 
 def vie_scatter_sparse_logits(idx: int, logits: int, batch: int, k: int, V: int, out: int,
@@ -1074,9 +1083,11 @@ def e2m1_logits(x, weights, out=None, out_dtype=None, x_quantized=None, stream=N
         out_dtype = _torch.float32 if out is None else out.dtype
     out, ld = _matrix_output(out, "out", (n, V), out_dtype, like)
     to = _dtype_code(out, "out")
-    if not given:
-        check(vie_e2m1_quantize(x.data_ptr(), _dtype_code(x, "x"), n, d, ld_x, *q, 0, VIE_DTYPE_F32, 0, stream))
-    check(vie_e2m1_logits(*q, n, *w, V, d, out.data_ptr(), to, ld, stream))
+    if given:
+        check(vie_e2m1_logits(*q, n, *w, V, d, out.data_ptr(), to, ld, stream))
+    else:
+        check(vie_e2m1_quantize_logits(x.data_ptr(), _dtype_code(x, "x"), n, ld_x, *q, *w, V, d, out.data_ptr(), to, ld,
+                                       stream))
     return out
 
 

@@ -22,6 +22,7 @@ struct QuantizeParams {
     void *values;  // or NULL
     int64_t n, ld, ld_values;
     int d;
+    int late;  // the next kernel may read what the kernels before this one have written, as soon as it starts
 };
 
 constexpr int kQuantizeThreads = 256;
@@ -153,8 +154,9 @@ __global__ void __launch_bounds__(kQuantizeThreads, kQuantizeCtas<T, TV, ROW_WAR
     const int tiles = e2m1_tiles(a.d);
     const int64_t pitch = e2m1_pitch(a.d);
     const bool vectors = (reinterpret_cast<uintptr_t>(a.x) & 15u) == 0 && a.ld * sizeof(T) % 16 == 0;
-    griddep_launch_dependents();
+    if (!a.late) griddep_launch_dependents();
     griddep_wait();
+    if (a.late) griddep_launch_dependents();
     // CTA c of kMany takes rows 8 (c % 4) + 0 .. 7 of each 32 of tile c / 4
     const int64_t first = kMany ? static_cast<int64_t>(blockIdx.x / 4) * kE2m1TileRows + 8 * (blockIdx.x % 4) + warp
                                 : static_cast<int64_t>(blockIdx.x);
@@ -319,6 +321,39 @@ static cudaError_t start_quantize(const QuantizeParams &p, vie_dtype values_dtyp
     return values_dtype == VIE_DTYPE_BF16 ? start_quantize<T, __nv_bfloat16>(p, s) : start_quantize<T, float>(p, s);
 }
 
+static cudaError_t launch_quantize(const QuantizeParams &p, vie_dtype dtype, vie_dtype values_dtype, cudaStream_t s) {
+    return dtype == VIE_DTYPE_BF16 ? start_quantize<__nv_bfloat16>(p, values_dtype, s)
+                                   : start_quantize<float>(p, values_dtype, s);
+}
+
+static vie_status check_logits(const char *fn, int64_t n, int64_t V, int32_t d, const void *x_codes,
+                               const void *x_scales, const float *x_row_scales, const void *w_codes,
+                               const void *w_scales, const float *w_row_scales, const void *out, vie_dtype out_dtype,
+                               int64_t ld_out) {
+    vie_status st = check_shape(fn, V, d);
+    if (st == VIE_OK && V < 1) st = fail(VIE_ERR_INVALID_ARG, "%s: V=0", fn);
+    if (st == VIE_OK && (n < 0 || n > VIE_MANY_MAX))
+        st = fail(VIE_ERR_INVALID_ARG, "%s: n=%lld outside [0, %d]", fn, static_cast<long long>(n), VIE_MANY_MAX);
+    if (st == VIE_OK) st = check_e2m1(fn, n, x_codes, x_scales, x_row_scales);
+    if (st == VIE_OK) st = check_e2m1(fn, n == 0 ? 0 : V, w_codes, w_scales, w_row_scales);
+    if (st == VIE_OK) st = check_matrix(fn, "out", out, out_dtype, n, V, ld_out);
+    return st;
+}
+
+static vie_status start_logits(const char *fn, const void *x_codes, const void *x_scales, const float *x_row_scales,
+                               int64_t n, const void *w_codes, const void *w_scales, const float *w_row_scales,
+                               int64_t V, int32_t d, bool w_ready, void *out, vie_dtype out_dtype, int64_t ld_out,
+                               cudaStream_t s) {
+    E2m1Product p = {};
+    cudaError_t e = device_flag_word(&p.flag);
+    if (e != cudaSuccess) return fail_cuda(e, fn);
+    p.x_scales = static_cast<const uint8_t *>(x_scales), p.w_scales = static_cast<const uint8_t *>(w_scales);
+    p.x_row_scales = x_row_scales, p.w_row_scales = w_row_scales;
+    p.out = out, p.ld = ld_out, p.n = n, p.V = V, p.d = d, p.w_ready = w_ready;
+    e = launch_e2m1_logits(p, static_cast<const uint8_t *>(x_codes), static_cast<const uint8_t *>(w_codes), out_dtype, s);
+    return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
+}
+
 }  // namespace vie
 
 using namespace vie;
@@ -349,9 +384,7 @@ vie_status vie_e2m1_quantize(const void *x, vie_dtype dtype, int64_t n, int32_t 
     p.x = x, p.n = n, p.d = d, p.ld = ld;
     p.codes = static_cast<uint8_t *>(out_codes), p.scales = static_cast<uint8_t *>(out_scales);
     p.row_scales = out_row_scales, p.values = out_values, p.ld_values = ld_values;
-    const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = dtype == VIE_DTYPE_BF16 ? start_quantize<__nv_bfloat16>(p, values_dtype, s)
-                                                  : start_quantize<float>(p, values_dtype, s);
+    const cudaError_t e = launch_quantize(p, dtype, values_dtype, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
 
@@ -376,22 +409,30 @@ vie_status vie_e2m1_logits(const void *x_codes, const void *x_scales, const floa
                            const void *w_codes, const void *w_scales, const float *w_row_scales, int64_t V, int32_t d,
                            void *out, vie_dtype out_dtype, int64_t ld_out, vie_stream stream) {
     const char *fn = "vie_e2m1_logits";
-    vie_status st = check_shape(fn, V, d);
-    if (st == VIE_OK && V < 1) st = fail(VIE_ERR_INVALID_ARG, "%s: V=0", fn);
-    if (st == VIE_OK && (n < 0 || n > VIE_MANY_MAX))
-        st = fail(VIE_ERR_INVALID_ARG, "%s: n=%lld outside [0, %d]", fn, static_cast<long long>(n), VIE_MANY_MAX);
-    if (st == VIE_OK) st = check_e2m1(fn, n, x_codes, x_scales, x_row_scales);
-    if (st == VIE_OK) st = check_e2m1(fn, n == 0 ? 0 : V, w_codes, w_scales, w_row_scales);
-    if (st == VIE_OK) st = check_matrix(fn, "out", out, out_dtype, n, V, ld_out);
+    const vie_status st = check_logits(fn, n, V, d, x_codes, x_scales, x_row_scales, w_codes, w_scales, w_row_scales, out,
+                                       out_dtype, ld_out);
     if (st != VIE_OK || n == 0) return st;
-    E2m1Product p = {};
-    cudaError_t e = device_flag_word(&p.flag);
+    return start_logits(fn, x_codes, x_scales, x_row_scales, n, w_codes, w_scales, w_row_scales, V, d, false, out,
+                        out_dtype, ld_out, static_cast<cudaStream_t>(stream));
+}
+
+vie_status vie_e2m1_quantize_logits(const void *x, vie_dtype dtype, int64_t n, int64_t ld, void *x_codes,
+                                    void *x_scales, float *x_row_scales, const void *w_codes, const void *w_scales,
+                                    const float *w_row_scales, int64_t V, int32_t d, void *out, vie_dtype out_dtype,
+                                    int64_t ld_out, vie_stream stream) {
+    const char *fn = "vie_e2m1_quantize_logits";
+    vie_status st = check_logits(fn, n, V, d, x_codes, x_scales, x_row_scales, w_codes, w_scales, w_row_scales, out,
+                                 out_dtype, ld_out);
+    if (st == VIE_OK) st = check_matrix(fn, "x", x, dtype, n, d, ld);
+    if (st != VIE_OK || n == 0) return st;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    QuantizeParams p = {};
+    p.x = x, p.n = n, p.d = d, p.ld = ld, p.late = 1;
+    p.codes = static_cast<uint8_t *>(x_codes), p.scales = static_cast<uint8_t *>(x_scales), p.row_scales = x_row_scales;
+    const cudaError_t e = launch_quantize(p, dtype, VIE_DTYPE_F32, s);
     if (e != cudaSuccess) return fail_cuda(e, fn);
-    p.x_scales = static_cast<const uint8_t *>(x_scales), p.w_scales = static_cast<const uint8_t *>(w_scales);
-    p.x_row_scales = x_row_scales, p.w_row_scales = w_row_scales;
-    p.out = out, p.ld = ld_out, p.n = n, p.V = V, p.d = d;
-    e = launch_e2m1_logits(p, static_cast<const uint8_t *>(x_codes), static_cast<const uint8_t *>(w_codes), out_dtype, static_cast<cudaStream_t>(stream));
-    return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
+    return start_logits(fn, x_codes, x_scales, x_row_scales, n, w_codes, w_scales, w_row_scales, V, d, true, out,
+                        out_dtype, ld_out, s);
 }
 
 }  // extern "C"

@@ -171,7 +171,8 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
     tc_fence_after_sync();
     const uint32_t tmem = sm.tmem_base;
     griddep_launch_dependents();
-    griddep_wait();  // the inputs may come from the kernels before this one
+    // The inputs may come from the kernels before this one.
+    if (warp != 0 || !p.w_ready) griddep_wait();
 
     // Tiles: x fastest, so that the CTAs that share rows of W run together.
     if (warp == 0 || warp == 3) {

@@ -15,6 +15,9 @@ struct E2m1Product {
     void *out;
     int64_t ld, n, V;
     int d;
+    // The kernel before this one on the stream has let this one start after all
+    // before it had ended, and does not write W: W may be read at once.
+    int w_ready;
     uint32_t *flag;
 };
 

@@ -99,6 +99,10 @@ LOGITS = dict(x_codes=P, x_scales=P, x_row_scales=P, n=4, w_codes=P, w_scales=P,
               out_dtype=F32, ld_out=100)
 
 
+BOTH = dict(x=P, dtype=F32, n=4, ld=50, x_codes=P, x_scales=P, x_row_scales=P, w_codes=P, w_scales=P, w_row_scales=P,
+            V=100, d=50, out=P, out_dtype=F32, ld_out=100)
+
+
 def test_e2m1_refusals():
     shape = [dict(n=-1), dict(n=vie.VIE_E2M1_N_MAX + 1), dict(d=0), dict(d=vie.VIE_D_MAX + 1)]
     parts = [dict(codes=0), dict(scales=0), dict(row_scales=0), dict(codes=P + 8), dict(scales=P + 4),
@@ -110,16 +114,21 @@ def test_e2m1_refusals():
             (vie.vie_e2m1_logits, LOGITS,
              [dict(n=-1), dict(n=vie.VIE_MANY_MAX + 1), dict(V=0), dict(V=vie.VIE_E2M1_N_MAX + 1), dict(d=0),
               dict(d=vie.VIE_D_MAX + 1), dict(out=0), dict(out=P + 2), dict(ld_out=99)]
-             + [{p + k: v for k, v in b.items()} for p in ("x_", "w_") for b in parts])):
+             + [{p + k: v for k, v in b.items()} for p in ("x_", "w_") for b in parts]),
+            (vie.vie_e2m1_quantize_logits, BOTH,
+             [dict(n=-1), dict(n=vie.VIE_MANY_MAX + 1), dict(V=0), dict(V=vie.VIE_E2M1_N_MAX + 1), dict(d=0),
+              dict(d=vie.VIE_D_MAX + 1), dict(out=0), dict(out=P + 2), dict(ld_out=99), dict(x=0), dict(x=P + 2),
+              dict(ld=49)] + [{p + k: v for k, v in b.items()} for p in ("x_", "w_") for b in parts])):
         for bad in bads:
             assert _call(fn, ok, **bad) == INVALID, bad
             assert fn.__name__ in vie.vie_last_error()
+    assert _call(vie.vie_e2m1_quantize_logits, BOTH, dtype=2) == UNSUPPORTED
     assert _call(vie.vie_e2m1_quantize, QUANTIZE, dtype=2) == UNSUPPORTED
     assert _call(vie.vie_e2m1_quantize, QUANTIZE, values_dtype=2) == UNSUPPORTED
     assert _call(vie.vie_e2m1_dequantize, DEQUANTIZE, out_dtype=5) == UNSUPPORTED
     assert _call(vie.vie_e2m1_logits, LOGITS, out_dtype=2) == UNSUPPORTED
     for fn, ok in ((vie.vie_e2m1_quantize, QUANTIZE), (vie.vie_e2m1_dequantize, DEQUANTIZE),
-                   (vie.vie_e2m1_logits, LOGITS)):
+                   (vie.vie_e2m1_logits, LOGITS), (vie.vie_e2m1_quantize_logits, BOTH)):
         assert _call(fn, ok, n=0, **{p: 0 for p in ok if ok[p] == P}) == vie.VIE_OK
 
 
