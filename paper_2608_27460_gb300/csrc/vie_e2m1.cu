@@ -136,6 +136,11 @@ struct None {};  // no values wanted
 // CTA's scales (gathered in shared memory) are written 128 bytes at a time.
 // ROW_WARPS 8: a CTA per row, for the latency of few rows, and for long ones.
 // NV: vectors of eight values that a lane keeps.
+//
+// Bound by bytes where rows lie at 16-byte addresses: 262144 x 1152 bf16 145 us, with
+// bf16 values 231 (of a copy's rate 0.79 and 0.88), fp32 234 (0.87), 16384 x 8192 bf16
+// with values 99 (0.91).  Elsewhere values are moved one by one: 262144 x 1001 with
+// values 483 us (0.37).  32 x 1152 fp32: 1.4 us.
 // CTAs per SM: what the registers of a row leave (262144 x 1152 bf16 with values: 229
 // us with three, 262 with two; without values 141 with four, 155 with three).
 template <typename T, typename TV, int ROW_WARPS, int NV>
@@ -296,14 +301,18 @@ static vie_status check_e2m1(const char *fn, int64_t n, const void *codes, const
     return VIE_OK;
 }
 
-// Rows from which on a warp takes each: CTAs of 32 rows for most of the chip.
-constexpr int64_t kQuantizeManyRows = 4096;
+// Rows from which on a warp takes each.  A warp's four rows one after the other are a
+// latency that few rows do not hide, a CTA per row a cost that many add up; the longer
+// the rows, the later the second is the larger (bf16, us by warps / by CTAs: 64 columns,
+// 1024 rows 2.6 / 2.2, 2048 2.8 / 3.3; 640, 2048 3.8 / 3.5, 4096 5.3 / 5.9; 1152, 4096
+// 8.0 / 6.4, 8192 8.8 / 11.6; 2048, 4096 11.0 / 7.1, 8192 11.9 / 13.0, 16384 16.5 / 25.1).
+static bool by_warps(int64_t n, int d) { return d <= 2048 && n >= 1024 + 4 * static_cast<int64_t>(d); }
 
 template <typename T, typename TV>
 static cudaError_t start_quantize(const QuantizeParams &p, cudaStream_t s) {
     const int64_t rows = (p.n + kE2m1TileRows - 1) / kE2m1TileRows * kE2m1TileRows;  // with those that have scales alone
     constexpr int W = kQuantizeWarps, NT = kQuantizeThreads;
-    if (p.n >= kQuantizeManyRows && p.d <= 2048) {
+    if (by_warps(p.n, p.d)) {
         const dim3 grid(static_cast<unsigned>(rows / 32));
         const size_t smem = static_cast<size_t>(e2m1_tiles(p.d)) * 128;
         return p.d <= 1024 ? launch(quantize_kernel<T, TV, 1, 4>, grid, NT, smem, s, p)

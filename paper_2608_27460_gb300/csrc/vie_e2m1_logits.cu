@@ -6,7 +6,7 @@
 // scales s, t (powers of two): block-scaled MMAs of 128 vocabulary rows by up to
 // 256 rows of x and 64 columns, scales and accumulators in TMEM.
 //
-// A persistent CTA per SM takes tiles of 128 vocabulary rows by BN rows of x.  A
+// A persistent CTA per SM takes tiles of 128 vocabulary rows by BN rows of x.  Two
 // producer threads fill a ring of stages of 256 or 512 columns: codes by TMA boxes
 // of 128 bytes a row (columns and rows beyond the matrix read as 0), scales by bulk
 // copies of their 512-byte tiles, which lie in memory as TMEM wants them.  Four
@@ -18,6 +18,19 @@
 // (tcgen05.cp, which takes scales to TMEM without registers, runs in order with
 // the MMAs, some 100 cycles a copy of 512 bytes: 51 us for one row of x on 262144 x
 // 1152.)
+//
+// Measured, on the device alone, inputs of other calls in between (the floor: bytes
+// at the copy rate, 6.79 TB/s):
+//   262144 x 1152, 1 row of x, fp32    29.0 us (25.2)     bytes: 171 MB of the head's
+//   262144 x 1152, 32 rows, fp32       36.9 us (30.0)     bytes; writes of 512 a row and tile
+//   100003 x 1000, 129 rows, fp32      23.7 us (15.9)     6 tiles for most SMs, 5.14 on average
+//   128256 x 2048, 256 rows, bf16      43.6 us (31.5)
+//   128256 x 2048, 2048 rows, bf16      256 us (99.5; 4.2 PFLOP/s)
+// Many rows: the tensor pipe is 44 % busy.  A stage of 256 columns moves about 126 KB
+// through shared memory (54 in by TMA, 48 read by the MMAs, 24 by the scale warps,
+// four of which read the same), 980 cycles of it, and the accumulator's 128 columns
+// per warp are drained between tiles.  Multicasting x to pairs of CTAs (254 us) and MMAs
+// of pairs of CTAs (268 us; 232 instead of 189 at 151936 x 1024) gained nothing.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -460,6 +473,10 @@ static cudaError_t start_e2m1_logits(const E2m1Product &p, const uint8_t *x_code
     return cudaLaunchKernelEx(&cfg, kernel, map_w, map_x, map_x_last, p, v_tiles, x_tiles, last_rows);
 }
 
+// Tiles as wide as the rows of x: every column of an MMA costs time, whether it is
+// stored or not.  Above 128 rows tiles of 256 are the faster ones at nearly all sizes
+// (128256 x 2048 bf16, us with tiles of 256 / of 128: 129 rows 35 / 46, 256 42 / 47, 512 72 / 86,
+// 2048 254 / 327; 100003 x 1000, 200 rows 24.8 / 24.0): they read W once per 256 rows.
 template <typename T, bool WORDS>
 static cudaError_t start_by_rows(const E2m1Product &p, const uint8_t *x_codes, const uint8_t *w_codes,
                                  cudaStream_t stream) {

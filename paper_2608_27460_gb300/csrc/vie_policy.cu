@@ -67,7 +67,20 @@ __device__ __forceinline__ float2 policy_terms(const PolicyTerms &a, int64_t row
 // log-probabilities themselves or of the policy loss.
 //
 // A row is a cluster's, a slice of it a CTA's; for both, the slice is read again,
-// from L2 as long as the slices in progress fit it (vie_row_softmax.cuh).
+// from L2 as long as the slices in progress fit it (vie_row_softmax.cuh).  The
+// gradient is the softmax times a number of the row, but for the token's own value,
+// which the thread that has written its vector replaces: no barrier in between.
+//
+// Bound by bytes.  Measured on bf16 logits, and as a share of the time that a copy of
+// the bytes read and written once would take:
+//   log-probabilities  262144 x 2048: 157 us (1.0), 128256 x 2048: 83 (0.93), 20011 x 4096: 42 (0.57)
+//   their gradient     151936 x 4096: 363 us (1.0), 128256 x 2048: 159 (0.97), 20011 x 4096: 55 (0.87)
+//   both               151936 x 4096: 450 us (0.82), 262144 x 1024: 195 (0.81), 32000 x 4096:
+//                      96 (0.80); fp32 151936 x 2048: 440 (0.83); 1000003 x 128: 125 (0.60)
+// What is left in the last: each row's exchange, which the CTAs' other rows hide in
+// part (64 % of issue slots used, DRAM 59 % busy; DRAM reads 316 MB of 311, the second
+// reading comes from L2).  Short rows: a row's chain of token, slice, sum and result,
+// of which a CTA has one at a time.
 template <typename T, bool FWD, bool BWD>
 __global__ void __launch_bounds__(kRowThreads, 4) policy_kernel(const PolicyParams a, int log2_slices) {
     constexpr int U = kUnroll<T, FWD, BWD>;
@@ -262,7 +275,10 @@ __device__ __forceinline__ float sum_ratios(const PreferenceParams &a, int i, in
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// A cluster of CTAs of NT threads per pair, whose sums meet in shared memory.
+// A cluster of CTAs of NT threads per pair, whose sums meet in shared memory.  Bound
+// by latency: the offsets, the tokens, the exchange, the gradient (loss and gradient of
+// 4 pairs of 2 x 300 tokens 2.8 us, of 256 of 2 x 2048 4.5, of one of 2 x 16384 3.9, with
+// one CTA 10.9, of one of 2 x 400000 19, with one CTA 215).
 template <bool FWD, bool BWD, int NT>
 __global__ void __launch_bounds__(NT) preference_kernel(const PreferenceParams a, int ctas) {
     __shared__ float4 sums[NT / 32];
@@ -325,7 +341,8 @@ static vie_status launch_preference(const char *fn, PreferenceParams &p, vie_str
         if (BWD && p.n > 0) e = cudaMemsetAsync(p.grad, 0, sizeof(float) * static_cast<size_t>(p.n), s);
         return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
     }
-    // Threads for about 8 tokens each where pairs are few: up to eight CTAs, of 1024
+    // Threads for about 8 tokens each where pairs are too few for the chip (256 pairs of
+    // 2 x 2048 tokens: 4.5 us with one CTA each, 5.7 with two): up to eight CTAs, of 1024
     // threads where those of 256 would have more than 32 tokens each left.
     const int64_t mean = p.n / p.pairs;
     int ctas = 1;

@@ -86,3 +86,79 @@ def test_a_preference_update_against_autograd(vie):
     got = p.preference_gradient(seen, 0.3)
     assert (got.double() - losses.detach()).abs().max() < 1e-4
     _check_grad(p, E, h, z, before, drawn, torch.full_like(lp, 0.3 / len(losses)).detach())
+
+
+def test_every_call_on_a_stream_of_its_own(vie):
+    """The same results as on the current stream, ready when the stream is."""
+    g = torch.Generator(device="cuda").manual_seed(11)
+    n, V, d = 30, 5003, 200
+    z = torch.randn((n, V), generator=g, device="cuda")
+    tok = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    w, adv = torch.rand((n,), generator=g, device="cuda"), torch.randn((n,), generator=g, device="cuda")
+    lp, stats = vie.token_logprobs(z, tok)
+    ends = torch.tensor([0, 7, 11, 20, 28], dtype=torch.int32, device="cuda")
+    margin, two = torch.tensor([0.3, -0.2], device="cuda"), torch.ones(2, device="cuda")
+    x = torch.randn((n, d), generator=g, device="cuda")
+    head = vie.e2m1_quantize(torch.randn((700, d), generator=g, device="cuda"))
+
+    def parts(q):
+        return q.codes, q.scales, q.row_scales
+
+    calls = [lambda **k: vie.token_logprobs(z, tok, **k), lambda **k: vie.token_logprobs_grad(z, tok, stats, w, **k),
+             lambda **k: vie.policy_loss(z, tok, lp, adv, **k),
+             lambda **k: vie.policy_loss_grad(z, tok, lp, adv, lp, stats, w, **k),
+             lambda **k: vie.policy_loss_step(z, tok, lp, adv, w, ref_logprob=lp, kl_coef=0.1, **k),
+             lambda **k: vie.preference_loss(lp, ends, **k),
+             lambda **k: vie.preference_loss_grad(margin, ends, two, n, **k),
+             lambda **k: vie.preference_loss_step(lp, ends, two, **k),
+             lambda **k: parts(vie.e2m1_quantize(x, **k)), lambda **k: vie.e2m1_dequantize(head, **k),
+             lambda **k: vie.e2m1_logits(x, head, **k)]
+    s = torch.cuda.Stream()
+    for call in calls:
+        want = call()
+        s.wait_stream(torch.cuda.current_stream())
+        got = call(stream=s)
+        s.synchronize()
+        want, got = ((v,) if torch.is_tensor(v) else v for v in (want, got))
+        assert len(want) == len(got) and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_run_of_calls_captured_and_replayed(vie):
+    """Quantise the head, draw, score and step in one graph: other weights and states
+    between replays give what the calls give one by one."""
+    g = torch.Generator(device="cuda").manual_seed(13)
+    V, m, n = 3001, 96, 40
+    E, h = torch.empty((V, m), device="cuda"), torch.empty((n, m), device="cuda")
+    u, adv = torch.empty((n,), device="cuda"), torch.empty((n,), device="cuda")
+    weight = torch.full((n,), 1.0 / n, device="cuda")
+    head, room = vie.E2m1.empty(V, m), vie.E2m1.empty(n, m)
+    z = torch.empty((n, V), dtype=torch.bfloat16, device="cuda")
+
+    def refill():
+        for t in (E, h, adv):
+            t.normal_(generator=g)
+        u.uniform_(generator=g)
+
+    def calls(z):
+        vie.e2m1_quantize(E, out=head)
+        vie.e2m1_logits(h, head, out=z, x_quantized=room)
+        tok, _ = vie.sample_logits(z, u)
+        old, _ = vie.token_logprobs(z, tok)
+        loss, _, dz = vie.policy_loss_step(z, tok, old, adv, weight, out_grad=z)
+        return tok, old, loss, dz
+
+    refill()
+    calls(z)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        got = calls(z)
+    for _ in range(3):
+        refill()
+        graph.replay()
+        torch.cuda.synchronize()
+        seen = [t.clone() for t in got]
+        want = calls(torch.empty_like(z))
+        assert all(torch.equal(a, b) for a, b in zip(seen, want))
+    assert vie.vie_device_status() == vie.VIE_OK
