@@ -73,17 +73,23 @@ __device__ __forceinline__ float2 policy_terms(const PolicyTerms &a, int64_t row
 //
 // Bound by bytes.  Measured on bf16 logits, and as a share of the time that a copy of
 // the bytes read and written once would take:
-//   log-probabilities  262144 x 2048: 157 us (1.0), 128256 x 2048: 83 (0.93), 20011 x 4096: 42 (0.57)
-//   their gradient     151936 x 4096: 363 us (1.0), 128256 x 2048: 159 (0.97), 20011 x 4096: 55 (0.87)
+//   log-probabilities  262144 x 2048: 157 us (1.0), 128256 x 2048: 83 (0.93), 20011 x 4096: 38 (0.64)
+//   their gradient     151936 x 4096: 363 us (1.0), 128256 x 2048: 159 (0.97), 20011 x 4096: 55 (0.88)
 //   both               151936 x 4096: 450 us (0.82), 262144 x 1024: 195 (0.81), 32000 x 4096:
-//                      96 (0.80); fp32 151936 x 2048: 440 (0.83); 1000003 x 128: 125 (0.60)
+//                      96 (0.80); fp32 151936 x 2048: 433 (0.85); 1000003 x 128: 125 (0.60)
 // What is left in the last: each row's exchange, which the CTAs' other rows hide in
 // part (64 % of issue slots used, DRAM 59 % busy; DRAM reads 316 MB of 311, the second
 // reading comes from L2).  Short rows: a row's chain of token, slice, sum and result,
 // of which a CTA has one at a time.
+//
+// Vectors in flight per thread, and four CTAs per SM (loss and gradient of 151936 x 4096
+// bf16: 450 us; eight vectors with three CTAs 476, four with five 484, two with eight 561;
+// log-probabilities of 20011 x 4096: 38 us, 42 with eight vectors and four CTAs).
+constexpr int kPolicyUnroll = 6;
+
 template <typename T, bool FWD, bool BWD>
 __global__ void __launch_bounds__(kRowThreads, 4) policy_kernel(const PolicyParams a, int log2_slices) {
-    constexpr int U = kUnroll<T, FWD, BWD>;
+    constexpr int U = kPolicyUnroll;
     __shared__ RowSmem sm;
     const int tid = threadIdx.x, warp = tid >> 5;
     const int slices = 1 << log2_slices, rank = blockIdx.x & (slices - 1);
