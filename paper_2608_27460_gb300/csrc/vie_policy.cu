@@ -44,19 +44,32 @@ struct PolicyParams {
     uint32_t *flag;
 };
 
+// What a row's loss is made of besides its logits, read before those.
+struct RowTerms {
+    float old_lp = 0.0f, advantage = 0.0f, ref_lp = 0.0f, weight = 0.0f;
+    template <bool BWD>
+    __device__ __forceinline__ void load(const PolicyParams &a, int64_t row) {
+        if (a.terms.old_lp != nullptr) {
+            old_lp = a.terms.old_lp[row], advantage = a.terms.advantage[row];
+            if (a.terms.kl != 0.0f) ref_lp = a.terms.ref_lp[row];
+        }
+        if (BWD) weight = a.grad[row];
+    }
+};
+
 // The loss of one token and its derivative by lp:
 //   r = exp(lp - old), A the advantage,
 //   loss  = -min(r A, clip(r, 1 - low, 1 + high) A) + kl (exp(ref - lp) - (ref - lp) - 1)
 //   slope = -A r if r A is the smaller one, else 0, + kl (1 - exp(ref - lp))
 // No advantage, no first term, whatever the ratio; the second is +inf where one
 // of the two policies alone rules the token out.
-__device__ __forceinline__ float2 policy_terms(const PolicyTerms &a, int64_t row, float lp) {
-    const float r = expf(lp - a.old_lp[row]), A = a.advantage[row];
+__device__ __forceinline__ float2 policy_terms(const PolicyTerms &a, const RowTerms &t, float lp) {
+    const float r = expf(lp - t.old_lp), A = t.advantage;
     const float held = r < 1.0f - a.low ? 1.0f - a.low : r > 1.0f + a.high ? 1.0f + a.high : r;  // (NaN stays)
     const float free_ = A == 0.0f ? 0.0f : r * A, bound = A == 0.0f ? 0.0f : held * A;
     float loss = free_ <= bound ? -free_ : -bound, slope = free_ > bound ? 0.0f : -free_;
     if (a.kl != 0.0f) {
-        const float x = a.ref_lp[row] - lp, e = expm1f(x);
+        const float x = t.ref_lp - lp, e = expm1f(x);
         loss += a.kl * (e == INFINITY ? INFINITY : e - x);
         slope -= a.kl * e;
     }
@@ -87,14 +100,81 @@ __device__ __forceinline__ float2 policy_terms(const PolicyTerms &a, int64_t row
 // log-probabilities of 20011 x 4096: 38 us, 42 with eight vectors and four CTAs).
 constexpr int kPolicyUnroll = 6;
 
+// One CTA's part of a row with a token.
+template <typename T, bool FWD, bool BWD>
+struct PolicyRow {
+    const PolicyParams &a;
+    int64_t row;
+    int token;
+    Slice<T> sl;
+    GradSlice<T> out;
+    float c;
+    RowTerms terms;
+    // The thread that the token's vector is: it reads the token's logit before it
+    // writes a gradient there (which may be the same place), and afterwards
+    // replaces what the loop has written.
+    bool here;
+
+    __device__ __forceinline__ PolicyRow(const PolicyParams &a_, int64_t row_, int token_, int log2_slices, int rank)
+        : a(a_), row(row_), token(token_), sl(static_cast<const T *>(a.logits) + row * a.ld, a.V, log2_slices, rank),
+          out(static_cast<T *>(a.grad_logits) + row * a.ld_grad, sl), c(exponent_factor(a.T)) {
+        const int at = token - sl.e0, vec = at >= 0 ? at / Slice<T>::kVec : -1;
+        here = vec >= 0 && vec < sl.nv &&
+               static_cast<int>(threadIdx.x) ==
+                   (vec < sl.lo ? 0 : vec >= sl.hi ? (sl.nv > 1 ? 1 : 0) : (vec - sl.lo) % kRowThreads);
+    }
+    __device__ __forceinline__ bool live() const { return token >= 0 && token < a.V; }
+    __device__ __forceinline__ void write_row(float loss, float lp, float m, float s) const {
+        if (a.terms.old_lp != nullptr) a.loss[row] = loss;
+        a.lp_out[row] = lp;
+        if (a.stats_out != nullptr) {
+            a.stats_out[2 * row] = m;
+            a.stats_out[2 * row + 1] = s;
+        }
+    }
+    // An empty slot's results.
+    __device__ __forceinline__ void write_empty(bool leads) const {
+        if (BWD) clear_gradient(sl, out);
+        if (leads && token >= a.V) atomicOr(a.flag, kErrTokenIndex);
+        if (FWD && leads) write_row(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    // This CTA's statistics to sm.part, and the token's logit to *z_token (read while the
+    // slice is, and before anything is written).
+    __device__ __forceinline__ void measure(RowSmem &sm, float *z_token) {
+        T raw;
+        if (threadIdx.x == 0) raw = sl.z[token];
+        terms.load<BWD>(a, row);
+        slice_statistics<T, kPolicyUnroll, BWD>(sl, c, sm);
+        if (threadIdx.x == 0) *z_token = load_value(&raw);
+    }
+    __device__ __forceinline__ float log_prob(float z_token, float m, float s) const {
+        return s == 0.0f ? -INFINITY : (z_token - m) / a.T - logf(s);
+    }
+    // The gradient, and the row's results if this is the thread that writes them.
+    __device__ __forceinline__ void finish(float z_token, float lp, float m, float s, bool leads) const {
+        float2 loss = make_float2(0.0f, 1.0f);
+        if (a.terms.old_lp != nullptr) loss = policy_terms(a.terms, terms, lp);
+        if (BWD) {
+            const Exponent e{finite_max(m), c};
+            // (a weight of 0 masks a row, whatever its slope)
+            const float slope = terms.weight == 0.0f ? 0.0f : terms.weight * loss.y / a.T;
+            const float inv = s == 0.0f ? 0.0f : 1.0f / s;
+            if (slope == 0.0f) clear_gradient(sl, out);
+            else store_softmax<T, kPolicyUnroll>(sl, out, e, -slope * inv);
+            if (here && slope != 0.0f) store_value(out.g + token, slope * (1.0f - e(z_token) * inv));
+        }
+        if (FWD && leads) write_row(loss.x, lp, m, s);
+    }
+};
+
 template <typename T, bool FWD, bool BWD>
 __global__ void __launch_bounds__(kRowThreads, 4) policy_kernel(const PolicyParams a, int log2_slices) {
-    constexpr int U = kPolicyUnroll;
     __shared__ RowSmem sm;
-    const int tid = threadIdx.x, warp = tid >> 5;
+    __shared__ float z_shared;
+    const int tid = threadIdx.x;
     const int slices = 1 << log2_slices, rank = blockIdx.x & (slices - 1);
-    const int64_t row = blockIdx.x >> log2_slices;
-    if (FWD) {
+    const bool leads = rank == 0 && tid == 0;
+    if (FWD && slices > 1) {
         if (tid == 0) sm.init();
         __syncthreads();
         cluster_arrive_relaxed();  // all CTAs of the cluster run and wait, before their memory is written
@@ -102,63 +182,33 @@ __global__ void __launch_bounds__(kRowThreads, 4) policy_kernel(const PolicyPara
     griddep_launch_dependents();
     griddep_wait();  // the inputs may come from the kernel before this one
 
-    const int token = a.tokens[row];
-    const bool live = token >= 0 && token < a.V;
-    if (token >= a.V && rank == 0 && tid == 0) atomicOr(a.flag, kErrTokenIndex);
-    const Slice<T> sl(static_cast<const T *>(a.logits) + row * a.ld, a.V, log2_slices, rank);
-    const GradSlice<T> out(static_cast<T *>(a.grad_logits) + row * a.ld_grad, sl);
-    const bool policy = a.terms.old_lp != nullptr;
-    auto write_row = [&](float loss, float lp, float m, float s) {
-        if (policy) a.loss[row] = loss;
-        a.lp_out[row] = lp;
-        if (a.stats_out != nullptr) {
-            a.stats_out[2 * row] = m;
-            a.stats_out[2 * row + 1] = s;
-        }
-    };
-    if (FWD) cluster_wait();
-    if (!live) {
-        if (BWD) clear_gradient(sl, out);
-        if (FWD && rank == 0 && tid == 0) write_row(0.0f, 0.0f, 0.0f, 0.0f);
+    const int64_t row = blockIdx.x >> log2_slices;
+    PolicyRow<T, FWD, BWD> r(a, row, a.tokens[row], log2_slices, rank);
+    if (FWD && slices > 1) cluster_wait();
+    if (!r.live()) {
+        r.write_empty(leads);
         return;
     }
-    const float c = exponent_factor(a.T);
-    // The thread that the token's vector is: it reads the token's logit before it
-    // writes a gradient there (which may be the same place), and afterwards
-    // replaces what the loop has written.
-    const int at = token - sl.e0, vec = at >= 0 ? at / Slice<T>::kVec : -1;
-    const bool here = vec >= 0 && vec < sl.nv &&
-                      tid == (vec < sl.lo ? 0 : vec >= sl.hi ? (sl.nv > 1 ? 1 : 0) : (vec - sl.lo) % kRowThreads);
-    float m, s, z_token = 0.0f, lp;
+    float m, s, z_token = 0.0f, lp = 0.0f;
     if (FWD) {
-        T raw;  // read while the slice is, and consumed before the row's slices meet
-        if (tid == 0 || here) raw = sl.z[token];
-        slice_statistics<T, U, BWD>(sl, c, sm);
-        if (tid == 0 || here) z_token = load_value(&raw);
-        __shared__ float z_shared;
-        if (tid == 0) z_shared = z_token;
+        r.measure(sm, &z_shared);
         __syncthreads();
-        if (warp == 0) send_partial(sm, slices, rank, c);
-        join_partials(a.flag, sm, slices, c, &m, &s);
+        if (slices > 1) {
+            if (tid < 32) send_partial(sm, slices, rank, r.c);
+            join_partials(a.flag, sm, slices, r.c, &m, &s);
+        } else {
+            join_warps(sm, r.c, &m, &s);
+        }
         z_token = z_shared;
-        lp = s == 0.0f ? -INFINITY : (z_token - m) / a.T - logf(s);
+        lp = r.log_prob(z_token, m, s);
     } else {
         m = a.stats_in[2 * row];
         s = a.stats_in[2 * row + 1];
-        if (here) z_token = load_value(sl.z + token);
-        lp = policy ? a.lp_in[row] : 0.0f;
+        if (r.here) z_token = load_value(r.sl.z + r.token);
+        if (a.terms.old_lp != nullptr) lp = a.lp_in[row];
+        r.terms.template load<BWD>(a, row);
     }
-    float2 terms = make_float2(0.0f, 1.0f);
-    if (policy) terms = policy_terms(a.terms, row, lp);
-    if (BWD) {
-        const Exponent e{finite_max(m), c};
-        const float weight = a.grad[row];  // (one of 0 masks a row, whatever its slope)
-        const float slope = weight == 0.0f ? 0.0f : weight * terms.y / a.T, inv = s == 0.0f ? 0.0f : 1.0f / s;
-        if (slope == 0.0f) clear_gradient(sl, out);
-        else store_softmax<T, U>(sl, out, e, -slope * inv);
-        if (here && slope != 0.0f) store_value(out.g + token, slope * (1.0f - e(z_token) * inv));
-    }
-    if (FWD && rank == 0 && tid == 0) write_row(terms.x, lp, m, s);
+    r.finish(z_token, lp, m, s, leads);
 }
 
 template <typename T, bool FWD, bool BWD>
@@ -170,7 +220,7 @@ static cudaError_t start_policy(const PolicyParams &p, int64_t n, int slices, cu
             prepared.once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); });
         if (e != cudaSuccess) return e;
     }
-    RowLaunch l(n * slices, FWD ? slices : 0, 0, s);
+    RowLaunch l(n * slices, FWD && slices > 1 ? slices : 0, 0, s);
     return cudaLaunchKernelEx(&l.cfg, kernel, p, log2_of(slices));
 }
 

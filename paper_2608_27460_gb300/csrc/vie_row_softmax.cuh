@@ -172,13 +172,19 @@ __device__ __forceinline__ void slice_statistics(const Slice<T> &sl, float c, Ro
     if ((threadIdx.x & 31) == 0) sm.part[threadIdx.x >> 5] = make_float2(m, s);
 }
 
-// One warp: the maximum and sum of this CTA's slice, joined from its warps'
-// (sm.part, written before the last barrier), to all CTAs of the row.
-__device__ __forceinline__ void send_partial(RowSmem &sm, int slices, int rank, float c) {
+// The maximum and sum of this CTA's slice, joined from its warps' (sm.part, written
+// before the last barrier), in any warp.
+__device__ __forceinline__ void join_warps(const RowSmem &sm, float c, float *m, float *s) {
     const int lane = threadIdx.x & 31;
     const float2 part = lane < kRowWarps ? sm.part[lane] : make_float2(-INFINITY, 0.0f);
-    const float m = warp_max(part.x);
-    const float s = warp_sum(part.y != 0.0f ? part.y * Exponent{finite_max(m), c}(finite_max(part.x)) : 0.0f);
+    *m = warp_max(part.x);
+    *s = warp_sum(part.y != 0.0f ? part.y * Exponent{finite_max(*m), c}(finite_max(part.x)) : 0.0f);
+}
+// One warp: those to all CTAs of the row.
+__device__ __forceinline__ void send_partial(RowSmem &sm, int slices, int rank, float c) {
+    const int lane = threadIdx.x & 31;
+    float m, s;
+    join_warps(sm, c, &m, &s);
     if (lane == 0) mbar_arrive_expect_tx(&sm.gather_bar, 8u * slices);
     if (lane < slices)
         cluster_send(cluster_addr(&sm.gathered[rank], lane), make_float2(m, s),
