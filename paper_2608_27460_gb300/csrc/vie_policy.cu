@@ -86,22 +86,25 @@ __device__ __forceinline__ float2 policy_terms(const PolicyTerms &a, const RowTe
 //
 // Bound by bytes.  Measured on bf16 logits, and as a share of the time that a copy of
 // the bytes read and written once would take:
-//   log-probabilities  262144 x 2048: 157 us (1.0), 128256 x 2048: 83 (0.93), 20011 x 4096: 38 (0.64)
-//   their gradient     151936 x 4096: 363 us (1.0), 128256 x 2048: 159 (0.97), 20011 x 4096: 55 (0.88)
-//   both               151936 x 4096: 450 us (0.82), 262144 x 1024: 195 (0.81), 32000 x 4096:
-//                      96 (0.80); fp32 151936 x 2048: 433 (0.85); 1000003 x 128: 125 (0.60)
+//   log-probabilities  262144 x 1024: 79 us (1.0), 128256 x 2048: 83 (0.93), 20011 x 4096: 34 (0.71)
+//   their gradient     151936 x 4096: 363 us (1.0), 128256 x 2048: 159 (0.97), 20011 x 4096: 54 (0.89)
+//   both               151936 x 4096: 446 us (0.82), 262144 x 1024: 193 (0.82), 32000 x 4096:
+//                      92 (0.84); fp32 151936 x 2048: 426 (0.86); 1000003 x 128: 125 (0.60)
 // What is left in the last: each row's exchange, which the CTAs' other rows hide in
 // part (64 % of issue slots used, DRAM 59 % busy; DRAM reads 316 MB of 311, the second
 // reading comes from L2).  Short rows: a row's chain of token, slice, sum and result,
-// of which a CTA has one at a time.
+// of which a CTA has one at a time (CTAs that stay for more rows, with the next token
+// read ahead, were slower: 98 us for both at 20011 x 4096, 68 without; prefetching rows
+// before their token is known gains 2 %, and loses it where a tenth of them have none).
 //
-// Vectors in flight per thread, and four CTAs per SM (loss and gradient of 151936 x 4096
-// bf16: 450 us; eight vectors with three CTAs 476, four with five 484, two with eight 561;
-// log-probabilities of 20011 x 4096: 38 us, 42 with eight vectors and four CTAs).
-constexpr int kPolicyUnroll = 6;
+// U vectors in flight per thread, four CTAs per SM: six (loss and gradient of 151936 x
+// 4096 bf16, before a row's terms were read ahead: 450 us; eight vectors with three CTAs
+// 476, four with five 484, two with eight 561); for log-probabilities alone eight, but
+// where a slice leaves much of its last turn empty with them (262144 x 2048 148 us, 152
+// with six; 65536 x 4096 75, 78; 20011 x 4096 34, 31; 151936 x 64 in eight slices 6.7, 5.8).
 
 // One CTA's part of a row with a token.
-template <typename T, bool FWD, bool BWD>
+template <typename T, bool FWD, bool BWD, int U>
 struct PolicyRow {
     const PolicyParams &a;
     int64_t row;
@@ -144,7 +147,7 @@ struct PolicyRow {
         T raw;
         if (threadIdx.x == 0) raw = sl.z[token];
         terms.load<BWD>(a, row);
-        slice_statistics<T, kPolicyUnroll, BWD>(sl, c, sm);
+        slice_statistics<T, U, BWD>(sl, c, sm);
         if (threadIdx.x == 0) *z_token = load_value(&raw);
     }
     __device__ __forceinline__ float log_prob(float z_token, float m, float s) const {
@@ -160,14 +163,14 @@ struct PolicyRow {
             const float slope = terms.weight == 0.0f ? 0.0f : terms.weight * loss.y / a.T;
             const float inv = s == 0.0f ? 0.0f : 1.0f / s;
             if (slope == 0.0f) clear_gradient(sl, out);
-            else store_softmax<T, kPolicyUnroll>(sl, out, e, -slope * inv);
+            else store_softmax<T, U>(sl, out, e, -slope * inv);
             if (here && slope != 0.0f) store_value(out.g + token, slope * (1.0f - e(z_token) * inv));
         }
         if (FWD && leads) write_row(loss.x, lp, m, s);
     }
 };
 
-template <typename T, bool FWD, bool BWD>
+template <typename T, bool FWD, bool BWD, int U>
 __global__ void __launch_bounds__(kRowThreads, 4) policy_kernel(const PolicyParams a, int log2_slices) {
     __shared__ RowSmem sm;
     __shared__ float z_shared;
@@ -183,7 +186,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) policy_kernel(const PolicyPara
     griddep_wait();  // the inputs may come from the kernel before this one
 
     const int64_t row = blockIdx.x >> log2_slices;
-    PolicyRow<T, FWD, BWD> r(a, row, a.tokens[row], log2_slices, rank);
+    PolicyRow<T, FWD, BWD, U> r(a, row, a.tokens[row], log2_slices, rank);
     if (FWD && slices > 1) cluster_wait();
     if (!r.live()) {
         r.write_empty(leads);
@@ -211,9 +214,9 @@ __global__ void __launch_bounds__(kRowThreads, 4) policy_kernel(const PolicyPara
     r.finish(z_token, lp, m, s, leads);
 }
 
-template <typename T, bool FWD, bool BWD>
+template <typename T, bool FWD, bool BWD, int U>
 static cudaError_t start_policy(const PolicyParams &p, int64_t n, int slices, cudaStream_t s) {
-    auto kernel = policy_kernel<T, FWD, BWD>;
+    auto kernel = policy_kernel<T, FWD, BWD, U>;
     if (FWD && slices > kSlices) {
         static PerDevice prepared;
         const cudaError_t e =
@@ -231,8 +234,20 @@ static vie_status launch_policy(const char *fn, PolicyParams &p, vie_dtype dtype
     if (e != cudaSuccess) return fail_cuda(e, fn);
     const int slices = slices_of(FWD, BWD, static_cast<int64_t>(p.V) * dtype_size(dtype), n);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    e = dtype == VIE_DTYPE_BF16 ? start_policy<__nv_bfloat16, FWD, BWD>(p, n, slices, s)
-                                : start_policy<float, FWD, BWD>(p, n, slices, s);
+    const bool bf16 = dtype == VIE_DTYPE_BF16;
+    if constexpr (FWD && !BWD) {
+        // vectors per thread that a slice's turns have room for, with eight in flight and with six
+        const int64_t vectors = static_cast<int64_t>(p.V) * dtype_size(dtype) / slices / 16 + 1;
+        const int64_t by8 = (vectors + 8 * kRowThreads - 1) / (8 * kRowThreads) * 8;
+        const int64_t by6 = (vectors + 6 * kRowThreads - 1) / (6 * kRowThreads) * 6;
+        if (10 * by6 > 9 * by8) {
+            e = bf16 ? start_policy<__nv_bfloat16, FWD, BWD, 8>(p, n, slices, s)
+                     : start_policy<float, FWD, BWD, 8>(p, n, slices, s);
+            return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
+        }
+    }
+    e = bf16 ? start_policy<__nv_bfloat16, FWD, BWD, 6>(p, n, slices, s)
+             : start_policy<float, FWD, BWD, 6>(p, n, slices, s);
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
 
