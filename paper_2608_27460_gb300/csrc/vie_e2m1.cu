@@ -48,14 +48,25 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+// words[i] = all[i + first], first < 4 (the same in all lanes), without indexing registers.
+template <int N>
+__device__ __forceinline__ void take_words(const uint32_t (&all)[N], int first, uint32_t (&words)[N - 3]) {
+    uint32_t by2[N - 2];
+#pragma unroll
+    for (int i = 0; i < N - 2; ++i) by2[i] = (first & 2) != 0 ? all[i + 2] : all[i];
+#pragma unroll
+    for (int i = 0; i < N - 3; ++i) words[i] = (first & 1) != 0 ? by2[i + 1] : by2[i];
+}
+
 // Eight values of a row as they are stored, 0 beyond it.
 template <typename T>
 struct Raw8;
 template <>
 struct Raw8<__nv_bfloat16> {
     uint32_t w[4];
-    __device__ __forceinline__ void load(const __nv_bfloat16 *p, int left, bool vectors) {
-        if (vectors && left >= 8) {
+    // Of a row at a 16-byte address.
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p, int left) {
+        if (left >= 8) {
             const uint4 a = *reinterpret_cast<const uint4 *>(p);
             w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
             return;
@@ -64,6 +75,24 @@ struct Raw8<__nv_bfloat16> {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             w[i] = (2 * i < left ? q[2 * i] : 0u) | (2 * i + 1 < left ? static_cast<uint32_t>(q[2 * i + 1]) << 16 : 0u);
+    }
+    // Of one `shift` bytes behind such an address: vectors at such addresses that hold a
+    // value of the row are read whole.
+    __device__ __forceinline__ void load_shifted(const __nv_bfloat16 *p, int left, int shift) {
+        const uint4 *const v = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) - shift);
+        const uint4 a = v[0], b = shift + 2 * left > 16 ? v[1] : make_uint4(0, 0, 0, 0);
+        const uint32_t all[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        uint32_t words[5];
+        take_words(all, shift / 4, words);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(words[i], words[i + 1], 8 * (shift % 4));
+        if (left < 8) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (2 * i >= left) w[i] = 0;
+                else if (2 * i + 1 >= left) w[i] &= 0xFFFFu;
+            }
+        }
     }
     // The largest magnitude, as the bits of an fp32 value (NaN above infinity).
     __device__ __forceinline__ uint32_t top() const {
@@ -88,14 +117,29 @@ struct Raw8<__nv_bfloat16> {
 template <>
 struct Raw8<float> {
     uint32_t w[8];
-    __device__ __forceinline__ void load(const float *p, int left, bool vectors) {
-        if (vectors && left >= 8) {
+    __device__ __forceinline__ void load(const float *p, int left) {
+        if (left >= 8) {
             const uint4 a = reinterpret_cast<const uint4 *>(p)[0], b = reinterpret_cast<const uint4 *>(p)[1];
             w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
             return;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = i < left ? __float_as_uint(p[i]) : 0u;
+    }
+    __device__ __forceinline__ void load_shifted(const float *p, int left, int shift) {
+        const uint4 *const v = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p) - shift);
+        const uint4 none = make_uint4(0, 0, 0, 0), a = v[0], b = shift + 4 * left > 16 ? v[1] : none;
+        const uint4 c = shift + 4 * left > 32 ? v[2] : none;
+        const uint32_t all[12] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c.x, c.y, c.z, c.w};
+        uint32_t words[9];
+        take_words(all, shift / 4, words);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = words[i];
+        if (left < 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i >= left) w[i] = 0;
+        }
     }
     __device__ __forceinline__ uint32_t top() const {
         uint32_t t = 0;
@@ -126,6 +170,56 @@ __device__ __forceinline__ void store8(T *p, const float *v, int left, bool vect
         if (i < left) store_value(p + i, v[i]);
 }
 
+// The same for a row at any address: lane l of the warp has vector `vec` (lane 0's +
+// l) of a row of `width` values, in [0, width / 8] and beyond.  What lies between two
+// 16-byte addresses is of two vectors, so a lane gets the end of the one before its
+// own from its neighbour; the first and last lanes' halves go value by value.
+template <typename T>
+__device__ __forceinline__ void store8_shifted(T *row, int vec, const float *v, int width) {
+    constexpr int kWords = sizeof(T) == 2 ? 4 : 8;  // of eight values; 16 or 32 bytes
+    const int lane = threadIdx.x & 31, left = width - 8 * vec;
+    // values of this vector before the first 16-byte address in it (0: it starts there)
+    const int head = static_cast<int>(-(reinterpret_cast<uintptr_t>(row) & 15u) & 15u) / static_cast<int>(sizeof(T));
+    uint32_t own[kWords], before[kWords];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i)
+        own[i] = sizeof(T) == 2 ? pack_bf16(v[2 * i % 8], v[(2 * i + 1) % 8]) : __float_as_uint(v[i]);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) before[i] = __shfl_up_sync(0xFFFFFFFFu, own[i], 1);
+    // this lane's: the kWords words that end where its vector's values before `head` do
+    const int end = 8 * vec + head, start = end - 8;  // values of the row
+    T *const p = row + start;
+    if (lane > 0 && end <= width) {
+        uint32_t all[2 * kWords], words[kWords + 1];
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) all[i] = before[i], all[kWords + i] = own[i];
+        const int bytes = head * static_cast<int>(sizeof(T)), skip = bytes / 4;  // skip < 4
+        uint32_t by2[kWords + 3];
+#pragma unroll
+        for (int i = 0; i < kWords + 3; ++i) by2[i] = i + 2 < 2 * kWords && (skip & 2) != 0 ? all[i + 2] : all[i];
+#pragma unroll
+        for (int i = 0; i < kWords + 1; ++i) words[i] = (skip & 1) != 0 ? by2[i + 1] : by2[i];
+        uint4 q[kWords / 4];
+#pragma unroll
+        for (int i = 0; i < kWords / 4; ++i)
+            q[i] = make_uint4(__funnelshift_r(words[4 * i], words[4 * i + 1], 8 * (bytes % 4)),
+                              __funnelshift_r(words[4 * i + 1], words[4 * i + 2], 8 * (bytes % 4)),
+                              __funnelshift_r(words[4 * i + 2], words[4 * i + 3], 8 * (bytes % 4)),
+                              __funnelshift_r(words[4 * i + 3], words[4 * i + 4], 8 * (bytes % 4)));
+#pragma unroll
+        for (int i = 0; i < kWords / 4; ++i) reinterpret_cast<uint4 *>(p)[i] = q[i];
+    }
+    // value by value: this vector's own before `head` where no whole 16 bytes were
+    // written there, and its others where the next lane has not written them
+    const bool next_whole = lane < 31 && end + 8 <= width;
+    const bool whole = lane > 0 && end <= width;
+    if (!whole || !next_whole) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left && (i < head ? !whole : !next_whole)) store_value(row + 8 * vec + i, v[i]);
+    }
+}
+
 struct None {};  // no values wanted
 
 // Rows to codes and scales: a row in registers, its largest magnitude, its codes.  A
@@ -135,19 +229,22 @@ struct None {};  // no values wanted
 // rows of each of its warps are those whose scales lie side by side, so that the
 // CTA's scales (gathered in shared memory) are written 128 bytes at a time.
 // ROW_WARPS 8: a CTA per row, for the latency of few rows, and for long ones.
-// NV: vectors of eight values that a lane keeps.
+// NV: vectors of eight values that a lane keeps.  SHIFTED: not all rows of x and of
+// the values lie at 16-byte addresses.
 //
-// Bound by bytes where rows lie at 16-byte addresses: 262144 x 1152 bf16 145 us, with
-// bf16 values 231 (of a copy's rate 0.79 and 0.88), fp32 234 (0.87), 16384 x 8192 bf16
-// with values 99 (0.91).  Elsewhere values are moved one by one: 262144 x 1001 with
-// values 483 us (0.37).  32 x 1152 fp32: 1.4 us.
+// Bound by bytes where rows lie at 16-byte addresses: 262144 x 1152 bf16 144 us, with
+// bf16 values 225 (of a copy's rate 0.79 and 0.90), fp32 234 (0.87), 16384 x 8192 bf16
+// with values 99 (0.91).  Elsewhere by the instructions that take vectors apart and
+// join them: 262144 x 1001 bf16 194 us, with values 336 (0.51 and 0.52; value by value
+// 483), fp32 272 (0.65).  32 x 1152 fp32: 1.4 us.
+//
 // CTAs per SM: what the registers of a row leave (262144 x 1152 bf16 with values: 229
 // us with three, 262 with two; without values 141 with four, 155 with three).
 template <typename T, typename TV, int ROW_WARPS, int NV>
 constexpr int kQuantizeCtas = sizeof(T) == 4 ? (NV > 4 ? 2 : 3)
                               : ROW_WARPS == 1 && NV > 4 && !std::is_same<TV, None>::value ? 3 : 4;
 
-template <typename T, typename TV, int ROW_WARPS, int NV>
+template <typename T, typename TV, int ROW_WARPS, int NV, bool SHIFTED>
 __global__ void __launch_bounds__(kQuantizeThreads, kQuantizeCtas<T, TV, ROW_WARPS, NV>)
     quantize_kernel(const QuantizeParams a) {
     constexpr bool kMany = ROW_WARPS == 1;
@@ -158,7 +255,6 @@ __global__ void __launch_bounds__(kQuantizeThreads, kQuantizeCtas<T, TV, ROW_WAR
     const int warp = threadIdx.x >> 5, at = kMany ? threadIdx.x & 31 : threadIdx.x;
     const int tiles = e2m1_tiles(a.d);
     const int64_t pitch = e2m1_pitch(a.d);
-    const bool vectors = (reinterpret_cast<uintptr_t>(a.x) & 15u) == 0 && a.ld * sizeof(T) % 16 == 0;
     if (!a.late) griddep_launch_dependents();
     griddep_wait();
     if (a.late) griddep_launch_dependents();
@@ -171,13 +267,17 @@ __global__ void __launch_bounds__(kQuantizeThreads, kQuantizeCtas<T, TV, ROW_WAR
         const bool real = r < a.n;
         const T *const row = static_cast<const T *>(a.x) + (real ? r : 0) * a.ld;
         const int width = real ? a.d : 0;  // rows beyond the last have scales of 0 and nothing else
+        [[maybe_unused]] const int shift = static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15u);
         Raw8<T> raw[NV];
         uint32_t tops[NV], top = 0;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int j = 8 * (k * kRowLanes + at);
             raw[k] = {};
-            if (j < width) raw[k].load(row + j, width - j, vectors);
+            if (j < width) {
+                if constexpr (SHIFTED) raw[k].load_shifted(row + j, width - j, shift);
+                else raw[k].load(row + j, width - j);
+            }
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -221,14 +321,13 @@ __global__ void __launch_bounds__(kQuantizeThreads, kQuantizeCtas<T, TV, ROW_WAR
             }
             if (real && vec * 4 < pitch) *reinterpret_cast<uint32_t *>(a.codes + r * pitch + vec * 4) = codes;
             if constexpr (kValues) {
-                if (left > 0) {
-                    from_e2m1(codes, v);
-                    const float u = sigma * unit;
+                from_e2m1(codes, v);
+                const float u = sigma * unit;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] *= u;
-                    TV *const out = static_cast<TV *>(a.values) + r * a.ld_values + 8 * vec;
-                    store8(out, v, left, (reinterpret_cast<uintptr_t>(out) & 15u) == 0);
-                }
+                for (int i = 0; i < 8; ++i) v[i] *= u;
+                TV *const out = static_cast<TV *>(a.values) + r * a.ld_values;
+                if constexpr (SHIFTED) store8_shifted(out, vec, v, width);
+                else if (left > 0) store8(out + 8 * vec, v, left, true);
             }
         }
     }
@@ -308,20 +407,28 @@ static vie_status check_e2m1(const char *fn, int64_t n, const void *codes, const
 // 8.0 / 6.4, 8192 8.8 / 11.6; 2048, 4096 11.0 / 7.1, 8192 11.9 / 13.0, 16384 16.5 / 25.1).
 static bool by_warps(int64_t n, int d) { return d <= 2048 && n >= 1024 + 4 * static_cast<int64_t>(d); }
 
-template <typename T, typename TV>
-static cudaError_t start_quantize(const QuantizeParams &p, cudaStream_t s) {
+template <typename T, typename TV, bool SHIFTED>
+static cudaError_t start_quantize_rows(const QuantizeParams &p, cudaStream_t s) {
     const int64_t rows = (p.n + kE2m1TileRows - 1) / kE2m1TileRows * kE2m1TileRows;  // with those that have scales alone
     constexpr int W = kQuantizeWarps, NT = kQuantizeThreads;
     if (by_warps(p.n, p.d)) {
         const dim3 grid(static_cast<unsigned>(rows / 32));
         const size_t smem = static_cast<size_t>(e2m1_tiles(p.d)) * 128;
-        return p.d <= 1024 ? launch(quantize_kernel<T, TV, 1, 4>, grid, NT, smem, s, p)
-                           : launch(quantize_kernel<T, TV, 1, 8>, grid, NT, smem, s, p);
+        return p.d <= 1024 ? launch(quantize_kernel<T, TV, 1, 4, SHIFTED>, grid, NT, smem, s, p)
+                           : launch(quantize_kernel<T, TV, 1, 8, SHIFTED>, grid, NT, smem, s, p);
     }
     const dim3 grid(static_cast<unsigned>(rows));
-    return p.d <= 2048   ? launch(quantize_kernel<T, TV, W, 1>, grid, NT, 0, s, p)
-           : p.d <= 4096 ? launch(quantize_kernel<T, TV, W, 2>, grid, NT, 0, s, p)
-                         : launch(quantize_kernel<T, TV, W, VIE_D_MAX / (8 * NT)>, grid, NT, 0, s, p);
+    return p.d <= 2048   ? launch(quantize_kernel<T, TV, W, 1, SHIFTED>, grid, NT, 0, s, p)
+           : p.d <= 4096 ? launch(quantize_kernel<T, TV, W, 2, SHIFTED>, grid, NT, 0, s, p)
+                         : launch(quantize_kernel<T, TV, W, VIE_D_MAX / (8 * NT), SHIFTED>, grid, NT, 0, s, p);
+}
+
+template <typename T, typename TV>
+static cudaError_t start_quantize(const QuantizeParams &p, cudaStream_t s) {
+    bool aligned = aligned_to(p.x, 16) && (p.n == 1 || p.ld * sizeof(T) % 16 == 0);
+    if constexpr (!std::is_same<TV, None>::value)
+        aligned = aligned && aligned_to(p.values, 16) && (p.n == 1 || p.ld_values * sizeof(TV) % 16 == 0);
+    return aligned ? start_quantize_rows<T, TV, false>(p, s) : start_quantize_rows<T, TV, true>(p, s);
 }
 
 template <typename T>

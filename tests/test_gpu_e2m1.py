@@ -48,6 +48,43 @@ def test_sizes(vie, dtype, n, d):
     _check_rows(vie, _rows(n, d, dtype, seed=n + d))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,d", [(1300, 33), (1290, 64), (2100, 257), (2500, 300), (5200, 1001), (9300, 2048), (3000, 16)])
+def test_many_rows(vie, dtype, n, d):
+    """Rows that a warp takes each, 32 of a tile to a CTA; the last tile is not full."""
+    x = _rows(n, d, dtype, seed=n + d)
+    x[n - 2] = float("inf")
+    _check_rows(vie, x)
+
+
+@pytest.mark.parametrize("n", [40, 1500])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("values", ["bf16", "f32"])
+def test_rows_and_values_at_every_address(vie, n, dtype, values):
+    """Every alignment of a row of x with one of the values, widths that end anywhere in a vector."""
+    for d, (off, ld), (o, l) in ((99, (1, 99), (3, 101)), (97, (0, 97), (0, 97)), (104, (4, 104), (0, 104)),
+                                 (103, (5, 106), (7, 107)), (9, (2, 9), (1, 11)), (64, (0, 65), (0, 64)),
+                                 (250, (3, 251), (6, 253))):
+        x = _rows(n, d, dtype, seed=d)
+        want = ref.quantize(x)[3].to(DT[values])
+        big = torch.full((off + n * ld + 8,), float("nan"), dtype=DT[dtype], device="cuda")
+        xc = big[off:off + n * ld].view(n, ld)[:, :d]
+        xc.copy_(x)
+        out = torch.full((o + n * l + 16,), 7.0, dtype=DT[values], device="cuda")
+        view = out[o:o + n * l].view(n, l)[:, :d]
+        q = vie.e2m1_quantize(xc, out_values=view)
+        assert torch.equal(view.cpu(), want)
+        assert torch.equal(vie.e2m1_dequantize(q, out_dtype=DT[values]).cpu(), want)
+        view.fill_(7.0)
+        assert (out == 7.0).all()
+        if dtype == values:
+            own = xc.clone(memory_format=torch.preserve_format)
+            vie.e2m1_quantize(own, out_values=own)
+            assert torch.equal(own.cpu(), want)
+            vie.e2m1_quantize(xc, out_values=xc)
+            assert torch.equal(xc.cpu(), want)
+
+
 def test_ties_and_borders(vie):
     """Values on and beside the midpoints of codes and of scales, in blocks whose scale is known."""
     g = torch.Generator().manual_seed(3)
