@@ -495,6 +495,8 @@ vie_status vie_e2m1_quantize(const void *x, vie_dtype dtype, int64_t n, int32_t 
     if (st == VIE_OK) st = check_e2m1(fn, n, out_codes, out_scales, out_row_scales);
     if (st == VIE_OK && out_values != nullptr)
         st = check_matrix(fn, "out_values", out_values, values_dtype, n, d, ld_values);
+    if (st == VIE_OK && n > 0 && out_values == x && (values_dtype != dtype || (n > 1 && ld_values != ld)))
+        st = fail(VIE_ERR_INVALID_ARG, "%s: out_values in place of x with another type or row pitch", fn);
     if (st != VIE_OK || n == 0) return st;
     QuantizeParams p = {};
     p.x = x, p.n = n, p.d = d, p.ld = ld;
@@ -540,6 +542,8 @@ vie_status vie_e2m1_quantize_logits(const void *x, vie_dtype dtype, int64_t n, i
     vie_status st = check_logits(fn, n, V, d, x_codes, x_scales, x_row_scales, w_codes, w_scales, w_row_scales, out,
                                  out_dtype, ld_out);
     if (st == VIE_OK) st = check_matrix(fn, "x", x, dtype, n, d, ld);
+    if (st == VIE_OK && n > 0 && (x_codes == w_codes || x_scales == w_scales || x_row_scales == w_row_scales))
+        st = fail(VIE_ERR_INVALID_ARG, "%s: x_* in place of w_*", fn);
     if (st != VIE_OK || n == 0) return st;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     QuantizeParams p = {};

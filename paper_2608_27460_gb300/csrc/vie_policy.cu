@@ -270,6 +270,14 @@ static vie_status check_floats(const char *fn, int64_t n, const float *p, bool m
     return VIE_OK;
 }
 
+// A gradient apart from the logits, or in their place by rows.
+static vie_status check_grad(const char *fn, const void *logits, int64_t ld, const void *out_grad, vie_dtype dtype,
+                             int64_t n, int64_t V, int64_t ld_grad) {
+    if (n > 1 && out_grad == logits && ld_grad != ld)
+        return fail(VIE_ERR_INVALID_ARG, "%s: out_grad in place of logits with another row pitch", fn);
+    return check_matrix(fn, "out_grad", out_grad, dtype, n, V, ld_grad);
+}
+
 static vie_status check_terms(const char *fn, int64_t n, const PolicyTerms &t) {
     vie_status st = check_floats(fn, n, t.old_lp);
     if (st == VIE_OK) st = check_floats(fn, n, t.advantage);
@@ -484,7 +492,7 @@ vie_status vie_token_logprobs_grad(const void *logits, vie_dtype dtype, int64_t 
     vie_status st = check_rows(fn, logits, dtype, n, V, ld, tokens, temperature);
     if (st == VIE_OK) st = check_floats(fn, n, stats);
     if (st == VIE_OK) st = check_floats(fn, n, grad_logprob);
-    if (st == VIE_OK) st = check_matrix(fn, "out_grad", out_grad, dtype, n, V, ld_grad);
+    if (st == VIE_OK) st = check_grad(fn, logits, ld, out_grad, dtype, n, V, ld_grad);
     if (st != VIE_OK) return st;
     PolicyParams p = rows_of(logits, V, ld, tokens, temperature);
     p.stats_in = stats, p.grad = grad_logprob, p.grad_logits = out_grad, p.ld_grad = ld_grad;
@@ -519,7 +527,7 @@ vie_status vie_policy_loss_grad(const void *logits, vie_dtype dtype, int64_t n, 
     if (st == VIE_OK) st = check_floats(fn, n, logprob);
     if (st == VIE_OK) st = check_floats(fn, n, stats);
     if (st == VIE_OK) st = check_floats(fn, n, grad_loss);
-    if (st == VIE_OK) st = check_matrix(fn, "out_grad", out_grad, dtype, n, V, ld_grad);
+    if (st == VIE_OK) st = check_grad(fn, logits, ld, out_grad, dtype, n, V, ld_grad);
     if (st != VIE_OK) return st;
     p.lp_in = logprob, p.stats_in = stats, p.grad = grad_loss, p.grad_logits = out_grad, p.ld_grad = ld_grad;
     return launch_policy<false, true>(fn, p, dtype, n, stream);
@@ -537,7 +545,7 @@ vie_status vie_policy_loss_step(const void *logits, vie_dtype dtype, int64_t n, 
     if (st == VIE_OK) st = check_terms(fn, n, p.terms);
     if (st == VIE_OK) st = check_floats(fn, n, grad_loss);
     if (st == VIE_OK) st = check_results(fn, n, p.terms, out_loss, out_logprob, out_stats);
-    if (st == VIE_OK) st = check_matrix(fn, "out_grad", out_grad, dtype, n, V, ld_grad);
+    if (st == VIE_OK) st = check_grad(fn, logits, ld, out_grad, dtype, n, V, ld_grad);
     if (st != VIE_OK) return st;
     p.grad = grad_loss, p.loss = out_loss, p.lp_out = out_logprob, p.stats_out = out_stats;
     p.grad_logits = out_grad, p.ld_grad = ld_grad;

@@ -99,7 +99,8 @@ LOGITS = dict(x_codes=P, x_scales=P, x_row_scales=P, n=4, w_codes=P, w_scales=P,
               out_dtype=F32, ld_out=100)
 
 
-BOTH = dict(x=P, dtype=F32, n=4, ld=50, x_codes=P, x_scales=P, x_row_scales=P, w_codes=P, w_scales=P, w_row_scales=P,
+W = P + 0x1000
+BOTH = dict(x=P, dtype=F32, n=4, ld=50, x_codes=P, x_scales=P, x_row_scales=P, w_codes=W, w_scales=W, w_row_scales=W,
             V=100, d=50, out=P, out_dtype=F32, ld_out=100)
 
 
@@ -129,7 +130,21 @@ def test_e2m1_refusals():
     assert _call(vie.vie_e2m1_logits, LOGITS, out_dtype=2) == UNSUPPORTED
     for fn, ok in ((vie.vie_e2m1_quantize, QUANTIZE), (vie.vie_e2m1_dequantize, DEQUANTIZE),
                    (vie.vie_e2m1_logits, LOGITS), (vie.vie_e2m1_quantize_logits, BOTH)):
-        assert _call(fn, ok, n=0, **{p: 0 for p in ok if ok[p] == P}) == vie.VIE_OK
+        assert _call(fn, ok, n=0, **{p: 0 for p in ok if ok[p] in (P, W)}) == vie.VIE_OK
+
+
+def test_results_in_place_of_inputs():
+    """Where they may be, and with the layout that makes it safe."""
+    for name in ("vie_token_logprobs_grad", "vie_policy_loss_grad", "vie_policy_loss_step"):
+        apart = {r: W for r in ("out_loss", "out_logprob") if r in FORMS[name]}
+        bad = dict(FORMS[name], **apart, logits=P + 64, out_grad=P + 64, ld_grad=104)
+        assert _call(getattr(vie, name), bad) == INVALID and "pitch" in vie.vie_last_error()
+    apart = dict(QUANTIZE, values=P + 64)
+    for bad in (dict(x=P + 64, dtype=F32, ld_values=51), dict(x=P + 64)):  # (another pitch; another type)
+        assert _call(vie.vie_e2m1_quantize, apart, **bad) == INVALID and "in place" in vie.vie_last_error()
+    for part in ("codes", "scales", "row_scales"):
+        assert _call(vie.vie_e2m1_quantize_logits, BOTH, **{"x_" + part: W}) == INVALID
+        assert "in place" in vie.vie_last_error()
 
 
 def test_e2m1_bytes():
