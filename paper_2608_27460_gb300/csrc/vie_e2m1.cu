@@ -345,26 +345,68 @@ struct E2m1Matrix {
     int64_t n;
 };
 
-// What the codes stand for, a warp per row, eight values per lane.  Bound by bytes:
-// 262144 x 1152 to bf16 173 us, to fp32 253 (of a copy's rate 0.66 and 0.80).
-template <typename T>
+// What the codes stand for, a warp per row, eight values per lane, kUnpack such vectors
+// read before the first is written.  A CTA's rows are two neighbours in each quarter of
+// a tile of scales: the 32 bytes that are fetched for one of them are all of its.
+//
+// Bound by bytes: 262144 x 1152 to bf16 119 us, to fp32 203 (of a copy's rate 0.96 and
+// 1.0; with one vector read at a time, rows of a CTA next to each other and a lane's fp32
+// values written as one vector 173 and 252); 262144 x 1001 by what joins vectors, to bf16 211
+// us, to fp32 199 (0.47 and 0.88; value by value 503 and 481).  kUnpack: 3, 5 and 8 take
+// 125, 121 and 122 us at 1152 columns, 4 119.
+constexpr int kUnpack = 4;
+template <typename T, bool SHIFTED>
 __global__ void __launch_bounds__(kQuantizeThreads) dequantize_kernel(const E2m1Matrix q, int d, T *out, int64_t ld) {
-    const int64_t r = static_cast<int64_t>(blockIdx.x) * kQuantizeWarps + (threadIdx.x >> 5);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t r = static_cast<int64_t>(blockIdx.x) / 16 * kE2m1TileRows + warp / 2 * 32 + blockIdx.x % 16 * 2 + warp % 2;
     griddep_launch_dependents();
     griddep_wait();
     if (r >= q.n) return;
     const float s = q.row_scales[r];
     const uint32_t *const codes = reinterpret_cast<const uint32_t *>(q.codes + r * e2m1_pitch(d));
     const int tiles = e2m1_tiles(d);
-#pragma unroll 4
-    for (int vec = threadIdx.x & 31; vec * 8 < d; vec += 32) {
-        const float unit = from_e4m3(q.scales[e2m1_scale_at(r, vec / 2, tiles)]) * s;
-        float v[8];
-        from_e2m1(codes[vec], v);
+    T *const row = out + r * ld;
+    for (int first = 0; first * 8 < d; first += 32 * kUnpack) {
+        uint32_t word[kUnpack], sigma[kUnpack];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= unit;
-        T *const o = out + r * ld + vec * 8;
-        store8(o, v, d - vec * 8, (reinterpret_cast<uintptr_t>(o) & 15u) == 0);
+        for (int k = 0; k < kUnpack; ++k) {
+            const int vec = first + 32 * k + lane;
+            word[k] = sigma[k] = 0;
+            if (vec * 8 >= d) continue;
+            word[k] = codes[vec];
+            sigma[k] = q.scales[e2m1_scale_at(r, vec / 2, tiles)];
+        }
+#pragma unroll
+        for (int k = 0; k < kUnpack; ++k) {
+            const int vec = first + 32 * k + lane;
+            if ((first + 32 * k) * 8 >= d) break;  // (the same for all lanes: they exchange)
+            const float unit = from_e4m3(sigma[k]) * s;
+            float v[8];
+            if constexpr (sizeof(T) == 4 && !SHIFTED) {  // a lane writes half a vector, so that the warp's 16 bytes each adjoin
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int from = 16 * h + lane / 2, c = (first + 32 * k + from) * 8 + lane % 2 * 4;
+                    const uint32_t half = __shfl_sync(0xFFFFFFFFu, word[k], from) >> (lane % 2 * 16);
+                    const float u = __shfl_sync(0xFFFFFFFFu, unit, from);
+                    from_e2m1(half & 0xFFFFu, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] *= u;
+                    if (c + 4 <= d) {
+                        *reinterpret_cast<uint4 *>(row + c) = Vec16<T>::pack(v);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (c + i < d) store_value(row + c + i, v[i]);
+                    }
+                }
+            } else {
+                from_e2m1(word[k], v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= unit;
+                if constexpr (SHIFTED) store8_shifted(row, vec, v, d);
+                else if (vec * 8 < d) store8(row + 8 * vec, v, d - 8 * vec, true);
+            }
+        }
     }
 }
 
@@ -442,6 +484,15 @@ static cudaError_t launch_quantize(const QuantizeParams &p, vie_dtype dtype, vie
                                    : start_quantize<float>(p, values_dtype, s);
 }
 
+template <typename T>
+static cudaError_t start_dequantize(const E2m1Matrix &q, int d, T *out, int64_t ld, cudaStream_t s) {
+    static_assert(kQuantizeWarps == 8, "sixteen CTAs have a tile of rows");
+    const dim3 grid(static_cast<unsigned>((q.n + kE2m1TileRows - 1) / kE2m1TileRows * 16));
+    const bool aligned = aligned_to(out, 16) && (q.n == 1 || ld * sizeof(T) % 16 == 0);
+    return aligned ? launch(dequantize_kernel<T, false>, grid, kQuantizeThreads, 0, s, q, d, out, ld)
+                   : launch(dequantize_kernel<T, true>, grid, kQuantizeThreads, 0, s, q, d, out, ld);
+}
+
 static vie_status check_logits(const char *fn, int64_t n, int64_t V, int32_t d, const void *x_codes,
                                const void *x_scales, const float *x_row_scales, const void *w_codes,
                                const void *w_scales, const float *w_row_scales, const void *out, vie_dtype out_dtype,
@@ -514,12 +565,9 @@ vie_status vie_e2m1_dequantize(const void *codes, const void *scales, const floa
     if (st == VIE_OK) st = check_matrix(fn, "out", out, out_dtype, n, d, ld_out);
     if (st != VIE_OK || n == 0) return st;
     const E2m1Matrix q = {static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), row_scales, n};
-    const dim3 grid(static_cast<unsigned>((n + kQuantizeWarps - 1) / kQuantizeWarps));
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e =
-        out_dtype == VIE_DTYPE_BF16
-            ? launch(dequantize_kernel<__nv_bfloat16>, grid, kQuantizeThreads, 0, s, q, d, static_cast<__nv_bfloat16 *>(out), ld_out)
-            : launch(dequantize_kernel<float>, grid, kQuantizeThreads, 0, s, q, d, static_cast<float *>(out), ld_out);
+    const cudaError_t e = out_dtype == VIE_DTYPE_BF16 ? start_dequantize(q, d, static_cast<__nv_bfloat16 *>(out), ld_out, s)
+                                                      : start_dequantize(q, d, static_cast<float *>(out), ld_out, s);
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
 

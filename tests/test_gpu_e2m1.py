@@ -85,6 +85,25 @@ def test_rows_and_values_at_every_address(vie, n, dtype, values):
             assert torch.equal(xc.cpu(), want)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,d", [(1, 5), (2, 1023), (33, 1024), (130, 1025), (257, 1030), (3, 2052), (300, 64), (1, 16384)])
+def test_values_at_every_address(vie, dtype, n, d):
+    """Widths about the 1024 columns that a warp reads at once, rows at and off 16-byte addresses; what lies
+    beside and behind them stays."""
+    x = _rows(n, d, "f32", seed=3 * n + d)
+    x[n // 2, d // 2] = float("nan")
+    want = ref.quantize(x)[3].to(DT[dtype]).nan_to_num(9.0)
+    q = vie.e2m1_quantize(x.cuda())
+    for o, pad in ((0, 0), (0, 8 - d % 8), (1, 0), (4, 3), (7, 5), (8, 4 - d % 4), (2, 16 - d % 16)):
+        ld = d + pad
+        out = torch.full((o + n * ld + 16,), 7.0, dtype=DT[dtype], device="cuda")
+        view = out[o:o + n * ld].view(n, ld)[:, :d]
+        vie.e2m1_dequantize(q, out=view)
+        assert torch.equal(view.cpu().nan_to_num(9.0), want)
+        view.fill_(7.0)
+        assert (out == 7.0).all()
+
+
 def test_ties_and_borders(vie):
     """Values on and beside the midpoints of codes and of scales, in blocks whose scale is known."""
     g = torch.Generator().manual_seed(3)
