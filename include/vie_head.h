@@ -682,7 +682,7 @@ vie_status vie_policy_loss_step(const void *logits, vie_dtype dtype, int64_t n, 
  *               flag that vie_device_status reports.
  *   pairs       0 <= pairs <= VIE_MANY_MAX.
  *   beta        finite;  label_smoothing in [0, 1].
- *   out_loss, out_margin  device, fp32 [pairs].
+ *   out_loss, out_margin  device, fp32 [pairs]; must not overlap the inputs.
  *
  * Errors: VIE_ERR_INVALID_ARG, VIE_ERR_CUDA.
  */
@@ -694,7 +694,7 @@ vie_status vie_preference_loss(const float *logprob, const float *ref_logprob, i
  * vie_preference_loss_grad - the gradient of sum_p grad_loss[p] loss[p] with
  * respect to each token's logprob: beta grad_loss (label_smoothing -
  * sigmoid(-margin)) for the tokens of a chosen sequence, the negative for those
- * of a rejected one, 0 for the others (all n are written).  It is what
+ * of a rejected one, 0 for the others (all n are written) and where grad_loss is 0.  It is what
  * vie_token_logprobs_grad takes as grad_logprob.
  *   margin      device, fp32 [pairs]: out_margin.
  *   grad_loss   device, fp32 [pairs].

@@ -293,17 +293,24 @@ static vie_status check_terms(const char *fn, int64_t n, const PolicyTerms &t) {
     return VIE_OK;
 }
 
+// No result where other threads may still read an input.
+static vie_status check_apart(const char *fn, std::initializer_list<const float *> results,
+                              std::initializer_list<const float *> inputs, const char *what) {
+    for (const float *out : results)
+        for (const float *in : inputs)
+            if (out != nullptr && out == in) return fail(VIE_ERR_INVALID_ARG, "%s: a result in place of %s", fn, what);
+    return VIE_OK;
+}
+
 // What is written per row while other CTAs may still read the terms of that row.
-static vie_status check_results(const char *fn, int64_t n, const PolicyTerms &t, const float *out_loss,
-                                const float *out_logprob, const float *out_stats) {
+static vie_status check_results(const char *fn, int64_t n, const PolicyTerms &t, const float *grad_loss,
+                                const float *out_loss, const float *out_logprob, const float *out_stats) {
     vie_status st = check_floats(fn, n, out_loss);
     if (st == VIE_OK) st = check_floats(fn, n, out_logprob);
     if (st == VIE_OK) st = check_floats(fn, n, out_stats, true);
     if (st != VIE_OK || n == 0) return st;
-    for (const float *out : {out_loss, out_logprob, out_stats})
-        if (out != nullptr && (out == t.old_lp || out == t.advantage || out == t.ref_lp))
-            return fail(VIE_ERR_INVALID_ARG, "%s: a result in place of old_logprob, advantage or ref_logprob", fn);
-    return VIE_OK;
+    return check_apart(fn, {out_loss, out_logprob, out_stats}, {t.old_lp, t.advantage, t.ref_lp, grad_loss},
+                       "old_logprob, advantage, ref_logprob or grad_loss");
 }
 
 static PolicyParams rows_of(const void *logits, int64_t V, int64_t ld, const int32_t *tokens, float T) {
@@ -400,7 +407,9 @@ __global__ void __launch_bounds__(NT) preference_kernel(const PreferenceParams a
         a.margin_out[p] = h;
     }
     if (BWD) {
-        const float slope = a.beta * a.grad_loss[p] * (a.smoothing - 1.0f / (1.0f + expf(h)));
+        const float weight = a.grad_loss[p];
+        // (a weight of 0 masks a pair, whatever its margin)
+        const float slope = weight == 0.0f ? 0.0f : a.beta * weight * (a.smoothing - 1.0f / (1.0f + expf(h)));
         for (int i = o[0] + first; i < o[2]; i += step) a.grad[i] = i < o[1] ? slope : -slope;
         // tokens of no sequence, shared among all pairs
         const int begin = min(max(a.offsets[0], 0), n), end = min(max(a.offsets[2 * a.pairs], 0), n);
@@ -508,7 +517,7 @@ vie_status vie_policy_loss(const void *logits, vie_dtype dtype, int64_t n, int64
     p.terms = {old_logprob, advantage, ref_logprob, clip_low, clip_high, kl_coef};
     vie_status st = check_rows(fn, logits, dtype, n, V, ld, tokens, temperature);
     if (st == VIE_OK) st = check_terms(fn, n, p.terms);
-    if (st == VIE_OK) st = check_results(fn, n, p.terms, out_loss, out_logprob, out_stats);
+    if (st == VIE_OK) st = check_results(fn, n, p.terms, nullptr, out_loss, out_logprob, out_stats);
     if (st != VIE_OK) return st;
     p.loss = out_loss, p.lp_out = out_logprob, p.stats_out = out_stats;
     return launch_policy<true, false>(fn, p, dtype, n, stream);
@@ -544,7 +553,7 @@ vie_status vie_policy_loss_step(const void *logits, vie_dtype dtype, int64_t n, 
     vie_status st = check_rows(fn, logits, dtype, n, V, ld, tokens, temperature);
     if (st == VIE_OK) st = check_terms(fn, n, p.terms);
     if (st == VIE_OK) st = check_floats(fn, n, grad_loss);
-    if (st == VIE_OK) st = check_results(fn, n, p.terms, out_loss, out_logprob, out_stats);
+    if (st == VIE_OK) st = check_results(fn, n, p.terms, grad_loss, out_loss, out_logprob, out_stats);
     if (st == VIE_OK) st = check_grad(fn, logits, ld, out_grad, dtype, n, V, ld_grad);
     if (st != VIE_OK) return st;
     p.grad = grad_loss, p.loss = out_loss, p.lp_out = out_logprob, p.stats_out = out_stats;
@@ -561,6 +570,7 @@ vie_status vie_preference_loss(const float *logprob, const float *ref_logprob, i
     if (st == VIE_OK) st = check_floats(fn, n, ref_logprob, true);
     if (st == VIE_OK) st = check_floats(fn, pairs, out_loss);
     if (st == VIE_OK) st = check_floats(fn, pairs, out_margin);
+    if (st == VIE_OK && pairs > 0) st = check_apart(fn, {out_loss, out_margin}, {logprob, ref_logprob}, "an input");
     if (st != VIE_OK) return st;
     PreferenceParams p = pairs_of(n, offsets, pairs, beta, label_smoothing);
     p.lp = logprob, p.ref = ref_logprob, p.loss = out_loss, p.margin_out = out_margin;
@@ -575,6 +585,7 @@ vie_status vie_preference_loss_grad(const float *margin, int64_t n, const int32_
     if (st == VIE_OK) st = check_floats(fn, pairs, margin);
     if (st == VIE_OK) st = check_floats(fn, pairs, grad_loss);
     if (st == VIE_OK) st = check_floats(fn, n, out_grad);
+    if (st == VIE_OK && pairs > 0) st = check_apart(fn, {out_grad}, {margin, grad_loss}, "an input");
     if (st != VIE_OK) return st;
     PreferenceParams p = pairs_of(n, offsets, pairs, beta, label_smoothing);
     p.margin_in = margin, p.grad_loss = grad_loss, p.grad = out_grad;
@@ -592,6 +603,8 @@ vie_status vie_preference_loss_step(const float *logprob, const float *ref_logpr
     if (st == VIE_OK) st = check_floats(fn, pairs, out_loss);
     if (st == VIE_OK) st = check_floats(fn, pairs, out_margin);
     if (st == VIE_OK) st = check_floats(fn, n, out_grad);
+    if (st == VIE_OK && pairs > 0)
+        st = check_apart(fn, {out_loss, out_margin, out_grad}, {logprob, ref_logprob, grad_loss}, "an input");
     if (st != VIE_OK) return st;
     PreferenceParams p = pairs_of(n, offsets, pairs, beta, label_smoothing);
     p.lp = logprob, p.ref = ref_logprob, p.grad_loss = grad_loss;

@@ -88,6 +88,15 @@ def test_infinite_log_probabilities_stay_in_their_pair(vie):
     assert torch.isnan(loss).tolist() == [True, False, False]
 
 
+def test_a_weight_of_zero_masks_a_pair(vie):
+    lp, r, ends, grad = _inputs([9, 9, 9, 9], 0, 0, seed=11)
+    lp[2] = float("nan")
+    w = torch.tensor([0.0, 1.0], device="cuda")
+    _, h, dlp = vie.preference_loss_step(lp.cuda(), ends.cuda(), w, ref_logprob=r.cuda())
+    assert torch.isnan(h[0]) and not dlp[:18].any() and dlp[18:].all()
+    assert torch.equal(vie.preference_loss_grad(h, ends.cuda(), w, len(lp)), dlp)
+
+
 def test_bad_offsets_are_held_inside_and_reported(vie):
     """Host and kernel keep every access inside the n tokens."""
     lp, r, ends, grad = _inputs([9, 9, 9, 9], 2, 2, seed=9)

@@ -147,6 +147,22 @@ def test_results_in_place_of_inputs():
         assert "in place" in vie.vie_last_error()
 
 
+def test_policy_results_in_place_of_weights():
+    ok = dict(FORMS["vie_policy_loss_step"], out_loss=P + 16, out_logprob=P + 32, out_stats=P + 64, grad_loss=W)
+    for out in ("out_loss", "out_logprob", "out_stats"):
+        assert _call(vie.vie_policy_loss_step, ok, **{out: W}) == INVALID and "in place" in vie.vie_last_error()
+
+
+@pytest.mark.parametrize("name", PREFERENCE)
+def test_preference_results_in_place_of_inputs(name):
+    fn, args = getattr(vie, name), PREFERENCE[name]
+    ok = {k: P + 16 * i if v == P else v for i, (k, v) in enumerate(args.items())}
+    for out in (k for k in ok if k.startswith("out_")):
+        for term in ("logprob", "ref_logprob", "margin", "grad_loss"):
+            if term in ok:
+                assert _call(fn, ok, **{out: W, term: W}) == INVALID and "in place" in vie.vie_last_error()
+
+
 def test_e2m1_bytes():
     assert vie.load().vie_e2m1_bytes(4, 100, None, None) == INVALID
     for n, d in ((-1, 5), (5, 0), (5, vie.VIE_D_MAX + 1), (vie.VIE_E2M1_N_MAX + 1, 5)):
