@@ -214,6 +214,35 @@ __global__ void __launch_bounds__(kRowThreads, 4) policy_kernel(const PolicyPara
     r.finish(z_token, lp, m, s, leads);
 }
 
+// CTAs per row of n rows of this many bytes.
+//
+// Of a long row a slice that a CTA can take without losing what it read from L2, or its
+// turn: 64 KB of a gradient alone (128256 x 2048 bf16 166 us, in slices of 125 KB 171;
+// 217047 x 1500 195, in slices of 106 KB 199), 112 KB of loss and gradient (us with slices
+// of 40 / 81 KB, fp32 41353 x 2183: 131 / 123; of 53 / 106, bf16 217047 x 1500: 250 / 233;
+// of 62 / 125, 128256 x 1500: 138 / 146).
+//
+// Of few rows as many as fill the chip's four CTAs per SM, once: CTAs beyond that are a
+// second round.  With partials to exchange, clusters of four and eight only where they
+// leave more of it free, or slices stay long (us with 1 / 2 / 4 / 8, fp32 27566: 300 rows'
+// log-probabilities 7.2 / 6.6 / 9.3 / 13.3, loss and gradient 15.4 / 12.7 / 18.0 / 21.1; 150 rows
+// 10.3 / 9.0 / 10.3 / 11.6; 434 20.8 / 22.4 / 23.2 / 29.0; log-probabilities of 84 rows of
+// fp32 41353 6.2 / 5.8 / 4.9 / 6.2, of bf16 217047 20.2 / 14.6 / 12.9 / 12.2).
+static int slices_of_row(bool fwd, bool bwd, int64_t bytes, int64_t n) {
+    int slices = 1;
+    if (!fwd) {
+        while (bytes / slices > 64 * 1024 && n * slices < (1 << 30)) slices *= 2;
+        while (slices < kMaxSlices && 2 * n * slices <= 672 && bytes / slices > 16 * 1024) slices *= 2;
+        return slices;
+    }
+    if (bwd)
+        while (slices < kSlices && bytes / slices > 112 * 1024) slices *= 2;
+    auto most = [&] { return slices == 1 ? 608 : slices == 4 && bytes / slices > 64 * 1024 ? 700 : 512; };
+    while (slices < (n <= kFewRows ? kMaxSlices : kSlices) && 2 * n * slices <= most() && bytes / slices > 32 * 1024)
+        slices *= 2;
+    return slices;
+}
+
 template <typename T, bool FWD, bool BWD, int U>
 static cudaError_t start_policy(const PolicyParams &p, int64_t n, int slices, cudaStream_t s) {
     auto kernel = policy_kernel<T, FWD, BWD, U>;
@@ -232,7 +261,7 @@ static vie_status launch_policy(const char *fn, PolicyParams &p, vie_dtype dtype
     if (n == 0) return VIE_OK;
     cudaError_t e = device_flag_word(&p.flag);
     if (e != cudaSuccess) return fail_cuda(e, fn);
-    const int slices = slices_of(FWD, BWD, static_cast<int64_t>(p.V) * dtype_size(dtype), n);
+    const int slices = slices_of_row(FWD, BWD, static_cast<int64_t>(p.V) * dtype_size(dtype), n);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool bf16 = dtype == VIE_DTYPE_BF16;
     if constexpr (FWD && !BWD) {
