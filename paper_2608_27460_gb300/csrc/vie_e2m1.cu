@@ -228,13 +228,15 @@ struct None {};  // no values wanted
 // ROW_WARPS 1: a warp per row, a CTA for 32 rows of a tile, 8 at a time: the four
 // rows of each of its warps are those whose scales lie side by side, so that the
 // CTA's scales (gathered in shared memory) are written 128 bytes at a time.
-// ROW_WARPS 8: a CTA per row, for the latency of few rows, and for long ones.
+// ROW_WARPS 8: a CTA per row, for the latency of few rows, and for long ones; 0: with
+// fewer warps, as many as the launch has (fp32 40000 x 5120 141 us, with 256 threads of
+// which three eighths are idle 246; bf16 100000 x 2560 156, 210).
 // NV: vectors of eight values that a lane keeps.  SHIFTED: not all rows of x and of
 // the values lie at 16-byte addresses.
 //
 // Bound by bytes where rows lie at 16-byte addresses: 262144 x 1152 bf16 144 us, with
 // bf16 values 225 (of a copy's rate 0.79 and 0.90), fp32 234 (0.87), 16384 x 8192 bf16
-// with values 99 (0.91).  Elsewhere by the instructions that take vectors apart and
+// with values 99 (0.91), 100395 x 3008 256 (0.79).  Elsewhere by the instructions that take vectors apart and
 // join them: 262144 x 1001 bf16 194 us, with values 336 (0.51 and 0.52; value by value
 // 483), fp32 272 (0.65).  32 x 1152 fp32: 1.4 us.
 //
@@ -248,7 +250,8 @@ template <typename T, typename TV, int ROW_WARPS, int NV, bool SHIFTED>
 __global__ void __launch_bounds__(kQuantizeThreads, kQuantizeCtas<T, TV, ROW_WARPS, NV>)
     quantize_kernel(const QuantizeParams a) {
     constexpr bool kMany = ROW_WARPS == 1;
-    constexpr int kRowLanes = 32 * ROW_WARPS, kRounds = kMany ? 4 : 1;
+    constexpr int kRounds = kMany ? 4 : 1;
+    const int row_lanes = ROW_WARPS > 0 ? 32 * ROW_WARPS : static_cast<int>(blockDim.x);
     constexpr bool kValues = !std::is_same<TV, None>::value;
     extern __shared__ __align__(16) uint8_t scale_bytes[];  // kMany: [tiles][row % 8 of 32][row / 32][4]
     __shared__ uint32_t warp_top[kQuantizeWarps];
@@ -272,7 +275,7 @@ __global__ void __launch_bounds__(kQuantizeThreads, kQuantizeCtas<T, TV, ROW_WAR
         uint32_t tops[NV], top = 0;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int j = 8 * (k * kRowLanes + at);
+            const int j = 8 * (k * row_lanes + at);
             raw[k] = {};
             if (j < width) {
                 if constexpr (SHIFTED) raw[k].load_shifted(row + j, width - j, shift);
@@ -289,7 +292,7 @@ __global__ void __launch_bounds__(kQuantizeThreads, kQuantizeCtas<T, TV, ROW_WAR
             if ((threadIdx.x & 31) == 0) warp_top[warp] = top;
             __syncthreads();
 #pragma unroll
-            for (int w = 0; w < kQuantizeWarps; ++w) top = max(top, warp_top[w]);
+            for (int w = 0; w < kQuantizeWarps; ++w) top = max(top, 32 * w < row_lanes ? warp_top[w] : 0u);
         }
         const bool finite = top < 0x7F800000u;
         const int E = e2m1_exponent(finite ? top : 0u);
@@ -307,8 +310,8 @@ __global__ void __launch_bounds__(kQuantizeThreads, kQuantizeCtas<T, TV, ROW_WAR
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            if (k * kRowLanes >= 8 * tiles) break;  // (the same for all lanes: they exchange)
-            const int vec = k * kRowLanes + at, left = width - 8 * vec;
+            if (k * row_lanes >= 8 * tiles) break;  // (the same for all lanes: they exchange)
+            const int vec = k * row_lanes + at, left = width - 8 * vec;
             const uint32_t block_top = max(tops[k], __shfl_xor_sync(0xFFFFFFFFu, tops[k], 1));
             const uint32_t sigma8 = to_e4m3(quotient(__uint_as_float(block_top) * inv, 6.0f, 1.0f / 6.0f));
             const float sigma = from_e4m3(sigma8);
@@ -449,20 +452,31 @@ static vie_status check_e2m1(const char *fn, int64_t n, const void *codes, const
 // 8.0 / 6.4, 8192 8.8 / 11.6; 2048, 4096 11.0 / 7.1, 8192 11.9 / 13.0, 16384 16.5 / 25.1).
 static bool by_warps(int64_t n, int d) { return d <= 2048 && n >= 1024 + 4 * static_cast<int64_t>(d); }
 
+// With the warps that a row's vectors keep busy, or all (nine tenths of the time of a
+// kernel that has to ask; eight vectors of fp32 in 192 threads leave an SM 384 of them,
+// in 256 with a quarter idle 512: 16000 x 12288 173 us, 150).
+template <typename T, typename TV, int NV, bool SHIFTED>
+static cudaError_t start_by_cta(const QuantizeParams &p, int64_t rows, cudaStream_t s) {
+    const dim3 grid(static_cast<unsigned>(rows));
+    const int threads = (8 * e2m1_tiles(p.d) / NV + 31) / 32 * 32;
+    return threads > (NV == 8 ? 160 : kQuantizeThreads - 32)
+               ? launch(quantize_kernel<T, TV, kQuantizeWarps, NV, SHIFTED>, grid, kQuantizeThreads, 0, s, p)
+               : launch(quantize_kernel<T, TV, 0, NV, SHIFTED>, grid, threads, 0, s, p);
+}
+
 template <typename T, typename TV, bool SHIFTED>
 static cudaError_t start_quantize_rows(const QuantizeParams &p, cudaStream_t s) {
     const int64_t rows = (p.n + kE2m1TileRows - 1) / kE2m1TileRows * kE2m1TileRows;  // with those that have scales alone
-    constexpr int W = kQuantizeWarps, NT = kQuantizeThreads;
     if (by_warps(p.n, p.d)) {
         const dim3 grid(static_cast<unsigned>(rows / 32));
         const size_t smem = static_cast<size_t>(e2m1_tiles(p.d)) * 128;
-        return p.d <= 1024 ? launch(quantize_kernel<T, TV, 1, 4, SHIFTED>, grid, NT, smem, s, p)
-                           : launch(quantize_kernel<T, TV, 1, 8, SHIFTED>, grid, NT, smem, s, p);
+        return p.d <= 1024 ? launch(quantize_kernel<T, TV, 1, 4, SHIFTED>, grid, kQuantizeThreads, smem, s, p)
+                           : launch(quantize_kernel<T, TV, 1, 8, SHIFTED>, grid, kQuantizeThreads, smem, s, p);
     }
-    const dim3 grid(static_cast<unsigned>(rows));
-    return p.d <= 2048   ? launch(quantize_kernel<T, TV, W, 1, SHIFTED>, grid, NT, 0, s, p)
-           : p.d <= 4096 ? launch(quantize_kernel<T, TV, W, 2, SHIFTED>, grid, NT, 0, s, p)
-                         : launch(quantize_kernel<T, TV, W, VIE_D_MAX / (8 * NT), SHIFTED>, grid, NT, 0, s, p);
+    if (p.d <= 2048) return start_by_cta<T, TV, 1, SHIFTED>(p, rows, s);
+    if (p.d <= 4096) return start_by_cta<T, TV, 2, SHIFTED>(p, rows, s);
+    if (p.d <= 8192) return start_by_cta<T, TV, 4, SHIFTED>(p, rows, s);
+    return start_by_cta<T, TV, 8, SHIFTED>(p, rows, s);
 }
 
 template <typename T, typename TV>

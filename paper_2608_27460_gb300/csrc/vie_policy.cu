@@ -86,8 +86,8 @@ __device__ __forceinline__ float2 policy_terms(const PolicyTerms &a, const RowTe
 //
 // Bound by bytes.  Measured on bf16 logits, and as a share of the time that a copy of
 // the bytes read and written once would take:
-//   log-probabilities  262144 x 1024: 79 us (1.0), 128256 x 2048: 83 (0.93), 20011 x 4096: 34 (0.71)
-//   their gradient     151936 x 4096: 363 us (1.0), 128256 x 2048: 159 (0.97), 20011 x 4096: 54 (0.89)
+//   log-probabilities  262144 x 2048: 155 us (1.0), 128256 x 2048: 81 (0.96), 20011 x 4096: 34 (0.71)
+//   their gradient     151936 x 4096: 372 us (0.98), 128256 x 2048: 156 (1.0), 20011 x 4096: 54 (0.89)
 //   both               151936 x 4096: 446 us (0.82), 262144 x 1024: 193 (0.82), 32000 x 4096:
 //                      92 (0.84); fp32 151936 x 2048: 426 (0.86); 1000003 x 128: 125 (0.60)
 // What is left in the last: each row's exchange, which the CTAs' other rows hide in

@@ -86,6 +86,23 @@ def test_rows_and_values_at_every_address(vie, n, dtype, values):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [1793, 2049, 2500, 3585, 4097, 5376, 7169, 8193, 8200, 10240, 10241, 12289, 16383])
+def test_long_rows(vie, dtype, d):
+    """Rows about the widths at which a CTA has another number of warps or of vectors per lane."""
+    n = 5
+    for off, ld in ((0, (d + 15) // 16 * 16), (1, d), (6, d + 5)):
+        x = _rows(n, d, dtype, seed=d + off)
+        x[1, d - 1] = 300.0  # a row's largest at its end
+        big = torch.full((off + n * ld + 16,), float("nan"), dtype=DT[dtype], device="cuda")
+        xc = big[off:off + n * ld].view(n, ld)[:, :d]
+        xc.copy_(x)
+        _check_rows(vie, x, xc)
+        want = ref.quantize(x)[3].to(DT[dtype])
+        vie.e2m1_quantize(xc, out_values=xc)
+        assert torch.equal(xc.cpu(), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n,d", [(1, 5), (2, 1023), (33, 1024), (130, 1025), (257, 1030), (3, 2052), (300, 64), (1, 16384)])
 def test_values_at_every_address(vie, dtype, n, d):
     """Widths about the 1024 columns that a warp reads at once, rows at and off 16-byte addresses; what lies
