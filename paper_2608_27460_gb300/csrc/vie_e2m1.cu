@@ -234,20 +234,25 @@ struct None {};  // no values wanted
 // NV: vectors of eight values that a lane keeps.  SHIFTED: not all rows of x and of
 // the values lie at 16-byte addresses.
 //
-// Bound by bytes where rows lie at 16-byte addresses: 262144 x 1152 bf16 144 us, with
-// bf16 values 225 (of a copy's rate 0.79 and 0.90), fp32 234 (0.87), 16384 x 8192 bf16
-// with values 99 (0.91), 100395 x 3008 256 (0.79).  Elsewhere by the instructions that take vectors apart and
-// join them: 262144 x 1001 bf16 194 us, with values 336 (0.51 and 0.52; value by value
-// 483), fp32 272 (0.65).  32 x 1152 fp32: 1.4 us.
+// Bound by bytes where rows lie at 16-byte addresses: 262144 x 1152 bf16 127 us, with
+// bf16 values 202 (of a copy's rate 0.90 and 1.0), fp32 196 (1.0), 30000 x 8192 bf16
+// with values 175 (0.94), 100395 x 3008 256 (0.79).  Elsewhere by the instructions that
+// take vectors apart and join them: 262144 x 1001 bf16 171 us, with values 336 (0.58 and
+// 0.52; value by value 483), fp32 272 (0.65).  32 x 1152 fp32: 1.4 us.
 //
-// CTAs per SM: what the registers of a row leave (262144 x 1152 bf16 with values: 229
-// us with three, 262 with two; without values 141 with four, 155 with three).
+// CTAs per SM: what the registers of a row leave.  They are what bounds a warp per row,
+// and vectors that it does not have cost as many, so NV goes by one there (262144 x 1152
+// bf16: five vectors 127 us, with values 202; eight 145 and 225; fp32 196, 234).
 template <typename T, typename TV, int ROW_WARPS, int NV>
-constexpr int kQuantizeCtas = sizeof(T) == 4 ? (NV > 4 ? 2 : 3)
-                              : ROW_WARPS == 1 && NV > 4 && !std::is_same<TV, None>::value ? 3 : 4;
+constexpr int quantize_ctas() {
+    const bool values = !std::is_same<TV, None>::value;
+    if (sizeof(T) == 4) return ROW_WARPS != 1 ? (NV > 4 ? 2 : 3) : NV > 6 ? 2 : NV > 3 ? 3 : 4;
+    if (ROW_WARPS != 1) return 4;
+    return values ? (NV > 6 ? 3 : NV > 3 ? 4 : 5) : NV > 5 ? 4 : NV > 3 ? 5 : 6;
+}
 
 template <typename T, typename TV, int ROW_WARPS, int NV, bool SHIFTED>
-__global__ void __launch_bounds__(kQuantizeThreads, kQuantizeCtas<T, TV, ROW_WARPS, NV>)
+__global__ void __launch_bounds__(kQuantizeThreads, quantize_ctas<T, TV, ROW_WARPS, NV>())
     quantize_kernel(const QuantizeParams a) {
     constexpr bool kMany = ROW_WARPS == 1;
     constexpr int kRounds = kMany ? 4 : 1;
@@ -470,8 +475,12 @@ static cudaError_t start_quantize_rows(const QuantizeParams &p, cudaStream_t s) 
     if (by_warps(p.n, p.d)) {
         const dim3 grid(static_cast<unsigned>(rows / 32));
         const size_t smem = static_cast<size_t>(e2m1_tiles(p.d)) * 128;
-        return p.d <= 1024 ? launch(quantize_kernel<T, TV, 1, 4, SHIFTED>, grid, kQuantizeThreads, smem, s, p)
-                           : launch(quantize_kernel<T, TV, 1, 8, SHIFTED>, grid, kQuantizeThreads, smem, s, p);
+        auto by_warp = [&](auto kernel) { return launch(kernel, grid, kQuantizeThreads, smem, s, p); };
+        return p.d <= 768    ? by_warp(quantize_kernel<T, TV, 1, 3, SHIFTED>)
+               : p.d <= 1024 ? by_warp(quantize_kernel<T, TV, 1, 4, SHIFTED>)
+               : p.d <= 1280 ? by_warp(quantize_kernel<T, TV, 1, 5, SHIFTED>)
+               : p.d <= 1536 ? by_warp(quantize_kernel<T, TV, 1, 6, SHIFTED>)
+                             : by_warp(quantize_kernel<T, TV, 1, 8, SHIFTED>);
     }
     if (p.d <= 2048) return start_by_cta<T, TV, 1, SHIFTED>(p, rows, s);
     if (p.d <= 4096) return start_by_cta<T, TV, 2, SHIFTED>(p, rows, s);
