@@ -453,8 +453,9 @@ static vie_status check_e2m1(const char *fn, int64_t n, const void *codes, const
 // Rows from which on a warp takes each.  A warp's four rows one after the other are a
 // latency that few rows do not hide, a CTA per row a cost that many add up; the longer
 // the rows, the later the second is the larger (bf16, us by warps / by CTAs: 64 columns,
-// 1024 rows 2.6 / 2.2, 2048 2.8 / 3.3; 640, 2048 3.8 / 3.5, 4096 5.3 / 5.9; 1152, 4096
-// 8.0 / 6.4, 8192 8.8 / 11.6; 2048, 4096 11.0 / 7.1, 8192 11.9 / 13.0, 16384 16.5 / 25.1).
+// 1024 rows 3.1 / 2.0, 2048 2.9 / 2.9; 640, 2048 3.9 / 2.9, 4096 4.0 / 5.3; 1152, 4096
+// 5.7 / 6.0, 8192 8.2 / 9.9; 2048, 4096 8.0 / 7.2, 8192 11.6 / 12.8, 16384 16.7 / 24.7;
+// with values 1152, 6000 9.7 / 8.5, 8192 10.8 / 10.9).
 static bool by_warps(int64_t n, int d) { return d <= 2048 && n >= 1024 + 4 * static_cast<int64_t>(d); }
 
 // With the warps that a row's vectors keep busy, or all (nine tenths of the time of a
