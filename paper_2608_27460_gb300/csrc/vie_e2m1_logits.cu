@@ -313,6 +313,9 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
                     ok = false;
                     break;
                 }
+                // The MMAs that read these columns are over (their commit freed the stage that
+                // `full` says is filled again): the stores to them come behind that.
+                tc_fence_after_sync();
                 // (what lies behind the matrix's last scales is not used by an MMA)
                 const uint4 *const sc = reinterpret_cast<const uint4 *>(ring_s + s * (1 + Sh::kXTiles) * Sh::kSet) + lane;
                 constexpr int kTile = kE2m1TileBytes / 16, kSet = Sh::kSet / 16;

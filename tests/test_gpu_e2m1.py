@@ -235,6 +235,26 @@ def test_logits_of_whole_numbers_are_exact(vie, n, V, d):
     assert vie.vie_device_status() == vie.VIE_OK
 
 
+@pytest.mark.parametrize("n,V,d", [(1, 60001, 4096), (16, 60001, 4096), (40, 60001, 4096), (100, 60001, 4096), (257, 60001, 4096),
+                                   (600, 40000, 1152)])
+def test_scales_of_their_own_stage(vie, n, V, d):
+    """Block scales that differ from each 64 columns to the next, by powers that cancel between the two
+    matrices, so that a sum is a whole number again only if each product meets the scales of its own
+    columns: tens of stages a tile and several tiles a CTA, whose scales go through the same columns of
+    tensor memory in turn."""
+    g = torch.Generator().manual_seed(61)
+    power = 2.0 ** torch.randint(-3, 4, ((d + 63) // 64,), generator=g).float().repeat_interleave(64)[:d]
+    v = torch.tensor([0.0, 1.0, 2.0, 3.0, 4.0, 6.0, -1.0, -2.0, -3.0, -4.0, -6.0])
+    x, w = (v[torch.randint(0, len(v), (rows, d), generator=g)] for rows in (n, V))
+    x[:, ::16], w[:, ::16] = 6.0, -6.0
+    want = x.cuda().double() @ w.cuda().double().t()
+    xq, wq = vie.e2m1_quantize((x * power).cuda()), vie.e2m1_quantize((w / power).cuda())
+    assert torch.equal(vie.e2m1_dequantize(wq), (w / power).cuda()) and torch.equal(vie.e2m1_dequantize(xq), (x * power).cuda())
+    for _ in range(3):
+        assert torch.equal(vie.e2m1_logits(xq, wq).double(), want)
+    assert vie.vie_device_status() == vie.VIE_OK
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n,V,d", SHAPES[:14])
 def test_logits_of_any_rows(vie, dtype, n, V, d):
