@@ -753,8 +753,8 @@ vie_status vie_e2m1_dequantize(const void *codes, const void *scales, const floa
  * vie_e2m1_logits - full logits of a head whose rows are e2m1, for hidden states
  * that are e2m1 as well:
  *   out[i, v] = sum_j x[i, j] w[v, j],
- * products exact, sums fp32, rounded once to out_dtype.  (Where the product of the
- * rows' powers of two s is below 2^-149 or above 2^127, results are 0 or infinite.)
+ * products exact, sums fp32, rounded once to out_dtype (results below 2^-126 to fp32
+ * before that), whatever the rows' powers of two.
  * vie_sample_logits draws from them, vie_token_logprobs scores them.
  *   x_*         device, n rows of d values;  0 <= n <= VIE_MANY_MAX.
  *   w_*         device, V rows of d values;  1 <= V <= VIE_E2M1_N_MAX.

@@ -538,10 +538,11 @@ static vie_status start_logits(const char *fn, const void *x_codes, const void *
     E2m1Product p = {};
     cudaError_t e = device_flag_word(&p.flag);
     if (e != cudaSuccess) return fail_cuda(e, fn);
+    p.x_codes = static_cast<const uint8_t *>(x_codes), p.w_codes = static_cast<const uint8_t *>(w_codes);
     p.x_scales = static_cast<const uint8_t *>(x_scales), p.w_scales = static_cast<const uint8_t *>(w_scales);
     p.x_row_scales = x_row_scales, p.w_row_scales = w_row_scales;
     p.out = out, p.ld = ld_out, p.n = n, p.V = V, p.d = d, p.w_ready = w_ready;
-    e = launch_e2m1_logits(p, static_cast<const uint8_t *>(x_codes), static_cast<const uint8_t *>(w_codes), out_dtype, s);
+    e = launch_e2m1_logits(p, out_dtype, s);
     return e == cudaSuccess ? VIE_OK : fail_cuda(e, fn);
 }
 

@@ -74,12 +74,47 @@ struct E2m1Shape {
     static_assert(kStages >= 2 && kStages <= 16, "ring");
 };
 
+// Whether s t, the powers of two of a row of x and of a vocabulary row, is infinite or 0
+// where their result, sum s t, may be neither: a sum is 0 or between 2^-20 (codes 1/2,
+// scales 2^-9) and 2^37 (2^14 products of 2688^2), so below 2^-187 all results are 0 (those
+// of two rows of zeros, whose powers are 2^-126, among them).
+__device__ __forceinline__ bool is_far(float s, float t) {
+    const float both = s * t;
+    return both == INFINITY || (both == 0.0f && s * 0x1p40f * t != 0.0f);
+}
+// Some rows' powers s: the least above 2^-126, the largest, and 2^-126 if it is among them
+// (rows of zeros, as padding has them, are apart) or 1.  is_far has no s for a t from `from`
+// to below `to`.
+struct PowerRange {
+    float from, to, least, largest, lowest;
+    __device__ __forceinline__ void set(float least_, float largest_, float lowest_) {
+        least = least_, largest = largest_, lowest = lowest_;
+        from = fmaxf(0x1p-149f / least, lowest < 1.0f ? 0x1p-23f : 0.0f);
+        to = largest > 2.0f ? 0x1p127f / (0.5f * largest) : INFINITY;
+    }
+    __device__ __forceinline__ bool may_be_far(float t) const {
+        return !(t >= from && t < to) && (least * t == 0.0f || largest * t == INFINITY || is_far(lowest, t));
+    }
+};
+// sum s t then.  t = first last, and of sum * first * s * last one product is inexact, at
+// most, which is the result's own: s and t are between 2^-126 and 2^117.  For t from
+// 2^-100 to 2^90, sum t is a number.  Where t is larger, sum first is one, times s it is
+// above 2^-82, and infinite only where the result is; where t is smaller, sum first is above
+// 2^-106, times s below 2^94, and below 2^-126 only where the result is below 2^-166,
+// which is 0.
+__device__ __forceinline__ float far_product(float sum, float s, float t) {
+    const float last = t < 0x1p-100f ? 0x1p-40f : t > 0x1p90f ? 0x1p27f : 1.0f;
+    const float first = t < 0x1p-100f ? t * 0x1p40f : t > 0x1p90f ? t * 0x1p-27f : t;
+    return sum * first * s * last;
+}
+
 template <int BN>
 struct E2m1Smem {
     uint64_t full[16], scaled[16], empty[16], acc_full[2], acc_empty[2], final_bar;
     uint32_t tmem_base;
-    int abort;
+    int abort, any_far;
     float x_scale[E2m1Shape<BN>::kEpilogueWarps][E2m1Shape<BN>::kWarpCols];  // (no barrier between warps: one may give up)
+    PowerRange x_range[E2m1Shape<BN>::kEpilogueWarps];  // of those
 };
 
 // Ends a wait that ran out: the flag for the host, `abort` for the other roles.
@@ -139,11 +174,45 @@ struct ColumnStore {
     }
 };
 
+// Those results of a tile (vocabulary rows from v0 on, rows of x from i0 on), over what the
+// epilogue has written there; all threads of the CTA call, after its tiles.  Such rows are
+// hardly ever met, so this is the simplest way: a pair of rows per thread, from the codes.
+// (In the epilogue, any code besides sum (s t) costs all calls 2 to 16 %: its warps hand an
+// accumulator back while the MMAs wait for it.)  2.6 ms where all rows of 262144 x 1152
+// for 32 rows are such.
+template <typename T>
+__device__ __noinline__ void far_results(const E2m1Product &p, int64_t v0, int64_t i0, int rows) {
+    griddep_wait();
+    const int blocks = (p.d + 15) / 16, tiles = e2m1_tiles(p.d);
+    const int64_t pitch = e2m1_pitch(p.d);
+    for (int k = threadIdx.x; k < kE2m1TileRows * rows; k += blockDim.x) {
+        const int64_t v = v0 + k % kE2m1TileRows, i = i0 + k / kE2m1TileRows;
+        if (v >= p.V || i >= p.n) continue;
+        const float s = p.x_row_scales[i], t = p.w_row_scales[v];
+        if (!is_far(s, t)) continue;
+        const uint2 *const x = reinterpret_cast<const uint2 *>(p.x_codes + i * pitch);
+        const uint2 *const w = reinterpret_cast<const uint2 *>(p.w_codes + v * pitch);
+        float sum = 0.0f;
+        for (int b = 0; b < blocks; ++b) {
+            const uint2 cx = x[b], cw = w[b];
+            float xv[16], wv[16], part = 0.0f;
+            from_e2m1(cx.x, xv), from_e2m1(cx.y, xv + 8);
+            from_e2m1(cw.x, wv), from_e2m1(cw.y, wv + 8);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) part = fmaf(xv[j], wv[j], part);
+            const float sigma = from_e4m3(p.x_scales[e2m1_scale_at(i, b, tiles)]);
+            const float tau = from_e4m3(p.w_scales[e2m1_scale_at(v, b, tiles)]);
+            sum = fmaf(part, sigma * tau, sum);
+        }
+        store_value(static_cast<T *>(p.out) + i * p.ld + v, far_product(sum, s, t));
+    }
+}
+
 template <int BN, typename T, bool WORDS>
 __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
     e2m1_logits_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
-                       const __grid_constant__ CUtensorMap map_x_last, const E2m1Product p, int v_tiles, int x_tiles,
-                       int last_rows) {
+                       const __grid_constant__ CUtensorMap map_x_last, const __grid_constant__ E2m1Product p, int v_tiles,
+                       int x_tiles, int last_rows) {
     using Sh = E2m1Shape<BN>;
     constexpr int S = Sh::kStages;
     extern __shared__ unsigned char e2m1_smem[];
@@ -172,7 +241,7 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
             mbar_init(&sm.acc_empty[b], Sh::kEpilogueWarps);
         }
         mbar_init(&sm.final_bar, 1);
-        sm.abort = 0;
+        sm.abort = sm.any_far = 0;
         fence_mbar_init();
     }
     if (warp == 2) {
@@ -359,11 +428,22 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
             const int64_t i0 = static_cast<int64_t>(xt) * BN, v = vt * kE2m1TileRows + 32 * quarter + lane;
             if (xt != last_xt) {
                 __syncwarp();  // the scales of the last tile have been read
-                for (int c = lane; c < kCols; c += 32) x_scale[c] = i0 + c0 + c < p.n ? p.x_row_scales[i0 + c0 + c] : 0.0f;
+                float least = INFINITY, largest = 0.0f, lowest = 1.0f;
+                for (int c = lane; c < kCols; c += 32) {
+                    const bool real = i0 + c0 + c < p.n;
+                    const float s = real ? p.x_row_scales[i0 + c0 + c] : 0.0f;
+                    x_scale[c] = s;
+                    if (real && s > 0x1p-126f) least = fminf(least, s), largest = fmaxf(largest, s);
+                    else if (real && s <= 0x1p-126f) lowest = s;
+                }
+                least = -warp_max(-least), largest = warp_max(largest), lowest = -warp_max(-lowest);
+                if (lane == 0) sm.x_range[warp - 4].set(least, largest, lowest);
                 __syncwarp();
                 last_xt = xt;
             }
             const float tv = v < p.V ? p.w_row_scales[v] : 0.0f;
+            const int rows = static_cast<int>(min(static_cast<int64_t>(kCols), p.n - i0 - c0));
+            ColumnStore<T, WORDS> put(static_cast<T *>(p.out) + (i0 + c0) * p.ld, p.ld, v, p.V, rows);
             if (!mbar_wait(&sm.acc_full[b], ub & 1, abort)) {
                 if (lane == 0) give_up(p.flag, &sm.abort);
                 break;
@@ -372,13 +452,13 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
             const uint32_t acc = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + b * BN + c0;
             // The accumulator is handed back as soon as its last columns are in registers:
             // 64 of fp32, or 128 rounded to bf16.
-            const int rows = static_cast<int>(min(static_cast<int64_t>(kCols), p.n - i0 - c0));
-            ColumnStore<T, WORDS> put(static_cast<T *>(p.out) + (i0 + c0) * p.ld, p.ld, v, p.V, rows);
-            // (the powers of two first: of large rows with small ones neither product overflows)
-            auto scaled = [&](uint32_t bits, int c) { return __uint_as_float(bits) * (x_scale[c] * tv); };
+            auto scaled = [&](uint32_t sum, int c) { return __uint_as_float(sum) * (x_scale[c] * tv); };
             auto hand_back = [&] {
                 tc_fence_before_sync();
                 if (lane == 0) mbar_arrive(&sm.acc_empty[b]);
+                if (v < p.V && sm.x_range[warp - 4].may_be_far(tv))
+                    for (int c = 0; c < kCols; ++c)  // (of columns beyond the last, s is 0)
+                        if (is_far(x_scale[c], tv)) *static_cast<volatile int *>(&sm.any_far) = 1;
             };
             if constexpr (sizeof(T) == 2 && kCols == 128) {
                 uint32_t r[64];
@@ -425,6 +505,9 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
         tc_fence_after_sync();
         tmem_dealloc(tmem, 512);
     }
+    if (sm.any_far && sm.abort == 0)
+        for (int64_t t = blockIdx.x; t < total; t += gridDim.x)
+            far_results<T>(p, t / x_tiles * kE2m1TileRows, t % x_tiles * BN, BN);
 }
 
 // SMs of the current device.
@@ -440,8 +523,7 @@ static cudaError_t sm_count(int *sms) {
 }
 
 template <int BN, typename T, bool WORDS>
-static cudaError_t start_e2m1_logits(const E2m1Product &p, const uint8_t *x_codes, const uint8_t *w_codes,
-                                     cudaStream_t stream) {
+static cudaError_t start_e2m1_logits(const E2m1Product &p, cudaStream_t stream) {
     using Sh = E2m1Shape<BN>;
     auto kernel = e2m1_logits_kernel<BN, T, WORDS>;
     static PerDevice prepared;
@@ -454,12 +536,12 @@ static cudaError_t start_e2m1_logits(const E2m1Product &p, const uint8_t *x_code
     const int x_tiles = static_cast<int>((p.n + BN - 1) / BN);
     const int last_rows = static_cast<int>(p.n - static_cast<int64_t>(x_tiles - 1) * BN + 7) / 8 * 8;  // BN at most
     CUtensorMap map_w, map_x, map_x_last;
-    if (!make_map_u8(&map_w, const_cast<uint8_t *>(w_codes), static_cast<uint64_t>(p.V), pitch, pitch, kE2m1TileRows) ||
-        !make_map_u8(&map_x_last, const_cast<uint8_t *>(x_codes), static_cast<uint64_t>(p.n), pitch, pitch,
+    if (!make_map_u8(&map_w, const_cast<uint8_t *>(p.w_codes), static_cast<uint64_t>(p.V), pitch, pitch, kE2m1TileRows) ||
+        !make_map_u8(&map_x_last, const_cast<uint8_t *>(p.x_codes), static_cast<uint64_t>(p.n), pitch, pitch,
                      static_cast<uint32_t>(last_rows)))
         return cudaErrorInvalidValue;
     map_x = map_x_last;  // (the only one where there is one tile)
-    if (x_tiles > 1 && !make_map_u8(&map_x, const_cast<uint8_t *>(x_codes), static_cast<uint64_t>(p.n), pitch, pitch, BN))
+    if (x_tiles > 1 && !make_map_u8(&map_x, const_cast<uint8_t *>(p.x_codes), static_cast<uint64_t>(p.n), pitch, pitch, BN))
         return cudaErrorInvalidValue;
     const int v_tiles = static_cast<int>((p.V + kE2m1TileRows - 1) / kE2m1TileRows);
     const int64_t total = static_cast<int64_t>(v_tiles) * x_tiles;
@@ -481,21 +563,19 @@ static cudaError_t start_e2m1_logits(const E2m1Product &p, const uint8_t *x_code
 // (128256 x 2048 bf16, us with tiles of 256 / of 128: 129 rows 35 / 46, 256 42 / 47, 512 72 / 86,
 // 2048 254 / 327; 100003 x 1000, 200 rows 24.8 / 24.0): they read W once per 256 rows.
 template <typename T, bool WORDS>
-static cudaError_t start_by_rows(const E2m1Product &p, const uint8_t *x_codes, const uint8_t *w_codes,
-                                 cudaStream_t stream) {
-    if (p.n <= 16) return start_e2m1_logits<16, T, WORDS>(p, x_codes, w_codes, stream);
-    if (p.n <= 32) return start_e2m1_logits<32, T, WORDS>(p, x_codes, w_codes, stream);
-    if (p.n <= 64) return start_e2m1_logits<64, T, WORDS>(p, x_codes, w_codes, stream);
-    if (p.n <= 128) return start_e2m1_logits<128, T, WORDS>(p, x_codes, w_codes, stream);
-    return start_e2m1_logits<256, T, WORDS>(p, x_codes, w_codes, stream);
+static cudaError_t start_by_rows(const E2m1Product &p, cudaStream_t stream) {
+    if (p.n <= 16) return start_e2m1_logits<16, T, WORDS>(p, stream);
+    if (p.n <= 32) return start_e2m1_logits<32, T, WORDS>(p, stream);
+    if (p.n <= 64) return start_e2m1_logits<64, T, WORDS>(p, stream);
+    if (p.n <= 128) return start_e2m1_logits<128, T, WORDS>(p, stream);
+    return start_e2m1_logits<256, T, WORDS>(p, stream);
 }
 
-cudaError_t launch_e2m1_logits(const E2m1Product &p, const uint8_t *x_codes, const uint8_t *w_codes, vie_dtype dtype,
-                               cudaStream_t stream) {
-    if (dtype == VIE_DTYPE_F32) return start_by_rows<float, false>(p, x_codes, w_codes, stream);
+cudaError_t launch_e2m1_logits(const E2m1Product &p, vie_dtype dtype, cudaStream_t stream) {
+    if (dtype == VIE_DTYPE_F32) return start_by_rows<float, false>(p, stream);
     const bool words = p.V % 2 == 0 && (p.n == 1 || p.ld % 2 == 0) && aligned_to(p.out, 4);
-    return words ? start_by_rows<__nv_bfloat16, true>(p, x_codes, w_codes, stream)
-                 : start_by_rows<__nv_bfloat16, false>(p, x_codes, w_codes, stream);
+    return words ? start_by_rows<__nv_bfloat16, true>(p, stream)
+                 : start_by_rows<__nv_bfloat16, false>(p, stream);
 }
 
 }  // namespace vie

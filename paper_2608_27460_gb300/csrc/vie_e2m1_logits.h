@@ -10,7 +10,7 @@
 namespace vie {
 
 struct E2m1Product {
-    const uint8_t *x_scales, *w_scales;
+    const uint8_t *x_codes, *w_codes, *x_scales, *w_scales;
     const float *x_row_scales, *w_row_scales;
     void *out;
     int64_t ld, n, V;
@@ -22,7 +22,6 @@ struct E2m1Product {
 };
 
 // out[i, v] = sum_j x[i, j] w[v, j] (vie_e2m1_logits).
-cudaError_t launch_e2m1_logits(const E2m1Product &p, const uint8_t *x_codes, const uint8_t *w_codes, vie_dtype dtype,
-                               cudaStream_t stream);
+cudaError_t launch_e2m1_logits(const E2m1Product &p, vie_dtype dtype, cudaStream_t stream);
 
 }  // namespace vie

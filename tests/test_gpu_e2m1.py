@@ -308,6 +308,33 @@ def test_logits_of_far_powers(vie):
     assert ((got - values).abs()[~far] <= 98 * ref.U * scale[~far] + 2.0 ** -148 + lost[~far]).all()
 
 
+@pytest.mark.parametrize("n", [7, 16, 30, 60, 66, 200])
+def test_logits_of_all_powers_are_exact(vie, n):
+    """Rows from one end of fp32 to the other, whose sums of codes are whole numbers, small ones, and 0 (rows
+    that share no column, products that cancel): the definition's values rounded to fp32, then to bf16."""
+    d = 96
+    powers = torch.tensor([-149, -140, -130, -126, -120, -110, -101, -100, -99, -90, -64, -30, 0, 17, 40, 64, 75, 90, 91, 100,
+                           110, 124])
+    g = torch.Generator().manual_seed(71)
+    v = torch.tensor([0.0, 1.0, 2.0, 3.0, 4.0, 6.0, -1.0, -2.0, -3.0, -4.0, -6.0])
+
+    def rows(sign):
+        x = v[torch.randint(0, len(v), (3 * len(powers), d), generator=g)]
+        x[:, ::16] = 6.0
+        x[0::3, :16], x[0::3, 16:32] = 1.0, sign
+        x[0::3, 32:] = 0.0                              # 0 in the product of two such rows, or 16 * 2
+        x[1::3].view(-1, d // 16, 16)[:, 1::2] = 0.0    # blocks that the next row has not
+        x[2::3].view(-1, d // 16, 16)[:, 0::2] = 0.0
+        return (x.double() * 2.0 ** powers.double().repeat_interleave(3)[:, None]).float()
+
+    x, w = rows(1.0).repeat(4, 1)[torch.randperm(4 * 3 * len(powers), generator=g)[:n]], rows(-1.0)
+    want = (ref.quantize(x)[3] @ ref.quantize(w)[3].t()).float()
+    assert (want == 0).any() and torch.isinf(want).any() and (want.abs() > 2.0 ** 100).any()
+    wq = vie.e2m1_quantize(w.cuda())
+    assert torch.equal(vie.e2m1_logits(x.cuda(), wq).cpu(), want)
+    assert torch.equal(vie.e2m1_logits(x.cuda(), wq, out_dtype=torch.bfloat16).cpu(), want.bfloat16())
+
+
 def test_the_same_bits_again_on_streams_and_in_a_graph(vie):
     n, V, d = 40, 30011, 640
     x, w = _rows(n, d, "f32", seed=21).cuda(), _rows(V, d, "bf16", seed=22).cuda()
