@@ -716,7 +716,9 @@ vie_status vie_preference_loss_step(const float *logprob, const float *ref_logpr
  * whole number (-126 at the least) with max |x| <= 2688 s; each block of 16 values
  * has a scale sigma = e4m3(max |x| over the block / (6 s)); a value's code is
  * e2m1(x / (s sigma)), at most 6 in magnitude (0 where sigma is 0), and stands for
- * code * sigma * s.  Roundings are to nearest, ties to even.  A row that holds a
+ * code * sigma * s.  Roundings are to nearest, ties to even; what rounds to 0 has the
+ * code 0 whatever its sign (never 8).  The same values in bf16 and in fp32 have the same
+ * codes, scales and row scales.  A row that holds a
  * NaN or an infinity has s = NaN and codes of 0: all that is made of it is NaN.
  *   codes       uint8 [n, ceil(d / 32) * 16]: two codes to a byte, the even column
  *               in the low four bits; columns from d on are 0.

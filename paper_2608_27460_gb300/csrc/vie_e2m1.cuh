@@ -5,7 +5,8 @@
 // at the least) with max |x| <= 6 * 448 * 2^E; each block of 16 values has a scale
 // sigma = e4m3(max |x| over it / (6 s)); a value's code is e2m1(x / (s sigma)), and
 // stands for code * sigma * s.  Roundings are to nearest, ties to even; a code is
-// at most 6 in magnitude (sigma may have been rounded down).  sigma in e4m3 and s
+// at most 6 in magnitude (sigma may have been rounded down), and that of a value that
+// rounds to 0 is 0 whatever its sign (the code of -0 is not used).  sigma in e4m3 and s
 // apart cover what sigma in fp32 would; that s is a power of two makes the
 // scaling of values and results exact.
 #pragma once
@@ -50,7 +51,7 @@ __device__ __forceinline__ uint32_t to_e2m1(const float *v) {
         "mov.b32 %0, {a, b, c, d};\n\t}"
         : "=r"(r)
         : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
-    return r;
+    return r & (((r & 0x77777777u) + 0x77777777u) | 0x77777777u);  // + 7 reaches a sign where the magnitude is not 0
 }
 // Eight codes to values.
 __device__ __forceinline__ void from_e2m1(uint32_t codes, float *v) {

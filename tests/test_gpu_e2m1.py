@@ -149,6 +149,36 @@ def test_ties_and_borders(vie):
     _check_rows(vie, x)
 
 
+@pytest.mark.parametrize("n,d", [(5, 200), (40, 3000), (2100, 257), (1500, 96)])
+def test_zeros_have_one_code(vie, n, d):
+    """Values of both signs that round to 0, zeros of both signs, blocks whose scale is 0: code 0, and the same
+    bytes from bf16 and from fp32 rows, at and off 16-byte addresses."""
+    g = torch.Generator().manual_seed(n)
+    x = torch.randn(n, d, generator=g) * 2.0 ** torch.randint(-40, 1, (n, d), generator=g).float()
+    x[:, ::7] = torch.where(torch.rand(n, (d + 6) // 7, generator=g) < 0.5, -0.0, 0.0)
+    x[:, 32:64] = -(2.0 ** -60)
+    x[:, 64::16] *= 2.0 ** 12
+    x = x.bfloat16()
+    want = ref.quantize(x)[0]
+    want = torch.where(want == 8, 0, want)
+    for off, ld in ((0, (d + 7) // 8 * 8), (1, d)):
+        first = None
+        for dtype in (torch.bfloat16, torch.float32):
+            big = torch.zeros((off + n * ld + 16,), dtype=dtype, device="cuda")
+            xc = big[off:off + n * ld].view(n, ld)[:, :d]
+            xc.copy_(x)
+            values = torch.empty((n, d), device="cuda")
+            for q in (vie.e2m1_quantize(xc), vie.e2m1_quantize(xc, out_values=values)):
+                codes = ref.unpack(q)[0]
+                assert torch.equal(codes[:, :d].long(), want) and not codes[:, d:].any()
+                assert not torch.signbit(vie.e2m1_dequantize(q)[vie.e2m1_dequantize(q) == 0]).any()
+                if first is None:
+                    first = q
+                assert torch.equal(q.codes, first.codes) and torch.equal(q.scales, first.scales)
+                assert torch.equal(q.row_scales, first.row_scales)
+            assert not torch.signbit(values[values == 0]).any()
+
+
 def test_ranges(vie):
     """Rows from subnormal numbers to the largest ones, rows of zeros, blocks that vanish beside others."""
     x = _rows(60, 96, "f32", seed=5)
