@@ -155,7 +155,15 @@ __device__ __forceinline__ uint64_t l2_evict_first_policy() {
     return pol;
 }
 
-// L2 policy for what is read again soon: its lines are the last to be evicted.
+// L2 policy of an access without one, where an instruction wants one.
+__device__ __forceinline__ uint64_t l2_normal_policy() {
+    uint64_t pol;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
+    return pol;
+}
+
+// L2 policy for what is read again soon: its lines are the last to be evicted, and stay
+// so behind the kernel, for little only.
 __device__ __forceinline__ uint64_t l2_evict_last_policy() {
     uint64_t pol;
     asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(pol));

@@ -49,6 +49,7 @@ namespace vie {
 
 constexpr int kE2m1Kb = 256;                // columns of a K-block: 128 bytes of codes a row, a box
 constexpr int kE2m1KbTiles = kE2m1Kb / 64;  // its scale tiles, and MMAs
+constexpr int64_t kMarkedBytes = 4 << 20;   // of x's codes: one thirtieth of L2
 
 template <int BN>
 struct E2m1Shape {
@@ -263,7 +264,13 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
         // its wait, its expected bytes and four or five copies.
         if (lane == 0) {
             const bool of_w = warp == 0;
-            const uint64_t policy = of_w && x_tiles == 1 ? l2_evict_first_policy() : l2_evict_last_policy();
+            // W that is read again for the next tile of x stays in L2 without a mark.  Marked as
+            // the last to be evicted, 128256 x 2048 for 2048 rows takes 257 us instead of 260, but
+            // such lines outlive the kernel: sums of 100 MB, read again and again, take 25.6 us
+            // after it for good, and 17.4 without.  x may have the mark up to what L2 does not miss
+            // (2.4 MB: 17.4; 9 MB 21.5).
+            const uint64_t policy = of_w ? x_tiles == 1 ? l2_evict_first_policy() : l2_normal_policy()
+                                    : p.n * e2m1_pitch(p.d) <= kMarkedBytes ? l2_evict_last_policy() : l2_normal_policy();
             unsigned char *const codes = of_w ? ring : ring_x;
             const int stage_codes = of_w ? Sh::kStageW : Sh::kStageX;
             const int sets = of_w ? 1 : Sh::kXTiles;
