@@ -40,6 +40,19 @@ class PerDevice {
     std::atomic<uint64_t> done_{0};
 };
 
+// SMs of the current device.
+inline cudaError_t sm_count(int *sms) {
+    static std::atomic<int> known[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const bool kept = dev >= 0 && dev < 64;
+    if (kept && (*sms = known[dev].load(std::memory_order_relaxed)) > 0) return cudaSuccess;
+    e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess && kept) known[dev].store(*sms, std::memory_order_relaxed);
+    return e;
+}
+
 inline bool aligned_to(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 inline int dtype_size(vie_dtype t) { return t == VIE_DTYPE_BF16 ? 2 : 4; }

@@ -34,7 +34,6 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
-#include <atomic>
 #include <cstdint>
 
 #include "vie_api.h"
@@ -515,18 +514,6 @@ __global__ void __launch_bounds__(E2m1Shape<BN>::kThreads, 1)
     if (sm.any_far && sm.abort == 0)
         for (int64_t t = blockIdx.x; t < total; t += gridDim.x)
             far_results<T>(p, t / x_tiles * kE2m1TileRows, t % x_tiles * BN, BN);
-}
-
-// SMs of the current device.
-static cudaError_t sm_count(int *sms) {
-    static std::atomic<int> known[64];
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev < 64 && (*sms = known[dev].load(std::memory_order_relaxed)) > 0) return cudaSuccess;
-    e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess && dev < 64) known[dev].store(*sms, std::memory_order_relaxed);
-    return e;
 }
 
 template <int BN, typename T, bool WORDS>

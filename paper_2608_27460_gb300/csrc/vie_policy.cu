@@ -214,33 +214,53 @@ __global__ void __launch_bounds__(kRowThreads, 4) policy_kernel(const PolicyPara
     r.finish(z_token, lp, m, s, leads);
 }
 
-// CTAs per row of n rows of this many bytes.
+// CTAs per row of n rows of this many bytes, on so many SMs (four CTAs each).
 //
-// Of a long row a slice that a CTA can take without losing what it read from L2, or its
-// turn: 64 KB of a gradient alone (128256 x 2048 bf16 166 us, in slices of 125 KB 171;
-// 217047 x 1500 195, in slices of 106 KB 199), 112 KB of loss and gradient (us with slices
-// of 40 / 81 KB, fp32 41353 x 2183: 131 / 123; of 53 / 106, bf16 217047 x 1500: 250 / 233;
-// of 62 / 125, 128256 x 1500: 138 / 146).
+// At most a slice that a CTA can take without losing what it read from L2, or its turn:
+// 64 KB of a gradient alone (128256 x 2048 bf16 166 us, in slices of 125 KB 171; 217047 x
+// 1500 195, in slices of 106 KB 199), 112 KB of loss and gradient (us with slices of 40 /
+// 81 KB, fp32 41353 x 2183: 131 / 123; of 53 / 106, bf16 217047 x 1500: 250 / 233; of 62 /
+// 125, 128256 x 1500: 138 / 146).
 //
-// Of few rows as many as fill the chip's four CTAs per SM, once: CTAs beyond that are a
-// second round.  With partials to exchange, clusters of four and eight only where they
-// leave more of it free, or slices stay long (us with 1 / 2 / 4 / 8, fp32 27566: 300 rows'
-// log-probabilities 7.2 / 6.6 / 9.3 / 13.3, loss and gradient 15.4 / 12.7 / 18.0 / 21.1; 150 rows
-// 10.3 / 9.0 / 10.3 / 11.6; 434 20.8 / 22.4 / 23.2 / 29.0; log-probabilities of 84 rows of
-// fp32 41353 6.2 / 5.8 / 4.9 / 6.2, of bf16 217047 20.2 / 14.6 / 12.9 / 12.2).
-static int slices_of_row(bool fwd, bool bwd, int64_t bytes, int64_t n) {
-    int slices = 1;
+// Among smaller ones, the quickest by what CTAs cost that run in rounds of as many as the
+// device has places for, in KB that one of a full round's CTAs reads: a round its slice and
+// 24 for the chain of token, slice, sum and result; a last round that is not full by its
+// share of the places, but no less than 1 / 1.6 of the slice (what one CTA alone can read);
+// an exchange 4.  Clusters of four and more find 24 of 25 places (of 152 SMs: 146 rows in
+// four slices already take a second round).  Slices of 12 KB or more, eight for a row
+// (sixteen up to kFewRows).
+//
+// Against the best number of slices, over 800 calls of 1 to 2048 rows of 40 to 1000 KB, rows
+// of other calls in between: 1 % slower on average, 17 % at the most (log-probabilities of
+// 305 rows of 424 KB: [35.3] us whole, 30.8 in halves, 30.1 in quarters).  (us with 1 / 2 / 4 / 8
+// slices, the rule's in brackets: log-probabilities of 620 rows of 217047 bf16 57.0 / [50.9] /
+// 52.1 / 59.2, of 300 of 27566 fp32 9.1 / [8.5] / 10.8 / 15.1; loss and gradient of 61 rows of
+// 65536 bf16 13.4 / 9.1 / 9.0 / [6.9], of 256 22.3 / [15.7] / 18.2 / 22.4.)
+//
+// A gradient's rounds wait for nothing: as many slices of 16 KB as an eighth more than one
+// round has places for (us with 4 / 8 / 16: 40 rows of 151936 bf16 7.8 / 6.2 / [5.8], 84 of
+// 27566 fp32 5.5 / [4.9] / -, 180 of 20011 bf16, which would take 720 CTAs, [4.6] in two, 5.2).
+static int slices_of_row(bool fwd, bool bwd, int64_t bytes, int64_t n, int sms) {
+    const int64_t places = 4 * static_cast<int64_t>(sms);
+    int64_t slices = 1;
     if (!fwd) {
         while (bytes / slices > 64 * 1024 && n * slices < (1 << 30)) slices *= 2;
-        while (slices < kMaxSlices && 2 * n * slices <= 672 && bytes / slices > 16 * 1024) slices *= 2;
-        return slices;
+        while (slices < kMaxSlices && 2 * n * slices <= places + places / 8 && bytes / slices > 16 * 1024) slices *= 2;
+        return static_cast<int>(slices);
     }
     if (bwd)
         while (slices < kSlices && bytes / slices > 112 * 1024) slices *= 2;
-    auto most = [&] { return slices == 1 ? 608 : slices == 4 && bytes / slices > 64 * 1024 ? 700 : 512; };
-    while (slices < (n <= kFewRows ? kMaxSlices : kSlices) && 2 * n * slices <= most() && bytes / slices > 32 * 1024)
-        slices *= 2;
-    return slices;
+    int64_t best = slices;
+    double least = INFINITY;
+    for (; slices <= (n <= kFewRows ? kMaxSlices : kSlices); slices *= 2) {
+        if (best != slices && bytes / slices < 12 * 1024) break;
+        const int64_t here = slices <= 2 ? places : places * 24 / 25, ctas = n * slices, rest = ctas % here;
+        const double kb = static_cast<double>(bytes) / 1024 / slices;
+        double cost = static_cast<double>(ctas / here) * (kb + 24) + (slices > 1 ? 4 : 0);
+        if (rest > 0) cost += fmax(kb * rest / here, kb / 1.6) + 24;
+        if (cost < least) least = cost, best = slices;
+    }
+    return static_cast<int>(best);
 }
 
 template <typename T, bool FWD, bool BWD, int U>
@@ -261,7 +281,10 @@ static vie_status launch_policy(const char *fn, PolicyParams &p, vie_dtype dtype
     if (n == 0) return VIE_OK;
     cudaError_t e = device_flag_word(&p.flag);
     if (e != cudaSuccess) return fail_cuda(e, fn);
-    const int slices = slices_of_row(FWD, BWD, static_cast<int64_t>(p.V) * dtype_size(dtype), n);
+    int sms = 0;
+    e = sm_count(&sms);
+    if (e != cudaSuccess) return fail_cuda(e, fn);
+    const int slices = slices_of_row(FWD, BWD, static_cast<int64_t>(p.V) * dtype_size(dtype), n, sms);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool bf16 = dtype == VIE_DTYPE_BF16;
     if constexpr (FWD && !BWD) {

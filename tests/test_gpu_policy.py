@@ -106,6 +106,18 @@ def test_rows_longer_than_any_slice(vie, dtype):
     _check(vie, z, tok, 1.0, grad, g, kls=(0.05,))
 
 
+@pytest.mark.parametrize("n,V,dtype", [(8, 51001, "bf16"), (9, 51001, "bf16"), (72, 51001, "bf16"), (73, 51001, "bf16"),
+                                       (85, 33001, "bf16"), (86, 33001, "bf16"), (145, 25003, "f32"), (146, 25003, "f32"),
+                                       (304, 13001, "bf16"), (305, 13001, "bf16"), (342, 8200, "f32"), (343, 8200, "f32"),
+                                       (608, 7001, "f32"), (609, 7001, "f32"), (1217, 7001, "bf16")])
+def test_rows_on_both_sides_of_a_round(vie, n, V, dtype):
+    """As many rows as one round of CTAs takes in each number of slices, and one more."""
+    z, tok, grad, g = _inputs(n, V, dtype, seed=n)
+    tok[::11] = -1
+    tok[1] = V - 1
+    _check(vie, z, tok, 1.0, grad, g, kls=(0.05,))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_every_place_of_the_token(vie, dtype):
     """All tokens of a small row, at every alignment: the edges' vectors and those between."""
