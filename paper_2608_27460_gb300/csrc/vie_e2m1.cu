@@ -451,12 +451,18 @@ static vie_status check_e2m1(const char *fn, int64_t n, const void *codes, const
 }
 
 // Rows from which on a warp takes each.  A warp's four rows one after the other are a
-// latency that few rows do not hide, a CTA per row a cost that many add up; the longer
-// the rows, the later the second is the larger (bf16, us by warps / by CTAs: 64 columns,
-// 1024 rows 3.1 / 2.0, 2048 2.9 / 2.9; 640, 2048 3.9 / 2.9, 4096 4.0 / 5.3; 1152, 4096
-// 5.7 / 6.0, 8192 8.2 / 9.9; 2048, 4096 8.0 / 7.2, 8192 11.6 / 12.8, 16384 16.7 / 24.7;
-// with values 1152, 6000 9.7 / 8.5, 8192 10.8 / 10.9).
-static bool by_warps(int64_t n, int d) { return d <= 2048 && n >= 1024 + 4 * static_cast<int64_t>(d); }
+// latency that few rows do not hide, a CTA per row a cost that many add up; the longer the
+// rows, the later the second is the larger, up to rows of 768 columns, and the later where
+// rows lie off 16-byte addresses and a warp has more to do for each (us by warps / by CTAs,
+// rows of other calls in between, bf16: 64 columns, 2048 rows 2.9 / 2.5, 4096 3.4 / 4.6; 512,
+// 8192 8.9 / 8.7; 1152, 6144 12.6 / 9.0, 12288 18.0 / 16.7, 16384 18.6 / 21.7; with values 1024,
+// 5120 12.9 / 7.3, 1152, 8192 14.8 / 13.3, 16384 19.9 / 25.8; 401 off, 16384 14.7 / 17.1, with
+// values 21.4 / 17.1, 20000 21.8 / 21.0).  Against the quicker one of the two, over 2100 calls of
+// 512 to 24576 rows: 0.5 % slower on average, at the most 22 % where rows lie at 16-byte
+// addresses, else 43 % (24576 x 2047 fp32: 78.6 us, by CTAs 54.9).
+static bool by_warps(int64_t n, int d, bool shifted, bool values) {
+    return d <= 2048 && n >= (2000 + 12 * static_cast<int64_t>(d < 768 ? d : 768)) * (shifted ? values ? 3 : 2 : 1);
+}
 
 // With the warps that a row's vectors keep busy, or all (nine tenths of the time of a
 // kernel that has to ask; eight vectors of fp32 in 192 threads leave an SM 384 of them,
@@ -473,7 +479,7 @@ static cudaError_t start_by_cta(const QuantizeParams &p, int64_t rows, cudaStrea
 template <typename T, typename TV, bool SHIFTED>
 static cudaError_t start_quantize_rows(const QuantizeParams &p, cudaStream_t s) {
     const int64_t rows = (p.n + kE2m1TileRows - 1) / kE2m1TileRows * kE2m1TileRows;  // with those that have scales alone
-    if (by_warps(p.n, p.d)) {
+    if (by_warps(p.n, p.d, SHIFTED, !std::is_same<TV, None>::value)) {
         const dim3 grid(static_cast<unsigned>(rows / 32));
         const size_t smem = static_cast<size_t>(e2m1_tiles(p.d)) * 128;
         auto by_warp = [&](auto kernel) { return launch(kernel, grid, kQuantizeThreads, smem, s, p); };

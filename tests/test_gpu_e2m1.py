@@ -58,22 +58,25 @@ def test_many_rows(vie, dtype, n, d):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("d", [767, 768, 769, 1024, 1025, 1152, 1280, 1281, 1400, 1536, 1537, 1800, 2040])
+@pytest.mark.parametrize("d", [1, 9, 16, 33, 64, 97, 250, 257, 300, 640, 767, 768, 769, 1001, 1024, 1025, 1152, 1280, 1281, 1400,
+                               1536, 1537, 1800, 2040, 2048])
 def test_many_rows_of_every_width(vie, dtype, d):
     """Rows that a warp takes each, on both sides of the widths at which its lanes keep another number of vectors,
     with both kinds of values, apart and in place of the rows, at and off 16-byte addresses: the definition's
     bytes in the first and last tile, and those of calls of few rows (a CTA each) in all others."""
-    n = 1024 + 4 * d + 200
-    x = _rows(n, d, dtype, seed=d)
+    n = 3 * (2000 + 12 * min(d, 768)) + 200
+    g = torch.Generator(device="cuda").manual_seed(d)
+    x = torch.randn(n, d, generator=g, device="cuda") * torch.exp(2.0 * torch.randn(n, 1, generator=g, device="cuda"))
+    x = x.to(DT[dtype])
     x[n - 2, d - 1], x[5, 0], x[131] = math.inf, math.nan, 0.0
     x[n - 1, d - 1] = 300.0  # a row's largest at its end
-    for off, ld in ((0, (d + 7) // 8 * 8), (3, d + 1)):
+    for (off, ld), (o, l) in (((0, (d + 7) // 8 * 8), (0, (d + 7) // 8 * 8)), ((3, d + 1), (3, d + 1)), ((1, d), (7, d + 2))):
         big = torch.full((off + n * ld + 16,), float("nan"), dtype=DT[dtype], device="cuda")
         xc = big[off:off + n * ld].view(n, ld)[:, :d]
         xc.copy_(x)
         q = vie.e2m1_quantize(xc)
         for rows in (slice(0, 128), slice((n - 1) // 128 * 128, n)):
-            code, byte, s, want = ref.quantize(x[rows])
+            code, byte, s, want = ref.quantize(x[rows].cpu())
             tiles = slice(rows.start // 128, rows.start // 128 + 1)
             codes, scales, row = ref.unpack(vie.E2m1(q.codes[rows], q.scales[tiles], q.row_scales[rows], d))
             good = torch.isfinite(s)
@@ -82,22 +85,23 @@ def test_many_rows_of_every_width(vie, dtype, d):
             assert torch.equal(scales[:m, :blocks][good], byte[good]) and not scales[m:].any() and not scales[:, blocks:].any()
             assert torch.equal(torch.isnan(row), ~good) and torch.equal(row[good].double(), s[good])
         few = torch.empty((n, d), device="cuda")
-        for r0 in range(0, n, 512):
-            part = vie.e2m1_quantize(xc[r0:r0 + 512], out_values=few[r0:r0 + 512])
+        for r0 in range(0, n, 1024):
+            part = vie.e2m1_quantize(xc[r0:r0 + 1024], out_values=few[r0:r0 + 1024])
             m = part.codes.shape[0]
             assert torch.equal(q.codes[r0:r0 + m], part.codes)
             assert torch.equal(q.scales[r0 // 128:(r0 + m + 127) // 128], part.scales)
             assert torch.equal(q.row_scales[r0:r0 + m].nan_to_num(9.0), part.row_scales.nan_to_num(9.0))
+        few = few.nan_to_num(9.0)
         for values in ("bf16", "f32"):
-            out = torch.full((off + n * ld + 16,), 7.0, dtype=DT[values], device="cuda")
-            view = out[off:off + n * ld].view(n, ld)[:, :d]
+            out = torch.full((o + n * l + 16,), 7.0, dtype=DT[values], device="cuda")
+            view = out[o:o + n * l].view(n, l)[:, :d]
             q2 = vie.e2m1_quantize(xc, out_values=view)
             assert torch.equal(q2.codes, q.codes) and torch.equal(q2.scales, q.scales)
-            assert torch.equal(view.nan_to_num(9.0), few.to(DT[values]).nan_to_num(9.0))
+            assert torch.equal(view.nan_to_num(9.0), few.to(DT[values]))
             view.fill_(7.0)
             assert (out == 7.0).all()
         vie.e2m1_quantize(xc, out_values=xc)
-        assert torch.equal(xc.nan_to_num(9.0), few.to(DT[dtype]).nan_to_num(9.0))
+        assert torch.equal(xc.nan_to_num(9.0), few.to(DT[dtype]))
 
 
 @pytest.mark.parametrize("n", [40, 1500])
