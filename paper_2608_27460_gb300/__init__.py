@@ -1059,8 +1059,11 @@ def e2m1_logits(x, weights, out=None, out_dtype=None, x_quantized=None, stream=N
     """Full logits [n, V] (bf16 or fp32) of a head whose rows are an E2m1 of V
     rows of d values.  x: hidden states [n, d] in bf16 or fp32, which the call
     quantises as well (into x_quantized, an E2m1 of n rows of d values that a
-    program keeps, if given), or an E2m1.  out_dtype (of a new `out`) defaults
-    to float32.  The logits have no graph."""
+    program keeps, if given), or an E2m1 (for which x_quantized is refused).
+    out_dtype (of a new `out`) defaults to float32.  The logits have no graph."""
+    given = isinstance(x, E2m1)
+    if given and x_quantized is not None and x_quantized is not x:
+        raise ValueError("x_quantized is for states that the call quantises: x is an E2m1")
     like = weights.codes
     if not _here(like, "weights") or stream is not None:
         with _on(like, stream):
@@ -1068,7 +1071,6 @@ def e2m1_logits(x, weights, out=None, out_dtype=None, x_quantized=None, stream=N
     V, d = weights.shape
     w = weights._pointers("weights", V, d, like)
     stream = _stream_ptr(None)
-    given = isinstance(x, E2m1)
     if given:
         x_quantized, n = x, x.codes.shape[0]
     else:

@@ -196,6 +196,15 @@ def test_binding_refuses_cpu_tensors():
             call()
 
 
+def test_binding_refuses_room_for_states_that_are_quantised_already():
+    q, room, w = (vie.E2m1.empty(n, 8, device="cpu") for n in (2, 2, 5))
+    with pytest.raises(ValueError, match="x_quantized"):
+        vie.e2m1_logits(q, w, x_quantized=room)
+    for same in (None, q):  # (as far as the next check)
+        with pytest.raises(ValueError, match="CUDA"):
+            vie.e2m1_logits(q, w, x_quantized=same)
+
+
 class _Tensor:
     """A tensor of device 0, as far as the binding asks before it launches."""
     is_cuda, dtype = True, torch.float32
