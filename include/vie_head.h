@@ -734,7 +734,7 @@ vie_status vie_e2m1_bytes(int64_t n, int32_t d, int64_t *code_bytes, int64_t *sc
 /*
  * vie_e2m1_quantize - rows to e2m1.
  *   x           device, dtype [n, d], row pitch ld.
- *   out_codes, out_scales, out_row_scales  device, as above.
+ *   out_codes, out_scales, out_row_scales  device, as above; do not overlap x or each other.
  *   out_values  device, values_dtype [n, d], row pitch ld_values, or NULL: what the
  *               codes stand for, e.g. the weights that a training step computes
  *               with (exact in fp32, and in bf16 above its subnormal numbers); may
@@ -747,7 +747,10 @@ vie_status vie_e2m1_quantize(const void *x, vie_dtype dtype, int64_t n, int32_t 
                              void *out_scales, float *out_row_scales, void *out_values, vie_dtype values_dtype,
                              int64_t ld_values, vie_stream stream);
 
-/* vie_e2m1_dequantize - out[i, j] = what the codes stand for (out_dtype [n, d], row pitch ld_out). */
+/*
+ * vie_e2m1_dequantize - out[i, j] = what the codes stand for (out_dtype [n, d], row pitch ld_out);
+ * out does not overlap them.
+ */
 vie_status vie_e2m1_dequantize(const void *codes, const void *scales, const float *row_scales, int64_t n, int32_t d,
                                void *out, vie_dtype out_dtype, int64_t ld_out, vie_stream stream);
 
@@ -760,7 +763,7 @@ vie_status vie_e2m1_dequantize(const void *codes, const void *scales, const floa
  * vie_sample_logits draws from them, vie_token_logprobs scores them.
  *   x_*         device, n rows of d values;  0 <= n <= VIE_MANY_MAX.
  *   w_*         device, V rows of d values;  1 <= V <= VIE_E2M1_N_MAX.
- *   out         device, out_dtype [n, V], row pitch ld_out.
+ *   out         device, out_dtype [n, V], row pitch ld_out; does not overlap x_* and w_*.
  *
  * Errors: VIE_ERR_INVALID_ARG, VIE_ERR_UNSUPPORTED (dtype), VIE_ERR_CUDA.
  */
@@ -771,7 +774,7 @@ vie_status vie_e2m1_logits(const void *x_codes, const void *x_scales, const floa
 /*
  * vie_e2m1_quantize_logits - vie_e2m1_quantize of x (device, dtype [n, d], row pitch
  * ld) into x_* and vie_e2m1_logits of those, in one call: the head's rows are
- * fetched while x is quantised.  x_* do not overlap w_*.  Arguments and errors as
+ * fetched while x is quantised.  x_* do not overlap w_* or x.  Arguments and errors as
  * for those two.
  */
 vie_status vie_e2m1_quantize_logits(const void *x, vie_dtype dtype, int64_t n, int64_t ld, void *x_codes,

@@ -5,6 +5,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <type_traits>
 
 #include "vie_api.h"
@@ -450,6 +451,14 @@ static vie_status check_e2m1(const char *fn, int64_t n, const void *codes, const
     return VIE_OK;
 }
 
+// No result where threads of other rows may still read an input, or write another result.
+static vie_status check_apart(const char *fn, const void *result, std::initializer_list<const void *> others) {
+    for (const void *p : others)
+        if (result != nullptr && result == p)
+            return fail(VIE_ERR_INVALID_ARG, "%s: a result in place of an input or of another result", fn);
+    return VIE_OK;
+}
+
 // Rows from which on a warp takes each.  A warp's four rows one after the other are a
 // latency that few rows do not hide, a CTA per row a cost that many add up; the longer the
 // rows, the later the second is the larger, up to rows of 768 columns, and the later where
@@ -580,6 +589,9 @@ vie_status vie_e2m1_quantize(const void *x, vie_dtype dtype, int64_t n, int32_t 
     if (st == VIE_OK && n > 0 && out_values == x && (values_dtype != dtype || (n > 1 && ld_values != ld)))
         st = fail(VIE_ERR_INVALID_ARG, "%s: out_values in place of x with another type or row pitch", fn);
     if (st != VIE_OK || n == 0) return st;
+    st = check_apart(fn, x, {out_codes, out_scales, out_row_scales});
+    if (st == VIE_OK) st = check_apart(fn, out_values, {out_codes, out_scales, out_row_scales});
+    if (st != VIE_OK) return st;
     QuantizeParams p = {};
     p.x = x, p.n = n, p.d = d, p.ld = ld;
     p.codes = static_cast<uint8_t *>(out_codes), p.scales = static_cast<uint8_t *>(out_scales);
@@ -594,6 +606,7 @@ vie_status vie_e2m1_dequantize(const void *codes, const void *scales, const floa
     vie_status st = check_shape(fn, n, d);
     if (st == VIE_OK) st = check_e2m1(fn, n, codes, scales, row_scales);
     if (st == VIE_OK) st = check_matrix(fn, "out", out, out_dtype, n, d, ld_out);
+    if (st == VIE_OK && n > 0) st = check_apart(fn, out, {codes, scales, row_scales});
     if (st != VIE_OK || n == 0) return st;
     const E2m1Matrix q = {static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), row_scales, n};
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -606,8 +619,10 @@ vie_status vie_e2m1_logits(const void *x_codes, const void *x_scales, const floa
                            const void *w_codes, const void *w_scales, const float *w_row_scales, int64_t V, int32_t d,
                            void *out, vie_dtype out_dtype, int64_t ld_out, vie_stream stream) {
     const char *fn = "vie_e2m1_logits";
-    const vie_status st = check_logits(fn, n, V, d, x_codes, x_scales, x_row_scales, w_codes, w_scales, w_row_scales, out,
-                                       out_dtype, ld_out);
+    vie_status st = check_logits(fn, n, V, d, x_codes, x_scales, x_row_scales, w_codes, w_scales, w_row_scales, out,
+                                 out_dtype, ld_out);
+    if (st == VIE_OK && n > 0)
+        st = check_apart(fn, out, {x_codes, x_scales, x_row_scales, w_codes, w_scales, w_row_scales});
     if (st != VIE_OK || n == 0) return st;
     return start_logits(fn, x_codes, x_scales, x_row_scales, n, w_codes, w_scales, w_row_scales, V, d, false, out,
                         out_dtype, ld_out, static_cast<cudaStream_t>(stream));
@@ -623,6 +638,9 @@ vie_status vie_e2m1_quantize_logits(const void *x, vie_dtype dtype, int64_t n, i
     if (st == VIE_OK) st = check_matrix(fn, "x", x, dtype, n, d, ld);
     if (st == VIE_OK && n > 0 && (x_codes == w_codes || x_scales == w_scales || x_row_scales == w_row_scales))
         st = fail(VIE_ERR_INVALID_ARG, "%s: x_* in place of w_*", fn);
+    if (st == VIE_OK && n > 0) st = check_apart(fn, x, {x_codes, x_scales, x_row_scales});
+    if (st == VIE_OK && n > 0)
+        st = check_apart(fn, out, {x_codes, x_scales, x_row_scales, w_codes, w_scales, w_row_scales});
     if (st != VIE_OK || n == 0) return st;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     QuantizeParams p = {};

@@ -147,6 +147,22 @@ def test_results_in_place_of_inputs():
         assert "in place" in vie.vie_last_error()
 
 
+def test_e2m1_results_in_place_of_inputs_or_of_one_another():
+    def apart(ok):
+        return {k: P + 256 * i if v in (P, W) else v for i, (k, v) in enumerate(ok.items())}
+
+    parts = ("codes", "scales", "row_scales")
+    for fn, ok, pairs in (
+            (vie.vie_e2m1_quantize, QUANTIZE, [(p, o) for p in ("x", "values") for o in parts]),
+            (vie.vie_e2m1_dequantize, DEQUANTIZE, [("out", o) for o in parts]),
+            (vie.vie_e2m1_logits, LOGITS, [("out", m + o) for m in ("x_", "w_") for o in parts]),
+            (vie.vie_e2m1_quantize_logits, BOTH, [("out", m + o) for m in ("x_", "w_") for o in parts]
+             + [("x", "x_" + o) for o in parts])):
+        for a, b in pairs:
+            assert _call(fn, apart(ok), **{a: W, b: W}) == INVALID, (a, b)
+            assert "in place" in vie.vie_last_error() and fn.__name__ in vie.vie_last_error()
+
+
 def test_policy_results_in_place_of_weights():
     ok = dict(FORMS["vie_policy_loss_step"], out_loss=P + 16, out_logprob=P + 32, out_stats=P + 64, grad_loss=W)
     for out in ("out_loss", "out_logprob", "out_stats"):
