@@ -39,6 +39,10 @@ struct DistillParams {
     uint32_t *flag;
 };
 
+// Vectors in flight per thread: eight, but for loss and gradient on bf16 logits,
+// where a thread's 64 registers hold six (151936 x 4096: 450 us; 497 with eight).
+template <typename T, bool FWD, bool BWD>
+constexpr int kUnroll = FWD && BWD && sizeof(T) == 2 ? 6 : 8;
 constexpr int kTeacherEntries = 4;  // of a teacher, per thread of the warps that deal with it
 static_assert(VIE_K_MAX <= 32 * kTeacherEntries * kRowWarps, "warps for all entries");
 
@@ -308,6 +312,27 @@ static cudaError_t start_distill(const DistillParams &p, int64_t n, int slices, 
     }
     RowLaunch l(n * slices, FWD ? slices : 0, smem, s);
     return cudaLaunchKernelEx(&l.cfg, kernel, p, log2_of(slices));
+}
+
+// Bytes of a slice that one CTA takes, at most.  Gradient alone (128256 x 2048):
+// 155 us in slices of 128 KB, 163 of 256; each CTA reads the teacher's entries.
+constexpr int64_t kSliceBytes = 128 * 1024;
+// Loss and gradient, while a cluster can have more CTAs (fp32 128256 x 1024: 174 us in
+// slices of 64 KB, 186 of 128; bf16 151936 x 4096: 450 in slices of 76 KB, 556 of 38).
+constexpr int64_t kSliceStep = 80 * 1024;
+
+// CTAs per row of n rows of this many bytes.
+static int slices_of(bool fwd, bool bwd, int64_t bytes, int64_t n) {
+    int slices = 1;
+    if (!fwd) {  // no partials to join
+        while (bytes / slices > kSliceBytes && n * slices < (1 << 30)) slices *= 2;
+        return slices;
+    }
+    if (bwd)
+        while (slices < kSlices && bytes / slices > kSliceStep) slices *= 2;
+    // enough CTAs for the chip, of 32 KB of the row or more
+    while (slices < (n <= kFewRows ? kMaxSlices : kSlices) && n * slices < 1024 && bytes / slices > 32768) slices *= 2;
+    return slices;
 }
 
 template <bool FWD, bool BWD>

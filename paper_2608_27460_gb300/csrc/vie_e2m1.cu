@@ -44,10 +44,6 @@ __device__ __forceinline__ float reciprocal_approx(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
 
 // words[i] = all[i + first], first < 4 (the same in all lanes), without indexing registers.
 template <int N>
@@ -160,8 +156,8 @@ struct Raw8<float> {
 };
 
 template <typename T>
-__device__ __forceinline__ void store8(T *p, const float *v, int left, bool vectors) {
-    if (vectors && left >= 8) {
+__device__ __forceinline__ void store8(T *p, const float *v, int left) {
+    if (left >= 8) {
         reinterpret_cast<uint4 *>(p)[0] = Vec16<T>::pack(v);
         if constexpr (sizeof(T) == 4) reinterpret_cast<uint4 *>(p)[1] = Vec16<T>::pack(v + 4);
         return;
@@ -191,15 +187,13 @@ __device__ __forceinline__ void store8_shifted(T *row, int vec, const float *v, 
     const int end = 8 * vec + head, start = end - 8;  // values of the row
     T *const p = row + start;
     if (lane > 0 && end <= width) {
-        uint32_t all[2 * kWords], words[kWords + 1];
+        uint32_t all[kWords + 4], words[kWords + 1];
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) all[i] = before[i], all[kWords + i] = own[i];
-        const int bytes = head * static_cast<int>(sizeof(T)), skip = bytes / 4;  // skip < 4
-        uint32_t by2[kWords + 3];
+        for (int i = 0; i < kWords; ++i) all[i] = before[i];
 #pragma unroll
-        for (int i = 0; i < kWords + 3; ++i) by2[i] = i + 2 < 2 * kWords && (skip & 2) != 0 ? all[i + 2] : all[i];
-#pragma unroll
-        for (int i = 0; i < kWords + 1; ++i) words[i] = (skip & 1) != 0 ? by2[i + 1] : by2[i];
+        for (int i = 0; i < 4; ++i) all[kWords + i] = own[i];
+        const int bytes = head * static_cast<int>(sizeof(T));
+        take_words(all, bytes / 4, words);
         uint4 q[kWords / 4];
 #pragma unroll
         for (int i = 0; i < kWords / 4; ++i)
@@ -336,7 +330,7 @@ __global__ void __launch_bounds__(kQuantizeThreads, quantize_ctas<T, TV, ROW_WAR
                 for (int i = 0; i < 8; ++i) v[i] *= u;
                 TV *const out = static_cast<TV *>(a.values) + r * a.ld_values;
                 if constexpr (SHIFTED) store8_shifted(out, vec, v, width);
-                else if (left > 0) store8(out + 8 * vec, v, left, true);
+                else if (left > 0) store8(out + 8 * vec, v, left);
             }
         }
     }
@@ -413,7 +407,7 @@ __global__ void __launch_bounds__(kQuantizeThreads) dequantize_kernel(const E2m1
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] *= unit;
                 if constexpr (SHIFTED) store8_shifted(row, vec, v, d);
-                else if (vec * 8 < d) store8(row + 8 * vec, v, d - 8 * vec, true);
+                else if (vec * 8 < d) store8(row + 8 * vec, v, d - 8 * vec);
             }
         }
     }

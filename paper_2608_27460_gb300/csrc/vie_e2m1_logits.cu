@@ -123,11 +123,6 @@ __device__ __forceinline__ void give_up(uint32_t *flag, int *abort) {
     *static_cast<volatile int *>(abort) = 1;
 }
 
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-
 // Where an epilogue lane writes its vocabulary row v: columns c and c + 1 of a
 // tile (rows of the output, ld apart) at a time, in ascending order; all lanes of
 // the warp call.  WORDS (bf16): lanes trade, an even lane writes its own and its
