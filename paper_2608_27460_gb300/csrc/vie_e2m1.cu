@@ -453,6 +453,10 @@ static vie_status check_apart(const char *fn, const void *result, std::initializ
     return VIE_OK;
 }
 
+// The longest rows that a warp takes.
+template <typename T, bool SHIFTED>
+constexpr int kWarpColumns = SHIFTED && sizeof(T) == 4 ? 1536 : 2048;
+
 // Rows from which on a warp takes each.  A warp's four rows one after the other are a
 // latency that few rows do not hide, a CTA per row a cost that many add up; the longer the
 // rows, the later the second is the larger, up to rows of 768 columns, and the later where
@@ -461,10 +465,14 @@ static vie_status check_apart(const char *fn, const void *result, std::initializ
 // 8192 8.9 / 8.7; 1152, 6144 12.6 / 9.0, 12288 18.0 / 16.7, 16384 18.6 / 21.7; with values 1024,
 // 5120 12.9 / 7.3, 1152, 8192 14.8 / 13.3, 16384 19.9 / 25.8; 401 off, 16384 14.7 / 17.1, with
 // values 21.4 / 17.1, 20000 21.8 / 21.0).  Against the quicker one of the two, over 2100 calls of
-// 512 to 24576 rows: 0.5 % slower on average, at the most 22 % where rows lie at 16-byte
-// addresses, else 43 % (24576 x 2047 fp32: 78.6 us, by CTAs 54.9).
-static bool by_warps(int64_t n, int d, bool shifted, bool values) {
-    return d <= 2048 && n >= (2000 + 12 * static_cast<int64_t>(d < 768 ? d : 768)) * (shifted ? values ? 3 : 2 : 1);
+// 512 to 24576 rows: 0.5 % slower on average, 23 % at the most.  Rows off 16-byte addresses of
+// which a lane would keep eight vectors of fp32 are a CTA's however many they are (100000 x
+// 1793 266 us by warps, 208 by CTAs).
+template <typename T, typename TV, bool SHIFTED>
+static bool by_warps(int64_t n, int d) {
+    constexpr bool kValues = !std::is_same<TV, None>::value;
+    return d <= kWarpColumns<T, SHIFTED> &&
+           n >= (2000 + 12 * static_cast<int64_t>(d < 768 ? d : 768)) * (SHIFTED ? kValues ? 3 : 2 : 1);
 }
 
 // With the warps that a row's vectors keep busy, or all (nine tenths of the time of a
@@ -482,15 +490,16 @@ static cudaError_t start_by_cta(const QuantizeParams &p, int64_t rows, cudaStrea
 template <typename T, typename TV, bool SHIFTED>
 static cudaError_t start_quantize_rows(const QuantizeParams &p, cudaStream_t s) {
     const int64_t rows = (p.n + kE2m1TileRows - 1) / kE2m1TileRows * kE2m1TileRows;  // with those that have scales alone
-    if (by_warps(p.n, p.d, SHIFTED, !std::is_same<TV, None>::value)) {
+    if (by_warps<T, TV, SHIFTED>(p.n, p.d)) {
         const dim3 grid(static_cast<unsigned>(rows / 32));
         const size_t smem = static_cast<size_t>(e2m1_tiles(p.d)) * 128;
         auto by_warp = [&](auto kernel) { return launch(kernel, grid, kQuantizeThreads, smem, s, p); };
-        return p.d <= 768    ? by_warp(quantize_kernel<T, TV, 1, 3, SHIFTED>)
-               : p.d <= 1024 ? by_warp(quantize_kernel<T, TV, 1, 4, SHIFTED>)
-               : p.d <= 1280 ? by_warp(quantize_kernel<T, TV, 1, 5, SHIFTED>)
-               : p.d <= 1536 ? by_warp(quantize_kernel<T, TV, 1, 6, SHIFTED>)
-                             : by_warp(quantize_kernel<T, TV, 1, 8, SHIFTED>);
+        if (p.d <= 768) return by_warp(quantize_kernel<T, TV, 1, 3, SHIFTED>);
+        if (p.d <= 1024) return by_warp(quantize_kernel<T, TV, 1, 4, SHIFTED>);
+        if (p.d <= 1280) return by_warp(quantize_kernel<T, TV, 1, 5, SHIFTED>);
+        if constexpr (kWarpColumns<T, SHIFTED> > 1536)
+            if (p.d > 1536) return by_warp(quantize_kernel<T, TV, 1, 8, SHIFTED>);
+        return by_warp(quantize_kernel<T, TV, 1, 6, SHIFTED>);
     }
     if (p.d <= 2048) return start_by_cta<T, TV, 1, SHIFTED>(p, rows, s);
     if (p.d <= 4096) return start_by_cta<T, TV, 2, SHIFTED>(p, rows, s);
