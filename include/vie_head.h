@@ -575,8 +575,8 @@ vie_status vie_sample_logits(const void *logits, vie_dtype dtype, int64_t batch,
  * Negative tokens are empty slots (a prompt's, padding): logprob 0 and stats
  * (0, 0), and the row's logits are not read.  A token of V or more is taken as
  * one and sets the device flag that vie_device_status reports.  A token whose
- * logit is -inf has logprob -inf, whatever the other logits.  NaN or +inf
- * logits give a NaN in their row only.
+ * logit is -inf has logprob -inf, also where no logit is above it.  A row with a
+ * NaN or +inf logit has logprob NaN, and no other row has.
  *
  *   logits      device, dtype [n, V], row pitch ld.
  *   n, V        0 <= n <= VIE_MANY_MAX;  1 <= V <= VIE_DISTILL_V_MAX.

@@ -225,19 +225,23 @@ struct None {};  // no values wanted
 // CTA's scales (gathered in shared memory) are written 128 bytes at a time.
 // ROW_WARPS 8: a CTA per row, for the latency of few rows, and for long ones; 0: with
 // fewer warps, as many as the launch has (fp32 40000 x 5120 141 us, with 256 threads of
-// which three eighths are idle 246; bf16 100000 x 2560 156, 210).
+// which three eighths are idle 246; bf16 100000 x 2560 158, 210).
 // NV: vectors of eight values that a lane keeps.  SHIFTED: not all rows of x and of
 // the values lie at 16-byte addresses.
 //
-// Bound by bytes where rows lie at 16-byte addresses: 262144 x 1152 bf16 127 us, with
-// bf16 values 202 (of a copy's rate 0.90 and 1.0), fp32 196 (1.0), 30000 x 8192 bf16
-// with values 175 (0.94), 100395 x 3008 256 (0.79).  Elsewhere by the instructions that
-// take vectors apart and join them: 262144 x 1001 bf16 171 us, with values 336 (0.58 and
-// 0.52; value by value 483), fp32 272 (0.65).  32 x 1152 fp32: 1.4 us.
+// Bound by bytes where rows lie at 16-byte addresses: 262144 x 1152 bf16 129 us, with
+// bf16 values 203 (of a copy's rate 0.88 and 1.0), fp32 197 (1.0), 30000 x 8192 bf16
+// with values 175 (0.94), 100395 x 3008 262 (0.78); rows of more than 2048 columns of bf16
+// without values by a CTA's chain of loads, barrier and stores (100000 x 2112 153 us, 60000 x
+// 4096 143, 40000 x 5120 109: 0.52, 0.65, 0.71), narrow ones by a warp's turns (300000 x 64 55
+// us, x 256 58: 0.13, 0.50).  Elsewhere by the instructions that take vectors apart and join
+// them: 262144 x 1001 bf16 173 us, with values 339 (0.57 and 0.52; value by value 483), fp32
+// 275 (0.64).  32 x 1152 fp32: 1.5 us.
 //
 // CTAs per SM: what the registers of a row leave.  They are what bounds a warp per row,
 // and vectors that it does not have cost as many, so NV goes by one there (262144 x 1152
-// bf16: five vectors 127 us, with values 202; eight 145 and 225; fp32 196, 234).
+// bf16: five vectors 127 us, with values 202; eight 145 and 225; fp32 196, 234: before zeros
+// had one code, which costs 1 to 3 %).
 template <typename T, typename TV, int ROW_WARPS, int NV>
 constexpr int quantize_ctas() {
     const bool values = !std::is_same<TV, None>::value;

@@ -22,15 +22,17 @@
 // Measured, on the device alone, inputs of other calls in between (the floor: bytes
 // at the copy rate, 6.79 TB/s):
 //   262144 x 1152, 1 row of x, fp32    29.0 us (25.2)     bytes: 171 MB of the head's
-//   262144 x 1152, 32 rows, fp32       36.9 us (30.0)     bytes; writes of 512 a row and tile
-//   100003 x 1000, 129 rows, fp32      23.7 us (15.9)     6 tiles for most SMs, 5.14 on average
-//   128256 x 2048, 256 rows, bf16      43.6 us (31.5)
-//   128256 x 2048, 2048 rows, bf16      256 us (99.5; 4.2 PFLOP/s)
-// Many rows: the tensor pipe is 44 % busy.  A stage of 256 columns moves about 126 KB
+//   262144 x 1152, 32 rows, fp32       32.0 us (30.0)     bytes; writes of 512 a row and tile
+//   100003 x 1000, 129 rows, fp32      20.9 us (15.9)     782 tiles on 152 SMs: 22 of them have a sixth
+//   128256 x 2048, 256 rows, bf16      41.9 us (31.5)
+//   128256 x 2048, 2048 rows, bf16      259 us (99.5; 4.2 PFLOP/s), fp32 305 us (177)
+// Many rows: the tensor pipe is 43 % busy.  A stage of 256 columns moves about 126 KB
 // through shared memory (54 in by TMA, 48 read by the MMAs, 24 by the scale warps,
-// four of which read the same), 980 cycles of it, and the accumulator's 128 columns
-// per warp are drained between tiles.  Multicasting x to pairs of CTAs (254 us) and MMAs
-// of pairs of CTAs (268 us; 232 instead of 189 at 151936 x 1024) gained nothing.
+// four of which read the same): 980 cycles at 128 bytes each, were they all to share one
+// path, beside some 190 of the epilogue's accesses, of the 1200 that the stage takes; and
+// the accumulator's 128 columns per warp are drained between tiles.  Multicasting x to
+// pairs of CTAs (254 us, 256 without) and MMAs of pairs of CTAs (268 us; 232 instead of 189 at
+// 151936 x 1024) gained nothing.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

@@ -215,6 +215,20 @@ def test_nan_and_inf_stay_in_their_row(vie):
         assert bool(torch.isfinite(dz[row]).all()) == (row in (0, 2))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_nan_and_inf_beside_a_masked_token(vie, dtype):
+    """A token at -inf: -inf beside numbers and where no logit is above it, NaN beside a NaN or +inf, at any place."""
+    V = 5003
+    z, tok, grad, g = _inputs(7, V, dtype, seed=53)
+    tok[:] = 100
+    z[:, 100] = -math.inf
+    z[1], z[2, 0], z[3, V - 1], z[4, 2500], z[5, 101] = -math.inf, math.nan, math.nan, math.inf, math.inf
+    z[6], z[6, 99] = -math.inf, math.nan
+    lp, stats = vie.token_logprobs(z.cuda(), tok.cuda())
+    assert (lp[:2] == -math.inf).all() and torch.isnan(lp[2:]).all()
+    assert stats[1, 0] == -math.inf and stats[1, 1] == 0
+
+
 def test_extreme_terms(vie):
     """Ratios of 0 and infinity, advantages of 0, references that rule a token out."""
     z, tok, grad, g = _inputs(8, 300, "f32", seed=17)
