@@ -385,10 +385,11 @@ def test_logits_of_far_powers(vie):
     assert ((got - values).abs()[~far] <= 98 * ref.U * scale[~far] + 2.0 ** -148 + lost[~far]).all()
 
 
-@pytest.mark.parametrize("n", [7, 16, 30, 60, 66, 200])
-def test_logits_of_all_powers_are_exact(vie, n):
+@pytest.mark.parametrize("n,copies", [(7, 1), (16, 1), (30, 1), (60, 1), (66, 1), (200, 1), (600, 61), (20, 999)])
+def test_logits_of_all_powers_are_exact(vie, n, copies):
     """Rows from one end of fp32 to the other, whose sums of codes are whole numbers, small ones, and 0 (rows
-    that share no column, products that cancel): the definition's values rounded to fp32, then to bf16."""
+    that share no column, products that cancel): the definition's values rounded to fp32, then to bf16.  With
+    copies of the vocabulary's rows, and plain rows between them, CTAs have tiles with and without such rows."""
     d = 96
     powers = torch.tensor([-149, -140, -130, -126, -120, -110, -101, -100, -99, -90, -64, -30, 0, 17, 40, 64, 75, 90, 91, 100,
                            110, 124])
@@ -404,7 +405,11 @@ def test_logits_of_all_powers_are_exact(vie, n):
         x[2::3].view(-1, d // 16, 16)[:, 0::2] = 0.0
         return (x.double() * 2.0 ** powers.double().repeat_interleave(3)[:, None]).float()
 
-    x, w = rows(1.0).repeat(4, 1)[torch.randperm(4 * 3 * len(powers), generator=g)[:n]], rows(-1.0)
+    x, w = rows(1.0).repeat(10, 1)[torch.randperm(10 * 3 * len(powers), generator=g)[:n]], rows(-1.0)
+    if copies > 1:
+        plain = torch.zeros((1, d))
+        plain[0, 5] = 3.0
+        w = torch.cat([w, plain.expand(255, d)]).repeat(copies, 1)
     want = (ref.quantize(x)[3] @ ref.quantize(w)[3].t()).float()
     assert (want == 0).any() and torch.isinf(want).any() and (want.abs() > 2.0 ** 100).any()
     wq = vie.e2m1_quantize(w.cuda())
